@@ -12,3 +12,4 @@ from .reorder import cuthill_mckee_order, reverse_cuthill_mckee, permute_mask, b
 from .brute import brute_attention, brute_block_counts, brute_bwd_magnitudes  # noqa: F401
 from .blocks import (block_counts, block_class, bin_blk_mat, run_index, sparse_index, packed_bits,  # noqa: F401
                      block_index, schedule, column_index, column_schedule)
+from . import tokens  # noqa: F401

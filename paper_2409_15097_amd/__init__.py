@@ -15,7 +15,12 @@ _NAMES = (
     "bbm_sched_bytes", "build_index", "bf16_from_bits", "bbm_rcm_workspace_bytes", "bbm_rcm_order", "bbm_permute_mask",
     "bbm_gather_rows", "bbm_probe_mfma_bf16", "bbm_probe_mfma_bf16_flop",
 )
-__all__ = list(_NAMES)
+# operators on packed tokens (include/bbm_tokens.h)
+_TOKEN_NAMES = (
+    "Slots", "KV4Cache", "kv4_cache", "rope_freqs", "bbm_build_slots", "bbm_rope", "bbm_prompt_attn_fwd",
+    "bbm_prompt_attn_bwd_workspace_bytes", "bbm_prompt_attn_bwd", "bbm_kv4_append", "bbm_kv4_read", "bbm_kv4_attn_workspace_bytes", "bbm_kv4_attn",
+)
+__all__ = list(_NAMES + _TOKEN_NAMES)
 
 
 def __getattr__(name):
@@ -24,8 +29,13 @@ def __getattr__(name):
         value = getattr(binding, name)
         globals()[name] = value
         return value
+    if name in _TOKEN_NAMES:
+        from . import tokens
+        value = getattr(tokens, name)
+        globals()[name] = value
+        return value
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
 def __dir__():
-    return sorted(list(globals()) + list(_NAMES))
+    return sorted(list(globals()) + list(_NAMES + _TOKEN_NAMES))

@@ -1,0 +1,80 @@
+// Packed tensors (include/bbm_tokens.h): their host checks, and the way from a work-group's number to its piece of a request.
+#pragma once
+#include "bbm_internal.h"
+#include "bbm_tokens.h"
+
+namespace bbm {
+
+constexpr int64_t kMaxTokens = 1ll << 30;
+constexpr int64_t kMaxRowStride = 1ll << 22;  // a tile of 128 rows stays within the 2^31 bytes of a buffer resource
+
+// `rows` x `heads` x d elements; an output's must not lie upon each other.
+inline int check_packed(const char* fn, const char* name, const bbm_packed* x, int64_t rows, int64_t heads, int64_t d, bool output) {
+  if (!x || (!x->ptr && rows > 0)) return fail(BBM_EINVAL, "%s: %s must not be NULL", fn, name);
+  if (!aligned(x->ptr, 16)) return fail(BBM_EINVAL, "%s: %s must be 16-byte aligned", fn, name);
+  if (x->row_stride < 0 || x->head_stride < 0 || x->row_stride % 8 || x->head_stride % 8)
+    return fail(BBM_EINVAL, "%s: strides of %s (%lld, %lld) must be multiples of 8 elements, not negative", fn, name, (long long)x->row_stride, (long long)x->head_stride);
+  if (rows > 1 && x->row_stride > kMaxRowStride) return fail(BBM_EUNSUPPORTED, "%s: row stride %lld of %s is beyond %lld elements", fn, (long long)x->row_stride, name, (long long)kMaxRowStride);
+  if (heads > 1 && x->head_stride > (1ll << 40)) return fail(BBM_EUNSUPPORTED, "%s: head stride %lld of %s is too large", fn, (long long)x->head_stride, name);
+  if (output) {
+    const bool rows_first = x->row_stride >= x->head_stride;  // (the longer stride; one that is never taken does not count)
+    const int64_t inner = rows_first ? x->head_stride : x->row_stride, n_inner = rows_first ? heads : rows;
+    const int64_t outer = rows_first ? x->row_stride : x->head_stride, n_outer = rows_first ? rows : heads;
+    if ((n_inner > 1 && inner < d) || (n_outer > 1 && outer < (n_inner > 1 ? (n_inner - 1) * inner : 0) + d))
+      return fail(BBM_EINVAL, "%s: rows or heads of %s overlap (strides %lld, %lld)", fn, name, (long long)x->row_stride, (long long)x->head_stride);
+  }
+  return BBM_OK;
+}
+
+// T rows, R requests, H query heads over Hk key heads.
+inline int check_tokens(const char* fn, int64_t T, int64_t R, const int32_t* cu, int64_t H, int64_t Hk) {
+  if (T < 0 || R < 1 || H < 1 || Hk < 1) return fail(BBM_EINVAL, "%s: T=%lld must be >= 0, R=%lld, H=%lld, Hk=%lld >= 1", fn, (long long)T, (long long)R, (long long)H, (long long)Hk);
+  if (H % Hk) return fail(BBM_EINVAL, "%s: H=%lld is no multiple of Hk=%lld", fn, (long long)H, (long long)Hk);
+  if (!cu || !aligned(cu, 4)) return fail(BBM_EINVAL, "%s: cu must be a non-NULL 4-byte aligned pointer", fn);
+  if (T > kMaxTokens || R > kMaxTokens || H > 65535 || T * H > (1ll << 36)) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, R=%lld, H=%lld)", fn, (long long)T, (long long)R, (long long)H);
+  return BBM_OK;
+}
+
+struct Span {
+  int r, begin, end;  // request, its first row and the one behind its last
+  int piece;          // which piece of it
+};
+
+// Which piece of which request is number `at`?  Requests are cut into pieces of `unit` rows; request r's pieces have the
+// numbers first(r) = cu[r] * mul / unit + r and those that follow (mul columns a row).  first() rises by at least the pieces of r, since
+// floor((a + n) / u) + 1 >= floor(a / u) + ceil(n / u): no number belongs to two requests, none is beyond T * mul / unit + R, and some
+// belong to nobody (begin = end).  All 64 lanes of a wave search together, a trip to memory for every factor of 64 in R.
+__device__ __forceinline__ Span find_piece(const int32_t* __restrict__ cu, int R, int T, int mul, int unit, int at) {
+  const int lane = threadIdx.x & 63;
+  auto first = [&](int c, int r) { return (int64_t)min(max(c, 0), T) * mul / unit + r; };
+  int lo = 0, n = R;  // the last r in lo .. lo + n - 1 with first(r) <= at (r = lo if there is none)
+  while (n > 1) {
+    const int step = (n + 63) / 64;
+    const int r = lo + lane * step;
+    const bool ok = lane * step < n && first(cu[min(r, R)], r) <= at;
+    const int hits = __popcll(__ballot(ok));
+    const int k = max(0, hits - 1) * step;
+    lo += k;
+    n = min(step, n - k);
+  }
+  const int c0 = cu[lo], c1 = cu[lo + 1];
+  Span s;
+  s.r = lo;
+  s.begin = min(max(c0, 0), T);
+  s.end = max(s.begin, min(max(c1, 0), T));
+  const int64_t piece = at - first(c0, lo);
+  if (piece < 0 || piece * unit >= (int64_t)(s.end - s.begin) * mul) {
+    s.end = s.begin;
+    s.piece = 0;
+  } else {
+    s.piece = (int)piece;
+  }
+  s.r = __builtin_amdgcn_readfirstlane(s.r);
+  s.begin = __builtin_amdgcn_readfirstlane(s.begin);
+  s.end = __builtin_amdgcn_readfirstlane(s.end);
+  s.piece = __builtin_amdgcn_readfirstlane(s.piece);
+  return s;
+}
+inline int64_t count_pieces(int64_t T, int64_t R, int64_t mul, int64_t unit) { return T * mul / unit + R; }
+
+}  // namespace bbm

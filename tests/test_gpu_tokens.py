@@ -1,0 +1,546 @@
+"""GPU: the operators on packed tokens against their definitions in 64 bits (oracle/tokens.py), at the sizes and masks where they can go wrong.
+Tolerances are the bounds derived there from the roundings that the kernels make."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import tokens as ot
+
+pytestmark = pytest.mark.gpu
+
+NAN = float("nan")
+
+
+@pytest.fixture(scope="module")
+def bbm():
+    import paper_2409_15097_amd as m
+    return m
+
+
+def i32(x):
+    return torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")
+
+
+def normal(seed, *shape, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * scale).to(torch.bfloat16).cuda()
+
+
+def f64(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def in_layout(x, layout):
+    """The packed tensor with the same values: contiguous, as a part of a wider projection, or with the heads outermost."""
+    T, H, d = x.shape
+    if layout == "fused":
+        wide = torch.full((T, (H + 3) * d + 8), NAN, dtype=x.dtype, device=x.device)
+        part = wide[:, d:(H + 1) * d].unflatten(1, (H, d))
+        part.copy_(x)
+        return part
+    return x.transpose(0, 1).contiguous().transpose(0, 1) if layout == "heads" else x
+
+
+def close(name, got, want, tol):
+    got = f64(got)
+    bad = ~(np.abs(got - want) <= tol) & ~((got == want) | (np.isnan(got) & np.isnan(want)))
+    assert not bad.any(), f"{name}: {bad.sum()} of {bad.size} values off, the worst {np.abs(got - want)[bad].max()} against {tol[bad].min()}; at {np.argwhere(bad)[:4].tolist()}"
+
+
+# ---- slots
+
+
+@pytest.mark.parametrize("R, new, ctx, page, short_list, narrow", [
+    (1, 1, 0, 16, 0, 0), (1, 200, 70, 64, 0, 0), (3, 5, 40, 16, 2, 0), (64, 1, 500, 64, 0, 0), (65, 3, 17, 32, 0, 1), (1000, 9, 300, 16, 40, 0),
+    (1500, 130, 100, 128, 0, 2), (8200, 2, 64, 16, 0, 0), (16384, 2, 33, 32, 100, 1)])
+def test_slots(bbm, R, new, ctx, page, short_list, narrow):
+    g = np.random.default_rng(R)
+    c, a = g.integers(0, ctx + 1, R), g.integers(0, new + 1, R)
+    c[g.random(R) < 0.1] = 0
+    a[-1], c[-1] = new, ctx
+    if R > 2:
+        c[0], a[1] = -3, -1                                              # stand for none
+    width = max(1, -(-(ctx + new) // page) - narrow)
+    held, want = (np.minimum(-(-np.maximum(x, 0) // page), width) for x in (c, np.maximum(c, 0) + np.maximum(a, 0)))
+    ids = g.permutation(int(want.sum()) + 40).astype(np.int32)
+    wide = np.full((R, width + 3), -7, np.int32)
+    wide[:, :width] = np.where(np.arange(width) < held[:, None], np.arange(R)[:, None] % 5 * 1000 + np.arange(width), -2)
+    first, n_free = 3, max(0, 3 + int((want - held).sum()) - short_list)
+    T = max(0, int(np.maximum(a, 0).sum()) + (7 if R % 2 else -2))
+    free = ids[:n_free]
+    wt, wcu, wlens, wpos, wslots, wnext = ot.build_slots(c, a, wide[:, :width], free, first, T, page)
+    buf = i32(wide)
+    for _ in range(2):                                                   # a repeated call finds what it left
+        r = bbm.bbm_build_slots(i32(c), i32(a), buf[:, :width], i32(free), i32([first]), T, page)
+        got = buf.cpu().numpy()
+        assert np.array_equal(got[:, :width], wt) and (got[:, width:] == -7).all()
+        for x, y in ((r.cu_new, wcu), (r.lens, wlens), (r.positions, wpos), (r.slots, wslots), (r.free_next, [wnext])):
+            assert np.array_equal(x.cpu().numpy(), y)
+
+
+# ---- rotary positions
+
+
+@pytest.mark.parametrize("T, H, Hk, d, rot, interleaved, layout", [
+    (1, 1, 1, 16, 2, False, "plain"), (1, 4, 0, 64, 64, True, "plain"), (33, 32, 8, 128, 128, False, "fused"), (7, 3, 1, 64, 62, False, "fused"),
+    (7, 3, 1, 64, 62, True, "heads"), (130, 8, 2, 128, 64, True, "fused"), (130, 8, 2, 128, 40, False, "heads"), (65, 5, 5, 80, 20, False, "plain"),
+    (65, 5, 5, 80, 6, True, "plain"), (3000, 4, 2, 128, 96, False, "plain"), (5000, 2, 1, 512, 512, True, "plain"), (40, 2, 1, 112, 112, False, "heads")])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_rope(bbm, T, H, Hk, d, rot, interleaved, layout, inverse):
+    g = np.random.default_rng(T + rot)
+    pos = g.integers(-5, 1 << 20, T)
+    pos[0] = (1 << 31) - 1
+    freqs, mscale = bbm.rope_freqs(rot, factor=8.0, method="yarn", trained_len=4096)
+    q, k = normal(1, T, H, d), normal(2, T, Hk, d) if Hk else None
+    ql, kl = in_layout(q, layout), None if k is None else in_layout(k, layout)
+    got = bbm.bbm_rope(ql, kl, i32(pos), freqs, interleaved=interleaved, mscale=mscale, inverse=inverse)
+    for name, x, y in (("q", q, got[0]), ("k", k, got[1])):
+        if x is None:
+            assert y is None
+            continue
+        want = ot.rope(f64(x), pos, f64(freqs), interleaved, mscale, inverse)
+        x = f64(x)
+        one = np.arange(0, rot, 2) if interleaved else np.arange(rot // 2)
+        two = one + (1 if interleaved else rot // 2)
+        size = np.zeros_like(want)
+        size[..., one] = size[..., two] = mscale * (np.abs(x[..., one]) + np.abs(x[..., two]))
+        close(name, y, want, ot.B * np.abs(want) + 16 * ot.F * size)     # a sine off by a few steps of 1, three products and a sum
+        assert (f64(y)[..., rot:] == x[..., rot:]).all()
+    # in place, and back again
+    a, b = bbm.bbm_rope(ql, kl, i32(pos), freqs, interleaved=interleaved, mscale=mscale, inverse=inverse, out_q=ql, out_k=kl)
+    assert a is ql and torch.equal(ql, got[0]) and (k is None or torch.equal(kl, got[1]))
+
+
+# ---- prompts
+
+
+LENS = {
+    "one": [1], "two": [2, 1], "empty": [0, 5, 0, 0, 70, 0], "tiles": [64, 65, 63, 128, 127, 129], "ragged": [1, 200, 3, 33, 257, 2, 1, 90],
+    "many": [int(x) for x in np.random.default_rng(3).integers(0, 12, 150)], "long": [700, 1], "longer": [1300],
+}
+
+
+def prompt_case(name, H, Hk, d, layout, seed=0, before=2, behind=3, scale=1.0):
+    lens = LENS[name]
+    cu = np.concatenate([[0], np.cumsum(lens)]) + before                   # rows in front of the first sequence and behind the last
+    T = int(cu[-1]) + behind
+    x = {n: normal(seed + i, T, h, d, scale=scale) for i, (n, h) in enumerate((("q", H), ("k", Hk), ("v", Hk), ("d_o", H)))}
+    for t in x.values():                                                   # rows of nobody hold anything
+        t[:before] = NAN
+        t[cu[-1]:] = float("inf")
+    return cu, T, {n: in_layout(t, layout) for n, t in x.items()}
+
+
+def check_prompt(bbm, cu, T, x, H, Hk, d, scale=None, bwd=True):
+    sm = d ** -0.5 if scale is None else scale
+    out = torch.full((T, H, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((H, T), 7.0, device="cuda")
+    o, lse = bbm.bbm_prompt_attn_fwd(x["q"], x["k"], x["v"], i32(cu), softmax_scale=scale, out=out, lse=lse)
+    grads = [torch.full((T, h, d), 7.0, dtype=torch.bfloat16, device="cuda") for h in (H, Hk, Hk)]
+    if bwd:
+        bbm.bbm_prompt_attn_bwd(x["q"], x["k"], x["v"], o, x["d_o"], lse, i32(cu), softmax_scale=scale, dq=grads[0], dk=grads[1], dv=grads[2])
+    real = np.zeros(T, bool)
+    real[cu[0]:cu[-1]] = True
+    for t in [o, lse.t()] + grads:
+        assert (f64(t)[~real] == 7.0).all(), "rows of nobody are left as they were"
+    n = {a: f64(t) for a, t in x.items()}
+    oo, ll, gg = f64(o), f64(lse), [f64(t) for t in grads]
+    worst = 0.0
+    for a, b in zip(cu[:-1], cu[1:]):
+        if a == b:
+            continue
+        seen = np.tril(np.ones((b - a, b - a), bool))
+        for hk in range(Hk):
+            k, v = n["k"][a:b, hk], n["v"][a:b, hk]
+            dk, dv, e_dk, e_dv = (np.zeros((b - a, d)) for _ in range(4))
+            for h in range(hk * (H // Hk), (hk + 1) * (H // Hk)):
+                q, d_o = n["q"][a:b, h], n["d_o"][a:b, h]
+                wo, wl, p = ot.attention(q, k, v, seen, sm)
+                at = f"rows {a}..{b}, head {h}: "
+                if not bwd:
+                    e_o, e_l = ot.bounds(q, k, v, seen, sm, p, wo, wl)
+                    close(at + "O", o[a:b, h], wo, e_o), close(at + "lse", lse[h, a:b], wl, e_l)
+                    continue
+                delta = (d_o * oo[a:b, h]).sum(1)
+                g = ot.attention_bwd(q, k, v, d_o, p, sm, delta)
+                e_o, e_l, e_dq, e1, e2 = ot.bounds(q, k, v, seen, sm, p, wo, wl, d_o, delta, g)
+                close(at + "O", o[a:b, h], wo, e_o), close(at + "lse", lse[h, a:b], wl, e_l), close(at + "dQ", grads[0][a:b, h], g[0], e_dq)
+                dk, dv, e_dk, e_dv = dk + g[1], dv + g[2], e_dk + e1, e_dv + e2
+            if bwd:
+                close(f"rows {a}..{b}, key head {hk}: dK", grads[1][a:b, hk], dk, e_dk), close(f"rows {a}..{b}, key head {hk}: dV", grads[2][a:b, hk], dv, e_dv)
+    return o, lse, grads
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("name, H, Hk, layout", [("one", 1, 1, "plain"), ("two", 6, 2, "fused"), ("empty", 4, 4, "heads"), ("tiles", 3, 1, "plain"),
+                                                 ("ragged", 8, 2, "fused"), ("many", 4, 1, "heads"), ("long", 2, 2, "plain"), ("longer", 5, 1, "fused")])
+def test_prompt(bbm, name, H, Hk, d, layout):
+    cu, T, x = prompt_case(name, H, Hk, d, layout)
+    o, lse, grads = check_prompt(bbm, cu, T, x, H, Hk, d)
+    # the same bits again, and without a log-sum-exp in the C call's place of one
+    o2, lse2 = bbm.bbm_prompt_attn_fwd(x["q"], x["k"], x["v"], i32(cu))
+    g2 = bbm.bbm_prompt_attn_bwd(x["q"], x["k"], x["v"], o2, x["d_o"], lse2, i32(cu))
+    a, b = int(cu[0]), int(cu[-1])
+    assert torch.equal(o[a:b], o2[a:b]) and torch.equal(lse[:, a:b], lse2[:, a:b]) and all(torch.equal(u[a:b], w[a:b]) for u, w in zip(grads, g2))
+
+
+@pytest.mark.parametrize("scale, size", [(1.0, 1.0), (0.01, 1.0), (0.125, 6.0)])
+def test_prompt_with_other_scales(bbm, scale, size):
+    cu, T, x = prompt_case("ragged", 2, 1, 64, "plain", seed=9, scale=size)
+    check_prompt(bbm, cu, T, x, 2, 1, 64, scale=scale)
+
+
+def test_prompt_rows_that_see_large_values(bbm):
+    """Keys and values of 1e30 behind a query leave its row alone; a row of equal large scores is an average."""
+    cu, T, x = prompt_case("long", 1, 1, 64, "plain", seed=4)
+    a, b = int(cu[0]), int(cu[1])
+    x["k"][b - 40:b] = 1e30
+    x["v"][b - 40:b] = -1e30
+    o, lse = bbm.bbm_prompt_attn_fwd(x["q"], x["k"], x["v"], i32(cu))
+    n = {m: f64(t)[a:b - 40, 0] for m, t in x.items()}
+    seen = np.tril(np.ones((b - 40 - a,) * 2, bool))
+    wo, wl, p = ot.attention(n["q"], n["k"], n["v"], seen, 0.125)
+    e_o, e_l = ot.bounds(n["q"], n["k"], n["v"], seen, 0.125, p, wo, wl)
+    close("O", o[a:b - 40, 0], wo, e_o), close("lse", lse[0, a:b - 40], wl, e_l)
+
+
+# ---- the cache in 4 bits
+
+
+def host_cache(c):
+    k, v = (ot.unpack_nibbles(t.cpu().numpy()) for t in (c.k, c.v))
+    return ot.kv4_decode(k, c.k_scale.cpu().numpy()), ot.kv4_decode(v, c.v_scale.transpose(-1, -2).cpu().numpy())     # [pages, Hk, page, d]
+
+
+@pytest.mark.parametrize("T, Hk, d, page, layout", [(1, 1, 64, 16, "plain"), (3, 2, 128, 32, "fused"), (130, 3, 64, 64, "heads"), (700, 2, 128, 128, "fused"), (2100, 1, 64, 16, "plain")])
+def test_append_and_read(bbm, T, Hk, d, page, layout):
+    g = np.random.default_rng(T)
+    pages = -(-T // page) + 2
+    c = bbm.kv4_cache(pages, Hk, d, page)
+    for t in (c.k, c.v, c.k_scale, c.v_scale):
+        t.fill_(0x55)
+    spread = torch.exp2(torch.from_numpy(g.integers(-20, 20, (T, Hk, 1))).cuda().float())
+    k = (normal(1, T, Hk, d).float() * spread).to(torch.bfloat16)
+    v = normal(2, T, Hk, d)
+    grid = torch.tensor([0, .25, .5, .75, 1.25, 1.75, 2.5, 3.5, 5, 6, 7, -.25, -2.5, -5, -7, 0.0])
+    v[0, 0, :16] = grid.to(torch.bfloat16).cuda()                          # halfway values
+    v[0, 0, 16:32] = 0
+    if T > 1:
+        k[1] = 0
+        k[2, 0, :32], k[2, 0, 32:64] = 3.3e38, -1e-38                      # the largest and smallest scales
+        k[2, 0, 7] = 2.0 ** -133
+    slots = g.permutation(pages * page - 1)[:T].astype(np.int64)
+    if T > 2:
+        slots[1::7] = -1
+        slots[2] = pages * page - 1
+        slots[5::100] = pages * page + 3
+    inside = (slots >= 0) & (slots < pages * page)
+    bbm.bbm_kv4_append(in_layout(k, layout), in_layout(v, layout), i32(slots), c)
+    pg, at = slots[inside] // page, slots[inside] % page
+    for x, codes, scales, v_order in ((k, c.k, c.k_scale, False), (v, c.v, c.v_scale, True)):
+        want_codes, want_scales = ot.kv4_encode(f64(x)[inside])
+        got_codes, got_scales = ot.unpack_nibbles(codes.cpu().numpy()), scales.cpu().numpy()
+        got_scales = got_scales.swapaxes(-1, -2) if v_order else got_scales
+        assert np.array_equal(got_scales[pg, :, at], want_scales)
+        assert np.array_equal(ot.kv4_decode(got_codes[pg, :, at], got_scales[pg, :, at]), ot.kv4_decode(want_codes, want_scales))
+        got_codes[pg, :, at], got_scales[pg, :, at] = 5, 0x55
+        assert (got_codes == 5).all() and (got_scales == 0x55).all(), "other slots are left as they were"
+    rk, rv = (in_layout(torch.full((T, Hk, d), NAN, dtype=torch.bfloat16, device="cuda"), layout) for _ in range(2))
+    bbm.bbm_kv4_read(i32(slots), c, out_k=rk, out_v=rv)
+    hk, hv = host_cache(c)
+    for got, want in ((rk, hk), (rv, hv)):
+        assert np.array_equal(f64(got)[inside], want[pg, :, at]) and (f64(got)[~inside] == 0).all()
+
+
+def test_groups_that_are_not_finite(bbm):
+    c = bbm.kv4_cache(1, 1, 64, 16)
+    k, v = normal(1, 2, 1, 64), normal(2, 2, 1, 64)
+    k[0, 0, 3], v[1, 0, 40] = float("inf"), NAN
+    bbm.bbm_kv4_append(k, v, i32([4, 5]), c)
+    rk, rv = bbm.bbm_kv4_read(i32([4, 5]), c)
+    assert torch.isnan(rk[0, 0, :32]).all() and torch.isfinite(rk[0, 0, 32:]).all() and torch.isfinite(rk[1]).all()
+    assert torch.isnan(rv[1, 0, 32:]).all() and torch.isfinite(rv[1, 0, :32]).all() and torch.isfinite(rv[0]).all()
+
+
+def cached_case(bbm, lens, news, H, Hk, d, page, layout="plain", seed=0, tree=None, before=0, behind=0, extra_pages=2, width=None):
+    """Random pages; slots behind a request's length and pages of nobody hold NaN scales."""
+    g = np.random.default_rng(seed)
+    R = len(lens)
+    need = [-(-n // page) for n in lens]
+    width = max(1, max(need) + 1) if width is None else width
+    pages = sum(need) + extra_pages
+    ids = g.permutation(pages)
+    table = np.full((R, width), -1, np.int64)
+    c = bbm.kv4_cache(pages, Hk, d, page)
+    c.k.copy_(torch.from_numpy(g.integers(0, 256, c.k.shape, dtype=np.uint8)))
+    c.v.copy_(torch.from_numpy(g.integers(0, 256, c.v.shape, dtype=np.uint8)))
+    ks, vs = np.full(c.k_scale.shape, 255, np.uint8), np.full(c.v_scale.shape, 255, np.uint8)
+    at = 0
+    for r, n in enumerate(lens):
+        for p in range(need[r]):
+            if p < width:
+                table[r, p] = ids[at]
+            m = min(page, n - p * page)
+            ks[ids[at], :, :m] = g.integers(125, 128, (Hk, m, d // 32))
+            vs[ids[at], :, :, :m] = g.integers(125, 128, (Hk, d // 32, m))
+            at += 1
+    c.k_scale.copy_(torch.from_numpy(ks)), c.v_scale.copy_(torch.from_numpy(vs))
+    cu = np.concatenate([[0], np.cumsum(news)]) + before
+    T = int(cu[-1]) + behind
+    q = normal(seed + 5, T, H, d)
+    words = None
+    if tree is not None:
+        words = g.integers(0, 1 << 62, (T, tree), dtype=np.int64) * 2 + g.integers(0, 2, (T, tree))
+        words[g.random(T) < 0.2] = 0                                       # nodes that see none of the new tokens
+    return c, table, cu, T, in_layout(q, layout), words
+
+
+def check_cached(bbm, c, table, lens, cu, T, q, words, H, Hk, d, page, **kw):
+    out, lse = torch.full((T, H, d), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((H, T), 7.0, device="cuda")
+    bbm.bbm_kv4_attn(q, c, i32(table), i32(lens), i32(cu), mask=None if words is None else torch.from_numpy(words).cuda(), out=out, lse=lse, **kw)
+    real = np.zeros(T, bool)
+    real[cu[0]:cu[-1]] = True
+    assert (f64(out)[~real] == 7.0).all() and (f64(lse)[:, ~real] == 7.0).all()
+    hk, hv = host_cache(c)
+    nq, G = f64(q), H // Hk
+    for r, n in enumerate(lens):
+        a, b = int(cu[r]), int(cu[r + 1])
+        new = b - a
+        if not new:
+            continue
+        m = min(max(n, 0), table.shape[1] * page)
+        pg = table[r, np.arange(m) // page]
+        ok = (pg >= 0) & (pg < c.k.shape[0])
+        j, i = np.arange(m), np.arange(new)[:, None]
+        if words is None:
+            seen = (j <= n - new + i) & ok
+        else:
+            nj = j - (n - new)
+            bit = np.zeros((new, m), bool)
+            inside = (nj >= 0) & (nj < 64 * words.shape[1])
+            bit[:, inside] = (words[a:b][:, nj[inside] // 64] >> (nj[inside] % 64)) & 1 != 0
+            seen = ((nj < 0) | bit) & ok
+        for h in range(H):
+            k, v = (np.where(ok[:, None], x[np.where(ok, pg, 0), h // G, j % page], 0.0) if m else np.zeros((0, d)) for x in (hk, hv))
+            wo, wl, p = ot.attention(nq[a:b, h], k, v, seen, d ** -0.5)
+            e_o, e_l = ot.bounds(nq[a:b, h], k, v, seen, d ** -0.5, p, wo, wl)
+            close(f"request {r}, head {h}: O", out[a:b, h], wo, e_o), close(f"request {r}, head {h}: lse", lse[h, a:b], wl, e_l)
+    return out, lse
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens, news, H, Hk, page, layout, tree", [
+    ([1], [1], 1, 1, 16, "plain", None), ([0, 3, 17], [1, 1, 1], 4, 2, 16, "fused", None), ([63, 64, 65, 200, 1, 0], [1] * 6, 8, 1, 32, "plain", None),
+    ([130, 300, 31], [1, 0, 1], 6, 2, 64, "heads", None), ([40, 500, 7], [5, 33, 7], 6, 2, 16, "fused", None), ([40, 90], [40, 60], 32, 2, 128, "plain", None),
+    ([20, 70, 5], [20, 6, 5], 4, 4, 16, "plain", 1), ([300, 129], [70, 129], 3, 1, 64, "heads", 2), ([300, 150], [100, 100], 5, 1, 32, "plain", 1),
+    ([3, 2], [5, 4], 4, 2, 16, "plain", None), ([3000, 9, 1700], [1, 1, 2], 12, 4, 64, "plain", None), ([33] * 70, [1] * 70, 2, 1, 16, "plain", None)])
+def test_cached(bbm, lens, news, H, Hk, d, page, layout, tree):
+    c, table, cu, T, q, words = cached_case(bbm, lens, news, H, Hk, d, page, layout, seed=len(lens), tree=tree, before=2, behind=3)
+    first = check_cached(bbm, c, table, lens, cu, T, q, words, H, Hk, d, page)
+    again = check_cached(bbm, c, table, lens, cu, T, q, words, H, Hk, d, page, max_len=max(1, max(lens)))
+    some = check_cached(bbm, c, table, lens, cu, T, q, words, H, Hk, d, page)
+    assert all(torch.equal(x, y) for x, y in zip(first, some)) and again is not None
+
+
+def test_cached_pages_outside_and_a_narrow_table(bbm):
+    lens, news, H, Hk, d, page = [500, 300, 90], [1, 3, 2], 4, 2, 128, 32
+    c, table, cu, T, q, _ = cached_case(bbm, lens, news, H, Hk, d, page, seed=3)
+    table[0, 3], table[0, 15], table[1, 0], table[2, :] = -1, 1 << 30, c.k.shape[0], -5
+    check_cached(bbm, c, table, lens, cu, T, q, None, H, Hk, d, page)
+    check_cached(bbm, c, table[:, :5], lens, cu, T, q, None, H, Hk, d, page)
+    check_cached(bbm, c, table[:, :5], [700, -4, 1 << 30], cu, T, q, None, H, Hk, d, page)
+
+
+def test_cached_pages_shared_by_requests(bbm):
+    """A common prefix is kept once."""
+    lens, H, Hk, d, page = [200, 200, 200], 4, 1, 64, 64
+    c, table, cu, T, q, _ = cached_case(bbm, lens, [1, 2, 1], H, Hk, d, page, seed=8)
+    table[1, :3] = table[2, :3] = table[0, :3]
+    check_cached(bbm, c, table, lens, cu, T, q, None, H, Hk, d, page)
+
+
+def test_offsets_past_32_bits(bbm):
+    """A cache whose codes take more than 2^32 bytes: its last pages are written, read and attended."""
+    Hk, d, page = 8, 128, 128
+    pages = (1 << 32) // (Hk * page * d // 2) + 64
+    c = bbm.kv4_cache(pages, Hk, d, page)
+    T = 150
+    k, v, q = normal(1, T, Hk, d), normal(2, T, Hk, d), normal(3, 1, Hk, d)
+    slots = np.arange(T) + (pages - 2) * page
+    bbm.bbm_kv4_append(k, v, i32(slots), c)
+    rk, rv = bbm.bbm_kv4_read(i32(slots), c)
+    small = bbm.kv4_cache(2, Hk, d, page)
+    bbm.bbm_kv4_append(k, v, i32(np.arange(T)), small)
+    sk, sv = bbm.bbm_kv4_read(i32(np.arange(T)), small)
+    assert torch.equal(rk, sk) and torch.equal(rv, sv) and not (rk == 0).all()
+    a = bbm.bbm_kv4_attn(q, c, i32([[pages - 2, pages - 1]]), i32([T]), i32([0, 1]))
+    b = bbm.bbm_kv4_attn(q, small, i32([[0, 1]]), i32([T]), i32([0, 1]))
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+# ---- together
+
+
+def layer(bbm, s, w):
+    """A step of one attention layer over the cache: slots, rotary positions, attention of prompts or of new tokens, and the cache behind it."""
+    r = bbm.bbm_build_slots(s["ctx"], s["new"], s["table"], s["free"], s["at"], w.shape[0], s["cache"].k.shape[2])
+    H, Hk, d = s["H"], s["Hk"], s["cache"].k.shape[3] * 2
+    q, k, v = w[:, :H * d].unflatten(1, (H, d)), w[:, H * d:(H + Hk) * d].unflatten(1, (Hk, d)), w[:, (H + Hk) * d:].unflatten(1, (Hk, d))
+    q, k = bbm.bbm_rope(q, k, r.positions, s["freqs"])
+    bbm.bbm_kv4_append(k, v, r.slots, s["cache"])
+    if s["prompt"]:
+        return (r, q, k, v) + bbm.bbm_prompt_attn_fwd(q, k, v, r.cu_new)
+    return (r, q, k, v) + bbm.bbm_kv4_attn(q, s["cache"], s["table"], r.lens, r.cu_new)
+
+
+def test_prompt_then_steps(bbm):
+    H, Hk, d, page, lens = 4, 2, 64, 16, [30, 1, 47, 16]
+    R = len(lens)
+    s = dict(H=H, Hk=Hk, cache=bbm.kv4_cache(40, Hk, d, page), table=i32(np.full((R, 6), -1)), free=i32(np.random.default_rng(1).permutation(40)), at=i32([0]),
+             freqs=bbm.rope_freqs(d)[0], ctx=i32([0] * R), new=i32(lens), prompt=True)
+    w = normal(1, sum(lens) + 3, (H + 2 * Hk) * d)
+    r, q, k, v, o, lse = layer(bbm, s, w)
+    n = {a: f64(t) for a, t in (("q", q), ("k", k), ("v", v))}
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    for h in range(H):
+        for a, b in zip(cu, cu[1:]):
+            seen = np.tril(np.ones((b - a, b - a), bool))
+            x = n["q"][a:b, h], n["k"][a:b, h // 2], n["v"][a:b, h // 2]
+            wo, wl, p = ot.attention(*x, seen, d ** -0.5)
+            e_o, e_l = ot.bounds(*x, seen, d ** -0.5, p, wo, wl)
+            close("O", o[a:b, h], wo, e_o), close("lse", lse[h, a:b], wl, e_l)
+    past = [[n[x][a:b] for a, b in zip(cu, cu[1:])] for x in "kv"]
+    for step, new in enumerate(([1, 1, 1, 1], [1, 0, 3, 1], [2, 1, 1, 0])):
+        s |= dict(ctx=r.lens, at=r.free_next, new=i32(new), prompt=False)
+        w = normal(10 + step, sum(new) + 2, (H + 2 * Hk) * d)
+        r, q, k, v, o, lse = layer(bbm, s, w)
+        cu = np.concatenate([[0], np.cumsum(new)])
+        pos = r.positions.cpu().numpy()
+        assert r.free_next.item() == sum(-(-len(x) // page) for x in past[0]) + sum(-(-(len(x) + m) // page) - -(-len(x) // page) for x, m in zip(past[0], new))
+        for i, (x, t) in enumerate((("k", k), ("v", v))):
+            past[i] = [np.concatenate([y, f64(t)[a:b]]) for y, a, b in zip(past[i], cu, cu[1:])]
+        for i in range(R):
+            a, b, m = cu[i], cu[i + 1], len(past[0][i])
+            assert list(pos[a:b]) == list(range(m - new[i], m))
+            kk, vv = (ot.kv4_decode(*ot.kv4_encode(y[i])) for y in past)
+            seen = np.arange(m) <= m - new[i] + np.arange(new[i])[:, None]
+            for h in range(H):
+                x = f64(q)[a:b, h], kk[:, h // 2], vv[:, h // 2]
+                wo, wl, p = ot.attention(*x, seen, d ** -0.5)
+                if new[i]:
+                    e_o, e_l = ot.bounds(*x, seen, d ** -0.5, p, wo, wl)
+                    close(f"step {step}: O", o[a:b, h], wo, e_o), close("lse", lse[h, a:b], wl, e_l)
+
+
+def test_training_step_through_the_rotation(bbm):
+    """Gradients of w in <attention(rope(q), rope(k), v), d_o>, against differences of the definition in 64 bits."""
+    H, Hk, d, lens = 2, 1, 64, [5, 9]
+    T, cu = sum(lens), np.concatenate([[0], np.cumsum(lens)])
+    pos = np.concatenate([np.arange(n) for n in lens])
+    freqs = bbm.rope_freqs(d)[0]
+    q, k, v, d_o = normal(1, T, H, d), normal(2, T, Hk, d), normal(3, T, Hk, d), normal(4, T, H, d)
+    rq, rk = bbm.bbm_rope(q, k, i32(pos), freqs)
+    o, lse = bbm.bbm_prompt_attn_fwd(rq, rk, v, i32(cu))
+    dq, dk, dv = bbm.bbm_prompt_attn_bwd(rq, rk, v, o, d_o, lse, i32(cu))
+    dq, dk = bbm.bbm_rope(dq, dk, i32(pos), freqs, inverse=True)
+
+    def loss(q, k, v):
+        q, k, total = ot.rope(q, pos, f64(freqs), False), ot.rope(k, pos, f64(freqs), False), 0.0
+        for a, b in zip(cu, cu[1:]):
+            for h in range(H):
+                total += (ot.attention(q[a:b, h], k[a:b, 0], v[a:b, 0], np.tril(np.ones((b - a, b - a), bool)), d ** -0.5)[0] * f64(d_o)[a:b, h]).sum()
+        return total
+    x, grads = [f64(q), f64(k), f64(v)], [f64(dq), f64(dk), f64(dv)]
+    g = np.random.default_rng(0)
+    for at in range(3):
+        step = g.standard_normal(x[at].shape)
+        up, down = (loss(*[y + s * 1e-5 * step if i == at else y for i, y in enumerate(x)]) for s in (1, -1))
+        want, got = (up - down) / 2e-5, (grads[at] * step).sum()
+        # seven roundings to bf16 on the way (rotated q or k, P, dS twice, the gradient, its rotation, O): each moves a term of the sum by at most half
+        # a step; with signs at random over the terms, eight times the root of the sum of squares is far out
+        size = np.sqrt(((np.abs(grads[at]) + np.abs(grads[at]).mean()) ** 2 * step ** 2).sum())
+        assert abs(got - want) <= 8 * 7 * ot.B * size, (at, got, want)
+
+
+@pytest.mark.parametrize("prompt", [True, False])
+def test_graphs_replay(bbm, prompt):
+    """A step recorded into a graph: replays give the eager results bit for bit, with eager work between them and other inputs; two graphs of
+    one stream do not share memory."""
+    H, Hk, d, page, R = 8, 2, 128, 32, 5
+    g = np.random.default_rng(2)
+    ctx, new = ([0] * R, [40, 3, 100, 1, 64]) if prompt else ([700, 33, 4000, 0, 64], [1, 1, 2, 1, 1])
+    T = sum(new) + 4
+
+    def state(seed):
+        s = dict(H=H, Hk=Hk, cache=bbm.kv4_cache(200, Hk, d, page), free=i32(np.arange(160, 200)), at=i32([0]), freqs=bbm.rope_freqs(d)[0], ctx=i32(ctx),
+                 new=i32(new), prompt=prompt, table=i32(np.arange(R * 140).reshape(R, 140) % 160))
+        for t, lo, hi in ((s["cache"].k, 0, 256), (s["cache"].v, 0, 256), (s["cache"].k_scale, 120, 128), (s["cache"].v_scale, 120, 128)):
+            t.copy_(torch.from_numpy(np.random.default_rng(seed).integers(lo, hi, t.shape, dtype=np.uint8)))
+        return s, normal(seed, T, (H + 2 * Hk) * d)
+
+    def step(s, w):
+        r, q, k, v, o, lse = layer(bbm, s, w)
+        n = sum(new)
+        out = [r.slots, r.positions, q, k, o[:n], lse[:, :n]]
+        if prompt:
+            out += [t[:n] for t in bbm.bbm_prompt_attn_bwd(q, k, v, o, q, lse, r.cu_new)]
+        return out
+    states = [state(1), state(2)]
+    want = [[t.clone() for t in step(*s)] for s in states]
+    torch.cuda.synchronize()
+    side, graphs, outs = torch.cuda.Stream(), [], []
+    for s in states:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            outs.append(step(*s))
+    other = torch.cuda.Stream()
+    for replay in range(3):
+        for out in outs:
+            for t in out:
+                t.fill_(5)
+        step(*state(7 + replay))                                           # eager work on the default stream
+        torch.cuda.synchronize()
+        graphs[0].replay()
+        with torch.cuda.stream(other):
+            graphs[1].replay()
+        torch.cuda.synchronize()
+        for i in range(2):
+            for n, (a, b) in enumerate(zip(outs[i], want[i])):
+                assert torch.equal(a, b), (replay, i, n)
+
+
+def test_another_stream(bbm):
+    """Inputs that a stream still writes when the call is made on it."""
+    cu, T, x = prompt_case("ragged", 4, 2, 128, "plain", before=0, behind=0)
+    want = bbm.bbm_prompt_attn_fwd(x["q"], x["k"], x["v"], i32(cu))
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    cuu = i32(cu)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        a = torch.randn(4096, 4096, device="cuda")
+        for _ in range(20):
+            a = a @ a * 1e-3
+        late = x["q"] + (a[0, 0] * 0).to(torch.bfloat16).nan_to_num()
+    late.record_stream(side)
+    got = bbm.bbm_prompt_attn_fwd(late, x["k"], x["v"], cuu, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_binding_refuses(bbm):
+    q, k = normal(1, 4, 4, 64), normal(2, 4, 2, 64)
+    cu, pos, f = i32([0, 4]), i32([0, 1, 2, 3]), bbm.rope_freqs(64)[0]
+    c = bbm.kv4_cache(2, 2, 64, 16)
+    for bad in (lambda: bbm.bbm_prompt_attn_fwd(q.float(), k, k, cu), lambda: bbm.bbm_prompt_attn_fwd(q, k, k[:3], cu), lambda: bbm.bbm_prompt_attn_fwd(q, k, k, cu.long()),
+                lambda: bbm.bbm_prompt_attn_fwd(q.cpu(), k, k, cu), lambda: bbm.bbm_prompt_attn_fwd(q.transpose(0, 2).contiguous().transpose(0, 2), k, k, cu),
+                lambda: bbm.bbm_rope(q, k, pos[:3], f), lambda: bbm.bbm_rope(q, k, pos, f.double()), lambda: bbm.bbm_kv4_append(q, q, pos, c),
+                lambda: bbm.bbm_kv4_append(k, k, pos.long(), c), lambda: bbm.bbm_kv4_attn(q, c, pos[None], i32([4]), i32([0, 4, 4])),
+                lambda: bbm.bbm_kv4_attn(q, c, pos[None], i32([4]), cu, mask=torch.zeros(4, 1, device="cuda")),
+                lambda: bbm.bbm_build_slots(pos, pos[:2], pos[:, None], pos, pos[:1], 4, 16)):
+        with pytest.raises(AssertionError):
+            bad()
+    with pytest.raises(bbm.BbmError):
+        bbm.bbm_prompt_attn_fwd(normal(1, 4, 3, 64), k, k, cu)
+    with pytest.raises(bbm.BbmError):
+        bbm.bbm_rope(normal(1, 4, 4, 72), None, pos, f)
