@@ -1,64 +1,189 @@
 // Causal attention over packed prompts with grouped heads (include/bbm_tokens.h): forward.
-// A wave takes a query row of one head, 64 keys at a time, a key a lane.
+//
+// One pass over the keys with the running maximum and sum of a softmax.  A work-group takes 32 * NW query rows of one head of one sequence, a
+// wave 32 of them, one lane a row (with its partner l ^ 32): the transposed products S^T = K Q^T and O^T += V^T P^T, as in the forward under
+// masks.  Keys come in tiles of 64 through LDS, copied while the tile before is multiplied.  No mask is in memory: the tiles in front of
+// the work-group's first row are seen whole; of those from there on a lane's row gives the keys that it sees.
+// Scores are not rounded between the products: the scale multiplies them inside the exponential, in fp32, one fused multiply-add an
+// element.
 #include "bbm_mfma.h"
-#include "bbm_packed.h"
+#include "bbm_prompt.h"
 
 namespace {
 
-using bbm::bf16x8;
+using bbm::bf16x8, bbm::f32x16, bbm::global, bbm::IntC, bbm::mfma_ring, bbm::partner_sum, bbm::scalar, bbm::TileAddr, bbm::TL;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLazy = 8.0f;  // the running maximum moves when a row exceeds it by a factor of 2^8: P and its sum keep their relative precision
 
 struct PromptParams {
-  const __bf16 *q, *k, *v;
-  __bf16* o;
+  bbm::Rows q, k, v, o;
   float* lse;
-  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;
   const int32_t* cu;
-  int32_t T, R, G;
-  float scale;
+  int32_t T, R, G, H, pieces;
+  float rc;  // softmax_scale * log2(e)
 };
+typedef bbm::InPlace<PromptParams> Args;
 
-constexpr int kRows = 4;  // rows of a work-group, one a wave
+__device__ __forceinline__ float partner_max(float x) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 
-template <int D>
-__global__ __launch_bounds__(64 * kRows) void prompt_fwd_kernel(const PromptParams P) {
-  __shared__ float q_s[kRows][D];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.y, hk = h / P.G;
-  const bbm::Span s = bbm::find_piece(P.cu, P.R, P.T, 1, kRows, blockIdx.x);
-  const int i = s.piece * kRows + wave, t = s.begin + i;
-  const bool live = t < s.end;
-  if (live)
-    for (int e = lane; e < D; e += 64) q_s[wave][e] = (float)P.q[(int64_t)t * P.q_row + h * P.q_head + e];
-  __syncthreads();
-  if (!live) return;
-  float m = -INFINITY, l = 0.0f, o[D / 64] = {};
-  for (int j0 = 0; j0 <= i; j0 += 64) {
-    const int j = j0 + lane;
-    float x = -INFINITY;
-    if (j <= i) {
-      x = 0.0f;
-      const __bf16* const row = P.k + (int64_t)(s.begin + j) * P.k_row + hk * P.k_head;
-      for (int c = 0; c < D; c += 8) {
-        const bf16x8 kk = *reinterpret_cast<const bf16x8*>(row + c);
-        for (int e = 0; e < 8; ++e) x += q_s[wave][c + e] * (float)kk[e];
+template <int D, int NW>
+__global__ __launch_bounds__(NW * 64, NW == 2 ? 1 : D == 64 ? 3 : 2) void prompt_fwd_kernel(const PromptParams) {
+  Args P = bbm::kernel_args<PromptParams>();
+  using L = TL<D>;
+  constexpr int BR = NW * 32, KS = D / 16, DB = D / 32;
+  static_assert(2 * 32 * D <= L::ELEMS, "two 32 x D slabs must fit in a tile buffer");
+  __shared__ __attribute__((aligned(16))) __bf16 k_s0[L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 k_s1[L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 v_s0[L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 v_s1[L::ELEMS];
+
+  const int lane = threadIdx.x & 63, lq = lane & 31, hh = lane >> 5;
+  const int wave = (int)scalar(threadIdx.x >> 6);
+  const bbm::Work work = bbm::work_of(blockIdx.x, P->H);
+  const int h = work.plane;
+  if (work.number >= P->pieces) return;
+  const bbm::Span s = bbm::find_piece(global(P->cu), P->R, P->T, 1, BR, P->pieces - 1 - work.number);  // (long rows first)
+  const int n = s.end - s.begin, row0 = s.piece * BR;
+  if (n <= 0) return;
+  const int wrow = row0 + 32 * wave, wrows = max(0, min(32, n - wrow));  // this wave's rows
+  const int n_tiles = (min(n, row0 + BR) + 63) / 64, n_full = row0 / 64 & ~1;
+  const float rc = P->rc;
+
+  const int k_row = P->k.row, v_row = P->v.row;
+  const __bf16* const kg = global(P->k.p) + h / P->G * P->k.head + (int64_t)s.begin * k_row;
+  const __bf16* const vg = global(P->v.p) + h / P->G * P->v.head + (int64_t)s.begin * v_row;
+  bbm::TileCopy<D, NW> kc, vc;
+  kc.init(wave, lane, k_row);
+  vc.init(wave, lane, v_row);
+  constexpr int LPW = bbm::TileCopy<D, NW>::PIECES;
+  auto copy_piece = [&](int jt, int rows, __bf16* kd, __bf16* vd, int i) {
+    if (i < LPW)
+      kc.piece(kg + (int64_t)jt * 64 * k_row, rows, k_row, kd, i, wave);
+    else
+      vc.piece(vg + (int64_t)jt * 64 * v_row, rows, v_row, vd, i - LPW, wave);
+  };
+  auto rows_at = [&](int jt) { return jt < n_tiles ? bbm::rows_of_tile(jt * 64, n) : 0; };
+
+  // Q by way of the buffers of parity 1, the first tile into those of parity 0
+  __bf16* const q_stage = (wave / 2 == 0 ? k_s1 : v_s1) + wave % 2 * 32 * D;
+  bbm::copy_slab<D>(global(P->q.p) + h * P->q.head + (int64_t)(s.begin + wrow) * P->q.row, wrows, P->q.row, q_stage, lane);
+#pragma unroll
+  for (int i = 0; i < 2 * LPW; ++i) copy_piece(0, rows_at(0), k_s0, v_s0, i);
+  TileAddr<D> A;
+  A.init(lane);
+  bf16x8 qf[KS];
+  f32x16 oacc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+    for (int e = 0; e < 16; ++e) oacc[db][e] = 0.0f;
+  float m_run = -INFINITY, nm = 0.0f, l_run = 0.0f;  // running maximum in exponent units; what is added to exponents: its negative, or 0
+  __builtin_amdgcn_s_waitcnt(0);
+#pragma unroll
+  for (int t = 0; t < KS; ++t) qf[t] = bbm::slab_frag<D>(q_stage, t, lane);
+
+  auto step = [&](auto pb, auto part, int jt) __attribute__((always_inline)) {
+    constexpr int PB = decltype(pb)::value;
+    constexpr bool PART = decltype(part)::value != 0;
+    __builtin_amdgcn_s_waitcnt(0);  // this wave's copies of the tile have landed
+    __syncthreads();                // ... and everyone's; every wave is done with the buffers refilled below
+    __bf16* const k_cur = PB ? k_s1 : k_s0;
+    __bf16* const v_cur = PB ? v_s1 : v_s0;
+    __bf16* const k_oth = PB ? k_s0 : k_s1;
+    __bf16* const v_oth = PB ? v_s0 : v_s1;
+    // the next tile's copies go out between the matrix instructions of the first product; behind the last tile they copy zero rows
+    const int rows1 = rows_at(jt + 1);
+    const bool live = wrows > 0 && (!PART || jt * 64 < wrow + wrows);
+    if (!live) {
+#pragma unroll
+      for (int i = 0; i < 2 * LPW; ++i) copy_piece(jt + 1, rows1, k_oth, v_oth, i);
+      return;
+    }
+    f32x16 sc[2];
+    __builtin_amdgcn_s_setprio(2);
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+      for (int e = 0; e < 16; ++e) sc[kb][e] = 0.0f;
+    mfma_ring<2 * KS, 4>([&](auto i) { return A.row_frag(k_cur, decltype(i)::value & 1, decltype(i)::value >> 1); },
+                         [&](auto i, bf16x8 f) {
+                           constexpr int x = decltype(i)::value;
+                           sc[x & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[x >> 1], sc[x & 1], 0, 0, 0);
+                         },
+                         [&](auto i) {
+                           constexpr int x = decltype(i)::value, GAP = 2 * KS / (2 * LPW) ? 2 * KS / (2 * LPW) : 1, PER = 2 * LPW > 2 * KS ? LPW / KS : 1;
+                           if constexpr (x % GAP == 0) {
+#pragma unroll
+                             for (int y = 0; y < PER; ++y) copy_piece(jt + 1, rows1, k_oth, v_oth, x / GAP * PER + y);
+                           }
+                         });
+    __builtin_amdgcn_s_setprio(0);
+    if constexpr (PART) {
+      const uint64_t seen = bbm::bits_up_to(wrow + lq - jt * 64);
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const uint32_t w = (uint32_t)(seen >> (32 * kb)) >> (4 * hh);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[kb][e] = bbm::keep_if(w, e, sc[kb][e]);
       }
-      x *= P.scale;
     }
-    float top = x;
-    for (int b = 32; b; b >>= 1) top = fmaxf(top, __shfl_xor(top, b));
-    const float m_new = fmaxf(m, top), alpha = __expf(m - m_new), p = __expf(x - m_new);
-    float sum = p;
-    for (int b = 32; b; b >>= 1) sum += __shfl_xor(sum, b);
-    l = l * alpha + sum;
-    m = m_new;
-    for (int e = 0; e < D / 64; ++e) o[e] *= alpha;
-    for (int jj = 0; jj < min(64, i + 1 - j0); ++jj) {
-      const float pj = __shfl(p, jj);
-      const __bf16* const row = P.v + (int64_t)(s.begin + j0 + jj) * P.v_row + hk * P.v_head;
-      for (int e = 0; e < D / 64; ++e) o[e] += pj * (float)row[e * 64 + lane];
+    float mx = sc[0][0];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[kb][e]);
+    mx = partner_max(mx) * rc;
+    if (__any(mx > m_run + kLazy ? 1 : 0)) {
+      const float m_new = fmaxf(m_run, mx), m_fin = m_new == -INFINITY ? 0.0f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_fin);
+      l_run *= alpha;
+      m_run = m_new;
+      nm = -m_fin;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        for (int e = 0; e < 16; ++e) oacc[db][e] *= alpha;
     }
+    __builtin_amdgcn_s_setprio(1);
+    // the exponentials of 16 keys behind the matrix instructions of the 16 before
+    bf16x8 pf[2];
+    auto exps = [&](int u, int e0, int e1) {
+#pragma unroll
+      for (int e = e0; e < e1; ++e) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[u / 2][8 * (u % 2) + e], rc, nm));
+        l_run += p;  // (before it is rounded: the log-sum-exp is an fp32 result)
+        pf[u & 1][e] = (__bf16)p;
+      }
+    };
+    exps(0, 0, 8);
+    mfma_ring<4 * DB, 3>([&](auto i) { return A.tr_frag(v_cur, decltype(i)::value / DB, decltype(i)::value % DB); },
+                         [&](auto i, bf16x8 f) {
+                           constexpr int x = decltype(i)::value;
+                           oacc[x % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pf[x / DB & 1], oacc[x % DB], 0, 0, 0);
+                         },
+                         [&](auto i) {
+                           constexpr int x = decltype(i)::value, PER = 8 / DB;
+                           if constexpr (x / DB < 3) exps(x / DB + 1, x % DB * PER, (x % DB + 1) * PER);
+                         });
+    __builtin_amdgcn_s_setprio(0);
+  };
+
+  // tiles seen whole, two at a time (the buffers change places with every tile), then one or two that are not, or of which one is
+#pragma unroll 1
+  for (int jt = 0; jt < n_full; jt += 2) {
+    step(IntC<0>{}, IntC<0>{}, jt);
+    step(IntC<1>{}, IntC<0>{}, jt + 1);
   }
-  for (int e = 0; e < D / 64; ++e) P.o[(int64_t)t * P.o_row + h * P.o_head + e * 64 + lane] = (__bf16)(o[e] / l);
-  if (P.lse && lane == 0) P.lse[(int64_t)h * P.T + t] = m + __logf(l);
+  step(IntC<0>{}, IntC<1>{}, n_full);
+  if (n_full + 1 < n_tiles) step(IntC<1>{}, IntC<1>{}, n_full + 1);
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();  // the output is staged in the tile buffers
+  if (wrows == 0) return;
+  const float l_tot = partner_sum(l_run);
+  __bf16* const stage = (wave / 2 == 0 ? k_s0 : v_s0) + wave % 2 * 32 * D;
+  bbm::store_strided<D>(oacc, 1.0f / l_tot, stage, global(P->o.p) + h * P->o.head + (int64_t)(s.begin + wrow) * P->o.row, wrows, P->o.row, lane);
+  if (global(P->lse) && hh == 0 && lq < wrows) global(P->lse)[(int64_t)h * P->T + s.begin + wrow + lq] = (m_run + __log2f(l_tot)) * kLn2;
 }
 
 }  // namespace
@@ -71,20 +196,21 @@ extern "C" __attribute__((visibility("default"))) int bbm_prompt_attn_fwd(const 
   clear_error();
   if (int rc = check_tokens(fn, T, R, cu, H, Hk)) return rc;
   if (d != 64 && d != 128) return fail(BBM_EUNSUPPORTED, "%s: d=%d has no kernel instance (64, 128)", fn, d);
-  if (int rc = check_packed(fn, "q", q, T, H, d, false)) return rc;
-  if (int rc = check_packed(fn, "k", k, T, Hk, d, false)) return rc;
-  if (int rc = check_packed(fn, "v", v, T, Hk, d, false)) return rc;
-  if (int rc = check_packed(fn, "o", o, T, H, d, true)) return rc;
+  if (int rc = check_rows(fn, "q", q, T, H, d, false)) return rc;
+  if (int rc = check_rows(fn, "k", k, T, Hk, d, false)) return rc;
+  if (int rc = check_rows(fn, "v", v, T, Hk, d, false)) return rc;
+  if (int rc = check_rows(fn, "o", o, T, H, d, true)) return rc;
   if (!aligned(lse, 4)) return fail(BBM_EINVAL, "%s: lse must be 4-byte aligned", fn);
   if (!(softmax_scale > 0.0f) || !(softmax_scale < INFINITY)) return fail(BBM_EINVAL, "%s: softmax_scale must be finite and > 0", fn);
   if (T == 0) return BBM_OK;
   PromptParams P;
-  P.q = static_cast<const __bf16*>(q->ptr), P.k = static_cast<const __bf16*>(k->ptr), P.v = static_cast<const __bf16*>(v->ptr), P.o = static_cast<__bf16*>(o->ptr);
-  P.q_row = q->row_stride, P.q_head = q->head_stride, P.k_row = k->row_stride, P.k_head = k->head_stride;
-  P.v_row = v->row_stride, P.v_head = v->head_stride, P.o_row = o->row_stride, P.o_head = o->head_stride;
-  P.lse = lse, P.cu = cu, P.T = (int32_t)T, P.R = (int32_t)R, P.G = (int32_t)(H / Hk), P.scale = softmax_scale;
-  const dim3 grid((unsigned)count_pieces(T, R, 1, kRows), (unsigned)H);
-  if (d == 64) prompt_fwd_kernel<64><<<grid, 64 * kRows, 0, static_cast<hipStream_t>(stream)>>>(P);
-  else prompt_fwd_kernel<128><<<grid, 64 * kRows, 0, static_cast<hipStream_t>(stream)>>>(P);
+  P.q = rows_of(q, T, d), P.k = rows_of(k, T, d), P.v = rows_of(v, T, d), P.o = rows_of(o, T, d);
+  P.lse = lse, P.cu = cu, P.T = (int32_t)T, P.R = (int32_t)R, P.G = (int32_t)(H / Hk), P.H = (int32_t)H, P.rc = softmax_scale * kLog2e;
+  const int64_t pieces = count_pieces(T, R, 1, 128), wgs = work_groups(H, pieces);
+  if (wgs >= 1ll << 31) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld)", fn, (long long)T, (long long)H);
+  P.pieces = (int32_t)pieces;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (d == 64) prompt_fwd_kernel<64, 4><<<(unsigned)wgs, 256, 0, s>>>(P);
+  else prompt_fwd_kernel<128, 4><<<(unsigned)wgs, 256, 0, s>>>(P);
   return launch_status(fn);
 }
