@@ -51,7 +51,7 @@ struct TileCopy {
     const int blk = n * NW + wave, part = n * NW >> 2 & 3;
     const int bytes = rows > 0 ? ((rows - 1) * stride + D) * 2 : 0;
     uint32_t at = row_off;
-    asm volatile("" : "+v"(at));  // one register throughout the tile loop, not one for every instruction
+    asm volatile("" : "+v"(at));  // one register, not one for every instruction
     copy_async<16>(tile, bytes, at + (uint32_t)(n * NW * stride) * 2u + ((uint32_t)(chunk ^ part) << 4), dst + blk * L::TBLK);
   }
 };

@@ -1,120 +1,456 @@
 // Causal attention over packed prompts with grouped heads (include/bbm_tokens.h): gradients.
-// A wave takes a query row (dQ) or a key row (dK, dV), 64 keys or queries at a time, one a lane.
+//
+// With P = exp(scale Q K^T - lse) on the pairs that are seen, dP = dO V^T, D_i = <dO_i, O_i>, dS = P o (dP - D):
+//   dV = P^T dO,   dK = scale * dS^T Q,   dQ = scale * dS K,   dK and dV summed over the heads of a group.
+// Two kernels, both without atomics, so that results do not depend on an order:
+//   dq kernel   a work-group takes 128 query rows of one head, a lane a row, and walks its tiles of 64 keys: S^T = K Q^T, dP^T = V dO^T,
+//               dQ^T += K^T dS^T.  It leaves -D and -lse / scale in the workspace for the other one.
+//   dkv kernel  a work-group takes 64 keys of one key head and walks the tiles of 64 queries of every head of the group, a wave 32 keys and
+//               32 queries of a tile: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS, all in its registers.
+// Each step is one chain of matrix instructions with the copies of the next tile, the exponentials and the roundings behind them.  As in the forward
+// the scale multiplies the scores inside the exponential in fp32; P and dS are rounded to bf16 for the products that they enter.
 #include "bbm_mfma.h"
-#include "bbm_packed.h"
+#include "bbm_prompt.h"
 
 namespace {
 
-using bbm::bf16x8;
+using bbm::bf16x8, bbm::buffer_of, bbm::copy_async, bbm::f32x16, bbm::global, bbm::IntC, bbm::lane_now, bbm::mfma_ring, bbm::operand, bbm::pack, bbm::Rows,
+    bbm::scalar, bbm::TileAddr, bbm::TL;
 
-struct Tensor {
-  __bf16* p;
-  int64_t row, head;
-  __device__ __forceinline__ __bf16* at(int64_t t, int h) const { return p + t * row + h * head; }
-};
+constexpr float kLog2e = 1.4426950408889634f;
 
 struct PromptBwdParams {
-  Tensor q, k, v, o, d_o, dq, dk, dv;
+  Rows q, k, v, o, d_o, dq, dk, dv;
   const float* lse;
-  float* delta;  // [H][T]
+  float* nls;     // workspace [H][T]: -lse / scale, what the scores start at
+  float* ndelta;  // workspace [H][T]: -<dO, O>
   const int32_t* cu;
-  int32_t T, R, G;
+  int32_t T, R, G, H, row_pieces, key_pieces;
+  float rc;  // softmax_scale * log2(e)
   float scale;
 };
-
-constexpr int kRows = 4;
+typedef bbm::InPlace<PromptBwdParams> Args;
 
 template <int D>
-__device__ __forceinline__ float dot(const float* a, const __bf16* row) {
-  float x = 0.0f;
-  for (int c = 0; c < D; c += 8) {
-    const bf16x8 b = *reinterpret_cast<const bf16x8*>(row + c);
-    for (int e = 0; e < 8; ++e) x += a[c + e] * (float)b[e];
+__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dq_kernel(const PromptBwdParams) {
+  Args P = bbm::kernel_args<PromptBwdParams>();
+  using L = TL<D>;
+  constexpr int NW = 4, BR = 32 * NW, KS = D / 16, DB = D / 32, RC = D / 8, RPB = 64 / RC;
+  __shared__ __attribute__((aligned(16))) __bf16 k_s0[L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 k_s1[L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 v_s0[L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 v_s1[L::ELEMS];
+  __shared__ float delta_s[NW][32];
+
+  const int lane = threadIdx.x & 63, lq = lane & 31, hh = lane >> 5;
+  const int wave = (int)scalar(threadIdx.x >> 6);
+  const bbm::Work work = bbm::work_of(blockIdx.x, P->H);
+  const int h = work.plane;
+  if (work.number >= P->row_pieces) return;
+  const bbm::Span s = bbm::find_piece(global(P->cu), P->R, P->T, 1, BR, P->row_pieces - 1 - work.number);
+  const int n = s.end - s.begin, row0 = s.piece * BR;
+  if (n <= 0) return;
+  const int wrow = row0 + 32 * wave, wrows = max(0, min(32, n - wrow));
+  const int n_tiles = (min(n, row0 + BR) + 63) / 64, n_full = row0 / 64;
+  const float rc = P->rc;
+
+  const int k_row = P->k.row, v_row = P->v.row;
+  const __bf16* const kg = global(P->k.p) + h / P->G * P->k.head + (int64_t)s.begin * k_row;
+  const __bf16* const vg = global(P->v.p) + h / P->G * P->v.head + (int64_t)s.begin * v_row;
+  bbm::TileCopy<D, NW> kc, vc;
+  kc.init(wave, lane, k_row);
+  vc.init(wave, lane, v_row);
+  constexpr int LPW = bbm::TileCopy<D, NW>::PIECES;
+  auto copy_piece = [&](int jt, int rows, __bf16* kd, __bf16* vd, int i) {
+    if (i < LPW)
+      kc.piece(kg + (int64_t)jt * 64 * k_row, rows, k_row, kd, i, wave);
+    else
+      vc.piece(vg + (int64_t)jt * 64 * v_row, rows, v_row, vd, i - LPW, wave);
+  };
+  auto rows_at = [&](int jt) { return jt < n_tiles ? bbm::rows_of_tile(jt * 64, n) : 0; };
+
+  // This lane's query as operands, Q by way of the buffers of parity 1, dO through registers, where <dO, O> is formed, to the same place.
+  TileAddr<D> A;
+  A.init(lane);
+  bf16x8 qf[KS], dof[KS];
+  float nl, nd;
+  {
+    __bf16* const stage = (wave / 2 == 0 ? k_s1 : v_s1) + wave % 2 * 32 * D;
+    const int64_t t0 = s.begin + wrow;
+    bbm::copy_slab<D>(global(P->q.p) + h * P->q.head + t0 * P->q.row, wrows, P->q.row, stage, lane);
+    const int g_row = lane / RC, g_chunk = lane % RC;
+    const __amdgpu_buffer_rsrc_t do_r = buffer_of(global(P->d_o.p) + h * P->d_o.head + t0 * P->d_o.row, wrows > 0 ? ((wrows - 1) * P->d_o.row + D) * 2 : 0);
+    const __amdgpu_buffer_rsrc_t o_r = buffer_of(global(P->o.p) + h * P->o.head + t0 * P->o.row, wrows > 0 ? ((wrows - 1) * P->o.row + D) * 2 : 0);
+    const int64_t row_at = (int64_t)h * P->T + t0;
+    const float lse = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer_of(P->lse + row_at, wrows * 4), lq * 4, 0, 0));
+    bf16x8 gr[32 / RPB], orow[32 / RPB];
+#pragma unroll
+    for (int i = 0; i < 32 / RPB; ++i) {
+      const int r = i * RPB + g_row;
+      gr[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(do_r, (r * P->d_o.row + g_chunk * 8) * 2, 0, 0));
+      orow[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(o_r, (r * P->o.row + g_chunk * 8) * 2, 0, 0));
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * LPW; ++i) copy_piece(0, rows_at(0), k_s0, v_s0, i);
+#pragma unroll
+    for (int i = 0; i < 32 / RPB; ++i) {
+      float x = 0.0f;
+      for (int e = 0; e < 8; ++e) x += (float)gr[i][e] * (float)orow[i][e];
+      x = bbm::row_sum<RC>(x);
+      if (g_chunk == 0) delta_s[wave][i * RPB + g_row] = x;
+    }
+    __builtin_amdgcn_s_waitcnt(0);  // this wave's own copies have landed (no other wave touches its slab)
+#pragma unroll
+    for (int t = 0; t < KS; ++t) qf[t] = bbm::slab_frag<D>(stage, t, lane);
+#pragma unroll
+    for (int i = 0; i < 32 / RPB; ++i) {
+      const int r = i * RPB + g_row;
+      *reinterpret_cast<bf16x8*>(stage + r * D + (g_chunk ^ r % RC) * 8) = gr[i];
+    }
+#pragma unroll
+    for (int t = 0; t < KS; ++t) dof[t] = bbm::slab_frag<D>(stage, t, lane);
+    nl = -lse * kLog2e;
+    nd = -delta_s[wave][lq];
+    if (hh == 0) {
+      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(nl / rc), buffer_of(P->nls + row_at, wrows * 4), lq * 4, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(nd), buffer_of(P->ndelta + row_at, wrows * 4), lq * 4, 0, 0);
+    }
   }
-  return x;
-}
+  f32x16 dq[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+    for (int e = 0; e < 16; ++e) dq[db][e] = 0.0f;
 
-template <int D>
-__global__ __launch_bounds__(64 * kRows) void prompt_dq_kernel(const PromptBwdParams P) {
-  __shared__ float q_s[kRows][D], g_s[kRows][D];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.y, hk = h / P.G;
-  const bbm::Span s = bbm::find_piece(P.cu, P.R, P.T, 1, kRows, blockIdx.x);
-  const int i = s.piece * kRows + wave, t = s.begin + i;
-  const bool live = t < s.end;
-  float delta = 0.0f;
-  if (live)
-    for (int e = lane; e < D; e += 64) {
-      q_s[wave][e] = (float)P.q.at(t, h)[e];
-      g_s[wave][e] = (float)P.d_o.at(t, h)[e];
-      delta += g_s[wave][e] * (float)P.o.at(t, h)[e];
+  // One tile: a chain of matrix instructions over its two halves of 32 keys, S0, dP0, S1, dP1, dQ0, dQ1, with the exponentials of a half behind its
+  // dP, dS0 behind S1, dS1 behind dQ0.
+  auto step = [&](auto pb, auto part, int jt) __attribute__((always_inline)) {
+    constexpr int PB = decltype(pb)::value;
+    constexpr bool PART = decltype(part)::value != 0;
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    __bf16* const k_cur = PB ? k_s1 : k_s0;
+    __bf16* const v_cur = PB ? v_s1 : v_s0;
+    __bf16* const k_oth = PB ? k_s0 : k_s1;
+    __bf16* const v_oth = PB ? v_s0 : v_s1;
+    const int rows1 = rows_at(jt + 1);
+    const bool live = wrows > 0 && (!PART || jt * 64 < wrow + wrows);
+    if (!live) {
+#pragma unroll
+      for (int i = 0; i < 2 * LPW; ++i) copy_piece(jt + 1, rows1, k_oth, v_oth, i);
+      return;
     }
-  __syncthreads();
-  if (!live) return;
-  for (int b = 32; b; b >>= 1) delta += __shfl_xor(delta, b);
-  if (lane == 0) P.delta[(int64_t)h * P.T + t] = delta;
-  const float lse = P.lse[(int64_t)h * P.T + t];
-  float dq[D / 64] = {};
-  for (int j0 = 0; j0 <= i; j0 += 64) {
-    const int j = j0 + lane;
-    float ds = 0.0f;
-    if (j <= i) {
-      const float p = __expf(dot<D>(q_s[wave], P.k.at(s.begin + j, hk)) * P.scale - lse);
-      ds = p * (dot<D>(g_s[wave], P.v.at(s.begin + j, hk)) - delta);
+    constexpr int N1 = KS, N2 = 2 * KS, N3 = 3 * KS, N4 = 4 * KS, N5 = N4 + 2 * DB, N6 = N5 + 2 * DB;
+    constexpr int PER = D == 128 ? 4 : 8;  // elements behind a matrix instruction
+    static_assert(PER * (KS - 2) >= 16 && PER * (2 * DB - 2) >= 16, "all 16 must find room");
+    f32x16 sc[2], dp[2];
+    uint32_t dsf[2][2][4];  // dS of [half][16-key step], pairs of bf16
+    uint32_t seen[2] = {0, 0};
+    if constexpr (PART) {
+      const uint64_t bits = bbm::bits_up_to(wrow + lq - jt * 64) >> (4 * hh);
+      seen[0] = (uint32_t)bits, seen[1] = (uint32_t)(bits >> 32);
     }
-    for (int jj = 0; jj < min(64, i + 1 - j0); ++jj) {
-      const float x = __shfl(ds, jj);
-      const __bf16* const row = P.k.at(s.begin + j0 + jj, hk);
-      for (int e = 0; e < D / 64; ++e) dq[e] += x * (float)row[e * 64 + lane];
-    }
-  }
-  for (int e = 0; e < D / 64; ++e) P.dq.at(t, h)[e * 64 + lane] = (__bf16)(dq[e] * P.scale);
-}
-
-template <int D>
-__global__ __launch_bounds__(64 * kRows) void prompt_dkv_kernel(const PromptBwdParams P) {
-  __shared__ float k_s[kRows][D], v_s[kRows][D];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hk = blockIdx.y;
-  const bbm::Span s = bbm::find_piece(P.cu, P.R, P.T, 1, kRows, blockIdx.x);
-  const int j = s.piece * kRows + wave, t = s.begin + j, n = s.end - s.begin;
-  const bool live = t < s.end;
-  if (live)
-    for (int e = lane; e < D; e += 64) {
-      k_s[wave][e] = (float)P.k.at(t, hk)[e];
-      v_s[wave][e] = (float)P.v.at(t, hk)[e];
-    }
-  __syncthreads();
-  if (!live) return;
-  float dk[D / 64] = {}, dv[D / 64] = {};
-  for (int h = hk * P.G; h < (hk + 1) * P.G; ++h)
-    for (int i0 = j; i0 < n; i0 += 64) {
-      const int i = i0 + lane;
-      float p = 0.0f, ds = 0.0f;
-      if (i < n) {
-        const int64_t at = (int64_t)h * P.T + s.begin + i;
-        p = __expf(dot<D>(k_s[wave], P.q.at(s.begin + i, h)) * P.scale - P.lse[at]);
-        ds = p * (dot<D>(v_s[wave], P.d_o.at(s.begin + i, h)) - P.delta[at]);
+    auto start = [&](f32x16& acc, float x) {
+      asm volatile("" : "+v"(x));
+      for (int e = 0; e < 16; ++e) acc[e] = x;
+    };
+    auto exps = [&](int kb, int slot) {
+#pragma unroll
+      for (int e = slot * PER; e < min(16, (slot + 1) * PER); ++e) {
+        if constexpr (PART) sc[kb][e] = bbm::keep_if(seen[kb], e, sc[kb][e]);
+        sc[kb][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kb][e], rc, nl));
       }
-      for (int ii = 0; ii < min(64, n - i0); ++ii) {
-        const float pi = __shfl(p, ii), di = __shfl(ds, ii);
-        const __bf16* const g = P.d_o.at(s.begin + i0 + ii, h);
-        const __bf16* const q = P.q.at(s.begin + i0 + ii, h);
-        for (int e = 0; e < D / 64; ++e) {
-          dv[e] += pi * (float)g[e * 64 + lane];
-          dk[e] += di * (float)q[e * 64 + lane];
+    };
+    auto ds = [&](int kb, int slot) {
+#pragma unroll
+      for (int e = slot * PER; e < min(16, (slot + 1) * PER); e += 2)
+        dsf[kb][e / 8][e % 8 / 2] = pack(sc[kb][e] * dp[kb][e], sc[kb][e + 1] * dp[kb][e + 1]);
+    };
+    mfma_ring<N6, 3>(
+        [&](auto i) {
+          constexpr int x = decltype(i)::value;
+          if constexpr (x < N4)
+            return A.row_frag(x / KS % 2 ? v_cur : k_cur, x / N2, x % KS);
+          else
+            return A.tr_frag(k_cur, (x - N4) / DB, (x - N4) % DB);
+        },
+        [&](auto i, bf16x8 f) {
+          constexpr int x = decltype(i)::value;
+          if constexpr (x % N2 == 0 && x < N4) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[x / N2][e] = 0.0f;
+          }
+          if constexpr (x == N1) start(dp[0], nd);
+          if constexpr (x == N3) start(dp[1], nd);
+          if constexpr (x < N4 && x / KS % 2 == 0) {
+            sc[x / N2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[x % KS], sc[x / N2], 0, 0, 0);
+          } else if constexpr (x < N4) {
+            dp[x / N2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, dof[x % KS], dp[x / N2], 0, 0, 0);
+          } else {
+            constexpr int m = x - N4, u = m / DB;
+            dq[m % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, operand(dsf[u / 2][u % 2]), dq[m % DB], 0, 0, 0);
+          }
+        },
+        [&](auto i) {
+          constexpr int x = decltype(i)::value;
+          if constexpr (x < 2 * LPW) copy_piece(jt + 1, rows1, k_oth, v_oth, x);
+          // a product is complete two matrix instructions after its last one was issued
+          if constexpr (x >= N1 + 2 && x < N2) exps(0, x - N1 - 2);
+          if constexpr (x >= N2 + 2 && x < N3) ds(0, x - N2 - 2);
+          if constexpr (x >= N3 + 2 && x < N4) exps(1, x - N3 - 2);
+          if constexpr (x >= N4 + 2 && x < N5) ds(1, x - N4 - 2);
+        });
+  };
+#pragma unroll 1
+  for (int jt = 0; jt < n_full; jt += 2) {
+    step(IntC<0>{}, IntC<0>{}, jt);
+    step(IntC<1>{}, IntC<0>{}, jt + 1);
+  }
+  step(IntC<0>{}, IntC<1>{}, n_full);
+  if (n_full + 1 < n_tiles) step(IntC<1>{}, IntC<1>{}, n_full + 1);
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();  // the result is staged in the tile buffers
+  if (wrows == 0) return;
+  __bf16* const stage = (wave / 2 == 0 ? k_s0 : v_s0) + wave % 2 * 32 * D;
+  bbm::store_strided<D>(dq, P->scale, stage, global(P->dq.p) + h * P->dq.head + (int64_t)(s.begin + wrow) * P->dq.row, wrows, P->dq.row, lane);
+}
+
+// Registers are what this form lives by.  D = 128: 256, two pieces of the K operand in LDS, two waves a SIMD; D = 64: 168, three.
+template <int D>
+__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dkv_kernel(const PromptBwdParams) {
+  Args P = bbm::kernel_args<PromptBwdParams>();
+  using L = TL<D>;
+  constexpr int NW = 4, KS = D / 16, DB = D / 32, REGS = DB * 16;
+  static_assert(2 * 32 * D <= L::ELEMS, "two 32 x D slabs must fit in a tile buffer");
+  __shared__ __attribute__((aligned(16))) __bf16 t_s0[2 * L::ELEMS];  // [Q, dO] tiles, one variable per parity
+  __shared__ __attribute__((aligned(16))) __bf16 t_s1[2 * L::ELEMS];
+  __shared__ __attribute__((aligned(16))) float st_s0[2 * 64];  // [-lse / scale, -D] of the tile's queries
+  __shared__ __attribute__((aligned(16))) float st_s1[2 * 64];
+  constexpr int KL = D == 128 ? 2 : 0;  // the last pieces of the K operand, which find no room in the registers
+  __shared__ __attribute__((aligned(16))) bf16x8 kl_s[KL ? KL : 1][NW][64];
+
+  const int lane = threadIdx.x & 63;
+  const int wave = (int)scalar(threadIdx.x >> 6);
+  const int kh = wave & 1;   // key half of the tile
+  const int qh = wave >> 1;  // query half of a tile; behind the last one, 0: this wave writes dV, 1: dK
+  const float rc = P->rc;
+  const bbm::Work work = bbm::work_of(blockIdx.x, P->H / P->G);
+  const int hk = work.plane;
+  if (work.number >= P->key_pieces) return;
+  const bbm::Span s = bbm::find_piece(global(P->cu), P->R, P->T, 1, 64, work.number);  // (early keys first: most queries see them)
+  const int n = s.end - s.begin, j = s.piece;
+  if (n <= 0) return;
+  const int per_head = (n + 63) / 64 - j, n_steps = per_head * P->G;  // tiles of queries from the diagonal on
+
+  const int q_row = P->q.row, g_row = P->d_o.row, T = P->T;
+  const __bf16* const qg = global(P->q.p) + (int64_t)hk * P->G * P->q.head + (int64_t)s.begin * q_row;
+  const __bf16* const gg = global(P->d_o.p) + (int64_t)hk * P->G * P->d_o.head + (int64_t)s.begin * g_row;
+  const int64_t st0 = (int64_t)hk * P->G * T + s.begin;
+  const int64_t q_head = P->q.head, g_head = P->d_o.head;
+  constexpr int LPW = bbm::TileCopy<D, NW>::PIECES;
+  // the queries from row `row` on of head g of the group; queries past the end come as zeros everywhere, and add exact zeros
+  // (where a lane copies what is found anew for every tile: its registers are free for the rest of the step)
+  bbm::TileCopy<D, NW> qc, gc;
+  auto copy_from = [&]() __attribute__((always_inline)) {
+    const int ln = lane_now();
+    qc.init(wave, ln, q_row);
+    gc.init(wave, ln, g_row);
+  };
+  auto copy_piece = [&](int g, int row, int rows, __bf16* td, int i) {
+    if (i < LPW)
+      qc.piece(qg + g * q_head + (int64_t)row * q_row, rows, q_row, td, i, wave);
+    else
+      gc.piece(gg + g * g_head + (int64_t)row * g_row, rows, g_row, td + L::ELEMS, i - LPW, wave);
+  };
+  auto copy_stats = [&](int g, int row, int rows, float* sts) __attribute__((always_inline)) {
+    if (qh == 0) copy_async<4>((kh == 0 ? global(P->nls) : global(P->ndelta)) + st0 + (int64_t)g * T + row, rows * 4, lane_now() * 4, sts + kh * 64);
+  };
+
+  TileAddr<D> A;
+  A.init(lane);
+  bf16x8 kf[KS - KL], vf[KS];
+  f32x16 dk[DB], dv[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+    for (int e = 0; e < 16; ++e) dk[db][e] = dv[db][e] = 0.0f;
+  {
+    const int rows0 = bbm::rows_of_tile(j * 64, n);
+    copy_stats(0, j * 64, rows0, st_s0);
+    copy_from();
+#pragma unroll
+    for (int i = 0; i < 2 * LPW; ++i) copy_piece(0, j * 64, rows0, t_s0, i);
+    // K and V come through the buffers of parity 1
+    bbm::TileCopy<D, NW> c;
+    c.init(wave, lane, P->k.row);
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) c.piece(global(P->k.p) + hk * P->k.head + (int64_t)(s.begin + j * 64) * P->k.row, rows0, P->k.row, t_s1, i, wave);
+    c.init(wave, lane, P->v.row);
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) c.piece(global(P->v.p) + hk * P->v.head + (int64_t)(s.begin + j * 64) * P->v.row, rows0, P->v.row, t_s1 + L::ELEMS, i, wave);
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    // this lane's key: K and V as operands
+#pragma unroll
+    for (int t = 0; t < KS; ++t) {
+      const bf16x8 kt = A.row_frag(t_s1, kh, t);
+      vf[t] = A.row_frag(t_s1 + L::ELEMS, kh, t);
+      if (t >= KS - KL)
+        kl_s[t - (KS - KL)][wave][lane] = kt;  // (read back by this wave alone)
+      else
+        kf[t < KS - KL ? t : 0] = kt;
+    }
+  }
+  for (int i = 0; i < 2; ++i) {  // from here on, this wave's half of the queries
+    A.ra[i] += qh * (32 / L::NBLK) * D;
+    A.ta[i] += 2 * qh * (D == 64 ? 2 * D : D);
+  }
+
+  // Head by head, the tile on the diagonal first.  i0: this tile's place among the head's; g1, i1: the next one's.
+  int i0 = 0, g1 = 0, i1 = 0;
+  auto step = [&](auto pb) __attribute__((always_inline)) {
+    constexpr int PB = decltype(pb)::value;
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    __bf16* const q_cur = PB ? t_s1 : t_s0;
+    __bf16* const g_cur = q_cur + L::ELEMS;
+    __bf16* const t_oth = PB ? t_s0 : t_s1;
+    const float* const nl_cur = (PB ? st_s1 : st_s0) + 32 * qh;
+    const float* const nd_cur = nl_cur + 64;
+    const bool diagonal = i0 == 0;
+    if (++i1 == per_head) i1 = 0, ++g1;
+    i0 = i1;
+    const bool more = g1 < P->G;
+    const int gn = more ? g1 : 0, row1 = more ? (j + i1) * 64 : 0, rows1 = more ? bbm::rows_of_tile(row1, n) : 0;
+    if (more) copy_stats(gn, row1, rows1, PB ? st_s0 : st_s1);
+    copy_from();
+    const bool live = scalar(!diagonal || kh <= qh) != 0;  // else all queries are in front of this wave's keys.  (As a scalar the compiler
+    // leaves the test as it is; threaded through the steps it put 90 registers into scratch memory.)
+    if (!live) {
+#pragma unroll
+      for (int i = 0; i < 2 * LPW; ++i) copy_piece(gn, row1, rows1, t_oth, i);
+    }
+    if (live) {
+      f32x16 sc, dp;
+      constexpr bool P32 = D == 64;  // at D = 128 the fp32 probabilities do not outlive dP (registers): dS is formed from P as dV's product takes it
+      constexpr int N1 = KS, N2 = 2 * KS, N3 = N2 + 2 * DB, N4 = N3 + 2 * DB;
+      constexpr int PER = D == 128 ? 4 : 8;
+      static_assert(PER * (KS - 2) >= 16 && PER * (2 * DB - 2) >= 16, "all 16 must find room");
+      uint32_t pf[2][4], dsf[2][4];  // pairs of bf16
+      bf16x8 kl[2];
+      {
+        const float* const p = nl_cur + (lane_now() >> 5 << 2);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float4 y = *reinterpret_cast<const float4*>(p + 8 * g);
+          sc[4 * g + 0] = y.x, sc[4 * g + 1] = y.y, sc[4 * g + 2] = y.z, sc[4 * g + 3] = y.w;
+        }
+        // A pair that is not seen starts at -infinity and stays there.  (Behind the product the test costs 1 to 7 % in the kernels under masks.)
+        if (diagonal && kh == qh) {
+          const int ln = lane_now(), late = (ln & 31) - (ln >> 5 << 2);  // element e's query is 8 * (e / 4) + e % 4 - late rows behind this lane's key
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sc[e] = 8 * (e / 4) + e % 4 < late ? -INFINITY : sc[e];
         }
       }
+      mfma_ring<N4, 3>(
+          [&](auto i) {
+            constexpr int x = decltype(i)::value;
+            if constexpr (x < N2)
+              return A.row_frag(x < N1 ? q_cur : g_cur, 0, x % KS);
+            else
+              return A.tr_frag(x < N3 ? g_cur : q_cur, (x - N2) % (2 * DB) / DB, x % DB);
+          },
+          [&](auto i, bf16x8 f) {
+            constexpr int x = decltype(i)::value, db = x % DB, u = (x - N2) % (2 * DB) / DB;
+            if constexpr (x < N1 - KL)
+              sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, kf[x], sc, 0, 0, 0);
+            else if constexpr (x < N1)
+              sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, kl[x & 1], sc, 0, 0, 0);
+            else if constexpr (x < N2)
+              dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, vf[x - N1], dp, 0, 0, 0);
+            else if constexpr (x < N3)
+              dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, operand(pf[u]), dv[db], 0, 0, 0);
+            else
+              dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, operand(dsf[u]), dk[db], 0, 0, 0);
+          },
+          [&](auto i) {
+            constexpr int x = decltype(i)::value;
+            static_assert(2 * LPW == KS, "one copy behind every matrix instruction of S");
+            if constexpr (x < N1) copy_piece(gn, row1, rows1, t_oth, x);
+            if constexpr (x >= N1 - KL - 2 && x < N1 - 2) kl[x & 1] = kl_s[x - (N1 - KL - 2)][wave][lane_now()];
+            if constexpr (x == N1 - 2) {
+              const float* const nd = nd_cur + (lane_now() >> 5 << 2);
+#pragma unroll
+              for (int g = 0; g < 4; ++g) {
+                const float4 y = *reinterpret_cast<const float4*>(nd + 8 * g);
+                dp[4 * g + 0] = y.x, dp[4 * g + 1] = y.y, dp[4 * g + 2] = y.z, dp[4 * g + 3] = y.w;
+              }
+            }
+            if constexpr (x >= N1 + 2 && x < N2) {
+#pragma unroll
+              for (int e = (x - N1 - 2) * PER; e < min(16, (x - N1 - 1) * PER); e += 2) {
+                sc[e] = __builtin_amdgcn_exp2f(sc[e] * rc);
+                sc[e + 1] = __builtin_amdgcn_exp2f(sc[e + 1] * rc);
+                pf[e / 8][e % 8 / 2] = pack(sc[e], sc[e + 1]);
+                // (hides the pair's origin: the compiler otherwise rounds each of the two once more where dS takes it apart)
+                if constexpr (!P32) asm("" : "+v"(pf[e / 8][e % 8 / 2]));
+              }
+            }
+            if constexpr (x >= N2 + 2 && x < N3) {
+#pragma unroll
+              for (int e = (x - N2 - 2) * PER; e < min(16, (x - N2 - 1) * PER); e += 2) {
+                const uint32_t w = pf[e / 8][e % 8 / 2];
+                const float p0 = P32 ? sc[e] : __uint_as_float(w << 16), p1 = P32 ? sc[e + 1] : __uint_as_float(w & 0xffff0000u);
+                dsf[e / 8][e % 8 / 2] = pack(p0 * dp[e], p1 * dp[e + 1]);
+              }
+            }
+          });
     }
-  for (int e = 0; e < D / 64; ++e) {
-    P.dk.at(t, hk)[e * 64 + lane] = (__bf16)(dk[e] * P.scale);
-    P.dv.at(t, hk)[e * 64 + lane] = (__bf16)dv[e];
+  };
+  for (int t = 0; t < n_steps; t += 2) {
+    step(IntC<0>{});
+    if (t + 1 < n_steps) step(IntC<1>{});
   }
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+
+  // The two waves of a key half exchange: query half 0 hands over its dK and receives dV, query half 1 the other way round.
+  float4* const mine = reinterpret_cast<float4*>(qh == 0 ? t_s0 : t_s1) + kh * (REGS / 4) * 64;
+  const float4* const theirs = reinterpret_cast<const float4*>(qh == 0 ? t_s1 : t_s0) + kh * (REGS / 4) * 64;
+  static_assert(2 * REGS * 64 * sizeof(float) <= 2 * L::ELEMS * sizeof(__bf16), "two waves' sums must fit in the tile buffers of a parity");
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+    for (int g = 0; g < 4; ++g) {
+      float4 x;
+      x.x = qh ? dv[db][4 * g + 0] : dk[db][4 * g + 0];
+      x.y = qh ? dv[db][4 * g + 1] : dk[db][4 * g + 1];
+      x.z = qh ? dv[db][4 * g + 2] : dk[db][4 * g + 2];
+      x.w = qh ? dv[db][4 * g + 3] : dk[db][4 * g + 3];
+      mine[(db * 4 + g) * 64 + lane] = x;
+    }
+  __syncthreads();
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+    for (int g = 0; g < 4; ++g) {
+      const float4 x = theirs[(db * 4 + g) * 64 + lane];
+      dk[db][4 * g + 0] = x.x + (qh ? dk[db][4 * g + 0] : dv[db][4 * g + 0]);
+      dk[db][4 * g + 1] = x.y + (qh ? dk[db][4 * g + 1] : dv[db][4 * g + 1]);
+      dk[db][4 * g + 2] = x.z + (qh ? dk[db][4 * g + 2] : dv[db][4 * g + 2]);
+      dk[db][4 * g + 3] = x.w + (qh ? dk[db][4 * g + 3] : dv[db][4 * g + 3]);
+    }
+  __syncthreads();  // the results are staged in the same buffers
+  const int row0 = j * 64 + kh * 32, rows = max(0, min(32, n - row0));
+  if (qh == 0)
+    bbm::store_strided<D>(dk, 1.0f, t_s0 + L::ELEMS + kh * 32 * D, global(P->dv.p) + hk * P->dv.head + (int64_t)(s.begin + row0) * P->dv.row, rows, P->dv.row, lane);
+  else
+    bbm::store_strided<D>(dk, P->scale, t_s0 + kh * 32 * D, global(P->dk.p) + hk * P->dk.head + (int64_t)(s.begin + row0) * P->dk.row, rows, P->dk.row, lane);
 }
+
+inline size_t stats_bytes(int64_t T, int64_t H) { return ((size_t)(T * H) * sizeof(float) + 255) / 256 * 256; }
 
 }  // namespace
 
 extern "C" __attribute__((visibility("default"))) size_t bbm_prompt_attn_bwd_workspace_bytes(int64_t T, int64_t H) {
-  if (T < 0 || H < 1 || T > bbm::kMaxTokens || H > 65535) return 0;
-  return (size_t)(T * H) * sizeof(float);
+  if (T < 1 || H < 1 || T > bbm::kMaxTokens || H > 65535) return 0;
+  return 2 * stats_bytes(T, H);
 }
 
 extern "C" __attribute__((visibility("default"))) int bbm_prompt_attn_bwd(const bbm_packed* q, const bbm_packed* k, const bbm_packed* v, const bbm_packed* o,
@@ -133,7 +469,7 @@ extern "C" __attribute__((visibility("default"))) int bbm_prompt_attn_bwd(const 
     bool output;
   } all[] = {{"q", q, H, false}, {"k", k, Hk, false}, {"v", v, Hk, false}, {"o", o, H, false}, {"d_o", d_o, H, false}, {"dq", dq, H, true}, {"dk", dk, Hk, true}, {"dv", dv, Hk, true}};
   for (const auto& a : all)
-    if (int rc = check_packed(fn, a.name, a.x, T, a.heads, d, a.output)) return rc;
+    if (int rc = check_rows(fn, a.name, a.x, T, a.heads, d, a.output)) return rc;
   if ((T > 0 && !lse) || !aligned(lse, 4)) return fail(BBM_EINVAL, "%s: lse must be a non-NULL 4-byte aligned pointer", fn);
   if (!(softmax_scale > 0.0f) || !(softmax_scale < INFINITY)) return fail(BBM_EINVAL, "%s: softmax_scale must be finite and > 0", fn);
   const size_t need = bbm_prompt_attn_bwd_workspace_bytes(T, H);
@@ -142,14 +478,16 @@ extern "C" __attribute__((visibility("default"))) int bbm_prompt_attn_bwd(const 
   if (!aligned(workspace, 16)) return fail(BBM_EINVAL, "%s: workspace must be 16-byte aligned", fn);
   if (T == 0) return BBM_OK;
   PromptBwdParams P;
-  Tensor* const to[] = {&P.q, &P.k, &P.v, &P.o, &P.d_o, &P.dq, &P.dk, &P.dv};
-  for (int i = 0; i < 8; ++i) *to[i] = Tensor{static_cast<__bf16*>(all[i].x->ptr), all[i].x->row_stride, all[i].x->head_stride};
-  P.lse = lse, P.delta = static_cast<float*>(workspace), P.cu = cu;
-  P.T = (int32_t)T, P.R = (int32_t)R, P.G = (int32_t)(H / Hk), P.scale = softmax_scale;
+  Rows* const to[] = {&P.q, &P.k, &P.v, &P.o, &P.d_o, &P.dq, &P.dk, &P.dv};
+  for (int i = 0; i < 8; ++i) *to[i] = rows_of(all[i].x, T, d);
+  P.lse = lse, P.nls = static_cast<float*>(workspace), P.ndelta = reinterpret_cast<float*>(static_cast<char*>(workspace) + stats_bytes(T, H)), P.cu = cu;
+  P.T = (int32_t)T, P.R = (int32_t)R, P.G = (int32_t)(H / Hk), P.H = (int32_t)H, P.rc = softmax_scale * kLog2e, P.scale = softmax_scale;
+  const int64_t row_pieces = count_pieces(T, R, 1, 128), key_pieces = count_pieces(T, R, 1, 64);
+  const int64_t rows = work_groups(H, row_pieces), keys = work_groups(Hk, key_pieces);
+  if (rows >= 1ll << 31 || keys >= 1ll << 31) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld)", fn, (long long)T, (long long)H);
+  P.row_pieces = (int32_t)row_pieces, P.key_pieces = (int32_t)key_pieces;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const unsigned pieces = (unsigned)count_pieces(T, R, 1, kRows);
-  const dim3 rows(pieces, (unsigned)H), keys(pieces, (unsigned)Hk);
-  if (d == 64) prompt_dq_kernel<64><<<rows, 64 * kRows, 0, s>>>(P), prompt_dkv_kernel<64><<<keys, 64 * kRows, 0, s>>>(P);
-  else prompt_dq_kernel<128><<<rows, 64 * kRows, 0, s>>>(P), prompt_dkv_kernel<128><<<keys, 64 * kRows, 0, s>>>(P);
+  if (d == 64) prompt_dq_kernel<64><<<(unsigned)rows, 256, 0, s>>>(P), prompt_dkv_kernel<64><<<(unsigned)keys, 256, 0, s>>>(P);
+  else prompt_dq_kernel<128><<<(unsigned)rows, 256, 0, s>>>(P), prompt_dkv_kernel<128><<<(unsigned)keys, 256, 0, s>>>(P);
   return launch_status(fn);
 }
