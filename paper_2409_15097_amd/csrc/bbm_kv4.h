@@ -25,8 +25,9 @@ inline Kv4 kv4_of(const bbm_kv4_cache* c) {
   return Kv4{c->k, c->k_scale, c->v, c->v_scale, (int32_t)c->pages, (int32_t)c->Hk, c->page == 16 ? 4 : c->page == 32 ? 5 : c->page == 64 ? 6 : 7, c->page};
 }
 
-// A scale byte as the number 2^(s - 127); 255 (a group that is not finite) as a NaN, which the conversion passes on.
-__device__ __forceinline__ float scale_of(uint32_t s) { return __uint_as_float(s << 23 | (s == 255 ? 0x400000u : 0u)); }
+// A scale byte as the conversion takes it: in the exponent's place of a float.  It looks at nothing else (sign and fraction may be anything), 255
+// gives NaNs, 0 gives 2^-127.
+__device__ __forceinline__ float scale_of(uint32_t s) { return __uint_as_float(s << 23); }
 
 // The eight values of 32 bits of codes.
 __device__ __forceinline__ bf16x8 values_of(uint32_t codes, float scale) {

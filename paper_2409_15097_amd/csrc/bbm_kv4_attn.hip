@@ -1,14 +1,15 @@
 // Attention of new tokens over the 4-bit cache (include/bbm_tokens.h).
 //
-// Bound by the cache's bytes when few queries read it: 17/32 byte an element.  A piece is 16 * QT query columns of a request and a key head (column
-// c: query token c / G, head c % G of the group), so that the heads of a group and several new tokens share what is read.  A work-group takes a
-// piece and a part of the keys, its four waves blocks of 32 keys in turn; there is no barrier and no LDS in the loop:
+// The queries of a request and a key head are columns: column c is query token c / G, head c % G of the group, so that the heads of a group and
+// several new tokens share what is read.  A work-group takes a piece of the columns and a part of the keys; parts meet in the workspace, where a
+// second kernel joins them.  With few columns (the narrow kernel, 16 a piece) the cache's bytes are the bound, 17/32 byte an element; with many (the
+// wide kernel, 128 a piece) converting the codes and the products are.
+// Narrow: the four waves take blocks of 32 keys in turn; there is no barrier and no LDS in the loop:
 //   S^T = K Q^T       (16 keys x 16 columns x 32 elements an instruction): lane (n, q) = (l % 16, l / 16) of an A operand is key n, and what it
 //                     loads, D / 4 elements from q * D / 4 on, is the operand of all D / 32 steps once the codes are converted (with the group's scale, exactly);
 //   O^T += V^T P^T    over 32 keys: lane (n, q) loads elements n * D / 16 .. of the keys 4 q .. 4 q + 3 of both blocks of 16, converts pairs of elements,
 //                     and pairs the keys by byte permutes; row n of instruction j is element n * D / 16 + j.  The lane's scores are of the same eight keys
 //                     (the layout of the first product's result), so P goes from one product to the other in place.
-// The waves' results meet in LDS, those of parts in the workspace, where a second kernel joins them in the order of parts.
 #include "bbm_kv4.h"
 #include "bbm_tile.h"
 
@@ -16,7 +17,7 @@
 
 namespace {
 
-using bbm::bf16x2, bbm::bf16x8, bbm::Kv4, bbm::scalar;
+using bbm::bf16x8, bbm::f32x16, bbm::Kv4, bbm::scalar;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -33,8 +34,8 @@ struct Kv4AttnParams {
   int64_t q_row, q_head, o_row, o_head, table_stride;
   const int32_t *cu, *lens, *table;
   const uint64_t* mask;
-  float* partials;  // [piece][key head][part]: 16 * QT rows of D sums, then of a (maximum, sum) pair
-  int32_t T, R, G, max_pages, mask_words, pieces, parts, part_keys;
+  float* partials;  // [piece][key head][part]: `width` rows of D sums, then as many (maximum, sum) pairs
+  int32_t T, R, G, max_pages, mask_words, width, pieces, parts, part_keys;
   float rc;  // softmax_scale * log2(e)
 };
 
@@ -58,6 +59,11 @@ __device__ __forceinline__ Piece piece_of(const Kv4AttnParams& P, int number, in
   return x;
 }
 
+// A request's row of the block table, read by scalar loads (through the constant address space: no kernel that reads it writes it).  As a vector load a page's
+// number would be waited for together with the keys and values asked for before it.
+typedef const int32_t __attribute__((address_space(4)))* Table;
+__device__ __forceinline__ Table table_of(const Kv4AttnParams& P, const Piece& x) { return (Table)(uintptr_t)(P.table + x.s.r * P.table_stride); }
+
 template <int X>
 __device__ __forceinline__ float other_max(float x) {  // over lanes l and l ^ X
   auto r = X == 32 ? __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false)
@@ -69,6 +75,23 @@ __device__ __forceinline__ float other_sum(float x) {
   auto r = X == 32 ? __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false)
                    : __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+template <int D>
+__device__ __forceinline__ float* record_of(const Kv4AttnParams& P, int number, int hk, int part) {
+  return P.partials + (((int64_t)number * P.c.Hk + hk) * P.parts + part) * (P.width * (D + 2));
+}
+
+// Which of the keys j0 .. j0 + 63 new token i of the request may see, as far as its order or the mask goes.
+__device__ __forceinline__ uint64_t seen_from(const Kv4AttnParams& P, const Piece& x, int i, int j0) {
+  const int w0 = j0 - x.prefix;  // among the new tokens
+  if (!P.mask) return bbm::bits_up_to(i - w0);
+  const uint64_t* const words = P.mask + (int64_t)(x.s.begin + i) * P.mask_words;
+  auto word = [&](int n) { return n < P.mask_words ? words[n] : 0ull; };
+  if (w0 <= -64) return ~0ull;
+  if (w0 < 0) return word(0) << -w0 | ((1ull << -w0) - 1ull);
+  const int sh = w0 & 63;
+  return sh ? word(w0 >> 6) >> sh | word((w0 >> 6) + 1) << (64 - sh) : word(w0 >> 6);
 }
 
 // Writes D / 16 values of column `col`, from element e0 on.
@@ -84,8 +107,8 @@ __device__ __forceinline__ void put_column(const Kv4AttnParams& P, const Piece& 
   if (P.lse && e0 == 0) P.lse[(int64_t)h * P.T + t] = l > 0.0f ? (m + __log2f(l)) * kLn2 : -INFINITY;
 }
 
-template <int D, int QT>
-__global__ __launch_bounds__(64 * NW, QT == 4 ? 1 : QT == 2 ? 2 : 3) void kv4_attn_kernel(const Kv4AttnParams P) {
+template <int D>
+__global__ __launch_bounds__(64 * NW, D == 128 ? 3 : 5) void kv4_narrow_kernel(const Kv4AttnParams P) {
   constexpr int KD = D / 4;        // elements of K a lane loads of its key
   constexpr int KS = D / 32;       // steps of the first product
   constexpr int VD = D / 16;       // elements of V a lane loads of a key, instructions of the second product
@@ -97,152 +120,124 @@ __global__ __launch_bounds__(64 * NW, QT == 4 ? 1 : QT == 2 ? 2 : 3) void kv4_at
   const int wave = (int)scalar(tid >> 6);
   const int at = bbm::logical_wg(blockIdx.x, gridDim.x);
   const int number = at % P.pieces, rest = at / P.pieces, part = rest % P.parts, hk = rest / P.parts;
-  const Piece x = piece_of(P, number, 16 * QT);
+  const Piece x = piece_of(P, number, 16);
   if (x.s.end <= x.s.begin || part >= x.parts) return;
   const int first = part * x.keys, last = min(x.len, first + x.keys);
 
-  // this lane's columns: Q as operands, how far each sees
-  bf16x8 qf[QT][KS];
-  int sees[QT];               // of the new tokens, causal: keys 0 .. sees
-  const uint64_t* words[QT];  // with a mask: the row's
-  float m_run[QT], l_run[QT], nm[QT];
-  f32x4 acc[QT][VD];
+  // this lane's column: Q as operands, how far it sees (columns behind the last repeat it; they are not written)
+  const int my_i = min(x.col0 + n, x.cols - 1) / P.G, my_h = hk * P.G + (min(x.col0 + n, x.cols - 1) - my_i * P.G), my_t = x.s.begin + my_i;
+  bf16x8 qf[KS];
+  f32x4 acc[VD];
+  float m_run = -INFINITY, l_run = 0.0f, nm = 0.0f;
+  {
+    const __bf16* const row = P.q + (int64_t)my_t * P.q_row + my_h * P.q_head + kq * KD;
 #pragma unroll
-  for (int u = 0; u < QT; ++u) {
-    const int col = min(x.col0 + 16 * u + n, x.cols - 1);  // (columns behind the last repeat it; they are not written)
-    const int i = col / P.G, t = x.s.begin + i;
-    const __bf16* const row = P.q + (int64_t)t * P.q_row + (hk * P.G + (col - i * P.G)) * P.q_head + kq * KD;
-#pragma unroll
-    for (int j = 0; j < KS; ++j) qf[u][j] = *reinterpret_cast<const bf16x8*>(row + 8 * j);
-    sees[u] = x.prefix + i;
-    words[u] = P.mask + (int64_t)t * P.mask_words;
-    m_run[u] = -INFINITY, l_run[u] = 0.0f, nm[u] = 0.0f;
-#pragma unroll
-    for (int j = 0; j < VD; ++j) acc[u][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = 0; j < KS; ++j) qf[j] = *reinterpret_cast<const bf16x8*>(row + 8 * j);
   }
+#pragma unroll
+  for (int j = 0; j < VD; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   const int sees_all = P.mask ? x.prefix - 1 : x.prefix + x.col0 / P.G;  // the last key that every column of the piece sees
 
-  // 16 keys as they lie in the cache
+  // 16 keys as they lie in the cache.  Each array's bytes of a block are a buffer of their own: what a lane loads is a constant away from a
+  // scalar address, and of a block that is not there (behind the part's end, on a page outside the cache) zeros come.
   struct Block {
     uint32_t k[KD / 8], ks, v[4], vs;
-    int valid;  // keys that are there: 16, or fewer at the end, or none (a page outside the cache)
+    int valid;  // keys that are there: 16, or fewer at the end, or none
   };
-  const int32_t* const table = P.table + x.s.r * P.table_stride;
-  auto page_at = [&](int j) { return (int)scalar(j < last ? table[j >> P.c.page_shift] : -1); };
+  const Table table = table_of(P, x);
+  auto page_at = [&](int j) { return table[scalar(min(j, last - 1) >> P.c.page_shift)]; };
   auto load = [&](Block& b, int j, int page) __attribute__((always_inline)) {
-    const bool there = page >= 0 && page < P.c.pages;
-    b.valid = there ? min(16, last - j) : 0;
-    const int64_t head = (int64_t)(there ? page : 0) * P.c.Hk + hk;
+    const bool there = j < last && page >= 0 && page < P.c.pages;
+    b.valid = (int)scalar(there ? min(16, last - j) : 0);
+    const int64_t head = (int64_t)page * P.c.Hk + hk;
     const int in_page = j & (P.c.page - 1);
     const int64_t key = head * P.c.page + in_page;
-    const uint8_t* const kp = P.c.k + key * (D / 2);
-    const uint8_t* const vp = P.c.v + key * (D / 2);
+    const int all = b.valid ? 16 * (D / 2) : 0;
+    const __amdgpu_buffer_rsrc_t k_r = bbm::buffer_of(P.c.k + key * (D / 2), all), v_r = bbm::buffer_of(P.c.v + key * (D / 2), all);
+    const __amdgpu_buffer_rsrc_t ks_r = bbm::buffer_of(P.c.k_scale + key * (D / 32), all / 16);
+    const __amdgpu_buffer_rsrc_t vs_r = bbm::buffer_of(P.c.v_scale + head * (D / 32) * P.c.page + in_page, b.valid ? (D / 32 - 1) * P.c.page + 16 : 0);
     if constexpr (D == 128) {
-      const uint4 w = *reinterpret_cast<const uint4*>(kp + (uint32_t)(n * (D / 2) + kq * 16));
-      b.k[0] = w.x, b.k[1] = w.y, b.k[2] = w.z, b.k[3] = w.w;
+      const bbm::u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(k_r, n * (D / 2) + kq * 16, 0, 0);
+      for (int i = 0; i < 4; ++i) b.k[i] = w[i];
     } else {
-      const uint2 w = *reinterpret_cast<const uint2*>(kp + (uint32_t)(n * (D / 2) + kq * 8));
-      b.k[0] = w.x, b.k[1] = w.y;
+      const bbm::u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(k_r, n * (D / 2) + kq * 8, 0, 0);
+      for (int i = 0; i < 2; ++i) b.k[i] = w[i];
     }
-    b.ks = (P.c.k_scale + key * (D / 32))[(uint32_t)(n * (D / 32) + kq * KD / 32)];
+    b.ks = __builtin_amdgcn_raw_buffer_load_b8(ks_r, n * (D / 32) + kq * KD / 32, 0, 0);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const uint8_t* const p = vp + (uint32_t)((4 * kq + r) * (D / 2) + n * (VD / 2));
-      b.v[r] = D == 128 ? *reinterpret_cast<const uint32_t*>(p) : *reinterpret_cast<const uint16_t*>(p);
+      const int at = 4 * kq * (D / 2) + n * (VD / 2) + r * (D / 2);
+      if constexpr (D == 128) b.v[r] = __builtin_amdgcn_raw_buffer_load_b32(v_r, at, 0, 0);
+      else b.v[r] = __builtin_amdgcn_raw_buffer_load_b16(v_r, at, 0, 0);
     }
-    b.vs = *reinterpret_cast<const uint32_t*>(P.c.v_scale + head * (D / 32) * P.c.page + in_page + (uint32_t)(n * VD / 32 * P.c.page + 4 * kq));
+    b.vs = __builtin_amdgcn_raw_buffer_load_b32(vs_r, n * VD / 32 * P.c.page + 4 * kq, 0, 0);
   };
 
   auto compute = [&](Block& a, Block& b, int j0) __attribute__((always_inline)) {
     const bool full = a.valid == 16 && b.valid == 16 && j0 + 31 <= sees_all;
-    f32x4 sa[QT], sb[QT];
-#pragma unroll
-    for (int u = 0; u < QT; ++u) sa[u] = sb[u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    f32x4 sa = f32x4{0.0f, 0.0f, 0.0f, 0.0f}, sb = sa;
     const float ka = bbm::scale_of(a.ks), kb = bbm::scale_of(b.ks);
 #pragma unroll
     for (int j = 0; j < KS; ++j) {
-      const bf16x8 fa = bbm::values_of(a.k[j], ka), fb = bbm::values_of(b.k[j], kb);
-#pragma unroll
-      for (int u = 0; u < QT; ++u) {
-        sa[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa, qf[u][j], sa[u], 0, 0, 0);
-        sb[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb, qf[u][j], sb[u], 0, 0, 0);
-      }
+      sa = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bbm::values_of(a.k[j], ka), qf[j], sa, 0, 0, 0);
+      sb = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bbm::values_of(b.k[j], kb), qf[j], sb, 0, 0, 0);
     }
     if (!full) {
       // keys that are not there get scores of -infinity, and scales of 0, since a NaN would survive a probability of 0
-      auto there = [&](Block& z, f32x4 (&sz)[QT], int j) {
+      auto there = [&](Block& z, f32x4& sz, int j) {
         const int have = max(0, min(4, z.valid - 4 * kq));
         z.vs &= have == 4 ? ~0u : (1u << (8 * have)) - 1u;
+        const uint32_t bits = (uint32_t)seen_from(P, x, my_i, j + 4 * kq) & ((1u << have) - 1u);
 #pragma unroll
-        for (int u = 0; u < QT; ++u) {
-          uint32_t bits;  // which of the lane's four keys its column sees
-          const int k0 = j + 4 * kq;
-          if (!P.mask) {
-            bits = k0 + 3 <= sees[u] ? 15u : k0 > sees[u] ? 0u : (2u << (sees[u] - k0)) - 1u;
-          } else {
-            const int w0 = k0 - x.prefix;  // among the new tokens
-            auto word = [&](int i) { return i < P.mask_words ? words[u][i] : 0ull; };
-            if (w0 >= 0) {
-              const int sh = w0 & 63;
-              bits = (uint32_t)(word(w0 >> 6) >> sh);
-              if (sh > 60) bits |= (uint32_t)(word((w0 >> 6) + 1) << (64 - sh));
-            } else {
-              bits = w0 <= -4 ? 15u : ((1u << -w0) - 1u) | (uint32_t)(word(0) << -w0);
-            }
-          }
-          bits &= (1u << have) - 1u;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) sz[u][r] = bits >> r & 1 ? sz[u][r] : -INFINITY;
-        }
+        for (int r = 0; r < 4; ++r) sz[r] = bits >> r & 1 ? sz[r] : -INFINITY;
       };
       there(a, sa, j0);
       there(b, sb, j0 + 16);
     }
-    bf16x8 pf[QT];
+    float mx = fmaxf(fmaxf(fmaxf(sa[0], sa[1]), fmaxf(sa[2], sa[3])), fmaxf(fmaxf(sb[0], sb[1]), fmaxf(sb[2], sb[3])));
+    mx = other_max<16>(other_max<32>(mx)) * P.rc;
+    if (__any(mx > m_run + kLazy ? 1 : 0)) {
+      const float m_new = fmaxf(m_run, mx), m_fin = m_new == -INFINITY ? 0.0f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_fin);
+      l_run *= alpha;
+      m_run = m_new;
+      nm = -m_fin;
 #pragma unroll
-    for (int u = 0; u < QT; ++u) {
-      float mx = fmaxf(fmaxf(fmaxf(sa[u][0], sa[u][1]), fmaxf(sa[u][2], sa[u][3])), fmaxf(fmaxf(sb[u][0], sb[u][1]), fmaxf(sb[u][2], sb[u][3])));
-      mx = other_max<16>(other_max<32>(mx)) * P.rc;
-      if (__any(mx > m_run[u] + kLazy ? 1 : 0)) {
-        const float m_new = fmaxf(m_run[u], mx), m_fin = m_new == -INFINITY ? 0.0f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m_run[u] - m_fin);
-        l_run[u] *= alpha;
-        m_run[u] = m_new;
-        nm[u] = -m_fin;
-#pragma unroll
-        for (int j = 0; j < VD; ++j) acc[u][j] *= alpha;
-      }
-#pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(r < 4 ? sa[u][r & 3] : sb[u][r & 3], P.rc, nm[u]));
-        l_run[u] += p;
-        pf[u][r] = (__bf16)p;
-      }
+      for (int j = 0; j < VD; ++j) acc[j] *= alpha;
     }
-    uint32_t va[4][VD / 2], vb[4][VD / 2];  // pairs of elements of a key
+    bf16x8 pf;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(r < 4 ? sa[r & 3] : sb[r & 3], P.rc, nm));
+      l_run += p;
+      pf[r] = (__bf16)p;
+    }
+    // (byte r in the exponent's place, whatever lies around it, see scale_of)
+    float fa[4], fb[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const float fa = bbm::scale_of(a.vs >> (8 * r) & 255), fb = bbm::scale_of(b.vs >> (8 * r) & 255);
-      va[r][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a.v[r], fa, 0));
-      va[r][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a.v[r], fa, 1));
-      vb[r][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b.v[r], fb, 0));
-      vb[r][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b.v[r], fb, 1));
-      if constexpr (D == 128) {
-        va[r][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a.v[r], fa, 2));
-        va[r][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a.v[r], fa, 3));
-        vb[r][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b.v[r], fb, 2));
-        vb[r][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b.v[r], fb, 3));
-      }
+      fa[r] = __uint_as_float(r < 3 ? a.vs << (23 - 8 * r) : a.vs >> 1);
+      fb[r] = __uint_as_float(r < 3 ? b.vs << (23 - 8 * r) : b.vs >> 1);
     }
+    bbm::for_each_n(
+        [&](auto pair) {
+          constexpr int i = decltype(pair)::value;  // two neighbouring elements of each key
+          uint32_t va[4], vb[4];
 #pragma unroll
-    for (int j = 0; j < VD; ++j) {
-      const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;  // the pair's second or first element of two keys
-      const uint32_t w[4] = {__builtin_amdgcn_perm(va[1][j / 2], va[0][j / 2], sel), __builtin_amdgcn_perm(va[3][j / 2], va[2][j / 2], sel),
-                             __builtin_amdgcn_perm(vb[1][j / 2], vb[0][j / 2], sel), __builtin_amdgcn_perm(vb[3][j / 2], vb[2][j / 2], sel)};
-      const bf16x8 f = bbm::operand(w);
+          for (int r = 0; r < 4; ++r) {
+            va[r] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a.v[r], fa[r], i));
+            vb[r] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b.v[r], fb[r], i));
+          }
 #pragma unroll
-      for (int u = 0; u < QT; ++u) acc[u][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pf[u], acc[u][j], 0, 0, 0);
-    }
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t sel = e ? 0x07060302u : 0x05040100u;  // the first or the second of them, of two keys
+            const uint32_t w[4] = {__builtin_amdgcn_perm(va[1], va[0], sel), __builtin_amdgcn_perm(va[3], va[2], sel), __builtin_amdgcn_perm(vb[1], vb[0], sel),
+                                   __builtin_amdgcn_perm(vb[3], vb[2], sel)};
+            acc[2 * i + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bbm::operand(w), pf, acc[2 * i + e], 0, 0, 0);
+          }
+          if constexpr (D == 128) __builtin_amdgcn_sched_barrier(0);  // (not all of them at once: registers)
+        },
+        std::make_integer_sequence<int, VD / 2>{});
   };
 
   int j0 = first + 32 * wave;
@@ -271,83 +266,316 @@ __global__ __launch_bounds__(64 * NW, QT == 4 ? 1 : QT == 2 ? 2 : 3) void kv4_at
   }
 
   // The waves' results meet: columns on threads, 16 threads a column.
-  const int c = tid >> 4, e0 = (tid & 15) * VD;
-  float* const rec = x.parts > 1 ? P.partials + (((int64_t)number * P.c.Hk + hk) * P.parts + part) * (16 * QT * (D + 2)) : nullptr;
+  const float l = other_sum<16>(other_sum<32>(l_run));
+  if (kq == 0) m_s[wave][n] = m_run, l_s[wave][n] = l;
+  // lane (n, kq): rows 4 kq + r of instruction j, element (4 kq + r) * VD + j
 #pragma unroll
-  for (int u = 0; u < QT; ++u) {
-    if (u > 0) __syncthreads();
-    const float l = other_sum<16>(other_sum<32>(l_run[u]));
-    if (kq == 0) m_s[wave][n] = m_run[u], l_s[wave][n] = l;
-    // lane (n, kq): rows 4 kq + r of instruction j, element (4 kq + r) * VD + j
+  for (int r = 0; r < 4; ++r)
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int j = 0; j < VD; j += 4) *reinterpret_cast<f32x4*>(&o_s[wave][n][(4 * kq + r) * VD + j]) = f32x4{acc[j][r], acc[j + 1][r], acc[j + 2][r], acc[j + 3][r]};
+  __syncthreads();
+  const int c = tid >> 4, e0 = (tid & 15) * VD, col = x.col0 + c;
+  if (col >= x.cols) return;
+  float m = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < VD; j += 4) *reinterpret_cast<f32x4*>(&o_s[wave][n][(4 * kq + r) * VD + j]) = f32x4{acc[u][j][r], acc[u][j + 1][r], acc[u][j + 2][r], acc[u][j + 3][r]};
-    __syncthreads();
-    const int col = x.col0 + 16 * u + c;
-    float m = -INFINITY;
+  for (int w = 0; w < NW; ++w) m = fmaxf(m, m_s[w][c]);
+  const float m_fin = m == -INFINITY ? 0.0f : m;
+  float sum = 0.0f, v[VD] = {};
 #pragma unroll
-    for (int w = 0; w < NW; ++w) m = fmaxf(m, m_s[w][c]);
-    const float m_fin = m == -INFINITY ? 0.0f : m;
-    float sum = 0.0f, v[VD] = {};
+  for (int w = 0; w < NW; ++w) {
+    const float f = __builtin_amdgcn_exp2f(m_s[w][c] - m_fin);
+    sum += f * l_s[w][c];
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float f = __builtin_amdgcn_exp2f(m_s[w][c] - m_fin);
-      sum += f * l_s[w][c];
+    for (int e = 0; e < VD; ++e) v[e] += f * o_s[w][c][e0 + e];
+  }
+  if (x.parts == 1) {
+    put_column<D>(P, x, hk, col, e0, v, m, sum);
+  } else {
+    float* const rec = record_of<D>(P, number, hk, part);
 #pragma unroll
-      for (int e = 0; e < VD; ++e) v[e] += f * o_s[w][c][e0 + e];
-    }
-    if (col >= x.cols) continue;
-    if (!rec) {
-      put_column<D>(P, x, hk, col, e0, v, m, sum);
-    } else {
-#pragma unroll
-      for (int e = 0; e < VD; e += 4) *reinterpret_cast<f32x4*>(rec + (16 * u + c) * D + e0 + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
-      if (e0 == 0) *reinterpret_cast<float2*>(rec + 16 * QT * D + 2 * (16 * u + c)) = make_float2(m, sum);
-    }
+    for (int e = 0; e < VD; e += 4) *reinterpret_cast<f32x4*>(rec + c * D + e0 + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+    if (e0 == 0) *reinterpret_cast<float2*>(rec + P.width * D + 2 * c) = make_float2(m, sum);
   }
 }
 
-// Joins the parts of a piece's 16 columns, in their order.
-template <int D, int QT>
+// 128 columns of a piece, a wave 32 of them, one lane a column, with the products of the kernels for prompts: the codes of 64 keys at a time are converted once
+// for all of them, on their way to LDS, where the tile is read as keys and values in bf16 are.
+template <int D>
+__global__ __launch_bounds__(64 * NW, 2) void kv4_wide_kernel(const Kv4AttnParams P) {
+  using L = bbm::TL<D>;
+  constexpr int KS = D / 16, DB = D / 32, RC = D / 8, RPB = 64 / RC;
+  constexpr int W = D / 32;  // 32-bit words of codes a thread converts of a tensor
+  __shared__ __attribute__((aligned(16))) __bf16 k_s0[L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 k_s1[L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 v_s0[L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 v_s1[L::ELEMS];
+  __shared__ __attribute__((aligned(16))) uint32_t there_s[2][NW];  // which of a tile's keys are there, 16 a wave
+
+  const int tid = threadIdx.x, lane = tid & 63, lq = lane & 31, hh = lane >> 5;
+  const int wave = (int)scalar(tid >> 6);
+  const int at = bbm::logical_wg(blockIdx.x, gridDim.x);
+  const int number = at % P.pieces, rest = at / P.pieces, part = rest % P.parts, hk = rest / P.parts;
+  const Piece x = piece_of(P, number, 128);
+  if (x.s.end <= x.s.begin || part >= x.parts) return;
+  const int first = part * x.keys, last = min(x.len, first + x.keys);
+  const int n_tiles = (last - first + 63) / 64;
+
+  const int wcol = x.col0 + 32 * wave, my_col = min(wcol + lq, x.cols - 1), my_i = my_col / P.G, my_h = hk * P.G + (my_col - my_i * P.G);
+  const int wcols = max(0, min(32, x.cols - wcol));
+  const int sees_all = P.mask ? x.prefix - 1 : x.prefix + x.col0 / P.G;
+  bf16x8 qf[KS];
+  {
+    const __bf16* const row = P.q + (int64_t)(x.s.begin + my_i) * P.q_row + my_h * P.q_head + hh * 8;
+#pragma unroll
+    for (int t = 0; t < KS; ++t) qf[t] = *reinterpret_cast<const bf16x8*>(row + 16 * t);
+  }
+  f32x16 oacc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+    for (int e = 0; e < 16; ++e) oacc[db][e] = 0.0f;
+  float m_run = -INFINITY, l_run = 0.0f, nm = 0.0f;
+  bbm::TileAddr<D> A;
+  A.init(lane);
+
+  // A wave converts 16 keys of a tile, which lie on one page, a quarter of a key's elements a lane.  (Lanes take the keys in an order in which 16 of them
+  // write to all banks: rows four apart differ in the turn of their chunks.)
+  const Table table = table_of(P, x);
+  const int row = (lane >> 2 & 3) * 4 + (lane >> 4), quarter = lane & 3;  // of the wave's 16
+  struct Raw {
+    uint32_t k[W], v[W], ks, vs;
+    int valid;  // keys that are there
+  };
+  auto page_at = [&](int tile) { return table[scalar(min(first + tile * 64 + 16 * wave, max(0, last - 1)) >> P.c.page_shift)]; };
+  auto load = [&](Raw& z, int tile, int page) __attribute__((always_inline)) {
+    const int j = first + tile * 64 + 16 * wave;
+    z.valid = (int)scalar(j < last && page >= 0 && page < P.c.pages ? min(16, last - j) : 0);
+    const int64_t head = (int64_t)page * P.c.Hk + hk;
+    const int in_page = j & (P.c.page - 1);
+    const int64_t key = head * P.c.page + in_page;
+    const int all = z.valid ? 16 * (D / 2) : 0, at = row * (D / 2) + quarter * (D / 8);
+    const __amdgpu_buffer_rsrc_t k_r = bbm::buffer_of(P.c.k + key * (D / 2), all), v_r = bbm::buffer_of(P.c.v + key * (D / 2), all);
+    const __amdgpu_buffer_rsrc_t ks_r = bbm::buffer_of(P.c.k_scale + key * (D / 32), all / 16);
+    const __amdgpu_buffer_rsrc_t vs_r = bbm::buffer_of(P.c.v_scale + head * (D / 32) * P.c.page + in_page, z.valid ? (D / 32 - 1) * P.c.page + 16 : 0);
+    if constexpr (D == 128) {
+      const bbm::u32x4 a = __builtin_amdgcn_raw_buffer_load_b128(k_r, at, 0, 0), b = __builtin_amdgcn_raw_buffer_load_b128(v_r, at, 0, 0);
+      for (int i = 0; i < W; ++i) z.k[i] = a[i], z.v[i] = b[i];
+    } else {
+      const bbm::u32x2 a = __builtin_amdgcn_raw_buffer_load_b64(k_r, at, 0, 0), b = __builtin_amdgcn_raw_buffer_load_b64(v_r, at, 0, 0);
+      for (int i = 0; i < W; ++i) z.k[i] = a[i], z.v[i] = b[i];
+    }
+    z.ks = __builtin_amdgcn_raw_buffer_load_b8(ks_r, row * (D / 32) + quarter * D / 128, 0, 0);
+    z.vs = __builtin_amdgcn_raw_buffer_load_b8(vs_r, quarter * D / 128 * P.c.page + row, 0, 0);
+  };
+  // piece i of 2 W of what a lane converts
+  auto store_piece = [&](Raw& z, __bf16* kd, __bf16* vd, uint32_t* there_d, int i) __attribute__((always_inline)) {
+    const int r = 16 * wave + row, base = r % L::NBLK * L::TBLK + r / L::NBLK * D, turn = r >> 2 & 3;
+    const int chunk = (quarter * W + i % W) ^ turn;
+    if (i < W)
+      *reinterpret_cast<bf16x8*>(kd + base + chunk * 8) = bbm::values_of(z.k[i % W], bbm::scale_of(z.ks));
+    else  // (a NaN would survive a probability of 0)
+      *reinterpret_cast<bf16x8*>(vd + base + chunk * 8) = bbm::values_of(z.v[i % W], bbm::scale_of(row < z.valid ? z.vs : 0));
+    if (i == 2 * W - 1 && lane == 0) there_d[wave] = (1u << z.valid) - 1u;
+  };
+
+  Raw raw[2];  // of the tile behind the one in use, and of the next: asked for two steps before they are converted
+  auto step = [&](auto pb, int tile, int& page) __attribute__((always_inline)) {
+    constexpr int PB = decltype(pb)::value;
+    __syncthreads();  // the tile is there, and everyone is done with the one in the other buffers
+    __bf16* const k_cur = PB ? k_s1 : k_s0;
+    __bf16* const v_cur = PB ? v_s1 : v_s0;
+    __bf16* const k_oth = PB ? k_s0 : k_s1;
+    __bf16* const v_oth = PB ? v_s0 : v_s1;
+    const int j0 = first + tile * 64;
+    f32x16 sc[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+      for (int e = 0; e < 16; ++e) sc[kb][e] = 0.0f;
+    // The next tile is converted behind the matrix instructions of the first product.  (Behind the last tile too, of which zeros are loaded and stored:
+    // with loads behind a branch the compiler cannot count those under way, and waits for all of them.)
+    bbm::mfma_ring<2 * KS, 4>([&](auto i) { return A.row_frag(k_cur, decltype(i)::value & 1, decltype(i)::value >> 1); },
+                              [&](auto i, bf16x8 f) {
+                                constexpr int y = decltype(i)::value;
+                                sc[y & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[y >> 1], sc[y & 1], 0, 0, 0);
+                              },
+                              [&](auto i) {
+                                constexpr int y = decltype(i)::value, GAP = KS / W;
+                                if constexpr (y % GAP == 0) store_piece(raw[PB ^ 1], k_oth, v_oth, there_s[PB ^ 1], y / GAP);
+                              });
+    load(raw[PB ^ 1], tile + 3, page);
+    page = page_at(tile + 4);
+    {
+      const uint4 t4 = *reinterpret_cast<const uint4*>(there_s[PB]);
+      const uint32_t t_lo = scalar(t4.x | t4.y << 16), t_hi = scalar(t4.z | t4.w << 16);
+      if ((t_lo & t_hi) != ~0u || j0 + 63 > sees_all) {
+        const uint64_t seen = seen_from(P, x, my_i, j0) & ((uint64_t)t_hi << 32 | t_lo);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          const uint32_t w = (uint32_t)(seen >> (32 * kb)) >> (4 * hh);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sc[kb][e] = bbm::keep_if(w, e, sc[kb][e]);
+        }
+      }
+      float mx = sc[0][0];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[kb][e]);
+      mx = other_max<32>(mx) * P.rc;
+      if (__any(mx > m_run + kLazy ? 1 : 0)) {
+        const float m_new = fmaxf(m_run, mx), m_fin = m_new == -INFINITY ? 0.0f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f(m_run - m_fin);
+        l_run *= alpha;
+        m_run = m_new;
+        nm = -m_fin;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          for (int e = 0; e < 16; ++e) oacc[db][e] *= alpha;
+      }
+      bf16x8 pf[2];
+      auto exps = [&](int u, int e0, int e1) {
+#pragma unroll
+        for (int e = e0; e < e1; ++e) {
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[u / 2][8 * (u % 2) + e], P.rc, nm));
+          l_run += p;
+          pf[u & 1][e] = (__bf16)p;
+        }
+      };
+      exps(0, 0, 8);
+      bbm::mfma_ring<4 * DB, 3>([&](auto i) { return A.tr_frag(v_cur, decltype(i)::value / DB, decltype(i)::value % DB); },
+                                [&](auto i, bf16x8 f) {
+                                  constexpr int y = decltype(i)::value;
+                                  oacc[y % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pf[y / DB & 1], oacc[y % DB], 0, 0, 0);
+                                },
+                                [&](auto i) {
+                                  constexpr int y = decltype(i)::value, PER = 8 / DB;
+                                  if constexpr (y / DB < 3) exps(y / DB + 1, y % DB * PER, (y % DB + 1) * PER);
+                                });
+    }
+  };
+  if (n_tiles > 0) {
+    load(raw[0], 0, page_at(0));
+    load(raw[1], 1, page_at(1));
+    int page = page_at(2);
+#pragma unroll
+    for (int i = 0; i < 2 * W; ++i) store_piece(raw[0], k_s0, v_s0, there_s[0], i);
+    __builtin_amdgcn_sched_barrier(0);  // (tile 1 is asked for before tile 2: the first step waits for the older loads)
+    load(raw[0], 2, page);
+    page = page_at(3);
+    // (Q is waited for here; in the loop, where the compiler would have it, the wait takes the next tile's loads with it)
+#pragma unroll
+    for (int t = 0; t < KS; ++t) asm volatile("" : "+v"(qf[t]));
+#pragma unroll 1
+    for (int tile = 0; tile + 1 < n_tiles; tile += 2) {  // (with a way around the second step the compiler is not sure which loads are the older ones)
+      step(bbm::IntC<0>{}, tile, page);
+      step(bbm::IntC<1>{}, tile + 1, page);
+    }
+    if (n_tiles & 1) step(bbm::IntC<0>{}, n_tiles - 1, page);
+  }
+  __syncthreads();  // the result is staged in the tile buffers
+  if (wcols == 0) return;
+  const float l = other_sum<32>(l_run);
+  if (x.parts > 1) {
+    float* const rec = record_of<D>(P, number, hk, part);
+    if (lq < wcols) {
+      const int c = 32 * wave + lq;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<f32x4*>(rec + c * D + 32 * db + 8 * g + 4 * hh) = f32x4{oacc[db][4 * g], oacc[db][4 * g + 1], oacc[db][4 * g + 2], oacc[db][4 * g + 3]};
+      if (hh == 0) *reinterpret_cast<float2*>(rec + P.width * D + 2 * c) = make_float2(m_run, l);
+    }
+    return;
+  }
+  __bf16* const stage = (wave / 2 == 0 ? k_s0 : v_s0) + wave % 2 * 32 * D;
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      bbm::bf16x4 y;
+      for (int e = 0; e < 4; ++e) y[e] = (__bf16)(oacc[db][4 * g + e] * inv);
+      *reinterpret_cast<bbm::bf16x4*>(stage + lq * D + (((4 * db + g) ^ (lq % RC)) * 8) + 4 * hh) = y;
+    }
+#pragma unroll
+  for (int i = 0; i < 32 / RPB; ++i) {
+    const int r = i * RPB + lane / RC, col = wcol + r, tok = col / P.G, h = hk * P.G + (col - tok * P.G);
+    if (r < wcols)
+      *reinterpret_cast<bf16x8*>(P.o + (int64_t)(x.s.begin + tok) * P.o_row + h * P.o_head + lane % RC * 8) = *reinterpret_cast<const bf16x8*>(stage + r * D + (lane % RC ^ r % RC) * 8);
+  }
+  if (P.lse && hh == 0 && lq < wcols) P.lse[(int64_t)my_h * P.T + x.s.begin + my_i] = l > 0.0f ? (m_run + __log2f(l)) * kLn2 : -INFINITY;
+}
+
+// Joins the parts of a piece's columns in a fixed order, 16 lanes a column.  With many parts (SIDE = 4) a wave takes one column and four parts side by
+// side, whose sums meet at the end; with few, a column for every 16 lanes: a wave costs more to start than to add up four records.
+template <int D, int SIDE>
 __global__ __launch_bounds__(256) void kv4_join_kernel(const Kv4AttnParams P) {
   constexpr int VD = D / 16;
-  const int number = blockIdx.x, hk = blockIdx.y, u = blockIdx.z, c = 16 * u + (threadIdx.x >> 4), e0 = (threadIdx.x & 15) * VD;
-  const Piece x = piece_of(P, number, 16 * QT);
+  const int lane = threadIdx.x & 63, number = blockIdx.x, hk = blockIdx.y, e0 = (lane & 15) * VD;
+  const int c = SIDE == 4 ? 4 * blockIdx.z + (threadIdx.x >> 6) : 16 * blockIdx.z + (threadIdx.x >> 4);
+  const Piece x = piece_of(P, number, P.width);
   if (x.s.end <= x.s.begin || x.parts == 1 || x.col0 + c >= x.cols) return;
-  const int64_t stride = 16 * QT * (D + 2);
-  const float* const rec = P.partials + ((int64_t)number * P.c.Hk + hk) * P.parts * stride;
+  const int64_t stride = (int64_t)P.width * (D + 2);
+  const float* const rec = record_of<D>(P, number, hk, 0);
   float m = -INFINITY, l = 0.0f, v[VD] = {};
-  for (int p = 0; p < x.parts; ++p) m = fmaxf(m, rec[p * stride + 16 * QT * D + 2 * c]);
-  const float m_fin = m == -INFINITY ? 0.0f : m;
-#pragma unroll 4
-  for (int p = 0; p < x.parts; ++p) {
-    const float2 ml = *reinterpret_cast<const float2*>(rec + p * stride + 16 * QT * D + 2 * c);
-    const float f = __builtin_amdgcn_exp2f(ml.x - m_fin);
-    l += f * ml.y;
+#pragma unroll 1
+  for (int p = SIDE == 4 ? lane >> 4 : 0; p < x.parts; p += 4 * SIDE) {  // four records' loads in flight
+    float2 ml[4];
+    f32x4 y[4][VD / 4];
 #pragma unroll
-    for (int e = 0; e < VD; e += 4) {
-      const f32x4 y = *reinterpret_cast<const f32x4*>(rec + p * stride + c * D + e0 + e);
-      for (int i = 0; i < 4; ++i) v[e + i] += f * y[i];
+    for (int i = 0; i < 4; ++i) {
+      const float* const r = rec + min(p + SIDE * i, x.parts - 1) * stride;
+      ml[i] = *reinterpret_cast<const float2*>(r + P.width * D + 2 * c);
+      if (p + SIDE * i >= x.parts) ml[i] = make_float2(-INFINITY, 0.0f);
+#pragma unroll
+      for (int e = 0; e < VD / 4; ++e) y[i][e] = *reinterpret_cast<const f32x4*>(r + c * D + e0 + 4 * e);
+    }
+    const float m_new = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m), m_fin = m_new == -INFINITY ? 0.0f : m_new;
+    const float keep = __builtin_amdgcn_exp2f(m - m_fin);
+    m = m_new;
+    l *= keep;
+#pragma unroll
+    for (int e = 0; e < VD; ++e) v[e] *= keep;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float f = __builtin_amdgcn_exp2f(ml[i].x - m_fin);
+      l += f * ml[i].y;
+#pragma unroll
+      for (int e = 0; e < VD; ++e) v[e] += f * y[i][e / 4][e % 4];
     }
   }
-  put_column<D>(P, x, hk, x.col0 + c, e0, v, m, l);
+  if constexpr (SIDE == 4) {
+    const float m_all = other_max<16>(other_max<32>(m)), f = __builtin_amdgcn_exp2f(m - (m_all == -INFINITY ? 0.0f : m_all));
+    l = other_sum<16>(other_sum<32>(l * f));
+#pragma unroll
+    for (int e = 0; e < VD; ++e) v[e] = other_sum<16>(other_sum<32>(v[e] * f));
+    m = m_all;
+  }
+  if (SIDE == 1 || lane < 16) put_column<D>(P, x, hk, x.col0 + c, e0, v, m, l);
 }
 
-// How a call is cut: 16 * QT columns a piece, at most `parts` parts of the keys, of at least part_keys each.
+// How a call is cut: pieces of `width` columns, at most `parts` parts of the keys, of at least part_keys each.
 struct Plan {
-  int qt;
+  int width;
   int64_t pieces, parts, part_keys;
 };
-constexpr int64_t kFill = 2048;     // work-groups that keep the chip busy to the end of a call
-constexpr int64_t kPartKeys = 256;  // fewer keys than this are not worth a part of their own
+// Work-groups that occupy the chip, and that keep it busy to the end of a call whose requests differ in length; the keys that a part is worth for
+// either.  (Every part costs its record and a share of the join.)  D = 128, 32 / 8 heads, us: one token each of 128 requests of 2048 keys whole / in two
+// parts 49 / 56; of 64 requests of 16384 in 1 / 2 / 4 parts 206 / 182 / 173; of 8 requests of 8192 in 8 parts of 1024 / 16 of 512 22.3 / 20.7;
+// of one request of 32768 in 32 parts of 1024 / 64 of 512 16.4 / 18.0.
+constexpr int64_t kOccupy = 512, kBusy = 2048, kPartKeys = 1024, kLongPartKeys = 4096;
+// The wide kernel takes 128 columns at 1.5 us for 64 keys and has few work-groups; the narrow one reads the keys again for every 16 columns.
+// 32 / 8 heads over 4096 keys, us, narrow / wide: 16 requests of 8 tokens (32 columns) 30 / 42, of 16 40 / 44, of 32 (16 x 32 x 32 rows) 61 / 51; 4 requests
+// of 64 35 / 43; 3 of 32 over 1000 keys 10 / 25; trees of 256 nodes, 8 x 32 heads, 88 / 53.
+constexpr int64_t kWideColumns = 64, kWideRows = 16384;
 inline Plan plan_of(int64_t T, int64_t R, int64_t G, int64_t Hk, int64_t max_len) {
   Plan p;
-  const int64_t cols = bbm::ceil_div(T * G, R);
-  p.qt = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
-  p.pieces = bbm::count_pieces(T, R, G, 16 * p.qt);
-  const int64_t busy = std::max<int64_t>(1, std::min(p.pieces, bbm::ceil_div(T * G, 16 * p.qt) + R / 2)) * Hk;
-  p.parts = std::max<int64_t>(1, std::min(bbm::ceil_div(kFill, busy), max_len / kPartKeys));
+  const bool wide = T * G >= kWideColumns * R && T * G * Hk >= kWideRows;
+  p.width = wide ? 128 : 16;
+  p.pieces = bbm::count_pieces(T, R, G, p.width);
+  const int64_t busy = std::max(std::min(T, R), bbm::ceil_div(T * G, p.width)) * Hk;  // pieces that belong to a request, or few fewer
+  p.parts = std::min(bbm::ceil_div(kOccupy, busy), max_len / kPartKeys);
+  if (!wide) p.parts = std::max(p.parts, std::min(bbm::ceil_div(kBusy, busy), max_len / kLongPartKeys));
+  p.parts = std::max<int64_t>(p.parts, 1);
   p.part_keys = bbm::ceil_div(bbm::ceil_div(max_len, p.parts), kStep) * kStep;
   p.parts = bbm::ceil_div(max_len, p.part_keys);
   return p;
@@ -356,10 +584,13 @@ inline bool sizes_ok(int64_t T, int64_t R, int64_t H, int64_t Hk, int64_t max_le
   return T >= 1 && R >= 1 && H >= 1 && Hk >= 1 && H % Hk == 0 && max_len >= 1 && T <= bbm::kMaxTokens && R <= bbm::kMaxTokens && H <= 65535;
 }
 
-template <int D, int QT>
+template <int D>
 void launch(const Kv4AttnParams& P, hipStream_t s) {
-  kv4_attn_kernel<D, QT><<<(unsigned)((int64_t)P.pieces * P.c.Hk * P.parts), 64 * NW, 0, s>>>(P);
-  if (P.parts > 1) kv4_join_kernel<D, QT><<<dim3((unsigned)P.pieces, (unsigned)P.c.Hk, QT), 256, 0, s>>>(P);
+  const unsigned wgs = (unsigned)((int64_t)P.pieces * P.c.Hk * P.parts);
+  if (P.width == 16) kv4_narrow_kernel<D><<<wgs, 64 * NW, 0, s>>>(P);
+  else kv4_wide_kernel<D><<<wgs, 64 * NW, 0, s>>>(P);
+  if (P.parts > 4) kv4_join_kernel<D, 4><<<dim3((unsigned)P.pieces, (unsigned)P.c.Hk, (unsigned)P.width / 4), 256, 0, s>>>(P);
+  else if (P.parts > 1) kv4_join_kernel<D, 1><<<dim3((unsigned)P.pieces, (unsigned)P.c.Hk, (unsigned)P.width / 16), 256, 0, s>>>(P);
 }
 
 }  // namespace
@@ -367,7 +598,7 @@ void launch(const Kv4AttnParams& P, hipStream_t s) {
 extern "C" __attribute__((visibility("default"))) size_t bbm_kv4_attn_workspace_bytes(int64_t T, int64_t R, int64_t H, int64_t Hk, int d, int64_t max_len) {
   if (!sizes_ok(T, R, H, Hk, max_len) || (d != 64 && d != 128)) return 0;
   const Plan p = plan_of(T, R, H / Hk, Hk, std::min<int64_t>(max_len, 0x7fffffff));
-  return p.parts == 1 ? 0 : (size_t)(p.pieces * Hk * p.parts * 16 * p.qt * (d + 2)) * sizeof(float);
+  return p.parts == 1 ? 0 : (size_t)(p.pieces * Hk * p.parts * p.width * (d + 2)) * sizeof(float);
 }
 
 extern "C" __attribute__((visibility("default"))) int bbm_kv4_attn(const bbm_packed* q, const bbm_packed* o, float* lse, int64_t T, int64_t R, const int32_t* cu,
@@ -403,11 +634,9 @@ extern "C" __attribute__((visibility("default"))) int bbm_kv4_attn(const bbm_pac
   const Plan p = plan_of(T, R, P.G, cache->Hk, std::min<int64_t>(max_len, 0x7fffffff));
   if (p.pieces * cache->Hk * p.parts >= 1ll << 31) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, R=%lld, H=%lld)", fn, (long long)T, (long long)R, (long long)H);
   P.partials = static_cast<float*>(workspace);
-  P.pieces = (int32_t)p.pieces, P.parts = (int32_t)p.parts, P.part_keys = (int32_t)p.part_keys;
+  P.width = p.width, P.pieces = (int32_t)p.pieces, P.parts = (int32_t)p.parts, P.part_keys = (int32_t)p.part_keys;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (cache->d == 64)
-    p.qt == 1 ? launch<64, 1>(P, s) : p.qt == 2 ? launch<64, 2>(P, s) : launch<64, 4>(P, s);
-  else
-    p.qt == 1 ? launch<128, 1>(P, s) : p.qt == 2 ? launch<128, 2>(P, s) : launch<128, 4>(P, s);
+  if (cache->d == 64) launch<64>(P, s);
+  else launch<128>(P, s);
   return launch_status(fn);
 }

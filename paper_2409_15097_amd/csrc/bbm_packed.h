@@ -40,13 +40,49 @@ struct Span {
   int piece;          // which piece of it
 };
 
-// Which piece of which request is number `at`?  Requests are cut into pieces of `unit` rows; request r's pieces have the
-// numbers first(r) = cu[r] * mul / unit + r and those that follow (mul columns a row).  first() rises by at least the pieces of r, since
-// floor((a + n) / u) + 1 >= floor(a / u) + ceil(n / u): no number belongs to two requests, none is beyond T * mul / unit + R, and some
-// belong to nobody (begin = end).  All 64 lanes of a wave search together, a trip to memory for every factor of 64 in R.
+// Which piece of which request is number `at`?  Requests are cut into pieces of `unit` columns, `mul` columns a row; the host, which does not know the
+// offsets, launches for T * mul / unit + R of them, and no batch has more (floor((a + n) / u) + 1 >= floor(a / u) + ceil(n / u)).
+// Up to kCounted requests, all lanes of a wave count the pieces, 64 requests at a time: numbers follow each other without holes, and those that
+// belong to nobody (begin = end) are the last ones.  With the numbers below, requests of one piece each had every other number: work-groups go to
+// the shader engines of an XCD in turn, and half of them got nothing (16 requests of 128 columns over 4096 keys of the 4-bit cache: 82 us instead of 50).
+// Beyond, request r's pieces have the numbers from cu[r] * mul / unit + r on, found by a search that takes a trip to memory for every
+// factor of 64 in R, and there are holes.
+constexpr int kCounted = 512;
 __device__ __forceinline__ Span find_piece(const int32_t* __restrict__ cu, int R, int T, int mul, int unit, int at) {
   const int lane = threadIdx.x & 63;
-  auto first = [&](int c, int r) { return (int64_t)min(max(c, 0), T) * mul / unit + r; };
+  auto cut = [&](int c) { return min(max(c, 0), T); };
+  Span s;
+  s.r = s.begin = s.end = s.piece = 0;
+  if (R <= kCounted) {
+    int before = 0;  // pieces of the requests in front of these 64
+    for (int r0 = 0; r0 < R; r0 += 64) {
+      const int r = min(r0 + lane, R - 1), begin = cut(cu[r]), end = max(begin, cut(cu[r + 1]));
+      const int mine = r0 + lane < R ? (int)(((int64_t)(end - begin) * mul + unit - 1) / unit) : 0;
+      int sum = mine;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int x = __shfl_up(sum, d);
+        if (lane >= d) sum += x;
+      }
+      const int all = __builtin_amdgcn_readlane(sum, 63);
+      if (at < before + all) {
+        const uint64_t behind = __ballot(before + sum > at);
+        const int l = __ffsll((unsigned long long)behind) - 1;
+        s.r = r0 + l;
+        s.begin = __builtin_amdgcn_readlane(begin, l);
+        s.end = __builtin_amdgcn_readlane(end, l);
+        s.piece = at - before - __builtin_amdgcn_readlane(sum - mine, l);
+        break;
+      }
+      before += all;
+    }
+    s.r = __builtin_amdgcn_readfirstlane(s.r);
+    s.begin = __builtin_amdgcn_readfirstlane(s.begin);
+    s.end = __builtin_amdgcn_readfirstlane(s.end);
+    s.piece = __builtin_amdgcn_readfirstlane(s.piece);
+    return s;
+  }
+  auto first = [&](int c, int r) { return (int64_t)cut(c) * mul / unit + r; };
   int lo = 0, n = R;  // the last r in lo .. lo + n - 1 with first(r) <= at (r = lo if there is none)
   while (n > 1) {
     const int step = (n + 63) / 64;
@@ -58,21 +94,13 @@ __device__ __forceinline__ Span find_piece(const int32_t* __restrict__ cu, int R
     n = min(step, n - k);
   }
   const int c0 = cu[lo], c1 = cu[lo + 1];
-  Span s;
-  s.r = lo;
-  s.begin = min(max(c0, 0), T);
-  s.end = max(s.begin, min(max(c1, 0), T));
+  s.r = __builtin_amdgcn_readfirstlane(lo);
+  s.begin = __builtin_amdgcn_readfirstlane(cut(c0));
+  s.end = __builtin_amdgcn_readfirstlane(max(cut(c0), cut(c1)));
   const int64_t piece = at - first(c0, lo);
-  if (piece < 0 || piece * unit >= (int64_t)(s.end - s.begin) * mul) {
-    s.end = s.begin;
-    s.piece = 0;
-  } else {
-    s.piece = (int)piece;
-  }
-  s.r = __builtin_amdgcn_readfirstlane(s.r);
-  s.begin = __builtin_amdgcn_readfirstlane(s.begin);
-  s.end = __builtin_amdgcn_readfirstlane(s.end);
-  s.piece = __builtin_amdgcn_readfirstlane(s.piece);
+  const bool real = piece >= 0 && piece * unit < (int64_t)(s.end - s.begin) * mul;
+  s.piece = __builtin_amdgcn_readfirstlane(real ? (int)piece : 0);
+  if (__builtin_amdgcn_readfirstlane(real) == 0) s.end = s.begin;
   return s;
 }
 inline int64_t count_pieces(int64_t T, int64_t R, int64_t mul, int64_t unit) { return T * mul / unit + R; }

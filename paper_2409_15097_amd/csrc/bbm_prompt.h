@@ -97,12 +97,4 @@ __device__ __forceinline__ void store_strided(const f32x16 (&acc)[D / 32], float
   }
 }
 
-// Bits 0 .. lim of 64.
-__device__ __forceinline__ uint64_t bits_up_to(int lim) { return lim >= 63 ? ~0ull : lim < 0 ? 0ull : (2ull << lim) - 1ull; }
-// x where bit 8 * (e / 4) + e % 4 of w is set, else -infinity (by bits: x may be anything).
-__device__ __forceinline__ float keep_if(uint32_t w, int e, float x) {
-  const uint32_t keep = (uint32_t)((int32_t)(w << (31 - (8 * (e / 4) + e % 4))) >> 31);
-  return __uint_as_float((__float_as_uint(x) & keep) | (0xff800000u & ~keep));
-}
-
 }  // namespace bbm

@@ -9,7 +9,7 @@ from typing import Optional
 
 import torch
 
-from .binding import _check, _null_ctx, _ptr, _stream, lib
+from .binding import _check, _current_device, _null_ctx, _raw_stream, lib
 
 
 class _CPacked(C.Structure):
@@ -22,8 +22,8 @@ class _CCache(C.Structure):
 
 
 def _declare(L):
-    i64, vp, ci, cf, pk = C.c_int64, C.c_void_p, C.c_int, C.c_float, C.POINTER(_CPacked)
-    cache = C.POINTER(_CCache)
+    i64, vp, ci, cf = C.c_int64, C.c_void_p, C.c_int, C.c_float
+    pk = cache = vp  # (addresses of structures: a call fills one array with all of its packed tensors)
     for name, args in {
         "bbm_build_slots": [vp, vp, i64, vp, i64, i64, ci, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp],
         "bbm_rope": [pk, pk, i64, pk, pk, i64, i64, ci, ci, ci, ci, vp, vp, cf, vp],
@@ -44,25 +44,71 @@ def _declare(L):
 _declare(lib)
 
 
-def _on(device, stream, *others):
-    """The context in which a call on `device` allocates and launches; every tensor of `others` has to be there too."""
-    for t in others:
-        assert t is None or t.device == device, "the tensors of a call lie on one device"
+# A small call is all submission: of 10.8 us that a rotation of 33 tokens took the host, the launch is 3.2, allocating two results 2.9; structures a tensor,
+# contexts, devices compared as objects were the rest.  So: the current device's stream is asked for by its number, packed tensors go into one
+# array, and only a call for another device or stream enters a context (and then calls itself).
+_I64x6, _I64x12, _I64x24 = C.c_int64 * 6, C.c_int64 * 12, C.c_int64 * 24
+_address = C.addressof
+
+
+def _elsewhere(device: int, stream) -> bool:
+    if stream is None and _raw_stream is not None and _current_device is not None:
+        return device != _current_device()
+    return True
+
+
+def _context(device: int, stream):
+    """For a call on another device than the current one, or on a stream of its own."""
     if stream is not None:
-        assert stream.device == device, "the stream is another device's"
+        assert stream.device.index == device, "the stream is another device's"
         return torch.cuda.stream(stream)
-    return _null_ctx() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    return torch.cuda.device(device) if device != torch.cuda.current_device() else _null_ctx()
 
 
-def _packed(x: torch.Tensor, T: int, heads: int, d: int) -> _CPacked:
-    assert x.is_cuda and x.dtype == torch.bfloat16 and x.shape == (T, heads, d), "a packed bf16 tensor of this many tokens, heads and elements"
+def _here(device: int) -> int:
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+def _packed(x: torch.Tensor, device: int, T: int, heads: int, d: int):
+    """(address, row stride, head stride) of a packed tensor."""
+    assert x.dtype is torch.bfloat16 and x.shape == (T, heads, d), "a packed bf16 tensor of this many tokens, heads and elements"
+    assert x.get_device() == device, "the tensors of a call lie on one GPU"
     row, head, one = x.stride()
     assert one == 1, "the elements of a head lie one behind the other"
-    return _CPacked(x.data_ptr(), row if T > 1 else 0, head if heads > 1 else 0)   # (a stride that is never taken may be anything)
+    return x.data_ptr(), row if T > 1 else 0, head if heads > 1 else 0   # (a stride that is never taken may be anything)
 
 
-def _ints(x: torch.Tensor, n: Optional[int] = None):
-    assert x.is_cuda and x.dtype == torch.int32 and x.is_contiguous() and x.dim() == 1 and (n is None or x.numel() == n)
+def _ints(x: torch.Tensor, device: int, n: Optional[int] = None) -> int:
+    assert x.dtype is torch.int32 and x.is_contiguous() and x.dim() == 1 and (n is None or x.numel() == n), "a contiguous int32 vector of this length"
+    assert x.get_device() == device, "the tensors of a call lie on one GPU"
+    return x.data_ptr()
+
+
+def _table(x: torch.Tensor, device: int, R: int):
+    """(address, row stride, width) of a block table."""
+    assert x.dtype is torch.int32 and x.dim() == 2 and x.shape[0] == R and x.stride(1) == 1, "an int32 table of a row for each request"
+    assert x.get_device() == device, "the tensors of a call lie on one GPU"
+    width = x.shape[1]
+    return x.data_ptr(), x.stride(0) if R > 1 else width, width
+
+
+def _lse(x: torch.Tensor, device: int, H: int, T: int) -> int:
+    assert x.dtype is torch.float32 and x.is_contiguous() and x.shape == (H, T), "a contiguous fp32 log-sum-exp [H, T]"
+    assert x.get_device() == device, "the tensors of a call lie on one GPU"
+    return x.data_ptr()
+
+
+def _gpu(x: torch.Tensor) -> int:
+    device = x.get_device()
+    assert device >= 0, "the tensors of a call lie on one GPU"
+    return device
+
+
+def _workspace(x: Optional[torch.Tensor], device: int):
+    if x is None:
+        return None, 0
+    assert x.is_contiguous() and x.get_device() == device, "a contiguous workspace on the GPU of the call"
+    return x.data_ptr(), x.numel() * x.element_size()
 
 
 @dataclass
@@ -79,18 +125,20 @@ def bbm_build_slots(ctx_lens: torch.Tensor, new_lens: torch.Tensor, block_table:
                     num_tokens: int, page: int, stream=None) -> Slots:
     """ctx_lens, new_lens: int32 [R]; block_table: int32 [R, max_pages] (row stride may exceed max_pages), gets the pages that the step
     takes from free_pages (int32 [n]), index free_at (int32 [1]) on; num_tokens: rows of the step's tensors."""
-    R = ctx_lens.numel()
-    _ints(ctx_lens), _ints(new_lens, R), _ints(free_pages), _ints(free_at, 1)
-    assert block_table.is_cuda and block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.shape[0] == R and block_table.stride(1) == 1
-    width = block_table.shape[1]
-    with _on(ctx_lens.device, stream, new_lens, block_table, free_pages, free_at):
-        buf = torch.empty(2 * R + 2 + 2 * num_tokens, dtype=torch.int32, device=ctx_lens.device)
-        cu, lens, pos, slots, nxt = buf.split((R + 1, R, num_tokens, num_tokens, 1))
-        at = buf.data_ptr()
-        _check(lib.bbm_build_slots(_ptr(ctx_lens), _ptr(new_lens), R, _ptr(block_table), block_table.stride(0) if R > 1 else width, width, page,
-                                   _ptr(free_pages), free_pages.numel(), _ptr(free_at), num_tokens, at, at + 4 * (R + 1), at + 4 * (2 * R + 1),
-                                   at + 4 * (2 * R + 1 + num_tokens), at + 4 * (2 * R + 1 + 2 * num_tokens), _stream()))
-    return Slots(cu, lens, pos, slots, nxt)
+    dev, R = _gpu(ctx_lens), ctx_lens.numel()
+    if _elsewhere(dev, stream):
+        with _context(dev, stream):
+            return _build_slots(dev, R, ctx_lens, new_lens, block_table, free_pages, free_at, num_tokens, page)
+    return _build_slots(dev, R, ctx_lens, new_lens, block_table, free_pages, free_at, num_tokens, page)
+
+
+def _build_slots(dev, R, ctx_lens, new_lens, block_table, free_pages, free_at, T, page):
+    table, stride, width = _table(block_table, dev, R)
+    args = _ints(ctx_lens, dev), _ints(new_lens, dev, R), R, table, stride, width, page, _ints(free_pages, dev), free_pages.numel(), _ints(free_at, dev, 1)
+    buf = ctx_lens.new_empty(2 * R + 2 + 2 * T)
+    at = buf.data_ptr()
+    _check(lib.bbm_build_slots(*args, T, at, at + 4 * (R + 1), at + 4 * (2 * R + 1), at + 4 * (2 * R + 1 + T), at + 4 * (2 * R + 1 + 2 * T), _here(dev)))
+    return Slots(*torch.split_with_sizes(buf, (R + 1, R, T, T, 1)))
 
 
 def rope_freqs(rot: int, base: float = 10000.0, factor: float = 1.0, method: Optional[str] = None, trained_len: Optional[int] = None,
@@ -126,35 +174,51 @@ def bbm_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor
              inverse: bool = False, out_q: Optional[torch.Tensor] = None, out_k: Optional[torch.Tensor] = None, stream=None):
     """q: packed [T, H, d], k: packed [T, Hk, d] or None; positions int32 [T]; freqs fp32 [rot/2] (rope_freqs).  Returns (q, k) turned,
     contiguous unless out_q and out_k are given (out_q=q turns in place).  inverse=True is the gradient: of the outputs to that of the inputs."""
+    dev = _gpu(q)
+    if _elsewhere(dev, stream):
+        with _context(dev, stream):
+            return _rope(dev, q, k, positions, freqs, interleaved, mscale, inverse, out_q, out_k)
+    return _rope(dev, q, k, positions, freqs, interleaved, mscale, inverse, out_q, out_k)
+
+
+def _rope(dev, q, k, positions, freqs, interleaved, mscale, inverse, out_q, out_k):
     T, H, d = q.shape
-    Hk = 0 if k is None else k.shape[1]
-    _ints(positions, T)
-    assert freqs.is_cuda and freqs.dtype == torch.float32 and freqs.is_contiguous() and freqs.dim() == 1
-    with _on(q.device, stream, k, positions, freqs, out_q, out_k):
-        if out_q is None:
-            out_q = torch.empty((T, H, d), dtype=q.dtype, device=q.device)
-        if k is not None and out_k is None:
-            out_k = torch.empty((T, Hk, d), dtype=k.dtype, device=k.device)
-        _check(lib.bbm_rope(_packed(q, T, H, d), _packed(out_q, T, H, d), H, None if k is None else _packed(k, T, Hk, d),
-                            None if k is None else _packed(out_k, T, Hk, d), Hk, T, d, 2 * freqs.numel(), int(interleaved), int(inverse), _ptr(positions),
-                            _ptr(freqs), mscale, _stream()))
+    assert freqs.dtype is torch.float32 and freqs.is_contiguous() and freqs.dim() == 1 and freqs.get_device() == dev, "fp32 frequencies on the GPU of the call"
+    pos, packed = _ints(positions, dev, T), _packed(q, dev, T, H, d)
+    out_q = q.new_empty((T, H, d)) if out_q is None else out_q
+    packed += _packed(out_q, dev, T, H, d)
+    Hk = 0
+    if k is not None:
+        Hk = k.shape[1]
+        packed += _packed(k, dev, T, Hk, d)
+        out_k = k.new_empty((T, Hk, d)) if out_k is None else out_k
+        packed += _packed(out_k, dev, T, Hk, d)
+    keep = _I64x12(*packed)
+    at = _address(keep)
+    _check(lib.bbm_rope(at, at + 24, H, at + 48, at + 72, Hk, T, d, 2 * freqs.shape[0], interleaved, inverse, pos, freqs.data_ptr(), mscale, _here(dev)))
     return out_q, out_k
 
 
 def bbm_prompt_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torch.Tensor, softmax_scale: Optional[float] = None,
                         out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, stream=None):
     """q: packed [T, H, d], k, v: packed [T, Hk, d]; cu int32 [R + 1].  Returns (O bf16 [T, H, d], lse fp32 [H, T])."""
+    dev = _gpu(q)
+    if _elsewhere(dev, stream):
+        with _context(dev, stream):
+            return _prompt_fwd(dev, q, k, v, cu, softmax_scale, out, lse)
+    return _prompt_fwd(dev, q, k, v, cu, softmax_scale, out, lse)
+
+
+def _prompt_fwd(dev, q, k, v, cu, softmax_scale, out, lse):
     T, H, d = q.shape
-    Hk = k.shape[1]
-    _ints(cu)
-    assert lse is None or (lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (H, T))
-    with _on(q.device, stream, k, v, cu, out, lse):
-        if out is None:
-            out = torch.empty((T, H, d), dtype=q.dtype, device=q.device)
-        if lse is None:
-            lse = torch.empty((H, T), dtype=torch.float32, device=q.device)
-        _check(lib.bbm_prompt_attn_fwd(_packed(q, T, H, d), _packed(k, T, Hk, d), _packed(v, T, Hk, d), _packed(out, T, H, d), _ptr(lse), T, cu.numel() - 1,
-                                       _ptr(cu), H, Hk, d, float(d) ** -0.5 if softmax_scale is None else softmax_scale, _stream()))
+    Hk, offsets = k.shape[1], _ints(cu, dev)
+    packed = _packed(q, dev, T, H, d) + _packed(k, dev, T, Hk, d) + _packed(v, dev, T, Hk, d)
+    out = q.new_empty((T, H, d)) if out is None else out
+    lse = q.new_empty((H, T), dtype=torch.float32) if lse is None else lse
+    keep = _I64x12(*packed, *_packed(out, dev, T, H, d))
+    at = _address(keep)
+    _check(lib.bbm_prompt_attn_fwd(at, at + 24, at + 48, at + 72, _lse(lse, dev, H, T), T, cu.shape[0] - 1, offsets, H, Hk, d,
+                                   d ** -0.5 if softmax_scale is None else softmax_scale, _here(dev)))
     return out, lse
 
 
@@ -166,21 +230,26 @@ def bbm_prompt_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: to
                         softmax_scale: Optional[float] = None, dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
                         dv: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
     """Of what bbm_prompt_attn_fwd took and gave, and d_o as o: (dQ [T, H, d], dK, dV [T, Hk, d]), bf16."""
+    dev = _gpu(q)
+    if _elsewhere(dev, stream):
+        with _context(dev, stream):
+            return _prompt_bwd(dev, q, k, v, o, d_o, lse, cu, softmax_scale, dq, dk, dv, workspace)
+    return _prompt_bwd(dev, q, k, v, o, d_o, lse, cu, softmax_scale, dq, dk, dv, workspace)
+
+
+def _prompt_bwd(dev, q, k, v, o, d_o, lse, cu, softmax_scale, dq, dk, dv, workspace):
     T, H, d = q.shape
-    Hk = k.shape[1]
-    _ints(cu)
-    assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (H, T)
-    with _on(q.device, stream, k, v, o, d_o, lse, cu, dq, dk, dv, workspace):
-        dq = torch.empty((T, H, d), dtype=q.dtype, device=q.device) if dq is None else dq
-        dk = torch.empty((T, Hk, d), dtype=q.dtype, device=q.device) if dk is None else dk
-        dv = torch.empty((T, Hk, d), dtype=q.dtype, device=q.device) if dv is None else dv
-        if workspace is None:
-            workspace = torch.empty(bbm_prompt_attn_bwd_workspace_bytes(T, H), dtype=torch.uint8, device=q.device)
-        assert workspace.is_contiguous()
-        _check(lib.bbm_prompt_attn_bwd(_packed(q, T, H, d), _packed(k, T, Hk, d), _packed(v, T, Hk, d), _packed(o, T, H, d), _packed(d_o, T, H, d), _ptr(lse),
-                                       _packed(dq, T, H, d), _packed(dk, T, Hk, d), _packed(dv, T, Hk, d), T, cu.numel() - 1, _ptr(cu), H, Hk, d,
-                                       float(d) ** -0.5 if softmax_scale is None else softmax_scale, _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                       _stream()))
+    Hk, offsets = k.shape[1], _ints(cu, dev)
+    packed = _packed(q, dev, T, H, d) + _packed(k, dev, T, Hk, d) + _packed(v, dev, T, Hk, d) + _packed(o, dev, T, H, d) + _packed(d_o, dev, T, H, d)
+    dq = q.new_empty((T, H, d)) if dq is None else dq
+    dk = q.new_empty((T, Hk, d)) if dk is None else dk
+    dv = q.new_empty((T, Hk, d)) if dv is None else dv
+    if workspace is None:
+        workspace = q.new_empty(lib.bbm_prompt_attn_bwd_workspace_bytes(T, H), dtype=torch.uint8)
+    keep = _I64x24(*packed, *_packed(dq, dev, T, H, d), *_packed(dk, dev, T, Hk, d), *_packed(dv, dev, T, Hk, d))
+    at = _address(keep)
+    _check(lib.bbm_prompt_attn_bwd(at, at + 24, at + 48, at + 72, at + 96, _lse(lse, dev, H, T), at + 120, at + 144, at + 168, T, cu.shape[0] - 1, offsets, H, Hk, d,
+                                   d ** -0.5 if softmax_scale is None else softmax_scale, *_workspace(workspace, dev), _here(dev)))
     return dq, dk, dv
 
 
@@ -194,11 +263,12 @@ class KV4Cache:
     v_scale: torch.Tensor
 
     def c_struct(self) -> _CCache:
+        device = _gpu(self.k)
         pages, Hk, page, half = self.k.shape
         for t, shape in ((self.k, (pages, Hk, page, half)), (self.v, (pages, Hk, page, half)), (self.k_scale, (pages, Hk, page, half // 16)),
                          (self.v_scale, (pages, Hk, half // 16, page))):
-            assert t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous() and t.shape == shape, "a cache's tensors have the shapes of KV4Cache"
-        return _CCache(_ptr(self.k), _ptr(self.k_scale), _ptr(self.v), _ptr(self.v_scale), pages, Hk, page, 2 * half)
+            assert t.dtype is torch.uint8 and t.is_contiguous() and t.shape == shape and t.get_device() == device, "a cache's tensors have the shapes of KV4Cache, on one GPU"
+        return _CCache(self.k.data_ptr(), self.k_scale.data_ptr(), self.v.data_ptr(), self.v_scale.data_ptr(), pages, Hk, page, 2 * half)
 
 
 def kv4_cache(pages: int, heads: int, d: int, page: int, device="cuda") -> KV4Cache:
@@ -209,23 +279,41 @@ def kv4_cache(pages: int, heads: int, d: int, page: int, device="cuda") -> KV4Ca
 
 def bbm_kv4_append(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: KV4Cache, stream=None) -> KV4Cache:
     """k, v: packed [T, Hk, d] into the slots (int32 [T]) of the cache; rows with a slot outside the cache are left out."""
+    dev = _gpu(k)
+    if _elsewhere(dev, stream):
+        with _context(dev, stream):
+            return _kv4_append(dev, k, v, slots, cache)
+    return _kv4_append(dev, k, v, slots, cache)
+
+
+def _kv4_append(dev, k, v, slots, cache):
     T, Hk, d = k.shape
-    _ints(slots, T)
     c = cache.c_struct()
-    assert (Hk, d) == (c.Hk, c.d), "the cache has other heads"
-    with _on(k.device, stream, v, slots, cache.k, cache.k_scale, cache.v, cache.v_scale):
-        _check(lib.bbm_kv4_append(_packed(k, T, Hk, d), _packed(v, T, Hk, d), T, _ptr(slots), c, _stream()))
+    assert (Hk, d) == (c.Hk, c.d) and cache.k.get_device() == dev, "the cache has other heads, or lies elsewhere"
+    keep = _I64x6(*_packed(k, dev, T, Hk, d), *_packed(v, dev, T, Hk, d))
+    at = _address(keep)
+    _check(lib.bbm_kv4_append(at, at + 24, T, _ints(slots, dev, T), _address(c), _here(dev)))
     return cache
 
 
 def bbm_kv4_read(slots: torch.Tensor, cache: KV4Cache, out_k: Optional[torch.Tensor] = None, out_v: Optional[torch.Tensor] = None, stream=None):
     """The values (k, v) bf16 [T, Hk, d] that the cache holds for the slots (int32 [T]); zeros for a slot outside the cache."""
-    _ints(slots)
-    c, T = cache.c_struct(), slots.numel()
-    with _on(slots.device, stream, cache.k, cache.k_scale, cache.v, cache.v_scale, out_k, out_v):
-        out_k = torch.empty((T, c.Hk, c.d), dtype=torch.bfloat16, device=slots.device) if out_k is None else out_k
-        out_v = torch.empty((T, c.Hk, c.d), dtype=torch.bfloat16, device=slots.device) if out_v is None else out_v
-        _check(lib.bbm_kv4_read(_ptr(slots), T, c, _packed(out_k, T, c.Hk, c.d), _packed(out_v, T, c.Hk, c.d), _stream()))
+    dev = _gpu(slots)
+    if _elsewhere(dev, stream):
+        with _context(dev, stream):
+            return _kv4_read(dev, slots, cache, out_k, out_v)
+    return _kv4_read(dev, slots, cache, out_k, out_v)
+
+
+def _kv4_read(dev, slots, cache, out_k, out_v):
+    c, T = cache.c_struct(), slots.shape[0]
+    Hk, d = c.Hk, c.d
+    assert cache.k.get_device() == dev, "the cache lies elsewhere"
+    out_k = slots.new_empty((T, Hk, d), dtype=torch.bfloat16) if out_k is None else out_k
+    out_v = slots.new_empty((T, Hk, d), dtype=torch.bfloat16) if out_v is None else out_v
+    keep = _I64x6(*_packed(out_k, dev, T, Hk, d), *_packed(out_v, dev, T, Hk, d))
+    at = _address(keep)
+    _check(lib.bbm_kv4_read(_ints(slots, dev), T, _address(c), at, at + 24, _here(dev)))
     return out_k, out_v
 
 
@@ -239,27 +327,31 @@ def bbm_kv4_attn(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor, le
     """q: packed [T, H, d], the last cu[r+1] - cu[r] of the lens[r] tokens that request r has in the cache (append first); block_table int32
     [R, max_pages]; mask: int64 [T, words], bit j of a row's words: the row sees new token j of its request (None: causal); max_len: an upper
     bound of lens, for the work split (None: what the table holds).  Returns (O bf16 [T, H, d], lse fp32 [H, T])."""
+    dev = _gpu(q)
+    if _elsewhere(dev, stream):
+        with _context(dev, stream):
+            return _kv4_attn(dev, q, cache, block_table, lens, cu, mask, max_len, softmax_scale, out, lse, workspace)
+    return _kv4_attn(dev, q, cache, block_table, lens, cu, mask, max_len, softmax_scale, out, lse, workspace)
+
+
+def _kv4_attn(dev, q, cache, block_table, lens, cu, mask, max_len, softmax_scale, out, lse, workspace):
     T, H, d = q.shape
-    R = lens.numel()
-    c = cache.c_struct()
-    _ints(lens), _ints(cu, R + 1)
-    assert d == c.d, "the cache has another head size"
-    assert block_table.is_cuda and block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.shape[0] == R and block_table.stride(1) == 1
-    assert mask is None or (mask.is_cuda and mask.dtype == torch.int64 and mask.is_contiguous() and mask.dim() == 2 and mask.shape[0] == T)
-    assert lse is None or (lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (H, T))
-    width = block_table.shape[1]
+    R, c = lens.shape[0], cache.c_struct()
+    assert d == c.d and cache.k.get_device() == dev, "the cache has another head size, or lies elsewhere"
+    table, stride, width = _table(block_table, dev, R)
+    bits, words = None, 0
+    if mask is not None:
+        assert mask.dtype is torch.int64 and mask.is_contiguous() and mask.dim() == 2 and mask.shape[0] == T and mask.get_device() == dev, "an int64 mask of words for every row"
+        bits, words = mask.data_ptr(), mask.shape[1]
     max_len = width * c.page if max_len is None else max_len
-    with _on(q.device, stream, cache.k, cache.k_scale, cache.v, cache.v_scale, block_table, lens, cu, mask, out, lse, workspace):
-        if out is None:
-            out = torch.empty((T, H, d), dtype=q.dtype, device=q.device)
-        if lse is None:
-            lse = torch.empty((H, T), dtype=torch.float32, device=q.device)
-        if workspace is None:
-            need = bbm_kv4_attn_workspace_bytes(T, R, H, c.Hk, d, max_len)
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-        assert workspace is None or workspace.is_contiguous()
-        _check(lib.bbm_kv4_attn(_packed(q, T, H, d), _packed(out, T, H, d), _ptr(lse), T, R, _ptr(cu), _ptr(lens), _ptr(block_table),
-                                block_table.stride(0) if R > 1 else width, width, _ptr(mask), 0 if mask is None else mask.shape[1], c, H,
-                                float(d) ** -0.5 if softmax_scale is None else softmax_scale, max_len, _ptr(workspace),
-                                0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+    packed = _packed(q, dev, T, H, d)
+    out = q.new_empty((T, H, d)) if out is None else out
+    lse = q.new_empty((H, T), dtype=torch.float32) if lse is None else lse
+    if workspace is None:
+        need = lib.bbm_kv4_attn_workspace_bytes(T, R, H, c.Hk, d, max_len)
+        workspace = q.new_empty(need, dtype=torch.uint8) if need else None
+    keep = _I64x6(*packed, *_packed(out, dev, T, H, d))
+    at = _address(keep)
+    _check(lib.bbm_kv4_attn(at, at + 24, _lse(lse, dev, H, T), T, R, _ints(cu, dev, R + 1), _ints(lens, dev, R), table, stride, width, bits, words, _address(c), H,
+                            d ** -0.5 if softmax_scale is None else softmax_scale, max_len, *_workspace(workspace, dev), _here(dev)))
     return out, lse

@@ -333,7 +333,8 @@ def check_cached(bbm, c, table, lens, cu, T, q, words, H, Hk, d, page, **kw):
     ([1], [1], 1, 1, 16, "plain", None), ([0, 3, 17], [1, 1, 1], 4, 2, 16, "fused", None), ([63, 64, 65, 200, 1, 0], [1] * 6, 8, 1, 32, "plain", None),
     ([130, 300, 31], [1, 0, 1], 6, 2, 64, "heads", None), ([40, 500, 7], [5, 33, 7], 6, 2, 16, "fused", None), ([40, 90], [40, 60], 32, 2, 128, "plain", None),
     ([20, 70, 5], [20, 6, 5], 4, 4, 16, "plain", 1), ([300, 129], [70, 129], 3, 1, 64, "heads", 2), ([300, 150], [100, 100], 5, 1, 32, "plain", 1),
-    ([3, 2], [5, 4], 4, 2, 16, "plain", None), ([3000, 9, 1700], [1, 1, 2], 12, 4, 64, "plain", None), ([33] * 70, [1] * 70, 2, 1, 16, "plain", None)])
+    ([3, 2], [5, 4], 4, 2, 16, "plain", None), ([2900, 9, 1700], [1, 1, 2], 12, 4, 64, "plain", None), ([2500, 2100], [40, 30], 8, 2, 32, "fused", None), ([2500, 2100], [70, 20], 4, 2, 64, "plain", 1),
+    ([33] * 70, [1] * 70, 2, 1, 16, "plain", None)])
 def test_cached(bbm, lens, news, H, Hk, d, page, layout, tree):
     c, table, cu, T, q, words = cached_case(bbm, lens, news, H, Hk, d, page, layout, seed=len(lens), tree=tree, before=2, behind=3)
     first = check_cached(bbm, c, table, lens, cu, T, q, words, H, Hk, d, page)

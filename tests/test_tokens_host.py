@@ -34,7 +34,7 @@ def test_every_declared_symbol_is_exported_and_bound(bbm):
 
 def pk(ptr=P, row=1024, head=128):
     from paper_2409_15097_amd.tokens import _CPacked
-    return None if ptr is None else _CPacked(ptr, row, head)
+    return None if ptr is None else C.byref(_CPacked(ptr, row, head))
 
 
 def slots(bbm, ctx=P, new=P, R=4, table=P, stride=8, width=8, page=64, free=P, n_free=9, at=P, T=5, cu=2 * P, lens=3 * P, pos=4 * P, sl=5 * P, nxt=6 * P):
@@ -103,7 +103,7 @@ def test_prompt_attention_refuses(bbm):
 
 def cache(k=P, ks=P, v=P, vs=P, pages=8, Hk=2, page=64, d=64):
     from paper_2409_15097_amd.tokens import _CCache
-    return _CCache(k, ks, v, vs, pages, Hk, page, d)
+    return C.byref(_CCache(k, ks, v, vs, pages, Hk, page, d))
 
 
 BAD_CACHE = [dict(k=None), dict(ks=None), dict(v=None), dict(vs=None), dict(k=P + 8), dict(vs=P + 4), dict(pages=0), dict(Hk=0)]
