@@ -78,6 +78,14 @@ def _packed(x: torch.Tensor, device: int, T: int, heads: int, d: int):
     return x.data_ptr(), row if T > 1 else 0, head if heads > 1 else 0   # (a stride that is never taken may be anything)
 
 
+def _out(x: Optional[torch.Tensor], like: torch.Tensor, device: int, T: int, heads: int, d: int):
+    """A packed output, allocated if there is none, and what _packed says of it."""
+    if x is not None:
+        return x, _packed(x, device, T, heads, d)
+    x = like.new_empty((T, heads, d), dtype=torch.bfloat16)
+    return x, (x.data_ptr(), heads * d if T > 1 else 0, d if heads > 1 else 0)
+
+
 def _ints(x: torch.Tensor, device: int, n: Optional[int] = None) -> int:
     assert x.dtype is torch.int32 and x.is_contiguous() and x.dim() == 1 and (n is None or x.numel() == n), "a contiguous int32 vector of this length"
     assert x.get_device() == device, "the tensors of a call lie on one GPU"
@@ -96,6 +104,13 @@ def _lse(x: torch.Tensor, device: int, H: int, T: int) -> int:
     assert x.dtype is torch.float32 and x.is_contiguous() and x.shape == (H, T), "a contiguous fp32 log-sum-exp [H, T]"
     assert x.get_device() == device, "the tensors of a call lie on one GPU"
     return x.data_ptr()
+
+
+def _lse_out(x: Optional[torch.Tensor], like: torch.Tensor, device: int, H: int, T: int):
+    if x is not None:
+        return x, _lse(x, device, H, T)
+    x = like.new_empty((H, T), dtype=torch.float32)
+    return x, x.data_ptr()
 
 
 def _gpu(x: torch.Tensor) -> int:
@@ -185,15 +200,14 @@ def _rope(dev, q, k, positions, freqs, interleaved, mscale, inverse, out_q, out_
     T, H, d = q.shape
     assert freqs.dtype is torch.float32 and freqs.is_contiguous() and freqs.dim() == 1 and freqs.get_device() == dev, "fp32 frequencies on the GPU of the call"
     pos, packed = _ints(positions, dev, T), _packed(q, dev, T, H, d)
-    out_q = q.new_empty((T, H, d)) if out_q is None else out_q
-    packed += _packed(out_q, dev, T, H, d)
-    Hk = 0
-    if k is not None:
+    out_q, to = _out(out_q, q, dev, T, H, d)
+    if k is None:
+        Hk, keep = 0, _I64x12(*packed, *to)
+    else:
         Hk = k.shape[1]
-        packed += _packed(k, dev, T, Hk, d)
-        out_k = k.new_empty((T, Hk, d)) if out_k is None else out_k
-        packed += _packed(out_k, dev, T, Hk, d)
-    keep = _I64x12(*packed)
+        more = _packed(k, dev, T, Hk, d)
+        out_k, to_k = _out(out_k, k, dev, T, Hk, d)
+        keep = _I64x12(*packed, *to, *more, *to_k)
     at = _address(keep)
     _check(lib.bbm_rope(at, at + 24, H, at + 48, at + 72, Hk, T, d, 2 * freqs.shape[0], interleaved, inverse, pos, freqs.data_ptr(), mscale, _here(dev)))
     return out_q, out_k
@@ -213,11 +227,11 @@ def _prompt_fwd(dev, q, k, v, cu, softmax_scale, out, lse):
     T, H, d = q.shape
     Hk, offsets = k.shape[1], _ints(cu, dev)
     packed = _packed(q, dev, T, H, d) + _packed(k, dev, T, Hk, d) + _packed(v, dev, T, Hk, d)
-    out = q.new_empty((T, H, d)) if out is None else out
-    lse = q.new_empty((H, T), dtype=torch.float32) if lse is None else lse
-    keep = _I64x12(*packed, *_packed(out, dev, T, H, d))
+    out, to = _out(out, q, dev, T, H, d)
+    lse, lse_at = _lse_out(lse, q, dev, H, T)
+    keep = _I64x12(*packed, *to)
     at = _address(keep)
-    _check(lib.bbm_prompt_attn_fwd(at, at + 24, at + 48, at + 72, _lse(lse, dev, H, T), T, cu.shape[0] - 1, offsets, H, Hk, d,
+    _check(lib.bbm_prompt_attn_fwd(at, at + 24, at + 48, at + 72, lse_at, T, cu.shape[0] - 1, offsets, H, Hk, d,
                                    d ** -0.5 if softmax_scale is None else softmax_scale, _here(dev)))
     return out, lse
 
@@ -241,34 +255,36 @@ def _prompt_bwd(dev, q, k, v, o, d_o, lse, cu, softmax_scale, dq, dk, dv, worksp
     T, H, d = q.shape
     Hk, offsets = k.shape[1], _ints(cu, dev)
     packed = _packed(q, dev, T, H, d) + _packed(k, dev, T, Hk, d) + _packed(v, dev, T, Hk, d) + _packed(o, dev, T, H, d) + _packed(d_o, dev, T, H, d)
-    dq = q.new_empty((T, H, d)) if dq is None else dq
-    dk = q.new_empty((T, Hk, d)) if dk is None else dk
-    dv = q.new_empty((T, Hk, d)) if dv is None else dv
+    (dq, to_q), (dk, to_k), (dv, to_v) = _out(dq, q, dev, T, H, d), _out(dk, k, dev, T, Hk, d), _out(dv, v, dev, T, Hk, d)
     if workspace is None:
         workspace = q.new_empty(lib.bbm_prompt_attn_bwd_workspace_bytes(T, H), dtype=torch.uint8)
-    keep = _I64x24(*packed, *_packed(dq, dev, T, H, d), *_packed(dk, dev, T, Hk, d), *_packed(dv, dev, T, Hk, d))
+    keep = _I64x24(*packed, *to_q, *to_k, *to_v)
     at = _address(keep)
     _check(lib.bbm_prompt_attn_bwd(at, at + 24, at + 48, at + 72, at + 96, _lse(lse, dev, H, T), at + 120, at + 144, at + 168, T, cu.shape[0] - 1, offsets, H, Hk, d,
                                    d ** -0.5 if softmax_scale is None else softmax_scale, *_workspace(workspace, dev), _here(dev)))
     return dq, dk, dv
 
 
-@dataclass
 class KV4Cache:
-    """The tensors of a paged cache in 4 bits (uint8, contiguous): k, v [pages, Hk, page, d/2], k_scale [pages, Hk, page, d/32],
+    """The tensors of a paged cache in 4 bits (uint8, contiguous, on one GPU): k, v [pages, Hk, page, d/2], k_scale [pages, Hk, page, d/32],
     v_scale [pages, Hk, d/32, page]."""
-    k: torch.Tensor
-    k_scale: torch.Tensor
-    v: torch.Tensor
-    v_scale: torch.Tensor
+    __slots__ = ("k", "k_scale", "v", "v_scale", "device", "c_struct")
 
-    def c_struct(self) -> _CCache:
-        device = _gpu(self.k)
-        pages, Hk, page, half = self.k.shape
-        for t, shape in ((self.k, (pages, Hk, page, half)), (self.v, (pages, Hk, page, half)), (self.k_scale, (pages, Hk, page, half // 16)),
-                         (self.v_scale, (pages, Hk, half // 16, page))):
-            assert t.dtype is torch.uint8 and t.is_contiguous() and t.shape == shape and t.get_device() == device, "a cache's tensors have the shapes of KV4Cache, on one GPU"
-        return _CCache(self.k.data_ptr(), self.k_scale.data_ptr(), self.v.data_ptr(), self.v_scale.data_ptr(), pages, Hk, page, 2 * half)
+    def __init__(self, k: torch.Tensor, k_scale: torch.Tensor, v: torch.Tensor, v_scale: torch.Tensor):
+        device = _gpu(k)
+        pages, Hk, page, half = k.shape
+        values, groups = (pages, Hk, page, half), half // 16
+        assert v.shape == values and k_scale.shape == (pages, Hk, page, groups) and v_scale.shape == (pages, Hk, groups, page), "a cache's tensors have the shapes of KV4Cache"
+        u8 = torch.uint8
+        assert k.dtype is u8 and v.dtype is u8 and k_scale.dtype is u8 and v_scale.dtype is u8, "a cache's tensors are uint8"
+        assert k.is_contiguous() and v.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous(), "a cache's tensors are contiguous"
+        assert v.get_device() == device and k_scale.get_device() == device and v_scale.get_device() == device, "a cache's tensors lie on one GPU"
+        put = object.__setattr__
+        put(self, "k", k), put(self, "k_scale", k_scale), put(self, "v", v), put(self, "v_scale", v_scale), put(self, "device", device)
+        put(self, "c_struct", _CCache(k.data_ptr(), k_scale.data_ptr(), v.data_ptr(), v_scale.data_ptr(), pages, Hk, page, 2 * half))
+
+    def __setattr__(self, name, value):
+        raise AttributeError("a cache's tensors are what it was made of: make another KV4Cache")
 
 
 def kv4_cache(pages: int, heads: int, d: int, page: int, device="cuda") -> KV4Cache:
@@ -288,8 +304,8 @@ def bbm_kv4_append(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache:
 
 def _kv4_append(dev, k, v, slots, cache):
     T, Hk, d = k.shape
-    c = cache.c_struct()
-    assert (Hk, d) == (c.Hk, c.d) and cache.k.get_device() == dev, "the cache has other heads, or lies elsewhere"
+    c = cache.c_struct
+    assert (Hk, d) == (c.Hk, c.d) and cache.device == dev, "the cache has other heads, or lies elsewhere"
     keep = _I64x6(*_packed(k, dev, T, Hk, d), *_packed(v, dev, T, Hk, d))
     at = _address(keep)
     _check(lib.bbm_kv4_append(at, at + 24, T, _ints(slots, dev, T), _address(c), _here(dev)))
@@ -306,12 +322,11 @@ def bbm_kv4_read(slots: torch.Tensor, cache: KV4Cache, out_k: Optional[torch.Ten
 
 
 def _kv4_read(dev, slots, cache, out_k, out_v):
-    c, T = cache.c_struct(), slots.shape[0]
+    c, T = cache.c_struct, slots.shape[0]
     Hk, d = c.Hk, c.d
-    assert cache.k.get_device() == dev, "the cache lies elsewhere"
-    out_k = slots.new_empty((T, Hk, d), dtype=torch.bfloat16) if out_k is None else out_k
-    out_v = slots.new_empty((T, Hk, d), dtype=torch.bfloat16) if out_v is None else out_v
-    keep = _I64x6(*_packed(out_k, dev, T, Hk, d), *_packed(out_v, dev, T, Hk, d))
+    assert cache.device == dev, "the cache lies elsewhere"
+    (out_k, to_k), (out_v, to_v) = _out(out_k, slots, dev, T, Hk, d), _out(out_v, slots, dev, T, Hk, d)
+    keep = _I64x6(*to_k, *to_v)
     at = _address(keep)
     _check(lib.bbm_kv4_read(_ints(slots, dev), T, _address(c), at, at + 24, _here(dev)))
     return out_k, out_v
@@ -336,8 +351,8 @@ def bbm_kv4_attn(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor, le
 
 def _kv4_attn(dev, q, cache, block_table, lens, cu, mask, max_len, softmax_scale, out, lse, workspace):
     T, H, d = q.shape
-    R, c = lens.shape[0], cache.c_struct()
-    assert d == c.d and cache.k.get_device() == dev, "the cache has another head size, or lies elsewhere"
+    R, c = lens.shape[0], cache.c_struct
+    assert d == c.d and cache.device == dev, "the cache has another head size, or lies elsewhere"
     table, stride, width = _table(block_table, dev, R)
     bits, words = None, 0
     if mask is not None:
@@ -345,13 +360,13 @@ def _kv4_attn(dev, q, cache, block_table, lens, cu, mask, max_len, softmax_scale
         bits, words = mask.data_ptr(), mask.shape[1]
     max_len = width * c.page if max_len is None else max_len
     packed = _packed(q, dev, T, H, d)
-    out = q.new_empty((T, H, d)) if out is None else out
-    lse = q.new_empty((H, T), dtype=torch.float32) if lse is None else lse
+    out, to = _out(out, q, dev, T, H, d)
+    lse, lse_at = _lse_out(lse, q, dev, H, T)
     if workspace is None:
         need = lib.bbm_kv4_attn_workspace_bytes(T, R, H, c.Hk, d, max_len)
         workspace = q.new_empty(need, dtype=torch.uint8) if need else None
-    keep = _I64x6(*packed, *_packed(out, dev, T, H, d))
+    keep = _I64x6(*packed, *to)
     at = _address(keep)
-    _check(lib.bbm_kv4_attn(at, at + 24, _lse(lse, dev, H, T), T, R, _ints(cu, dev, R + 1), _ints(lens, dev, R), table, stride, width, bits, words, _address(c), H,
+    _check(lib.bbm_kv4_attn(at, at + 24, lse_at, T, R, _ints(cu, dev, R + 1), _ints(lens, dev, R), table, stride, width, bits, words, _address(c), H,
                             d ** -0.5 if softmax_scale is None else softmax_scale, max_len, *_workspace(workspace, dev), _here(dev)))
     return out, lse
