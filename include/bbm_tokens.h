@@ -70,8 +70,8 @@ int bbm_prompt_attn_fwd(const bbm_packed* q, const bbm_packed* k, const bbm_pack
                         int64_t R, const int32_t* cu, int64_t H, int64_t Hk, int d, float softmax_scale, void* stream);
 
 /* Its gradients: dQ, dK, dV (packed; dK and dV summed over the query heads of a group) from dO, O and lse of the forward.
- * Deterministic.  The workspace needs bbm_prompt_attn_bwd_workspace_bytes(T, H) bytes, 16-byte aligned, contents of no matter. */
-size_t bbm_prompt_attn_bwd_workspace_bytes(int64_t T, int64_t H);
+ * Deterministic.  The workspace needs bbm_prompt_attn_bwd_workspace_bytes(T, R, H, Hk, d) bytes, 16-byte aligned, contents of no matter. */
+size_t bbm_prompt_attn_bwd_workspace_bytes(int64_t T, int64_t R, int64_t H, int64_t Hk, int d);
 int bbm_prompt_attn_bwd(const bbm_packed* q, const bbm_packed* k, const bbm_packed* v, const bbm_packed* o, const bbm_packed* d_o,
                         const float* lse, const bbm_packed* dq, const bbm_packed* dk, const bbm_packed* dv, int64_t T, int64_t R,
                         const int32_t* cu, int64_t H, int64_t Hk, int d, float softmax_scale, void* workspace, size_t workspace_bytes,

@@ -31,19 +31,25 @@ __device__ __forceinline__ float partner_max(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-template <int D, int NW>
-__global__ __launch_bounds__(NW * 64, NW == 2 ? 1 : D == 64 ? 3 : 2) void prompt_fwd_kernel(const PromptParams) {
+// SPLIT = 2: two groups of four waves share the rows and take the tiles in turn; the second one's results are merged into the first one's behind
+// the last tile.
+template <int D, int SPLIT>
+__global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 && D == 64 ? 3 : 2) void prompt_fwd_kernel(const PromptParams) {
   Args P = bbm::kernel_args<PromptParams>();
   using L = TL<D>;
-  constexpr int BR = NW * 32, KS = D / 16, DB = D / 32;
+  constexpr int NW = 4, BR = 32 * NW, KS = D / 16, DB = D / 32;
   static_assert(2 * 32 * D <= L::ELEMS, "two 32 x D slabs must fit in a tile buffer");
-  __shared__ __attribute__((aligned(16))) __bf16 k_s0[L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 k_s1[L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 v_s0[L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 v_s1[L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 k_s0_all[SPLIT * L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 k_s1_all[SPLIT * L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 v_s0_all[SPLIT * L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 v_s1_all[SPLIT * L::ELEMS];
 
   const int lane = threadIdx.x & 63, lq = lane & 31, hh = lane >> 5;
-  const int wave = (int)scalar(threadIdx.x >> 6);
+  const int group = SPLIT == 1 ? 0 : (int)scalar(threadIdx.x >> 8), wave = (int)scalar(threadIdx.x >> 6 & 3);  // of the group
+  __bf16* const k_s0 = k_s0_all + group * L::ELEMS;
+  __bf16* const k_s1 = k_s1_all + group * L::ELEMS;
+  __bf16* const v_s0 = v_s0_all + group * L::ELEMS;
+  __bf16* const v_s1 = v_s1_all + group * L::ELEMS;
   const bbm::Work work = bbm::work_of(blockIdx.x, P->H);
   const int h = work.plane;
   if (work.number >= P->pieces) return;
@@ -51,7 +57,7 @@ __global__ __launch_bounds__(NW * 64, NW == 2 ? 1 : D == 64 ? 3 : 2) void prompt
   const int n = s.end - s.begin, row0 = s.piece * BR;
   if (n <= 0) return;
   const int wrow = row0 + 32 * wave, wrows = max(0, min(32, n - wrow));  // this wave's rows
-  const int n_tiles = (min(n, row0 + BR) + 63) / 64, n_full = row0 / 64 & ~1;
+  const int n_tiles = (min(n, row0 + BR) + 63) / 64, n_full = row0 / 64;  // (an even number)
   const float rc = P->rc;
 
   const int k_row = P->k.row, v_row = P->v.row;
@@ -73,7 +79,7 @@ __global__ __launch_bounds__(NW * 64, NW == 2 ? 1 : D == 64 ? 3 : 2) void prompt
   __bf16* const q_stage = (wave / 2 == 0 ? k_s1 : v_s1) + wave % 2 * 32 * D;
   bbm::copy_slab<D>(global(P->q.p) + h * P->q.head + (int64_t)(s.begin + wrow) * P->q.row, wrows, P->q.row, q_stage, lane);
 #pragma unroll
-  for (int i = 0; i < 2 * LPW; ++i) copy_piece(0, rows_at(0), k_s0, v_s0, i);
+  for (int i = 0; i < 2 * LPW; ++i) copy_piece(group, rows_at(group), k_s0, v_s0, i);
   TileAddr<D> A;
   A.init(lane);
   bf16x8 qf[KS];
@@ -96,11 +102,11 @@ __global__ __launch_bounds__(NW * 64, NW == 2 ? 1 : D == 64 ? 3 : 2) void prompt
     __bf16* const k_oth = PB ? k_s0 : k_s1;
     __bf16* const v_oth = PB ? v_s0 : v_s1;
     // the next tile's copies go out between the matrix instructions of the first product; behind the last tile they copy zero rows
-    const int rows1 = rows_at(jt + 1);
+    const int rows1 = rows_at(jt + SPLIT);
     const bool live = wrows > 0 && (!PART || jt * 64 < wrow + wrows);
     if (!live) {
 #pragma unroll
-      for (int i = 0; i < 2 * LPW; ++i) copy_piece(jt + 1, rows1, k_oth, v_oth, i);
+      for (int i = 0; i < 2 * LPW; ++i) copy_piece(jt + SPLIT, rows1, k_oth, v_oth, i);
       return;
     }
     f32x16 sc[2];
@@ -117,7 +123,7 @@ __global__ __launch_bounds__(NW * 64, NW == 2 ? 1 : D == 64 ? 3 : 2) void prompt
                            constexpr int x = decltype(i)::value, GAP = 2 * KS / (2 * LPW) ? 2 * KS / (2 * LPW) : 1, PER = 2 * LPW > 2 * KS ? LPW / KS : 1;
                            if constexpr (x % GAP == 0) {
 #pragma unroll
-                             for (int y = 0; y < PER; ++y) copy_piece(jt + 1, rows1, k_oth, v_oth, x / GAP * PER + y);
+                             for (int y = 0; y < PER; ++y) copy_piece(jt + SPLIT, rows1, k_oth, v_oth, x / GAP * PER + y);
                            }
                          });
     __builtin_amdgcn_s_setprio(0);
@@ -170,15 +176,50 @@ __global__ __launch_bounds__(NW * 64, NW == 2 ? 1 : D == 64 ? 3 : 2) void prompt
   };
 
   // tiles seen whole, two at a time (the buffers change places with every tile), then one or two that are not, or of which one is
+  if constexpr (SPLIT == 1) {
 #pragma unroll 1
-  for (int jt = 0; jt < n_full; jt += 2) {
-    step(IntC<0>{}, IntC<0>{}, jt);
-    step(IntC<1>{}, IntC<0>{}, jt + 1);
+    for (int jt = 0; jt < n_full; jt += 2) {
+      step(IntC<0>{}, IntC<0>{}, jt);
+      step(IntC<1>{}, IntC<0>{}, jt + 1);
+    }
+    step(IntC<0>{}, IntC<1>{}, n_full);
+    if (n_full + 1 < n_tiles) step(IntC<1>{}, IntC<1>{}, n_full + 1);
+  } else {
+    int jt = group;
+#pragma unroll 1
+    for (; jt + 2 < n_full; jt += 4) {
+      step(IntC<0>{}, IntC<0>{}, jt);
+      step(IntC<1>{}, IntC<0>{}, jt + 2);
+    }
+    step(IntC<0>{}, IntC<1>{}, jt);  // (with an odd number of whole tiles the last one of them, and then the one that is not)
+    if (jt < n_full) step(IntC<1>{}, IntC<1>{}, jt + 2);
   }
-  step(IntC<0>{}, IntC<1>{}, n_full);
-  if (n_full + 1 < n_tiles) step(IntC<1>{}, IntC<1>{}, n_full + 1);
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();  // the output is staged in the tile buffers
+  if constexpr (SPLIT == 2) {
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    static_assert((2 * 32 * D + 4 * 64) * sizeof(float) <= 2 * L::ELEMS * sizeof(__bf16), "two waves' sums and statistics must fit in the tile buffers of a kind");
+    f32x4* const both = reinterpret_cast<f32x4*>(wave / 2 == 0 ? k_s1_all : v_s1_all);
+    f32x4* const sums = both + wave % 2 * (32 * D / 4) + lane;
+    float2* const stats = reinterpret_cast<float2*>(both + 2 * (32 * D / 4)) + wave % 2 * 64 + lane;
+    if (group == 1) {
+#pragma unroll
+      for (int i = 0; i < 4 * DB; ++i) sums[i * 64] = f32x4{oacc[i / 4][i % 4 * 4], oacc[i / 4][i % 4 * 4 + 1], oacc[i / 4][i % 4 * 4 + 2], oacc[i / 4][i % 4 * 4 + 3]};
+      *stats = make_float2(m_run, l_run);
+    }
+    __syncthreads();
+    if (group == 1) return;
+    const float2 other = *stats;
+    const float m_new = fmaxf(m_run, other.x), m_fin = m_new == -INFINITY ? 0.0f : m_new;
+    const float w0 = __builtin_amdgcn_exp2f(m_run - m_fin), w1 = __builtin_amdgcn_exp2f(other.x - m_fin);
+    l_run = w0 * l_run + w1 * other.y;
+    m_run = m_new;
+#pragma unroll
+    for (int i = 0; i < 4 * DB; ++i) {
+      const f32x4 y = sums[i * 64];
+      for (int e = 0; e < 4; ++e) oacc[i / 4][i % 4 * 4 + e] = w0 * oacc[i / 4][i % 4 * 4 + e] + w1 * y[e];
+    }
+  }
   if (wrows == 0) return;
   const float l_tot = partner_sum(l_run);
   __bf16* const stage = (wave / 2 == 0 ? k_s0 : v_s0) + wave % 2 * 32 * D;
@@ -210,7 +251,12 @@ extern "C" __attribute__((visibility("default"))) int bbm_prompt_attn_fwd(const 
   if (wgs >= 1ll << 31) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld)", fn, (long long)T, (long long)H);
   P.pieces = (int32_t)pieces;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (d == 64) prompt_fwd_kernel<64, 4><<<(unsigned)wgs, 256, 0, s>>>(P);
-  else prompt_fwd_kernel<128, 4><<<(unsigned)wgs, 256, 0, s>>>(P);
+  if (split_tiles(T, R, H)) {
+    if (d == 64) prompt_fwd_kernel<64, 2><<<(unsigned)wgs, 512, 0, s>>>(P);
+    else prompt_fwd_kernel<128, 2><<<(unsigned)wgs, 512, 0, s>>>(P);
+  } else {
+    if (d == 64) prompt_fwd_kernel<64, 1><<<(unsigned)wgs, 256, 0, s>>>(P);
+    else prompt_fwd_kernel<128, 1><<<(unsigned)wgs, 256, 0, s>>>(P);
+  }
   return launch_status(fn);
 }

@@ -12,6 +12,8 @@
 #include "bbm_mfma.h"
 #include "bbm_prompt.h"
 
+#include <algorithm>
+
 namespace {
 
 using bbm::bf16x8, bbm::buffer_of, bbm::copy_async, bbm::f32x16, bbm::global, bbm::IntC, bbm::lane_now, bbm::mfma_ring, bbm::operand, bbm::pack, bbm::Rows,
@@ -24,26 +26,33 @@ struct PromptBwdParams {
   const float* lse;
   float* nls;     // workspace [H][T]: -lse / scale, what the scores start at
   float* ndelta;  // workspace [H][T]: -<dO, O>
+  float* partials;  // workspace [part][dV, dK][Hk][T][d], of more than one part
   const int32_t* cu;
-  int32_t T, R, G, H, row_pieces, key_pieces;
+  int32_t T, R, G, H, row_pieces, key_pieces, parts;
   float rc;  // softmax_scale * log2(e)
   float scale;
 };
 typedef bbm::InPlace<PromptBwdParams> Args;
 
-template <int D>
-__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dq_kernel(const PromptBwdParams) {
+// SPLIT = 2: two groups of four waves share the rows and take the tiles in turn, as in the forward.
+template <int D, int SPLIT>
+__global__ __launch_bounds__(256 * SPLIT, D == 128 || SPLIT == 2 ? 2 : 3) void prompt_dq_kernel(const PromptBwdParams) {
   Args P = bbm::kernel_args<PromptBwdParams>();
   using L = TL<D>;
   constexpr int NW = 4, BR = 32 * NW, KS = D / 16, DB = D / 32, RC = D / 8, RPB = 64 / RC;
-  __shared__ __attribute__((aligned(16))) __bf16 k_s0[L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 k_s1[L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 v_s0[L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 v_s1[L::ELEMS];
-  __shared__ float delta_s[NW][32];
+  __shared__ __attribute__((aligned(16))) __bf16 k_s0_all[SPLIT * L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 k_s1_all[SPLIT * L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 v_s0_all[SPLIT * L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 v_s1_all[SPLIT * L::ELEMS];
+  __shared__ float delta_all[SPLIT][NW][32];
 
   const int lane = threadIdx.x & 63, lq = lane & 31, hh = lane >> 5;
-  const int wave = (int)scalar(threadIdx.x >> 6);
+  const int group = SPLIT == 1 ? 0 : (int)scalar(threadIdx.x >> 8), wave = (int)scalar(threadIdx.x >> 6 & 3);  // of the group
+  __bf16* const k_s0 = k_s0_all + group * L::ELEMS;
+  __bf16* const k_s1 = k_s1_all + group * L::ELEMS;
+  __bf16* const v_s0 = v_s0_all + group * L::ELEMS;
+  __bf16* const v_s1 = v_s1_all + group * L::ELEMS;
+  float (*const delta_s)[32] = delta_all[group];
   const bbm::Work work = bbm::work_of(blockIdx.x, P->H);
   const int h = work.plane;
   if (work.number >= P->row_pieces) return;
@@ -91,7 +100,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dq_kernel(const 
       orow[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(o_r, (r * P->o.row + g_chunk * 8) * 2, 0, 0));
     }
 #pragma unroll
-    for (int i = 0; i < 2 * LPW; ++i) copy_piece(0, rows_at(0), k_s0, v_s0, i);
+    for (int i = 0; i < 2 * LPW; ++i) copy_piece(group, rows_at(group), k_s0, v_s0, i);
 #pragma unroll
     for (int i = 0; i < 32 / RPB; ++i) {
       float x = 0.0f;
@@ -111,7 +120,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dq_kernel(const 
     for (int t = 0; t < KS; ++t) dof[t] = bbm::slab_frag<D>(stage, t, lane);
     nl = -lse * kLog2e;
     nd = -delta_s[wave][lq];
-    if (hh == 0) {
+    if (hh == 0 && group == 0) {
       __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(nl / rc), buffer_of(P->nls + row_at, wrows * 4), lq * 4, 0, 0);
       __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(nd), buffer_of(P->ndelta + row_at, wrows * 4), lq * 4, 0, 0);
     }
@@ -132,11 +141,11 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dq_kernel(const 
     __bf16* const v_cur = PB ? v_s1 : v_s0;
     __bf16* const k_oth = PB ? k_s0 : k_s1;
     __bf16* const v_oth = PB ? v_s0 : v_s1;
-    const int rows1 = rows_at(jt + 1);
+    const int rows1 = rows_at(jt + SPLIT);
     const bool live = wrows > 0 && (!PART || jt * 64 < wrow + wrows);
     if (!live) {
 #pragma unroll
-      for (int i = 0; i < 2 * LPW; ++i) copy_piece(jt + 1, rows1, k_oth, v_oth, i);
+      for (int i = 0; i < 2 * LPW; ++i) copy_piece(jt + SPLIT, rows1, k_oth, v_oth, i);
       return;
     }
     constexpr int N1 = KS, N2 = 2 * KS, N3 = 3 * KS, N4 = 4 * KS, N5 = N4 + 2 * DB, N6 = N5 + 2 * DB;
@@ -192,7 +201,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dq_kernel(const 
         },
         [&](auto i) {
           constexpr int x = decltype(i)::value;
-          if constexpr (x < 2 * LPW) copy_piece(jt + 1, rows1, k_oth, v_oth, x);
+          if constexpr (x < 2 * LPW) copy_piece(jt + SPLIT, rows1, k_oth, v_oth, x);
           // a product is complete two matrix instructions after its last one was issued
           if constexpr (x >= N1 + 2 && x < N2) exps(0, x - N1 - 2);
           if constexpr (x >= N2 + 2 && x < N3) ds(0, x - N2 - 2);
@@ -200,15 +209,42 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dq_kernel(const 
           if constexpr (x >= N4 + 2 && x < N5) ds(1, x - N4 - 2);
         });
   };
+  if constexpr (SPLIT == 1) {
 #pragma unroll 1
-  for (int jt = 0; jt < n_full; jt += 2) {
-    step(IntC<0>{}, IntC<0>{}, jt);
-    step(IntC<1>{}, IntC<0>{}, jt + 1);
+    for (int jt = 0; jt < n_full; jt += 2) {
+      step(IntC<0>{}, IntC<0>{}, jt);
+      step(IntC<1>{}, IntC<0>{}, jt + 1);
+    }
+    step(IntC<0>{}, IntC<1>{}, n_full);
+    if (n_full + 1 < n_tiles) step(IntC<1>{}, IntC<1>{}, n_full + 1);
+  } else {
+    int jt = group;
+#pragma unroll 1
+    for (; jt + 2 < n_full; jt += 4) {
+      step(IntC<0>{}, IntC<0>{}, jt);
+      step(IntC<1>{}, IntC<0>{}, jt + 2);
+    }
+    step(IntC<0>{}, IntC<1>{}, jt);  // (with an odd number of whole tiles the last one of them, and then the one that is not)
+    if (jt < n_full) step(IntC<1>{}, IntC<1>{}, jt + 2);
   }
-  step(IntC<0>{}, IntC<1>{}, n_full);
-  if (n_full + 1 < n_tiles) step(IntC<1>{}, IntC<1>{}, n_full + 1);
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();  // the result is staged in the tile buffers
+  if constexpr (SPLIT == 2) {
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    static_assert(2 * 32 * D * sizeof(float) <= 2 * L::ELEMS * sizeof(__bf16), "two waves' sums must fit in the tile buffers of a kind");
+    f32x4* const sums = reinterpret_cast<f32x4*>((wave / 2 == 0 ? k_s1_all : v_s1_all)) + wave % 2 * (32 * D / 4) + lane;
+    if (group == 1) {
+#pragma unroll
+      for (int i = 0; i < 4 * DB; ++i) sums[i * 64] = f32x4{dq[i / 4][i % 4 * 4], dq[i / 4][i % 4 * 4 + 1], dq[i / 4][i % 4 * 4 + 2], dq[i / 4][i % 4 * 4 + 3]};
+    }
+    __syncthreads();
+    if (group == 1) return;
+#pragma unroll
+    for (int i = 0; i < 4 * DB; ++i) {
+      const f32x4 y = sums[i * 64];
+      for (int e = 0; e < 4; ++e) dq[i / 4][i % 4 * 4 + e] += y[e];
+    }
+  }
   if (wrows == 0) return;
   __bf16* const stage = (wave / 2 == 0 ? k_s0 : v_s0) + wave % 2 * 32 * D;
   bbm::store_strided<D>(dq, P->scale, stage, global(P->dq.p) + h * P->dq.head + (int64_t)(s.begin + wrow) * P->dq.row, wrows, P->dq.row, lane);
@@ -233,18 +269,20 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dkv_kernel(const
   const int kh = wave & 1;   // key half of the tile
   const int qh = wave >> 1;  // query half of a tile; behind the last one, 0: this wave writes dV, 1: dK
   const float rc = P->rc;
-  const bbm::Work work = bbm::work_of(blockIdx.x, P->H / P->G);
-  const int hk = work.plane;
+  const int parts = P->parts;
+  const bbm::Work work = bbm::work_of(blockIdx.x, P->H / P->G * parts);
+  const int hk = work.plane / parts, part = work.plane - hk * parts;
   if (work.number >= P->key_pieces) return;
   const bbm::Span s = bbm::find_piece(global(P->cu), P->R, P->T, 1, 64, work.number);  // (early keys first: most queries see them)
   const int n = s.end - s.begin, j = s.piece;
   if (n <= 0) return;
-  const int per_head = (n + 63) / 64 - j, n_steps = per_head * P->G;  // tiles of queries from the diagonal on
+  const int head0 = part * P->G / parts, heads = (part + 1) * P->G / parts - head0;  // this part's heads of the group
+  const int per_head = (n + 63) / 64 - j, n_steps = per_head * heads;               // tiles of queries from the diagonal on
 
   const int q_row = P->q.row, g_row = P->d_o.row, T = P->T;
-  const __bf16* const qg = global(P->q.p) + (int64_t)hk * P->G * P->q.head + (int64_t)s.begin * q_row;
-  const __bf16* const gg = global(P->d_o.p) + (int64_t)hk * P->G * P->d_o.head + (int64_t)s.begin * g_row;
-  const int64_t st0 = (int64_t)hk * P->G * T + s.begin;
+  const __bf16* const qg = global(P->q.p) + ((int64_t)hk * P->G + head0) * P->q.head + (int64_t)s.begin * q_row;
+  const __bf16* const gg = global(P->d_o.p) + ((int64_t)hk * P->G + head0) * P->d_o.head + (int64_t)s.begin * g_row;
+  const int64_t st0 = ((int64_t)hk * P->G + head0) * T + s.begin;
   const int64_t q_head = P->q.head, g_head = P->d_o.head;
   constexpr int LPW = bbm::TileCopy<D, NW>::PIECES;
   // the queries from row `row` on of head g of the group; queries past the end come as zeros everywhere, and add exact zeros
@@ -318,7 +356,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dkv_kernel(const
     const bool diagonal = i0 == 0;
     if (++i1 == per_head) i1 = 0, ++g1;
     i0 = i1;
-    const bool more = g1 < P->G;
+    const bool more = g1 < heads;
     const int gn = more ? g1 : 0, row1 = more ? (j + i1) * 64 : 0, rows1 = more ? bbm::rows_of_tile(row1, n) : 0;
     if (more) copy_stats(gn, row1, rows1, PB ? st_s0 : st_s1);
     copy_from();
@@ -438,19 +476,60 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dkv_kernel(const
     }
   __syncthreads();  // the results are staged in the same buffers
   const int row0 = j * 64 + kh * 32, rows = max(0, min(32, n - row0));
+  if (parts > 1) {  // fp32 rows for the kernel that adds the parts up
+    if ((lane & 31) < rows) {
+      float* const to = global(P->partials) + (((int64_t)(part * 2 + qh) * (P->H / P->G) + hk) * T + s.begin + row0 + (lane & 31)) * D + 4 * (lane >> 5);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        for (int g = 0; g < 4; ++g) *reinterpret_cast<float4*>(to + 32 * db + 8 * g) = make_float4(dk[db][4 * g], dk[db][4 * g + 1], dk[db][4 * g + 2], dk[db][4 * g + 3]);
+    }
+    return;
+  }
   if (qh == 0)
     bbm::store_strided<D>(dk, 1.0f, t_s0 + L::ELEMS + kh * 32 * D, global(P->dv.p) + hk * P->dv.head + (int64_t)(s.begin + row0) * P->dv.row, rows, P->dv.row, lane);
   else
     bbm::store_strided<D>(dk, P->scale, t_s0 + kh * 32 * D, global(P->dk.p) + hk * P->dk.head + (int64_t)(s.begin + row0) * P->dk.row, rows, P->dk.row, lane);
 }
 
+// Adds the parts of dK and dV up, in their order; eight elements of a row a thread.
+template <int D>
+__global__ __launch_bounds__(256) void prompt_sum_kernel(const PromptBwdParams P) {
+  const int Hk = P.H / P.G, T = P.T;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int chunk = (int)(at % (D / 8)), t = (int)(at / (D / 8) % T), rest = (int)(at / (D / 8) / T), hk = rest % Hk, which = rest / Hk;
+  if (which > 1 || t < P.cu[0] || t >= P.cu[P.R]) return;  // (rows of nobody are left as they are)
+  const float* from = P.partials + (((int64_t)which * Hk + hk) * T + t) * D + chunk * 8;
+  const int64_t stride = (int64_t)2 * Hk * T * D;
+  float x[8] = {};
+  for (int p = 0; p < P.parts; ++p, from += stride) {
+    const float4 a = *reinterpret_cast<const float4*>(from), b = *reinterpret_cast<const float4*>(from + 4);
+    x[0] += a.x, x[1] += a.y, x[2] += a.z, x[3] += a.w, x[4] += b.x, x[5] += b.y, x[6] += b.z, x[7] += b.w;
+  }
+  const Rows& to = which ? P.dk : P.dv;
+  bf16x8 y;
+  for (int e = 0; e < 8; ++e) y[e] = (__bf16)(which ? x[e] * P.scale : x[e]);
+  *reinterpret_cast<bf16x8*>(to.p + hk * to.head + (int64_t)t * to.row + chunk * 8) = y;
+}
+
+// Parts of a group's heads that the dkv kernel takes side by side: one key head's walk over all heads of its group is as long as they are many, and a
+// chip that is not full waits for it.  Worth the fp32 sums in memory where the walk is long.  Forward and backward, one / several parts, us: 1 x 1024
+// tokens, 8 / 2 heads of 128, 104 / 78; 1 x 4096, 8 / 2 of 64, 230 / 158; 1 x 2048, 32 / 8 of 128, 255 / 220; but 8 x 300, 16 / 4 of 64, 41 / 51.
+constexpr int64_t kDkvWgs = 512, kLongWalk = 2048;  // work-groups, two a CU; queries of all heads of a group
+inline int64_t head_parts(int64_t T, int64_t R, int64_t H, int64_t Hk) {
+  if (H / Hk * T < kLongWalk * R) return 1;
+  return std::min(H / Hk, std::max<int64_t>(1, kDkvWgs / (bbm::ceil_div(T, 64) * Hk)));
+}
+inline size_t partial_bytes(int64_t T, int64_t R, int64_t H, int64_t Hk, int d) {
+  const int64_t parts = head_parts(T, R, H, Hk);
+  return parts > 1 ? (size_t)(2 * parts * Hk * T * d) * sizeof(float) : 0;
+}
 inline size_t stats_bytes(int64_t T, int64_t H) { return ((size_t)(T * H) * sizeof(float) + 255) / 256 * 256; }
 
 }  // namespace
 
-extern "C" __attribute__((visibility("default"))) size_t bbm_prompt_attn_bwd_workspace_bytes(int64_t T, int64_t H) {
-  if (T < 1 || H < 1 || T > bbm::kMaxTokens || H > 65535) return 0;
-  return 2 * stats_bytes(T, H);
+extern "C" __attribute__((visibility("default"))) size_t bbm_prompt_attn_bwd_workspace_bytes(int64_t T, int64_t R, int64_t H, int64_t Hk, int d) {
+  if (T < 1 || R < 1 || R > bbm::kMaxTokens || H < 1 || Hk < 1 || H % Hk || T > bbm::kMaxTokens || H > 65535 || (d != 64 && d != 128)) return 0;
+  return 2 * stats_bytes(T, H) + partial_bytes(T, R, H, Hk, d);
 }
 
 extern "C" __attribute__((visibility("default"))) int bbm_prompt_attn_bwd(const bbm_packed* q, const bbm_packed* k, const bbm_packed* v, const bbm_packed* o,
@@ -472,7 +551,7 @@ extern "C" __attribute__((visibility("default"))) int bbm_prompt_attn_bwd(const 
     if (int rc = check_rows(fn, a.name, a.x, T, a.heads, d, a.output)) return rc;
   if ((T > 0 && !lse) || !aligned(lse, 4)) return fail(BBM_EINVAL, "%s: lse must be a non-NULL 4-byte aligned pointer", fn);
   if (!(softmax_scale > 0.0f) || !(softmax_scale < INFINITY)) return fail(BBM_EINVAL, "%s: softmax_scale must be finite and > 0", fn);
-  const size_t need = bbm_prompt_attn_bwd_workspace_bytes(T, H);
+  const size_t need = bbm_prompt_attn_bwd_workspace_bytes(T, R, H, Hk, d);
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(BBM_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, workspace ? workspace_bytes : (size_t)0);
   if (!aligned(workspace, 16)) return fail(BBM_EINVAL, "%s: workspace must be 16-byte aligned", fn);
@@ -482,12 +561,21 @@ extern "C" __attribute__((visibility("default"))) int bbm_prompt_attn_bwd(const 
   for (int i = 0; i < 8; ++i) *to[i] = rows_of(all[i].x, T, d);
   P.lse = lse, P.nls = static_cast<float*>(workspace), P.ndelta = reinterpret_cast<float*>(static_cast<char*>(workspace) + stats_bytes(T, H)), P.cu = cu;
   P.T = (int32_t)T, P.R = (int32_t)R, P.G = (int32_t)(H / Hk), P.H = (int32_t)H, P.rc = softmax_scale * kLog2e, P.scale = softmax_scale;
+  P.parts = (int32_t)head_parts(T, R, H, Hk);
+  P.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * stats_bytes(T, H));
   const int64_t row_pieces = count_pieces(T, R, 1, 128), key_pieces = count_pieces(T, R, 1, 64);
-  const int64_t rows = work_groups(H, row_pieces), keys = work_groups(Hk, key_pieces);
-  if (rows >= 1ll << 31 || keys >= 1ll << 31) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld)", fn, (long long)T, (long long)H);
+  const int64_t rows = work_groups(H, row_pieces), keys = work_groups(Hk * P.parts, key_pieces), sums = P.parts > 1 ? ceil_div(2 * Hk * T * (d / 8), 256) : 0;
+  if (rows >= 1ll << 31 || keys >= 1ll << 31 || sums >= 1ll << 31) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld)", fn, (long long)T, (long long)H);
   P.row_pieces = (int32_t)row_pieces, P.key_pieces = (int32_t)key_pieces;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (d == 64) prompt_dq_kernel<64><<<(unsigned)rows, 256, 0, s>>>(P), prompt_dkv_kernel<64><<<(unsigned)keys, 256, 0, s>>>(P);
-  else prompt_dq_kernel<128><<<(unsigned)rows, 256, 0, s>>>(P), prompt_dkv_kernel<128><<<(unsigned)keys, 256, 0, s>>>(P);
+  auto go = [&](auto size) {
+    constexpr int D = decltype(size)::value;
+    if (split_tiles(T, R, H)) prompt_dq_kernel<D, 2><<<(unsigned)rows, 512, 0, s>>>(P);
+    else prompt_dq_kernel<D, 1><<<(unsigned)rows, 256, 0, s>>>(P);
+    prompt_dkv_kernel<D><<<(unsigned)keys, 256, 0, s>>>(P);
+    if (P.parts > 1) prompt_sum_kernel<D><<<(unsigned)sums, 256, 0, s>>>(P);
+  };
+  if (d == 64) go(IntC<64>{});
+  else go(IntC<128>{});
   return launch_status(fn);
 }

@@ -36,7 +36,7 @@ def _declare(L):
         f = getattr(L, name)
         f.restype, f.argtypes = ci, args
     L.bbm_prompt_attn_bwd_workspace_bytes.restype = C.c_size_t
-    L.bbm_prompt_attn_bwd_workspace_bytes.argtypes = [i64, i64]
+    L.bbm_prompt_attn_bwd_workspace_bytes.argtypes = [i64, i64, i64, i64, ci]
     L.bbm_kv4_attn_workspace_bytes.restype = C.c_size_t
     L.bbm_kv4_attn_workspace_bytes.argtypes = [i64, i64, i64, i64, ci, i64]
 
@@ -236,8 +236,8 @@ def _prompt_fwd(dev, q, k, v, cu, softmax_scale, out, lse):
     return out, lse
 
 
-def bbm_prompt_attn_bwd_workspace_bytes(T: int, H: int) -> int:
-    return int(lib.bbm_prompt_attn_bwd_workspace_bytes(T, H))
+def bbm_prompt_attn_bwd_workspace_bytes(T: int, R: int, H: int, Hk: int, d: int) -> int:
+    return int(lib.bbm_prompt_attn_bwd_workspace_bytes(T, R, H, Hk, d))
 
 
 def bbm_prompt_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, d_o: torch.Tensor, lse: torch.Tensor, cu: torch.Tensor,
@@ -257,7 +257,7 @@ def _prompt_bwd(dev, q, k, v, o, d_o, lse, cu, softmax_scale, dq, dk, dv, worksp
     packed = _packed(q, dev, T, H, d) + _packed(k, dev, T, Hk, d) + _packed(v, dev, T, Hk, d) + _packed(o, dev, T, H, d) + _packed(d_o, dev, T, H, d)
     (dq, to_q), (dk, to_k), (dv, to_v) = _out(dq, q, dev, T, H, d), _out(dk, k, dev, T, Hk, d), _out(dv, v, dev, T, Hk, d)
     if workspace is None:
-        workspace = q.new_empty(lib.bbm_prompt_attn_bwd_workspace_bytes(T, H), dtype=torch.uint8)
+        workspace = q.new_empty(lib.bbm_prompt_attn_bwd_workspace_bytes(T, cu.shape[0] - 1, H, Hk, d), dtype=torch.uint8)
     keep = _I64x24(*packed, *to_q, *to_k, *to_v)
     at = _address(keep)
     _check(lib.bbm_prompt_attn_bwd(at, at + 24, at + 48, at + 72, at + 96, _lse(lse, dev, H, T), at + 120, at + 144, at + 168, T, cu.shape[0] - 1, offsets, H, Hk, d,

@@ -184,6 +184,13 @@ def test_prompt(bbm, name, H, Hk, d, layout):
     assert torch.equal(o[a:b], o2[a:b]) and torch.equal(lse[:, a:b], lse2[:, a:b]) and all(torch.equal(u[a:b], w[a:b]) for u, w in zip(grads, g2))
 
 
+@pytest.mark.parametrize("name, H, Hk, d", [("longer", 40, 8, 128), ("longer", 64, 8, 64), ("ragged", 64, 16, 64), ("ragged", 64, 64, 128)])
+def test_prompt_with_many_heads(bbm, name, H, Hk, d):
+    """Launches that fill the chip: a group of waves a piece, and (64 heads over 8 of 64) the heads of a group in three uneven parts."""
+    cu, T, x = prompt_case(name, H, Hk, d, "plain", seed=3)
+    check_prompt(bbm, cu, T, x, H, Hk, d)
+
+
 @pytest.mark.parametrize("scale, size", [(1.0, 1.0), (0.01, 1.0), (0.125, 6.0)])
 def test_prompt_with_other_scales(bbm, scale, size):
     cu, T, x = prompt_case("ragged", 2, 1, 64, "plain", seed=9, scale=size)

@@ -96,8 +96,8 @@ def test_prompt_attention_refuses(bbm):
     for bad in OVERLAP:
         assert fwd(bbm, o=pk(**bad)) == bbm.BBM_EINVAL and bwd(bbm, dk=pk(**bad)) == bbm.BBM_EINVAL
     assert bwd(bbm, lse=None) == bbm.BBM_EINVAL and bwd(bbm, ws=P + 8) == bbm.BBM_EINVAL
-    assert bbm.bbm_prompt_attn_bwd_workspace_bytes(0, 4) == 0 and bbm.bbm_prompt_attn_bwd_workspace_bytes(3, 0) == 0
-    need = bbm.bbm_prompt_attn_bwd_workspace_bytes(3, 4)
+    assert bbm.bbm_prompt_attn_bwd_workspace_bytes(0, 1, 4, 2, 64) == 0 and bbm.bbm_prompt_attn_bwd_workspace_bytes(3, 1, 4, 3, 64) == 0
+    need = bbm.bbm_prompt_attn_bwd_workspace_bytes(3, 2, 4, 2, 64)
     assert need > 0 and bwd(bbm, ws_bytes=need - 1) == bbm.BBM_EWORKSPACE and bwd(bbm, ws=None) == bbm.BBM_EWORKSPACE
 
 
