@@ -11,6 +11,10 @@
  * operator writes them (bbm_build_slots and bbm_kv4_read, which write all T rows, say what they write there).  Offsets outside
  * 0 .. T are cut to that range.
  *
+ * Unless a function says otherwise, outputs overlap neither inputs nor each other.  What rows of nobody hold does not matter (it may be
+ * an infinity or a NaN); the rows of requests are taken to be finite, as are the cache's groups: an infinity or a NaN among them may reach any
+ * row of its own request.
+ *
  * A packed tensor is bf16 [T][heads][d] with any row and head strides (in elements, multiples of 8; the d elements of a head
  * are contiguous and 16-byte aligned), so the q, k and v parts of one projection's output, or [heads][T][d], need no copy.
  */
@@ -64,7 +68,8 @@ int bbm_rope(const bbm_packed* q, const bbm_packed* q_out, int64_t H, const bbm_
  * Causal attention over packed prompts: query i of a sequence sees its keys 0 .. i; query head h reads key head h / (H / Hk), H a
  * multiple of Hk.  O bf16 packed, lse fp32 [H][T] (natural logarithm; may be NULL) are written for the rows of the sequences.
  * d 64 or 128.  Scores are formed from the bf16 inputs without a further rounding; probabilities are rounded to bf16 for the
- * second product, their sum is taken before that.
+ * second product, their sum is taken before that.  Rows must not lie upon each other (of more than one token, row strides of at least d), here and in
+ * the backward pass, inputs included; a head stride of 0, heads that share their values, is fine.
  */
 int bbm_prompt_attn_fwd(const bbm_packed* q, const bbm_packed* k, const bbm_packed* v, const bbm_packed* o, float* lse, int64_t T,
                         int64_t R, const int32_t* cu, int64_t H, int64_t Hk, int d, float softmax_scale, void* stream);

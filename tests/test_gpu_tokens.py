@@ -115,7 +115,8 @@ def test_rope(bbm, T, H, Hk, d, rot, interleaved, layout, inverse):
 
 
 LENS = {
-    "one": [1], "two": [2, 1], "empty": [0, 5, 0, 0, 70, 0], "tiles": [64, 65, 63, 128, 127, 129], "ragged": [1, 200, 3, 33, 257, 2, 1, 90],
+    "one": [1], "two": [2, 1], "empty": [0, 5, 0, 0, 70, 0], "tiles": [64, 65, 63, 128, 127, 129], "crowd": [int(x) for x in np.random.default_rng(4).integers(0, 4, 700)], "throng": [1] * 4200,
+    "ragged": [1, 200, 3, 33, 257, 2, 1, 90],
     "many": [int(x) for x in np.random.default_rng(3).integers(0, 12, 150)], "long": [700, 1], "longer": [1300],
 }
 
@@ -189,6 +190,20 @@ def test_prompt_with_many_heads(bbm, name, H, Hk, d):
     """Launches that fill the chip: a group of waves a piece, and (64 heads over 8 of 64) the heads of a group in three uneven parts."""
     cu, T, x = prompt_case(name, H, Hk, d, "plain", seed=3)
     check_prompt(bbm, cu, T, x, H, Hk, d)
+
+
+@pytest.mark.parametrize("name, d", [("crowd", 64), ("throng", 128)])
+def test_prompt_with_many_sequences(bbm, name, d):
+    """More requests than are counted through: their pieces are searched for."""
+    cu, T, x = prompt_case(name, 2, 1, d, "plain", seed=6)
+    check_prompt(bbm, cu, T, x, 2, 1, d)
+
+
+def test_prompt_with_heads_that_share_values(bbm):
+    """Keys and values expanded over the heads (stride 0) give the gradients of each head."""
+    cu, T, x = prompt_case("ragged", 4, 1, 64, "plain", seed=7)
+    x["k"], x["v"] = (x[n].expand(T, 4, 64) for n in ("k", "v"))
+    check_prompt(bbm, cu, T, x, 4, 4, 64)
 
 
 @pytest.mark.parametrize("scale, size", [(1.0, 1.0), (0.01, 1.0), (0.125, 6.0)])
@@ -341,7 +356,7 @@ def check_cached(bbm, c, table, lens, cu, T, q, words, H, Hk, d, page, **kw):
     ([130, 300, 31], [1, 0, 1], 6, 2, 64, "heads", None), ([40, 500, 7], [5, 33, 7], 6, 2, 16, "fused", None), ([40, 90], [40, 60], 32, 2, 128, "plain", None),
     ([20, 70, 5], [20, 6, 5], 4, 4, 16, "plain", 1), ([300, 129], [70, 129], 3, 1, 64, "heads", 2), ([300, 150], [100, 100], 5, 1, 32, "plain", 1),
     ([3, 2], [5, 4], 4, 2, 16, "plain", None), ([2900, 9, 1700], [1, 1, 2], 12, 4, 64, "plain", None), ([2500, 2100], [40, 30], 8, 2, 32, "fused", None), ([2500, 2100], [70, 20], 4, 2, 64, "plain", 1),
-    ([33] * 70, [1] * 70, 2, 1, 16, "plain", None)])
+    ([20] * 600, [1] * 600, 2, 1, 16, "plain", None), ([33] * 70, [1] * 70, 2, 1, 16, "plain", None)])
 def test_cached(bbm, lens, news, H, Hk, d, page, layout, tree):
     c, table, cu, T, q, words = cached_case(bbm, lens, news, H, Hk, d, page, layout, seed=len(lens), tree=tree, before=2, behind=3)
     first = check_cached(bbm, c, table, lens, cu, T, q, words, H, Hk, d, page)
@@ -357,6 +372,33 @@ def test_cached_pages_outside_and_a_narrow_table(bbm):
     check_cached(bbm, c, table, lens, cu, T, q, None, H, Hk, d, page)
     check_cached(bbm, c, table[:, :5], lens, cu, T, q, None, H, Hk, d, page)
     check_cached(bbm, c, table[:, :5], [700, -4, 1 << 30], cu, T, q, None, H, Hk, d, page)
+
+
+@pytest.mark.parametrize("max_len", [1, 300, 5000, 1 << 40])
+def test_cached_with_a_wrong_hint(bbm, max_len):
+    c, table, cu, T, q, _ = cached_case(bbm, [2300, 40], [1, 2], 4, 2, 64, 64, seed=5)
+    check_cached(bbm, c, table, [2300, 40], cu, T, q, None, 4, 2, 64, 64, max_len=max_len)
+
+
+def test_cached_many_heads_a_key_head(bbm):
+    c, table, cu, T, q, _ = cached_case(bbm, [200, 77], [1, 3], 71, 1, 64, 16, seed=6)
+    check_cached(bbm, c, table, [200, 77], cu, T, q, None, 71, 1, 64, 16)
+
+
+@pytest.mark.parametrize("d, tree, layout", [(64, None, "fused"), (128, None, "plain"), (128, 3, "heads")])
+def test_cached_wide_in_parts(bbm, d, tree, layout):
+    lens, news = [2500, 2100], [130, 130]
+    c, table, cu, T, q, words = cached_case(bbm, lens, news, 64, 8, d, 32, layout, seed=9, tree=tree, before=1, behind=2)
+    check_cached(bbm, c, table, lens, cu, T, q, words, 64, 8, d, 32, max_len=2500)
+
+
+def test_cached_wide_with_pages_outside(bbm):
+    """The kernel of many columns (more than 16384 rows of all heads), its last tile of a few keys, a page outside and a mask."""
+    lens, news = [300, 150], [140, 130]
+    for tree in (None, 3):
+        c, table, cu, T, q, words = cached_case(bbm, lens, news, 64, 64, 64, 16, seed=7, tree=tree)
+        table[0, 4], table[1, 0] = -1, c.k.shape[0] + 1
+        check_cached(bbm, c, table, lens, cu, T, q, words, 64, 64, 64, 16)
 
 
 def test_cached_pages_shared_by_requests(bbm):
