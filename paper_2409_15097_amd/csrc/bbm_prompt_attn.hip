@@ -31,33 +31,31 @@ __device__ __forceinline__ float partner_max(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// SPLIT = 2: two groups of four waves share the rows and take the tiles in turn; the second one's results are merged into the first one's behind
-// the last tile.
-template <int D, int SPLIT>
-__global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 && D == 64 ? 3 : 2) void prompt_fwd_kernel(const PromptParams) {
+// HALVES = 2 (short launches): a work-group takes 64 rows, and two waves share 32 of them, each with 32 keys of every tile; their results meet behind the
+// last one.
+template <int D, int HALVES>
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void prompt_fwd_kernel(const PromptParams) {
   Args P = bbm::kernel_args<PromptParams>();
   using L = TL<D>;
-  constexpr int NW = 4, BR = 32 * NW, KS = D / 16, DB = D / 32;
+  constexpr int NW = 4, BR = 32 * NW / HALVES, KS = D / 16, DB = D / 32;
+  constexpr int KB = 2 / HALVES;  // halves of a tile's keys that a wave takes
   static_assert(2 * 32 * D <= L::ELEMS, "two 32 x D slabs must fit in a tile buffer");
-  __shared__ __attribute__((aligned(16))) __bf16 k_s0_all[SPLIT * L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 k_s1_all[SPLIT * L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 v_s0_all[SPLIT * L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 v_s1_all[SPLIT * L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 k_s0[L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 k_s1[L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 v_s0[L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 v_s1[L::ELEMS];
 
   const int lane = threadIdx.x & 63, lq = lane & 31, hh = lane >> 5;
-  const int group = SPLIT == 1 ? 0 : (int)scalar(threadIdx.x >> 8), wave = (int)scalar(threadIdx.x >> 6 & 3);  // of the group
-  __bf16* const k_s0 = k_s0_all + group * L::ELEMS;
-  __bf16* const k_s1 = k_s1_all + group * L::ELEMS;
-  __bf16* const v_s0 = v_s0_all + group * L::ELEMS;
-  __bf16* const v_s1 = v_s1_all + group * L::ELEMS;
+  const int wave = (int)scalar(threadIdx.x >> 6);
+  const int half = HALVES == 2 ? wave & 1 : 0;  // of the keys
   const bbm::Work work = bbm::work_of(blockIdx.x, P->H);
   const int h = work.plane;
   if (work.number >= P->pieces) return;
   const bbm::Span s = bbm::find_piece(global(P->cu), P->R, P->T, 1, BR, P->pieces - 1 - work.number);  // (long rows first)
   const int n = s.end - s.begin, row0 = s.piece * BR;
   if (n <= 0) return;
-  const int wrow = row0 + 32 * wave, wrows = max(0, min(32, n - wrow));  // this wave's rows
-  const int n_tiles = (min(n, row0 + BR) + 63) / 64, n_full = row0 / 64;  // (an even number)
+  const int wrow = row0 + 32 * (wave / HALVES), wrows = max(0, min(32, n - wrow));  // this wave's rows
+  const int n_tiles = (min(n, row0 + BR) + 63) / 64, n_full = row0 / 64 & ~1;
   const float rc = P->rc;
 
   const int k_row = P->k.row, v_row = P->v.row;
@@ -79,9 +77,13 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 && D == 64 ? 3 : 2) void pr
   __bf16* const q_stage = (wave / 2 == 0 ? k_s1 : v_s1) + wave % 2 * 32 * D;
   bbm::copy_slab<D>(global(P->q.p) + h * P->q.head + (int64_t)(s.begin + wrow) * P->q.row, wrows, P->q.row, q_stage, lane);
 #pragma unroll
-  for (int i = 0; i < 2 * LPW; ++i) copy_piece(group, rows_at(group), k_s0, v_s0, i);
+  for (int i = 0; i < 2 * LPW; ++i) copy_piece(0, rows_at(0), k_s0, v_s0, i);
   TileAddr<D> A;
   A.init(lane);
+  for (int i = 0; i < 2; ++i) {  // this wave's keys of a tile
+    A.ra[i] += half * (32 / L::NBLK) * D;
+    A.ta[i] += 2 * half * (D == 64 ? 2 * D : D);
+  }
   bf16x8 qf[KS];
   f32x16 oacc[DB];
 #pragma unroll
@@ -102,35 +104,33 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 && D == 64 ? 3 : 2) void pr
     __bf16* const k_oth = PB ? k_s0 : k_s1;
     __bf16* const v_oth = PB ? v_s0 : v_s1;
     // the next tile's copies go out between the matrix instructions of the first product; behind the last tile they copy zero rows
-    const int rows1 = rows_at(jt + SPLIT);
-    const bool live = wrows > 0 && (!PART || jt * 64 < wrow + wrows);
+    const int rows1 = rows_at(jt + 1);
+    const bool live = wrows > 0 && (!PART || jt * 64 + 32 * half < wrow + wrows);
     if (!live) {
 #pragma unroll
-      for (int i = 0; i < 2 * LPW; ++i) copy_piece(jt + SPLIT, rows1, k_oth, v_oth, i);
+      for (int i = 0; i < 2 * LPW; ++i) copy_piece(jt + 1, rows1, k_oth, v_oth, i);
       return;
     }
-    f32x16 sc[2];
+    f32x16 sc[KB];
     __builtin_amdgcn_s_setprio(2);
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int kb = 0; kb < KB; ++kb)
       for (int e = 0; e < 16; ++e) sc[kb][e] = 0.0f;
-    mfma_ring<2 * KS, 4>([&](auto i) { return A.row_frag(k_cur, decltype(i)::value & 1, decltype(i)::value >> 1); },
-                         [&](auto i, bf16x8 f) {
-                           constexpr int x = decltype(i)::value;
-                           sc[x & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[x >> 1], sc[x & 1], 0, 0, 0);
-                         },
-                         [&](auto i) {
-                           constexpr int x = decltype(i)::value, GAP = 2 * KS / (2 * LPW) ? 2 * KS / (2 * LPW) : 1, PER = 2 * LPW > 2 * KS ? LPW / KS : 1;
-                           if constexpr (x % GAP == 0) {
-#pragma unroll
-                             for (int y = 0; y < PER; ++y) copy_piece(jt + SPLIT, rows1, k_oth, v_oth, x / GAP * PER + y);
-                           }
-                         });
+    mfma_ring<KB * KS, 4>([&](auto i) { return A.row_frag(k_cur, decltype(i)::value % KB, decltype(i)::value / KB); },
+                          [&](auto i, bf16x8 f) {
+                            constexpr int x = decltype(i)::value;
+                            sc[x % KB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[x / KB], sc[x % KB], 0, 0, 0);
+                          },
+                          [&](auto i) {
+                            constexpr int x = decltype(i)::value, GAP = KB * KS / (2 * LPW);  // matrix instructions per copy
+                            static_assert(GAP * 2 * LPW == KB * KS, "the copies must find room");
+                            if constexpr (x % GAP == 0) copy_piece(jt + 1, rows1, k_oth, v_oth, x / GAP);
+                          });
     __builtin_amdgcn_s_setprio(0);
     if constexpr (PART) {
-      const uint64_t seen = bbm::bits_up_to(wrow + lq - jt * 64);
+      const uint64_t seen = bbm::bits_up_to(wrow + lq - jt * 64 - 32 * half);
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
+      for (int kb = 0; kb < KB; ++kb) {
         const uint32_t w = (uint32_t)(seen >> (32 * kb)) >> (4 * hh);
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[kb][e] = bbm::keep_if(w, e, sc[kb][e]);
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 && D == 64 ? 3 : 2) void pr
     }
     float mx = sc[0][0];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int kb = 0; kb < KB; ++kb)
       for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[kb][e]);
     mx = partner_max(mx) * rc;
     if (__any(mx > m_run + kLazy ? 1 : 0)) {
@@ -163,52 +163,40 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 && D == 64 ? 3 : 2) void pr
       }
     };
     exps(0, 0, 8);
-    mfma_ring<4 * DB, 3>([&](auto i) { return A.tr_frag(v_cur, decltype(i)::value / DB, decltype(i)::value % DB); },
+    mfma_ring<2 * KB * DB, 3>([&](auto i) { return A.tr_frag(v_cur, decltype(i)::value / DB, decltype(i)::value % DB); },
                          [&](auto i, bf16x8 f) {
                            constexpr int x = decltype(i)::value;
                            oacc[x % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pf[x / DB & 1], oacc[x % DB], 0, 0, 0);
                          },
                          [&](auto i) {
                            constexpr int x = decltype(i)::value, PER = 8 / DB;
-                           if constexpr (x / DB < 3) exps(x / DB + 1, x % DB * PER, (x % DB + 1) * PER);
+                           if constexpr (x / DB < 2 * KB - 1) exps(x / DB + 1, x % DB * PER, (x % DB + 1) * PER);
                          });
     __builtin_amdgcn_s_setprio(0);
   };
 
   // tiles seen whole, two at a time (the buffers change places with every tile), then one or two that are not, or of which one is
-  if constexpr (SPLIT == 1) {
 #pragma unroll 1
-    for (int jt = 0; jt < n_full; jt += 2) {
-      step(IntC<0>{}, IntC<0>{}, jt);
-      step(IntC<1>{}, IntC<0>{}, jt + 1);
-    }
-    step(IntC<0>{}, IntC<1>{}, n_full);
-    if (n_full + 1 < n_tiles) step(IntC<1>{}, IntC<1>{}, n_full + 1);
-  } else {
-    int jt = group;
-#pragma unroll 1
-    for (; jt + 2 < n_full; jt += 4) {
-      step(IntC<0>{}, IntC<0>{}, jt);
-      step(IntC<1>{}, IntC<0>{}, jt + 2);
-    }
-    step(IntC<0>{}, IntC<1>{}, jt);  // (with an odd number of whole tiles the last one of them, and then the one that is not)
-    if (jt < n_full) step(IntC<1>{}, IntC<1>{}, jt + 2);
+  for (int jt = 0; jt < n_full; jt += 2) {
+    step(IntC<0>{}, IntC<0>{}, jt);
+    step(IntC<1>{}, IntC<0>{}, jt + 1);
   }
+  step(IntC<0>{}, IntC<1>{}, n_full);
+  if (n_full + 1 < n_tiles) step(IntC<1>{}, IntC<1>{}, n_full + 1);
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();  // the output is staged in the tile buffers
-  if constexpr (SPLIT == 2) {
+  if constexpr (HALVES == 2) {
     typedef float f32x4 __attribute__((ext_vector_type(4)));
-    static_assert((2 * 32 * D + 4 * 64) * sizeof(float) <= 2 * L::ELEMS * sizeof(__bf16), "two waves' sums and statistics must fit in the tile buffers of a kind");
-    f32x4* const both = reinterpret_cast<f32x4*>(wave / 2 == 0 ? k_s1_all : v_s1_all);
-    f32x4* const sums = both + wave % 2 * (32 * D / 4) + lane;
-    float2* const stats = reinterpret_cast<float2*>(both + 2 * (32 * D / 4)) + wave % 2 * 64 + lane;
-    if (group == 1) {
+    static_assert((32 * D + 2 * 64) * sizeof(float) <= L::ELEMS * sizeof(__bf16), "a wave's sums and statistics must fit in a tile buffer");
+    f32x4* const sums = reinterpret_cast<f32x4*>(wave / 2 == 0 ? k_s1 : v_s1) + lane;
+    float2* const stats = reinterpret_cast<float2*>((wave / 2 == 0 ? k_s1 : v_s1) + 32 * D * 2) + lane;
+    if (half == 1) {
 #pragma unroll
       for (int i = 0; i < 4 * DB; ++i) sums[i * 64] = f32x4{oacc[i / 4][i % 4 * 4], oacc[i / 4][i % 4 * 4 + 1], oacc[i / 4][i % 4 * 4 + 2], oacc[i / 4][i % 4 * 4 + 3]};
       *stats = make_float2(m_run, l_run);
     }
     __syncthreads();
-    if (group == 1) return;
+    if (half == 1) return;
     const float2 other = *stats;
     const float m_new = fmaxf(m_run, other.x), m_fin = m_new == -INFINITY ? 0.0f : m_new;
     const float w0 = __builtin_amdgcn_exp2f(m_run - m_fin), w1 = __builtin_amdgcn_exp2f(other.x - m_fin);
@@ -247,13 +235,14 @@ extern "C" __attribute__((visibility("default"))) int bbm_prompt_attn_fwd(const 
   PromptParams P;
   P.q = rows_of(q, T, d), P.k = rows_of(k, T, d), P.v = rows_of(v, T, d), P.o = rows_of(o, T, d);
   P.lse = lse, P.cu = cu, P.T = (int32_t)T, P.R = (int32_t)R, P.G = (int32_t)(H / Hk), P.H = (int32_t)H, P.rc = softmax_scale * kLog2e;
-  const int64_t pieces = count_pieces(T, R, 1, 128), wgs = work_groups(H, pieces);
+  const bool halves = split_keys(T, R, H);
+  const int64_t pieces = count_pieces(T, R, 1, halves ? 64 : 128), wgs = work_groups(H, pieces);
   if (wgs >= 1ll << 31) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld)", fn, (long long)T, (long long)H);
   P.pieces = (int32_t)pieces;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (split_tiles(T, R, H)) {
-    if (d == 64) prompt_fwd_kernel<64, 2><<<(unsigned)wgs, 512, 0, s>>>(P);
-    else prompt_fwd_kernel<128, 2><<<(unsigned)wgs, 512, 0, s>>>(P);
+  if (halves) {
+    if (d == 64) prompt_fwd_kernel<64, 2><<<(unsigned)wgs, 256, 0, s>>>(P);
+    else prompt_fwd_kernel<128, 2><<<(unsigned)wgs, 256, 0, s>>>(P);
   } else {
     if (d == 64) prompt_fwd_kernel<64, 1><<<(unsigned)wgs, 256, 0, s>>>(P);
     else prompt_fwd_kernel<128, 1><<<(unsigned)wgs, 256, 0, s>>>(P);

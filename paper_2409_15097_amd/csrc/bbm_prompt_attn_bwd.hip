@@ -34,33 +34,29 @@ struct PromptBwdParams {
 };
 typedef bbm::InPlace<PromptBwdParams> Args;
 
-// SPLIT = 2: two groups of four waves share the rows and take the tiles in turn, as in the forward.
-template <int D, int SPLIT>
-__global__ __launch_bounds__(256 * SPLIT, D == 128 || SPLIT == 2 ? 2 : 3) void prompt_dq_kernel(const PromptBwdParams) {
+// HALVES = 2: 64 rows a work-group, two waves share 32 of them and halve the keys of every tile, as in the forward.
+template <int D, int HALVES>
+__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dq_kernel(const PromptBwdParams) {
   Args P = bbm::kernel_args<PromptBwdParams>();
   using L = TL<D>;
-  constexpr int NW = 4, BR = 32 * NW, KS = D / 16, DB = D / 32, RC = D / 8, RPB = 64 / RC;
-  __shared__ __attribute__((aligned(16))) __bf16 k_s0_all[SPLIT * L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 k_s1_all[SPLIT * L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 v_s0_all[SPLIT * L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 v_s1_all[SPLIT * L::ELEMS];
-  __shared__ float delta_all[SPLIT][NW][32];
+  constexpr int NW = 4, BR = 32 * NW / HALVES, KB = 2 / HALVES, KS = D / 16, DB = D / 32, RC = D / 8, RPB = 64 / RC;
+  __shared__ __attribute__((aligned(16))) __bf16 k_s0[L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 k_s1[L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 v_s0[L::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 v_s1[L::ELEMS];
+  __shared__ float delta_s[NW][32];
 
   const int lane = threadIdx.x & 63, lq = lane & 31, hh = lane >> 5;
-  const int group = SPLIT == 1 ? 0 : (int)scalar(threadIdx.x >> 8), wave = (int)scalar(threadIdx.x >> 6 & 3);  // of the group
-  __bf16* const k_s0 = k_s0_all + group * L::ELEMS;
-  __bf16* const k_s1 = k_s1_all + group * L::ELEMS;
-  __bf16* const v_s0 = v_s0_all + group * L::ELEMS;
-  __bf16* const v_s1 = v_s1_all + group * L::ELEMS;
-  float (*const delta_s)[32] = delta_all[group];
+  const int wave = (int)scalar(threadIdx.x >> 6);
+  const int half = HALVES == 2 ? wave & 1 : 0;  // of the keys
   const bbm::Work work = bbm::work_of(blockIdx.x, P->H);
   const int h = work.plane;
   if (work.number >= P->row_pieces) return;
   const bbm::Span s = bbm::find_piece(global(P->cu), P->R, P->T, 1, BR, P->row_pieces - 1 - work.number);
   const int n = s.end - s.begin, row0 = s.piece * BR;
   if (n <= 0) return;
-  const int wrow = row0 + 32 * wave, wrows = max(0, min(32, n - wrow));
-  const int n_tiles = (min(n, row0 + BR) + 63) / 64, n_full = row0 / 64;
+  const int wrow = row0 + 32 * (wave / HALVES), wrows = max(0, min(32, n - wrow));
+  const int n_tiles = (min(n, row0 + BR) + 63) / 64, n_full = row0 / 64 & ~1;
   const float rc = P->rc;
 
   const int k_row = P->k.row, v_row = P->v.row;
@@ -100,7 +96,7 @@ __global__ __launch_bounds__(256 * SPLIT, D == 128 || SPLIT == 2 ? 2 : 3) void p
       orow[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(o_r, (r * P->o.row + g_chunk * 8) * 2, 0, 0));
     }
 #pragma unroll
-    for (int i = 0; i < 2 * LPW; ++i) copy_piece(group, rows_at(group), k_s0, v_s0, i);
+    for (int i = 0; i < 2 * LPW; ++i) copy_piece(0, rows_at(0), k_s0, v_s0, i);
 #pragma unroll
     for (int i = 0; i < 32 / RPB; ++i) {
       float x = 0.0f;
@@ -120,10 +116,14 @@ __global__ __launch_bounds__(256 * SPLIT, D == 128 || SPLIT == 2 ? 2 : 3) void p
     for (int t = 0; t < KS; ++t) dof[t] = bbm::slab_frag<D>(stage, t, lane);
     nl = -lse * kLog2e;
     nd = -delta_s[wave][lq];
-    if (hh == 0 && group == 0) {
+    if (hh == 0 && half == 0) {
       __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(nl / rc), buffer_of(P->nls + row_at, wrows * 4), lq * 4, 0, 0);
       __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(nd), buffer_of(P->ndelta + row_at, wrows * 4), lq * 4, 0, 0);
     }
+  }
+  for (int i = 0; i < 2; ++i) {  // this wave's keys of a tile
+    A.ra[i] += half * (32 / L::NBLK) * D;
+    A.ta[i] += 2 * half * (D == 64 ? 2 * D : D);
   }
   f32x16 dq[DB];
 #pragma unroll
@@ -141,21 +141,21 @@ __global__ __launch_bounds__(256 * SPLIT, D == 128 || SPLIT == 2 ? 2 : 3) void p
     __bf16* const v_cur = PB ? v_s1 : v_s0;
     __bf16* const k_oth = PB ? k_s0 : k_s1;
     __bf16* const v_oth = PB ? v_s0 : v_s1;
-    const int rows1 = rows_at(jt + SPLIT);
-    const bool live = wrows > 0 && (!PART || jt * 64 < wrow + wrows);
+    const int rows1 = rows_at(jt + 1);
+    const bool live = wrows > 0 && (!PART || jt * 64 + 32 * half < wrow + wrows);
     if (!live) {
 #pragma unroll
-      for (int i = 0; i < 2 * LPW; ++i) copy_piece(jt + SPLIT, rows1, k_oth, v_oth, i);
+      for (int i = 0; i < 2 * LPW; ++i) copy_piece(jt + 1, rows1, k_oth, v_oth, i);
       return;
     }
-    constexpr int N1 = KS, N2 = 2 * KS, N3 = 3 * KS, N4 = 4 * KS, N5 = N4 + 2 * DB, N6 = N5 + 2 * DB;
+    constexpr int N1 = KS, N2 = 2 * KS, N3 = 3 * KS, N4 = 2 * KB * KS, N5 = N4 + 2 * DB, N6 = N4 + 2 * KB * DB;
     constexpr int PER = D == 128 ? 4 : 8;  // elements behind a matrix instruction
     static_assert(PER * (KS - 2) >= 16 && PER * (2 * DB - 2) >= 16, "all 16 must find room");
-    f32x16 sc[2], dp[2];
-    uint32_t dsf[2][2][4];  // dS of [half][16-key step], pairs of bf16
+    f32x16 sc[KB], dp[KB];
+    uint32_t dsf[KB][2][4];  // dS of [half][16-key step], pairs of bf16
     uint32_t seen[2] = {0, 0};
     if constexpr (PART) {
-      const uint64_t bits = bbm::bits_up_to(wrow + lq - jt * 64) >> (4 * hh);
+      const uint64_t bits = bbm::bits_up_to(wrow + lq - jt * 64 - 32 * half) >> (4 * hh);
       seen[0] = (uint32_t)bits, seen[1] = (uint32_t)(bits >> 32);
     }
     auto start = [&](f32x16& acc, float x) {
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(256 * SPLIT, D == 128 || SPLIT == 2 ? 2 : 3) void p
             for (int e = 0; e < 16; ++e) sc[x / N2][e] = 0.0f;
           }
           if constexpr (x == N1) start(dp[0], nd);
-          if constexpr (x == N3) start(dp[1], nd);
+          if constexpr (KB == 2 && x == N3) start(dp[KB - 1], nd);
           if constexpr (x < N4 && x / KS % 2 == 0) {
             sc[x / N2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[x % KS], sc[x / N2], 0, 0, 0);
           } else if constexpr (x < N4) {
@@ -201,44 +201,41 @@ __global__ __launch_bounds__(256 * SPLIT, D == 128 || SPLIT == 2 ? 2 : 3) void p
         },
         [&](auto i) {
           constexpr int x = decltype(i)::value;
-          if constexpr (x < 2 * LPW) copy_piece(jt + SPLIT, rows1, k_oth, v_oth, x);
+          if constexpr (x < 2 * LPW) copy_piece(jt + 1, rows1, k_oth, v_oth, x);
           // a product is complete two matrix instructions after its last one was issued
-          if constexpr (x >= N1 + 2 && x < N2) exps(0, x - N1 - 2);
-          if constexpr (x >= N2 + 2 && x < N3) ds(0, x - N2 - 2);
-          if constexpr (x >= N3 + 2 && x < N4) exps(1, x - N3 - 2);
-          if constexpr (x >= N4 + 2 && x < N5) ds(1, x - N4 - 2);
+          if constexpr (KB == 2) {
+            if constexpr (x >= N1 + 2 && x < N2) exps(0, x - N1 - 2);
+            if constexpr (x >= N2 + 2 && x < N3) ds(0, x - N2 - 2);
+            if constexpr (x >= N3 + 2 && x < N4) exps(1, x - N3 - 2);
+            if constexpr (x >= N4 + 2 && x < N5) ds(1, x - N4 - 2);
+          } else {
+            if constexpr (x >= N1 + 2 && x < N2) exps(0, x - N1 - 2);
+            if constexpr (x == N2 - 1) {
+#pragma unroll
+              for (int i = 0; i < 16 / PER; ++i) ds(0, i);
+            }
+          }
         });
   };
-  if constexpr (SPLIT == 1) {
 #pragma unroll 1
-    for (int jt = 0; jt < n_full; jt += 2) {
-      step(IntC<0>{}, IntC<0>{}, jt);
-      step(IntC<1>{}, IntC<0>{}, jt + 1);
-    }
-    step(IntC<0>{}, IntC<1>{}, n_full);
-    if (n_full + 1 < n_tiles) step(IntC<1>{}, IntC<1>{}, n_full + 1);
-  } else {
-    int jt = group;
-#pragma unroll 1
-    for (; jt + 2 < n_full; jt += 4) {
-      step(IntC<0>{}, IntC<0>{}, jt);
-      step(IntC<1>{}, IntC<0>{}, jt + 2);
-    }
-    step(IntC<0>{}, IntC<1>{}, jt);  // (with an odd number of whole tiles the last one of them, and then the one that is not)
-    if (jt < n_full) step(IntC<1>{}, IntC<1>{}, jt + 2);
+  for (int jt = 0; jt < n_full; jt += 2) {
+    step(IntC<0>{}, IntC<0>{}, jt);
+    step(IntC<1>{}, IntC<0>{}, jt + 1);
   }
+  step(IntC<0>{}, IntC<1>{}, n_full);
+  if (n_full + 1 < n_tiles) step(IntC<1>{}, IntC<1>{}, n_full + 1);
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();  // the result is staged in the tile buffers
-  if constexpr (SPLIT == 2) {
+  if constexpr (HALVES == 2) {
     typedef float f32x4 __attribute__((ext_vector_type(4)));
-    static_assert(2 * 32 * D * sizeof(float) <= 2 * L::ELEMS * sizeof(__bf16), "two waves' sums must fit in the tile buffers of a kind");
-    f32x4* const sums = reinterpret_cast<f32x4*>((wave / 2 == 0 ? k_s1_all : v_s1_all)) + wave % 2 * (32 * D / 4) + lane;
-    if (group == 1) {
+    static_assert(32 * D * sizeof(float) <= L::ELEMS * sizeof(__bf16), "a wave's sums must fit in a tile buffer");
+    f32x4* const sums = reinterpret_cast<f32x4*>(wave / 2 == 0 ? k_s1 : v_s1) + lane;
+    if (half == 1) {
 #pragma unroll
       for (int i = 0; i < 4 * DB; ++i) sums[i * 64] = f32x4{dq[i / 4][i % 4 * 4], dq[i / 4][i % 4 * 4 + 1], dq[i / 4][i % 4 * 4 + 2], dq[i / 4][i % 4 * 4 + 3]};
     }
     __syncthreads();
-    if (group == 1) return;
+    if (half == 1) return;
 #pragma unroll
     for (int i = 0; i < 4 * DB; ++i) {
       const f32x4 y = sums[i * 64];
@@ -513,7 +510,7 @@ __global__ __launch_bounds__(256) void prompt_sum_kernel(const PromptBwdParams P
 
 // Parts of a group's heads that the dkv kernel takes side by side: one key head's walk over all heads of its group is as long as they are many, and a
 // chip that is not full waits for it.  Worth the fp32 sums in memory where the walk is long.  Forward and backward, one / several parts, us: 1 x 1024
-// tokens, 8 / 2 heads of 128, 104 / 78; 1 x 4096, 8 / 2 of 64, 230 / 158; 1 x 2048, 32 / 8 of 128, 255 / 220; but 8 x 300, 16 / 4 of 64, 41 / 51.
+// tokens, 8 / 2 heads of 128, 104 / 78; 1 x 4096, 8 / 2 of 64, 230 / 158; 1 x 2048, 32 / 8 of 128, 255 / 220; but 8 x 300, 16 / 4 of 64, 46 / 51.
 constexpr int64_t kDkvWgs = 512, kLongWalk = 2048;  // work-groups, two a CU; queries of all heads of a group
 inline int64_t head_parts(int64_t T, int64_t R, int64_t H, int64_t Hk) {
   if (H / Hk * T < kLongWalk * R) return 1;
@@ -563,14 +560,15 @@ extern "C" __attribute__((visibility("default"))) int bbm_prompt_attn_bwd(const 
   P.T = (int32_t)T, P.R = (int32_t)R, P.G = (int32_t)(H / Hk), P.H = (int32_t)H, P.rc = softmax_scale * kLog2e, P.scale = softmax_scale;
   P.parts = (int32_t)head_parts(T, R, H, Hk);
   P.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * stats_bytes(T, H));
-  const int64_t row_pieces = count_pieces(T, R, 1, 128), key_pieces = count_pieces(T, R, 1, 64);
+  const bool halves = split_keys(T, R, H);
+  const int64_t row_pieces = count_pieces(T, R, 1, halves ? 64 : 128), key_pieces = count_pieces(T, R, 1, 64);
   const int64_t rows = work_groups(H, row_pieces), keys = work_groups(Hk * P.parts, key_pieces), sums = P.parts > 1 ? ceil_div(2 * Hk * T * (d / 8), 256) : 0;
   if (rows >= 1ll << 31 || keys >= 1ll << 31 || sums >= 1ll << 31) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld)", fn, (long long)T, (long long)H);
   P.row_pieces = (int32_t)row_pieces, P.key_pieces = (int32_t)key_pieces;
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto go = [&](auto size) {
     constexpr int D = decltype(size)::value;
-    if (split_tiles(T, R, H)) prompt_dq_kernel<D, 2><<<(unsigned)rows, 512, 0, s>>>(P);
+    if (halves) prompt_dq_kernel<D, 2><<<(unsigned)rows, 256, 0, s>>>(P);
     else prompt_dq_kernel<D, 1><<<(unsigned)rows, 256, 0, s>>>(P);
     prompt_dkv_kernel<D><<<(unsigned)keys, 256, 0, s>>>(P);
     if (P.parts > 1) prompt_sum_kernel<D><<<(unsigned)sums, 256, 0, s>>>(P);
