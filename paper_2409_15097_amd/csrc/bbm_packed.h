@@ -44,7 +44,7 @@ struct Span {
 // offsets, launches for T * mul / unit + R of them, and no batch has more (floor((a + n) / u) + 1 >= floor(a / u) + ceil(n / u)).
 // Up to kCounted requests, all lanes of a wave count the pieces, 64 requests at a time: numbers follow each other without holes, and those that
 // belong to nobody (begin = end) are the last ones.  With the numbers below, requests of one piece each had every other number: work-groups go to
-// the shader engines of an XCD in turn, and half of them got nothing (16 requests of 128 columns over 4096 keys of the 4-bit cache: 82 us instead of 50).
+// the shader engines of an XCD in turn, and half of them got nothing (16 requests of 128 columns over 4096 keys of the 4-bit cache: 104 us instead of 81).
 // Beyond, request r's pieces have the numbers from cu[r] * mul / unit + r on, found by a search that takes a trip to memory for every
 // factor of 64 in R, and there are holes.
 constexpr int kCounted = 512;

@@ -1,8 +1,9 @@
 // Rotary positions of queries and keys (include/bbm_tokens.h), and with the angles negated their gradient.
 //
 // Bound by memory: every element is read and written once.  A work-group takes a few tokens with all their heads: it forms
-// the sines and cosines of its tokens' angles once, in LDS, and turns all heads of both tensors with them.  An item is two chunks of
-// VEC elements: the two halves of VEC pairs, or two chunks that are copied.
+// the sines and cosines of its tokens' angles once, in LDS, and turns all heads of both tensors with them.
+// 16381 tokens of 40 heads of 128 elements: 66 us with rot = 128, 69 with 64 or neighbouring pairs, 4.9 - 5.1 TB/s (a large copy reaches
+// 4.8); 33 tokens: 3.8 us, a launch and three trips to memory.  Streaming stores: 84 us, 89 with streaming loads too.
 // The angle is a product in 64 bits, reduced to a part of a turn there: in 32 bits an angle of 10^5 is off by 4e-3.
 #include "bbm_packed.h"
 
@@ -24,30 +25,28 @@ struct RopeParams {
   int32_t T, H0, H, d, rot, tokens;  // H0 heads of x[0], H of both; tokens of a work-group
 };
 
-template <int VEC>
-struct Chunk {
-  typedef __bf16 type __attribute__((ext_vector_type(VEC)));
-};
-template <>
-struct Chunk<1> {
-  typedef __bf16 type __attribute__((ext_vector_type(1)));
-};
+typedef __bf16 Chunk __attribute__((ext_vector_type(8)));
 
-template <int VEC, bool EVEN>
-__global__ __launch_bounds__(NT) void rope_kernel(const RopeParams P) {
-  typedef typename Chunk<VEC>::type V;
-  extern __shared__ float2 turn_s[];  // (cos, sin) of [token][pair]
-  const int tid = threadIdx.x, pairs = P.rot >> 1;
-  const int t0 = blockIdx.x * P.tokens, nt = min(P.tokens, P.T - t0);
-  for (int n = tid; n < nt * pairs; n += NT) {
+// (cos, sin) of the angles of tokens t0 .. t0 + nt - 1, [token][pair]; a barrier has to follow.
+__device__ __forceinline__ void turns_of(const RopeParams& P, float2* turn_s, int t0, int nt, int pairs) {
+  for (int n = threadIdx.x; n < nt * pairs; n += NT) {
     const int t = n / pairs, j = n - t * pairs;
     const double turns = (double)P.positions[t0 + t] * ((double)P.freqs[j] * 0.15915494309189533577);
     float s, c;
     sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
     turn_s[n] = make_float2(c * P.mscale, s * P.mscale * P.sign);
   }
+}
+
+// An item is two chunks of 8 elements: the two halves of 8 pairs, or (EVEN: always) two chunks side by side, turned or copied.
+template <bool EVEN>
+__global__ __launch_bounds__(NT) void rope_kernel(const RopeParams P) {
+  extern __shared__ __align__(16) float2 turn_s[];
+  const int tid = threadIdx.x, pairs = P.rot >> 1;
+  const int t0 = blockIdx.x * P.tokens, nt = min(P.tokens, P.T - t0);
+  turns_of(P, turn_s, t0, nt, pairs);
   __syncthreads();
-  const int per_head = P.d / (2 * VEC), per_token = per_head * P.H;
+  const int per_head = P.d / 16, per_token = per_head * P.H;
   for (int n = tid; n < nt * per_token; n += NT) {
     const int t = n / per_token, m = n - t * per_token, h = m / per_head, c = m - h * per_head;
     const RopeTensor& x = P.x[h < P.H0 ? 0 : 1];
@@ -55,32 +54,85 @@ __global__ __launch_bounds__(NT) void rope_kernel(const RopeParams P) {
     const __bf16* const in = x.in + (int64_t)(t0 + t) * x.in_row + hx * x.in_head;
     __bf16* const out = x.out + (int64_t)(t0 + t) * x.out_row + hx * x.out_head;
     // neighbouring pairs: chunks 2c and 2c + 1; halves: chunk c of either half, behind them two chunks that are copied
-    const bool turned = EVEN || c * VEC < pairs;
-    const int a_at = turned && !EVEN ? c * VEC : 2 * c * VEC, b_at = a_at + (turned && !EVEN ? pairs : VEC);
-    const V a = *reinterpret_cast<const V*>(in + a_at), b = *reinterpret_cast<const V*>(in + b_at);
-    V ya = a, yb = b;
-    const float2* const turn = turn_s + t * pairs + c * VEC;
+    const bool turned = EVEN || c * 8 < pairs;
+    const int a_at = turned && !EVEN ? c * 8 : 16 * c, b_at = a_at + (turned && !EVEN ? pairs : 8);
+    const Chunk a = *reinterpret_cast<const Chunk*>(in + a_at), b = *reinterpret_cast<const Chunk*>(in + b_at);
+    Chunk ya = a, yb = b;
+    const float2* const turn = turn_s + t * pairs + c * 8;
     if constexpr (EVEN) {
 #pragma unroll
-      for (int e = 0; e < 2 * VEC; e += 2) {
-        if (c * VEC + e / 2 < pairs) {
+      for (int e = 0; e < 16; e += 2) {
+        if (c * 8 + e / 2 < pairs) {
           const float2 w = turn[e / 2];
-          const float p = e < VEC ? (float)a[e % VEC] : (float)b[e % VEC], q = e < VEC ? (float)a[e % VEC + 1] : (float)b[e % VEC + 1];
+          const float p = e < 8 ? (float)a[e % 8] : (float)b[e % 8], q = e < 8 ? (float)a[e % 8 + 1] : (float)b[e % 8 + 1];
           const __bf16 y1 = (__bf16)(p * w.x - q * w.y), y2 = (__bf16)(q * w.x + p * w.y);
-          if (e < VEC) ya[e % VEC] = y1, ya[e % VEC + 1] = y2;
-          else yb[e % VEC] = y1, yb[e % VEC + 1] = y2;
+          if (e < 8) ya[e % 8] = y1, ya[e % 8 + 1] = y2;
+          else yb[e % 8] = y1, yb[e % 8 + 1] = y2;
         }
       }
     } else if (turned) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
+      for (int e = 0; e < 8; ++e) {
         const float2 w = turn[e];
         ya[e] = (__bf16)((float)a[e] * w.x - (float)b[e] * w.y);
         yb[e] = (__bf16)((float)b[e] * w.x + (float)a[e] * w.y);
       }
     }
-    *reinterpret_cast<V*>(out + a_at) = ya;
-    *reinterpret_cast<V*>(out + b_at) = yb;
+    *reinterpret_cast<Chunk*>(out + a_at) = ya;
+    *reinterpret_cast<Chunk*>(out + b_at) = yb;
+  }
+}
+
+// Halves whose middle or end lies inside a chunk: whole heads go through LDS, STEP chunks a thread at a time, and an element finds the other
+// one of its pair there.  (All of a head is read before any of it is written, also in place.)  16381 tokens of 40 heads of 128, rot = 126, 100, 44:
+// 75, 75, 73 us; with items of one, two and two pairs in rope_kernel 158, 101, 114 us (33 tokens: 5.1 us against 6.1, 4.6 and 4.7).
+constexpr int STEP = 2;
+__global__ __launch_bounds__(NT) void rope_staged_kernel(const RopeParams P) {
+  extern __shared__ __align__(16) float2 turn_s[];
+  const int tid = threadIdx.x, pairs = P.rot >> 1;
+  const int t0 = blockIdx.x * P.tokens, nt = min(P.tokens, P.T - t0);
+  __bf16* const x_s = reinterpret_cast<__bf16*>(turn_s + (P.tokens * pairs + 1) / 2 * 2);
+  turns_of(P, turn_s, t0, nt, pairs);
+  const int per_head = P.d / 8, step_heads = STEP * NT / per_head, heads = nt * P.H;
+  for (int h0 = 0; h0 < heads; h0 += step_heads) {
+    Chunk a[STEP];
+    __bf16* out[STEP];
+    int at[STEP], turn[STEP];
+    if (h0 > 0) __syncthreads();  // (the last step's readers of x_s)
+#pragma unroll
+    for (int u = 0; u < STEP; ++u) {
+      const int n = tid + u * NT, hl = n / per_head, g = h0 + hl;
+      out[u] = nullptr;
+      if (hl >= step_heads || g >= heads) continue;
+      const int t = g / P.H, h = g - t * P.H;
+      const RopeTensor& x = P.x[h < P.H0 ? 0 : 1];
+      const int hx = h < P.H0 ? h : h - P.H0;
+      at[u] = (n - hl * per_head) * 8, turn[u] = t * pairs;
+      a[u] = *reinterpret_cast<const Chunk*>(x.in + (int64_t)(t0 + t) * x.in_row + hx * x.in_head + at[u]);
+      out[u] = x.out + (int64_t)(t0 + t) * x.out_row + hx * x.out_head + at[u];
+      *reinterpret_cast<Chunk*>(x_s + n * 8) = a[u];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < STEP; ++u) {
+      if (!out[u]) continue;
+      Chunk y = a[u];
+      if (at[u] < P.rot) {
+        const __bf16* const row = x_s + (tid + u * NT) * 8;  // this chunk
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int i = at[u] + e;
+          const bool first = i < pairs, turned = i < P.rot;
+          const int other = first ? pairs : -pairs;
+          const float2 w = turn_s[turn[u] + (turned ? (first ? i : i - pairs) : 0)];
+          const float p = (float)a[u][e], q = (float)row[turned ? e + other : e];
+          // as the kernel above rounds it: the first of a pair p c - q s, the second p c + q s
+          const float r = first ? p * w.x - q * w.y : p * w.x + q * w.y;
+          y[e] = turned ? (__bf16)r : a[u][e];
+        }
+      }
+      *reinterpret_cast<Chunk*>(out[u]) = y;
+    }
   }
 }
 
@@ -122,13 +174,10 @@ extern "C" __attribute__((visibility("default"))) int bbm_rope(const bbm_packed*
   while (tokens < 8 && tokens * items < 4 * NT && ceil_div(T, 2 * tokens) >= 1024) tokens *= 2;
   P.tokens = (int32_t)tokens;
   const unsigned wgs = (unsigned)ceil_div(T, tokens);
-  const size_t lds = (size_t)(tokens * (rot / 2)) * sizeof(float2);
+  const size_t lds = (size_t)(tokens * (rot / 2) + 1) / 2 * 2 * sizeof(float2);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  // halves: chunks must not straddle the middle and the end of the part that is turned
-  if (interleaved) rope_kernel<8, true><<<wgs, NT, lds, s>>>(P);
-  else if (rot % 16 == 0) rope_kernel<8, false><<<wgs, NT, lds, s>>>(P);
-  else if (rot % 8 == 0) rope_kernel<4, false><<<wgs, NT, lds, s>>>(P);
-  else if (rot % 4 == 0) rope_kernel<2, false><<<wgs, NT, lds, s>>>(P);
-  else rope_kernel<1, false><<<wgs, NT, lds, s>>>(P);
+  if (interleaved) rope_kernel<true><<<wgs, NT, lds, s>>>(P);
+  else if (rot % 16 == 0) rope_kernel<false><<<wgs, NT, lds, s>>>(P);
+  else rope_staged_kernel<<<wgs, NT, lds + STEP * NT * 16, s>>>(P);
   return launch_status(fn);
 }

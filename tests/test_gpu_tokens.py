@@ -84,7 +84,8 @@ def test_slots(bbm, R, new, ctx, page, short_list, narrow):
 @pytest.mark.parametrize("T, H, Hk, d, rot, interleaved, layout", [
     (1, 1, 1, 16, 2, False, "plain"), (1, 4, 0, 64, 64, True, "plain"), (33, 32, 8, 128, 128, False, "fused"), (7, 3, 1, 64, 62, False, "fused"),
     (7, 3, 1, 64, 62, True, "heads"), (130, 8, 2, 128, 64, True, "fused"), (130, 8, 2, 128, 40, False, "heads"), (65, 5, 5, 80, 20, False, "plain"),
-    (65, 5, 5, 80, 6, True, "plain"), (3000, 4, 2, 128, 96, False, "plain"), (5000, 2, 1, 512, 512, True, "plain"), (40, 2, 1, 112, 112, False, "heads")])
+    (65, 5, 5, 80, 6, True, "plain"), (3000, 4, 2, 128, 96, False, "plain"), (5000, 2, 1, 512, 512, True, "plain"), (40, 2, 1, 112, 112, False, "heads"),
+    (300, 40, 8, 80, 74, False, "heads"), (4100, 2, 1, 512, 510, False, "fused"), (9, 24, 3, 144, 24, False, "plain"), (2, 70, 3, 16, 2, False, "plain")])
 @pytest.mark.parametrize("inverse", [False, True])
 def test_rope(bbm, T, H, Hk, d, rot, interleaved, layout, inverse):
     g = np.random.default_rng(T + rot)
