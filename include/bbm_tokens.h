@@ -13,7 +13,7 @@
  *
  * Unless a function says otherwise, outputs overlap neither inputs nor each other.  What rows of nobody hold does not matter (it may be
  * an infinity or a NaN); the rows of requests are taken to be finite, as are the cache's groups: an infinity or a NaN among them may reach any
- * row of its own request.
+ * row of its own request.  Scores are fp32 numbers: a softmax_scale lies within 2^-100 .. 2^100, and sums of products of q and k stay within fp32's range.
  *
  * A packed tensor is bf16 [T][heads][d] with any row and head strides (in elements, multiples of 8; the d elements of a head
  * are contiguous and 16-byte aligned), so the q, k and v parts of one projection's output, or [heads][T][d], need no copy.
@@ -122,6 +122,7 @@ int bbm_kv4_read(const int32_t* slots, int64_t T, const bbm_kv4_cache* cache, co
  * bbm_prompt_attn_fwd.  max_len is a hint for the work split (the longest of lens, or an upper bound); any positive number gives
  * correct results.  The workspace needs bbm_kv4_attn_workspace_bytes bytes for the same T, R, H, Hk, d and max_len, 16-byte aligned,
  * contents of no matter.
+ * max_pages * page and T * H / Hk at most 2^30.
  */
 size_t bbm_kv4_attn_workspace_bytes(int64_t T, int64_t R, int64_t H, int64_t Hk, int d, int64_t max_len);
 int bbm_kv4_attn(const bbm_packed* q, const bbm_packed* o, float* lse, int64_t T, int64_t R, const int32_t* cu, const int32_t* lens,

@@ -6,6 +6,7 @@
 namespace bbm {
 
 constexpr int64_t kMaxTokens = 1ll << 30;
+constexpr int64_t kMaxWgs = 1ll << 24;  // work-groups of 256 threads that a launch may have, less one: it counts threads in 32 bits
 constexpr int64_t kMaxRowStride = 1ll << 22;  // a tile of 128 rows stays within the 2^31 bytes of a buffer resource
 
 // `rows` x `heads` x d elements; an output's must not lie upon each other.
@@ -32,6 +33,13 @@ inline int check_tokens(const char* fn, int64_t T, int64_t R, const int32_t* cu,
   if (H % Hk) return fail(BBM_EINVAL, "%s: H=%lld is no multiple of Hk=%lld", fn, (long long)H, (long long)Hk);
   if (!cu || !aligned(cu, 4)) return fail(BBM_EINVAL, "%s: cu must be a non-NULL 4-byte aligned pointer", fn);
   if (T > kMaxTokens || R > kMaxTokens || H > 65535 || T * H > (1ll << 36)) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, R=%lld, H=%lld)", fn, (long long)T, (long long)R, (long long)H);
+  return BBM_OK;
+}
+
+// (Beyond these the factors that the kernels make of it are no finite numbers in fp32.)
+inline int check_scale(const char* fn, float softmax_scale) {
+  if (!(softmax_scale > 0.0f) || !(softmax_scale < INFINITY)) return fail(BBM_EINVAL, "%s: softmax_scale must be finite and > 0", fn);
+  if (softmax_scale < 0x1p-100f || softmax_scale > 0x1p100f) return fail(BBM_EUNSUPPORTED, "%s: softmax_scale=%g is outside 2^-100 .. 2^100", fn, (double)softmax_scale);
   return BBM_OK;
 }
 

@@ -168,11 +168,12 @@ extern "C" __attribute__((visibility("default"))) int bbm_rope(const bbm_packed*
   P.x[1] = Hk > 0 ? tensor(k, k_out) : P.x[0];
   P.positions = positions, P.freqs = freqs, P.mscale = mscale, P.sign = inverse ? -1.0f : 1.0f;
   P.T = (int32_t)T, P.H0 = (int32_t)H, P.H = (int32_t)(H + Hk), P.d = d, P.rot = rot;
-  // Tokens of a work-group: a few items for every thread, as long as there are four work-groups a CU
+  // Tokens of a work-group: a few items for every thread, as long as there are four work-groups a CU and 16 KiB hold their angles
   const int64_t items = (H + Hk) * d / 16;
   int64_t tokens = 1;
-  while (tokens < 8 && tokens * items < 4 * NT && ceil_div(T, 2 * tokens) >= 1024) tokens *= 2;
+  while (tokens * items < 4 * NT && 2 * tokens * (rot / 2) <= 2048 && ceil_div(T, 2 * tokens) >= 1024) tokens *= 2;
   P.tokens = (int32_t)tokens;
+  if (ceil_div(T, tokens) >= kMaxWgs) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld)", fn, (long long)T, (long long)H);
   const unsigned wgs = (unsigned)ceil_div(T, tokens);
   const size_t lds = (size_t)(tokens * (rot / 2) + 1) / 2 * 2 * sizeof(float2);
   hipStream_t s = static_cast<hipStream_t>(stream);

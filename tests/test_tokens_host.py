@@ -54,7 +54,7 @@ def rope(bbm, q=pk, qo=pk, H=4, k=pk, ko=pk, Hk=2, T=3, d=64, rot=64, pos=P, fre
     return bbm.lib.bbm_rope(f(q), f(qo), H, f(k), f(ko), Hk, T, d, rot, 0, 0, pos, freqs, mscale, None)
 
 
-BAD_PACKED = [None, pk(0), pk(P + 8), pk(row=1020), pk(head=100), pk(row=-8), pk(head=-8)] if os.path.exists(os.path.join(ROOT, "paper_2409_15097_amd", "libbbm.so")) else []
+BAD_PACKED = [None, pk(0), pk(P + 8), pk(row=1020), pk(head=100), pk(row=-8), pk(head=-8)]
 OVERLAP = [dict(row=0), dict(head=0), dict(row=64, head=64), dict(row=120, head=64), dict(head=56)]
 
 
@@ -67,7 +67,7 @@ def test_rope_refuses(bbm):
     for kw in (dict(T=-1), dict(H=0), dict(Hk=-1), dict(rot=0), dict(rot=63), dict(rot=66), dict(pos=None), dict(freqs=None), dict(pos=P + 1),
                dict(mscale=math.inf), dict(mscale=math.nan), dict(qo=pk(row=2048))):
         assert rope(bbm, **kw) == bbm.BBM_EINVAL, kw
-    for kw in (dict(d=72, rot=2), dict(d=528), dict(d=0), dict(T=1 << 31), dict(q=pk(row=(1 << 22) + 8))):
+    for kw in (dict(d=72, rot=2), dict(d=528), dict(d=0), dict(T=1 << 31), dict(q=pk(row=(1 << 22) + 8)), dict(T=1 << 30)):
         assert rope(bbm, **kw) == bbm.BBM_EUNSUPPORTED, kw
     assert rope(bbm, T=0) == bbm.BBM_OK
 
@@ -90,7 +90,7 @@ def test_prompt_attention_refuses(bbm):
         for kw in (dict(T=-1), dict(R=0), dict(H=0), dict(Hk=0), dict(H=3), dict(cu=None), dict(cu=P + 2), dict(lse=P + 2), dict(scale=0.0), dict(scale=-1.0),
                    dict(scale=math.inf), dict(scale=math.nan)):
             assert call(bbm, **kw) == bbm.BBM_EINVAL, kw
-        for kw in (dict(d=96), dict(T=1 << 31), dict(R=1 << 31), dict(H=1 << 17)):
+        for kw in (dict(d=96), dict(T=1 << 31), dict(R=1 << 31), dict(H=1 << 17), dict(scale=2.0 ** -101), dict(scale=2.0 ** 101)):
             assert call(bbm, **kw) == bbm.BBM_EUNSUPPORTED, kw
         assert call(bbm, T=0) == bbm.BBM_OK
     for bad in OVERLAP:
@@ -133,13 +133,12 @@ def test_cache_refuses(bbm):
                dict(lse=P + 2), dict(stride=3), dict(width=0), dict(max_len=0), dict(mask=P + 4, words=1), dict(mask=P, words=0), dict(words=1), dict(scale=0.0),
                dict(scale=math.nan), dict(ws=P + 8)):
         assert attn(bbm, **kw) == bbm.BBM_EINVAL, kw
-    for kw in (dict(T=1 << 31), dict(width=1 << 26, stride=1 << 26), dict(mask=P, words=(1 << 20) + 1)):
+    for kw in (dict(T=1 << 31), dict(T=1 << 30), dict(scale=2.0 ** -101), dict(width=(1 << 24) + 1, stride=1 << 26), dict(mask=P, words=(1 << 20) + 1)):
         assert attn(bbm, **kw) == bbm.BBM_EUNSUPPORTED, kw
     assert attn(bbm, T=0) == bbm.BBM_OK
     need = bbm.bbm_kv4_attn_workspace_bytes(1, 1, 8, 1, 128, 1 << 16)
     long = dict(T=1, R=1, H=8, c=cache(Hk=1, d=128), max_len=1 << 16)
-    if need:
-        assert attn(bbm, **long, ws_bytes=need - 1) == bbm.BBM_EWORKSPACE and attn(bbm, **long, ws=None) == bbm.BBM_EWORKSPACE
+    assert need > 0 and attn(bbm, **long, ws_bytes=need - 1) == bbm.BBM_EWORKSPACE and attn(bbm, **long, ws=None) == bbm.BBM_EWORKSPACE
     assert bbm.bbm_kv4_attn_workspace_bytes(0, 1, 8, 1, 128, 64) == 0 and bbm.bbm_kv4_attn_workspace_bytes(1, 1, 8, 3, 128, 64) == 0
 
 
