@@ -48,6 +48,17 @@ struct Span {
   int piece;          // which piece of it
 };
 
+// The sum of x over this lane and those in front of it: within rows of 16 lanes, then the last lanes of the rows in front.
+__device__ __forceinline__ int wave_prefix_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // from 1, 2, 4, 8 lanes in front
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // the last lane of rows 0 and 2 to rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // the last lane of row 1 to rows 2 and 3
+  return x;
+}
+
 // Which piece of which request is number `at`?  Requests are cut into pieces of `unit` columns, `mul` columns a row; the host, which does not know the
 // offsets, launches for T * mul / unit + R of them, and no batch has more (floor((a + n) / u) + 1 >= floor(a / u) + ceil(n / u)).
 // Up to kCounted requests, all lanes of a wave count the pieces, 64 requests at a time: numbers follow each other without holes, and those that
@@ -62,32 +73,39 @@ __device__ __forceinline__ Span find_piece(const int32_t* __restrict__ cu, int R
   Span s;
   s.r = s.begin = s.end = s.piece = 0;
   if (R <= kCounted) {
-    int before = 0;  // pieces of the requests in front of these 64
-    for (int r0 = 0; r0 < R; r0 += 64) {
-      const int r = min(r0 + lane, R - 1), begin = cut(cu[r]), end = max(begin, cut(cu[r + 1]));
-      const int mine = r0 + lane < R ? (int)(((int64_t)(end - begin) * mul + unit - 1) / unit) : 0;
-      int sum = mine;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int x = __shfl_up(sum, d);
-        if (lane >= d) sum += x;
+    int before = 0;  // pieces of the requests in front of these
+    // 64 requests from r0 on, of which the lane holds one; true if the piece was among them
+    auto among = [&](int r0, int c0, int c1) __attribute__((always_inline)) {
+      const int begin = cut(c0), end = max(begin, cut(c1));
+      const int mine = r0 + lane < R ? (int)(((uint32_t)(end - begin) * (uint32_t)mul + (uint32_t)(unit - 1)) / (uint32_t)unit) : 0;
+      const int sum = wave_prefix_sum(mine), all = __builtin_amdgcn_readlane(sum, 63);
+      if (at >= before + all) {
+        before += all;
+        return false;
       }
-      const int all = __builtin_amdgcn_readlane(sum, 63);
-      if (at < before + all) {
-        const uint64_t behind = __ballot(before + sum > at);
-        const int l = __ffsll((unsigned long long)behind) - 1;
-        s.r = r0 + l;
-        s.begin = __builtin_amdgcn_readlane(begin, l);
-        s.end = __builtin_amdgcn_readlane(end, l);
-        s.piece = at - before - __builtin_amdgcn_readlane(sum - mine, l);
-        break;
-      }
-      before += all;
+      const int l = __ffsll((unsigned long long)__ballot(before + sum > at)) - 1;
+      s.r = r0 + l;
+      s.begin = __builtin_amdgcn_readlane(begin, l);
+      s.end = __builtin_amdgcn_readlane(end, l);
+      s.piece = at - before - __builtin_amdgcn_readlane(sum - mine, l);
+      return true;
+    };
+    if (R <= 64) {
+      const int r = min(lane, R - 1);
+      among(0, cu[r], cu[r + 1]);
+      return s;
     }
-    s.r = __builtin_amdgcn_readfirstlane(s.r);
-    s.begin = __builtin_amdgcn_readfirstlane(s.begin);
-    s.end = __builtin_amdgcn_readfirstlane(s.end);
-    s.piece = __builtin_amdgcn_readfirstlane(s.piece);
+    for (int r0 = 0; r0 < R; r0 += 256) {  // (four times 64 in one trip to memory)
+      int c0[4], c1[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = min(r0 + 64 * i + lane, R - 1);
+        c0[i] = cu[r], c1[i] = cu[r + 1];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (among(r0 + 64 * i, c0[i], c1[i])) return s;
+    }
     return s;
   }
   auto first = [&](int c, int r) { return (int64_t)cut(c) * mul / unit + r; };
