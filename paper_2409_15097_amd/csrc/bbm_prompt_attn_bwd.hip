@@ -32,28 +32,24 @@ struct PromptBwdParams {
   float* ndelta;  // workspace [H][T]: -<dO, O>
   float* partials;  // workspace [part][dV, dK][Hk][T][d], of more than one part
   const int32_t* cu;
-  int32_t T, R, G, H, row_pieces, key_pieces, parts;
+  int32_t T, R, G, H, row_pieces, key_pieces, parts, key_wgs;
   float rc;  // softmax_scale * log2(e)
   float scale;
 };
 typedef bbm::InPlace<PromptBwdParams> Args;
 
 // HALVES = 2: 64 rows a work-group, two waves share 32 of them and halve the keys of every tile, as in the forward.
-template <int D, int HALVES>
-__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dq_kernel(const PromptBwdParams) {
-  Args P = bbm::kernel_args<PromptBwdParams>();
+// t_s0, t_s1: [K, V] tiles, one variable per parity.  DELTA: forms -D and -lse / scale and leaves them in the workspace; else they are there.
+template <int D, int HALVES, bool DELTA>
+__device__ __forceinline__ void dq_of(Args P, int wg, __bf16* t_s0, __bf16* t_s1, float (*delta_s)[32]) {
   using L = TL<D>;
   constexpr int NW = 4, BR = 32 * NW / HALVES, KB = 2 / HALVES, KS = D / 16, DB = D / 32, RC = D / 8, RPB = 64 / RC;
-  __shared__ __attribute__((aligned(16))) __bf16 k_s0[L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 k_s1[L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 v_s0[L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 v_s1[L::ELEMS];
-  __shared__ float delta_s[NW][32];
+  __bf16 *const k_s0 = t_s0, *const v_s0 = t_s0 + L::ELEMS, *const k_s1 = t_s1, *const v_s1 = t_s1 + L::ELEMS;
 
   const int lane = threadIdx.x & 63, lq = lane & 31, hh = lane >> 5;
   const int wave = (int)scalar(threadIdx.x >> 6);
   const int half = HALVES == 2 ? wave & 1 : 0;  // of the keys
-  const bbm::Work work = bbm::work_of(blockIdx.x, P->H);
+  const bbm::Work work = bbm::work_of(wg, P->H);
   const int h = work.plane;
   if (work.number >= P->row_pieces) return;
   const bbm::Span s = bbm::find_piece(global(P->cu), P->R, P->T, 1, BR, P->row_pieces - 1 - work.number);
@@ -87,42 +83,55 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dq_kernel(const 
     __bf16* const stage = (wave / 2 == 0 ? k_s1 : v_s1) + wave % 2 * 32 * D;
     const int64_t t0 = s.begin + wrow;
     bbm::copy_slab<D>(global(P->q.p) + h * P->q.head + t0 * P->q.row, wrows, P->q.row, stage, lane);
-    const int g_row = lane / RC, g_chunk = lane % RC;
     const __amdgpu_buffer_rsrc_t do_r = buffer_of(global(P->d_o.p) + h * P->d_o.head + t0 * P->d_o.row, wrows > 0 ? ((wrows - 1) * P->d_o.row + D) * 2 : 0);
-    const __amdgpu_buffer_rsrc_t o_r = buffer_of(global(P->o.p) + h * P->o.head + t0 * P->o.row, wrows > 0 ? ((wrows - 1) * P->o.row + D) * 2 : 0);
     const int64_t row_at = (int64_t)h * P->T + t0;
-    const float lse = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer_of(P->lse + row_at, wrows * 4), lq * 4, 0, 0));
-    bf16x8 gr[32 / RPB], orow[32 / RPB];
+    if constexpr (DELTA) {
+      const int g_row = lane / RC, g_chunk = lane % RC;
+      const __amdgpu_buffer_rsrc_t o_r = buffer_of(global(P->o.p) + h * P->o.head + t0 * P->o.row, wrows > 0 ? ((wrows - 1) * P->o.row + D) * 2 : 0);
+      const float lse = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer_of(P->lse + row_at, wrows * 4), lq * 4, 0, 0));
+      bf16x8 gr[32 / RPB], orow[32 / RPB];
 #pragma unroll
-    for (int i = 0; i < 32 / RPB; ++i) {
-      const int r = i * RPB + g_row;
-      gr[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(do_r, (r * P->d_o.row + g_chunk * 8) * 2, 0, 0));
-      orow[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(o_r, (r * P->o.row + g_chunk * 8) * 2, 0, 0));
-    }
+      for (int i = 0; i < 32 / RPB; ++i) {
+        const int r = i * RPB + g_row;
+        gr[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(do_r, (r * P->d_o.row + g_chunk * 8) * 2, 0, 0));
+        orow[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(o_r, (r * P->o.row + g_chunk * 8) * 2, 0, 0));
+      }
 #pragma unroll
-    for (int i = 0; i < 2 * LPW; ++i) copy_piece(0, rows_at(0), k_s0, v_s0, i);
+      for (int i = 0; i < 2 * LPW; ++i) copy_piece(0, rows_at(0), k_s0, v_s0, i);
 #pragma unroll
-    for (int i = 0; i < 32 / RPB; ++i) {
-      float x = 0.0f;
-      for (int e = 0; e < 8; ++e) x += (float)gr[i][e] * (float)orow[i][e];
-      x = bbm::row_sum<RC>(x);
-      if (g_chunk == 0) delta_s[wave][i * RPB + g_row] = x;
-    }
-    __builtin_amdgcn_s_waitcnt(0);  // this wave's own copies have landed (no other wave touches its slab)
+      for (int i = 0; i < 32 / RPB; ++i) {
+        float x = 0.0f;
+        for (int e = 0; e < 8; ++e) x += (float)gr[i][e] * (float)orow[i][e];
+        x = bbm::row_sum<RC>(x);
+        if (g_chunk == 0) delta_s[wave][i * RPB + g_row] = x;
+      }
+      __builtin_amdgcn_s_waitcnt(0);  // this wave's own copies have landed (no other wave touches its slab)
 #pragma unroll
-    for (int t = 0; t < KS; ++t) qf[t] = bbm::slab_frag<D>(stage, t, lane);
+      for (int t = 0; t < KS; ++t) qf[t] = bbm::slab_frag<D>(stage, t, lane);
 #pragma unroll
-    for (int i = 0; i < 32 / RPB; ++i) {
-      const int r = i * RPB + g_row;
-      *reinterpret_cast<bf16x8*>(stage + r * D + (g_chunk ^ r % RC) * 8) = gr[i];
-    }
+      for (int i = 0; i < 32 / RPB; ++i) {
+        const int r = i * RPB + g_row;
+        *reinterpret_cast<bf16x8*>(stage + r * D + (g_chunk ^ r % RC) * 8) = gr[i];
+      }
 #pragma unroll
-    for (int t = 0; t < KS; ++t) dof[t] = bbm::slab_frag<D>(stage, t, lane);
-    nl = -lse * kLog2e;
-    nd = -delta_s[wave][lq];
-    if (hh == 0 && half == 0) {
-      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(nl / rc), buffer_of(P->nls + row_at, wrows * 4), lq * 4, 0, 0);
-      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(nd), buffer_of(P->ndelta + row_at, wrows * 4), lq * 4, 0, 0);
+      for (int t = 0; t < KS; ++t) dof[t] = bbm::slab_frag<D>(stage, t, lane);
+      nl = -lse * kLog2e;
+      nd = -delta_s[wave][lq];
+      if (hh == 0 && half == 0) {
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(nl / rc), buffer_of(P->nls + row_at, wrows * 4), lq * 4, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(nd), buffer_of(P->ndelta + row_at, wrows * 4), lq * 4, 0, 0);
+      }
+    } else {
+      const float nls = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer_of(P->nls + row_at, wrows * 4), lq * 4, 0, 0));
+      nd = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer_of(P->ndelta + row_at, wrows * 4), lq * 4, 0, 0));
+#pragma unroll
+      for (int t = 0; t < KS; ++t) dof[t] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(do_r, (lq * P->d_o.row + 16 * t + 8 * hh) * 2, 0, 0));
+#pragma unroll
+      for (int i = 0; i < 2 * LPW; ++i) copy_piece(0, rows_at(0), k_s0, v_s0, i);
+      __builtin_amdgcn_s_waitcnt(0);
+#pragma unroll
+      for (int t = 0; t < KS; ++t) qf[t] = bbm::slab_frag<D>(stage, t, lane);
+      nl = nls * rc;
     }
   }
   for (int i = 0; i < 2; ++i) {  // this wave's keys of a tile
@@ -251,19 +260,24 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dq_kernel(const 
   bbm::store_strided<D>(dq, P->scale, stage, global(P->dq.p) + h * P->dq.head + (int64_t)(s.begin + wrow) * P->dq.row, wrows, P->dq.row, lane);
 }
 
-// Registers are what this form lives by.  D = 128: 256, two pieces of the K operand in LDS, two waves a SIMD; D = 64: 168, three.
 template <int D>
-__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dkv_kernel(const PromptBwdParams) {
-  Args P = bbm::kernel_args<PromptBwdParams>();
+__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dq_kernel(const PromptBwdParams) {
+  __shared__ __attribute__((aligned(16))) __bf16 t_s0[2 * TL<D>::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 t_s1[2 * TL<D>::ELEMS];
+  __shared__ float delta_s[4][32];
+  dq_of<D, 1, true>(bbm::kernel_args<PromptBwdParams>(), blockIdx.x, t_s0, t_s1, delta_s);
+}
+
+// Registers are what this form lives by.  D = 128: 256, two pieces of the K operand in LDS, two waves a SIMD; D = 64: 168, three.
+// t_s0, t_s1: [Q, dO] tiles, one variable per parity; st_s0, st_s1: [-lse / scale, -D] of the tile's queries; kl_s: the last pieces of the K operand, which find
+// no room in the registers.
+template <int D>
+constexpr int kPiecesInLds = D == 128 ? 2 : 0;
+template <int D>
+__device__ __forceinline__ void dkv_of(Args P, int wg, __bf16* t_s0, __bf16* t_s1, float* st_s0, float* st_s1, bf16x8 (*kl_s)[4][64]) {
   using L = TL<D>;
-  constexpr int NW = 4, KS = D / 16, DB = D / 32, REGS = DB * 16;
+  constexpr int NW = 4, KS = D / 16, DB = D / 32, REGS = DB * 16, KL = kPiecesInLds<D>;
   static_assert(2 * 32 * D <= L::ELEMS, "two 32 x D slabs must fit in a tile buffer");
-  __shared__ __attribute__((aligned(16))) __bf16 t_s0[2 * L::ELEMS];  // [Q, dO] tiles, one variable per parity
-  __shared__ __attribute__((aligned(16))) __bf16 t_s1[2 * L::ELEMS];
-  __shared__ __attribute__((aligned(16))) float st_s0[2 * 64];  // [-lse / scale, -D] of the tile's queries
-  __shared__ __attribute__((aligned(16))) float st_s1[2 * 64];
-  constexpr int KL = D == 128 ? 2 : 0;  // the last pieces of the K operand, which find no room in the registers
-  __shared__ __attribute__((aligned(16))) bf16x8 kl_s[KL ? KL : 1][NW][64];
 
   const int lane = threadIdx.x & 63;
   const int wave = (int)scalar(threadIdx.x >> 6);
@@ -271,7 +285,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dkv_kernel(const
   const int qh = wave >> 1;  // query half of a tile; behind the last one, 0: this wave writes dV, 1: dK
   const float rc = P->rc;
   const int parts = P->parts;
-  const bbm::Work work = bbm::work_of(blockIdx.x, P->H / P->G * parts);
+  const bbm::Work work = bbm::work_of(wg, P->H / P->G * parts);
   const int hk = work.plane / parts, part = work.plane - hk * parts;
   if (work.number >= P->key_pieces) return;
   const bbm::Span s = bbm::find_piece(global(P->cu), P->R, P->T, 1, 64, work.number);  // (early keys first: most queries see them)
@@ -492,6 +506,52 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dkv_kernel(const
     bbm::store_strided<D>(dk, P->scale, t_s0 + kh * 32 * D, global(P->dk.p) + hk * P->dk.head + (int64_t)(s.begin + row0) * P->dk.row, rows, P->dk.row, lane);
 }
 
+template <int D>
+__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dkv_kernel(const PromptBwdParams) {
+  __shared__ __attribute__((aligned(16))) __bf16 t_s0[2 * TL<D>::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 t_s1[2 * TL<D>::ELEMS];
+  __shared__ __attribute__((aligned(16))) float st_s0[2 * 64];
+  __shared__ __attribute__((aligned(16))) float st_s1[2 * 64];
+  __shared__ __attribute__((aligned(16))) bf16x8 kl_s[kPiecesInLds<D> ? kPiecesInLds<D> : 1][4][64];
+  dkv_of<D>(bbm::kernel_args<PromptBwdParams>(), blockIdx.x, t_s0, t_s1, st_s0, st_s1, kl_s);
+}
+
+// Short launches, which wait for the longest sequence: both gradients side by side, from statistics that a kernel of their own has left.
+template <int D>
+__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_both_kernel(const PromptBwdParams) {
+  Args P = bbm::kernel_args<PromptBwdParams>();
+  __shared__ __attribute__((aligned(16))) __bf16 t_s0[2 * TL<D>::ELEMS];
+  __shared__ __attribute__((aligned(16))) __bf16 t_s1[2 * TL<D>::ELEMS];
+  __shared__ __attribute__((aligned(16))) float st_s0[2 * 64];
+  __shared__ __attribute__((aligned(16))) float st_s1[2 * 64];
+  __shared__ __attribute__((aligned(16))) bf16x8 kl_s[kPiecesInLds<D> ? kPiecesInLds<D> : 1][4][64];
+  const int wg = blockIdx.x, keys = P->key_wgs;
+  if (wg < keys)
+    dkv_of<D>(P, wg, t_s0, t_s1, st_s0, st_s1, kl_s);
+  else
+    dq_of<D, 2, false>(P, wg - keys, t_s0, t_s1, nullptr);
+}
+
+// -lse / scale and -D of all rows, a row of a head for D / 8 lanes.  (Of rows of nobody too, from whatever they hold: nobody reads those.)
+template <int D>
+__global__ __launch_bounds__(256) void prompt_stats_kernel(const PromptBwdParams P) {
+  constexpr int RC = D / 8;
+  const int64_t at = (int64_t)blockIdx.x * (256 / RC) + threadIdx.x / RC;
+  const int t = (int)(at / P.H), h = (int)(at - (int64_t)t * P.H), chunk = threadIdx.x % RC;
+  if (t >= P.T) return;  // (whole rows)
+  const bf16x8 g = *reinterpret_cast<const bf16x8*>(P.d_o.p + h * P.d_o.head + (int64_t)t * P.d_o.row + chunk * 8);
+  const bf16x8 o = *reinterpret_cast<const bf16x8*>(P.o.p + h * P.o.head + (int64_t)t * P.o.row + chunk * 8);
+  const int64_t row_at = (int64_t)h * P.T + t;
+  const float lse = P.lse[row_at];
+  float x = 0.0f;
+  for (int e = 0; e < 8; ++e) x += (float)g[e] * (float)o[e];
+  x = bbm::row_sum<RC>(x);
+  if (chunk == 0) {
+    P.nls[row_at] = -lse / P.scale;
+    P.ndelta[row_at] = -x;
+  }
+}
+
 // Adds the parts of dK and dV up, in their order; eight elements of a row a thread.
 template <int D>
 __global__ __launch_bounds__(256) void prompt_sum_kernel(const PromptBwdParams P) {
@@ -568,13 +628,17 @@ extern "C" __attribute__((visibility("default"))) int bbm_prompt_attn_bwd(const 
   const int64_t row_pieces = count_pieces(T, R, 1, halves ? 64 : 128), key_pieces = count_pieces(T, R, 1, 64);
   const int64_t rows = work_groups(H, row_pieces), keys = work_groups(Hk * P.parts, key_pieces), sums = P.parts > 1 ? ceil_div(2 * Hk * T * (d / 8), 256) : 0;
   if (rows >= kMaxWgs || keys >= kMaxWgs || sums >= kMaxWgs) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld)", fn, (long long)T, (long long)H);
-  P.row_pieces = (int32_t)row_pieces, P.key_pieces = (int32_t)key_pieces;
+  P.row_pieces = (int32_t)row_pieces, P.key_pieces = (int32_t)key_pieces, P.key_wgs = (int32_t)keys;
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto go = [&](auto size) {
     constexpr int D = decltype(size)::value;
-    if (halves) prompt_dq_kernel<D, 2><<<(unsigned)rows, 256, 0, s>>>(P);
-    else prompt_dq_kernel<D, 1><<<(unsigned)rows, 256, 0, s>>>(P);
-    prompt_dkv_kernel<D><<<(unsigned)keys, 256, 0, s>>>(P);
+    if (halves) {
+      prompt_stats_kernel<D><<<(unsigned)ceil_div(T * H * (D / 8), 256), 256, 0, s>>>(P);
+      prompt_both_kernel<D><<<(unsigned)(rows + keys), 256, 0, s>>>(P);
+    } else {
+      prompt_dq_kernel<D><<<(unsigned)rows, 256, 0, s>>>(P);
+      prompt_dkv_kernel<D><<<(unsigned)keys, 256, 0, s>>>(P);
+    }
     if (P.parts > 1) prompt_sum_kernel<D><<<(unsigned)sums, 256, 0, s>>>(P);
   };
   if (d == 64) go(IntC<64>{});
