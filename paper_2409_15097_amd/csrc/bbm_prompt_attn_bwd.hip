@@ -2,17 +2,17 @@
 //
 // With P = exp(scale Q K^T - lse) on the pairs that are seen, dP = dO V^T, D_i = <dO_i, O_i>, dS = P o (dP - D):
 //   dV = P^T dO,   dK = scale * dS^T Q,   dQ = scale * dS K,   dK and dV summed over the heads of a group.
-// Two kernels, both without atomics, so that results do not depend on an order:
-//   dq kernel   a work-group takes 128 query rows of one head, a lane a row (HALVES: 64, two lanes a row, each with half the keys), and walks its tiles of
-//               64 keys: S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.  It leaves -D and -lse / scale in the workspace for the other one.
-//   dkv kernel  a work-group takes 64 keys of one key head and walks the tiles of 64 queries of every head of the group, a wave 32 keys and
+// Without atomics, so that results do not depend on an order.  One kernel leaves -D and -lse / scale in the workspace, one launch takes both gradients:
+//   dQ          a work-group takes 128 query rows of one head, a lane a row (HALVES: 64, two lanes a row, each with half the keys), and walks its tiles of
+//               64 keys: S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T;
+//   dK and dV   a work-group takes 64 keys of one key head and walks the tiles of 64 queries of every head of the group, a wave 32 keys and
 //               32 queries of a tile: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS, all in its registers.
 // Each step is one chain of matrix instructions with the copies of the next tile, the exponentials and the roundings behind them.  As in the forward
 // the scale multiplies the scores inside the exponential in fp32; P and dS are rounded to bf16 for the products that they enter, and D is formed from the
 // O that the forward rounded, which is the O that was used: <dO, O> as a program would form it.
-// Bound by the matrix instructions: sequences of 4096 and 3277 tokens, 32 / 8 heads of 128, dq 0.34 TFLOP (pairs that are seen) in 325 - 333 us, 1.0 PFLOP/s, dkv
-// 0.45 in 479 - 490, 0.93; with the scores and dP that both form, 9 products are multiplied where 7 would do (forward included).  Short sequences
-// by one chain of steps of 1 us: 13 of 1 to 1024, 16 heads of 64, 18.7 and 20.4 us.
+// Bound by the matrix instructions: sequences of 4096 and 3277 tokens, 32 / 8 heads of 128, forward and backward, 0.79 TFLOP (pairs that are seen) in 930 - 960 us;
+// with the scores and dP that dQ and dK, dV both form, 9 products are multiplied where 7 are counted, 1.06 PFLOP/s.  Short sequences by a chain of steps of
+// 0.5 to 1 us: 13 of 1 to 1024, 16 heads of 64, 34 us.
 #include "bbm_mfma.h"
 #include "bbm_prompt.h"
 
@@ -39,11 +39,11 @@ struct PromptBwdParams {
 typedef bbm::InPlace<PromptBwdParams> Args;
 
 // HALVES = 2: 64 rows a work-group, two waves share 32 of them and halve the keys of every tile, as in the forward.
-// t_s0, t_s1: [K, V] tiles, one variable per parity.  DELTA: forms -D and -lse / scale and leaves them in the workspace; else they are there.
-template <int D, int HALVES, bool DELTA>
-__device__ __forceinline__ void dq_of(Args P, int wg, __bf16* t_s0, __bf16* t_s1, float (*delta_s)[32]) {
+// t_s0, t_s1: [K, V] tiles, one variable per parity.
+template <int D, int HALVES>
+__device__ __forceinline__ void dq_of(Args P, int wg, __bf16* t_s0, __bf16* t_s1) {
   using L = TL<D>;
-  constexpr int NW = 4, BR = 32 * NW / HALVES, KB = 2 / HALVES, KS = D / 16, DB = D / 32, RC = D / 8, RPB = 64 / RC;
+  constexpr int NW = 4, BR = 32 * NW / HALVES, KB = 2 / HALVES, KS = D / 16, DB = D / 32;
   __bf16 *const k_s0 = t_s0, *const v_s0 = t_s0 + L::ELEMS, *const k_s1 = t_s1, *const v_s1 = t_s1 + L::ELEMS;
 
   const int lane = threadIdx.x & 63, lq = lane & 31, hh = lane >> 5;
@@ -74,7 +74,7 @@ __device__ __forceinline__ void dq_of(Args P, int wg, __bf16* t_s0, __bf16* t_s1
   };
   auto rows_at = [&](int jt) { return jt < n_tiles ? bbm::rows_of_tile(jt * 64, n) : 0; };
 
-  // This lane's query as operands, Q by way of the buffers of parity 1, dO through registers, where <dO, O> is formed, to the same place.
+  // This lane's query as operands, Q by way of the buffers of parity 1.
   TileAddr<D> A;
   A.init(lane);
   bf16x8 qf[KS], dof[KS];
@@ -85,54 +85,16 @@ __device__ __forceinline__ void dq_of(Args P, int wg, __bf16* t_s0, __bf16* t_s1
     bbm::copy_slab<D>(global(P->q.p) + h * P->q.head + t0 * P->q.row, wrows, P->q.row, stage, lane);
     const __amdgpu_buffer_rsrc_t do_r = buffer_of(global(P->d_o.p) + h * P->d_o.head + t0 * P->d_o.row, wrows > 0 ? ((wrows - 1) * P->d_o.row + D) * 2 : 0);
     const int64_t row_at = (int64_t)h * P->T + t0;
-    if constexpr (DELTA) {
-      const int g_row = lane / RC, g_chunk = lane % RC;
-      const __amdgpu_buffer_rsrc_t o_r = buffer_of(global(P->o.p) + h * P->o.head + t0 * P->o.row, wrows > 0 ? ((wrows - 1) * P->o.row + D) * 2 : 0);
-      const float lse = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer_of(P->lse + row_at, wrows * 4), lq * 4, 0, 0));
-      bf16x8 gr[32 / RPB], orow[32 / RPB];
+    const float nls = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer_of(P->nls + row_at, wrows * 4), lq * 4, 0, 0));
+    nd = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer_of(P->ndelta + row_at, wrows * 4), lq * 4, 0, 0));
 #pragma unroll
-      for (int i = 0; i < 32 / RPB; ++i) {
-        const int r = i * RPB + g_row;
-        gr[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(do_r, (r * P->d_o.row + g_chunk * 8) * 2, 0, 0));
-        orow[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(o_r, (r * P->o.row + g_chunk * 8) * 2, 0, 0));
-      }
+    for (int t = 0; t < KS; ++t) dof[t] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(do_r, (lq * P->d_o.row + 16 * t + 8 * hh) * 2, 0, 0));
 #pragma unroll
-      for (int i = 0; i < 2 * LPW; ++i) copy_piece(0, rows_at(0), k_s0, v_s0, i);
+    for (int i = 0; i < 2 * LPW; ++i) copy_piece(0, rows_at(0), k_s0, v_s0, i);
+    __builtin_amdgcn_s_waitcnt(0);
 #pragma unroll
-      for (int i = 0; i < 32 / RPB; ++i) {
-        float x = 0.0f;
-        for (int e = 0; e < 8; ++e) x += (float)gr[i][e] * (float)orow[i][e];
-        x = bbm::row_sum<RC>(x);
-        if (g_chunk == 0) delta_s[wave][i * RPB + g_row] = x;
-      }
-      __builtin_amdgcn_s_waitcnt(0);  // this wave's own copies have landed (no other wave touches its slab)
-#pragma unroll
-      for (int t = 0; t < KS; ++t) qf[t] = bbm::slab_frag<D>(stage, t, lane);
-#pragma unroll
-      for (int i = 0; i < 32 / RPB; ++i) {
-        const int r = i * RPB + g_row;
-        *reinterpret_cast<bf16x8*>(stage + r * D + (g_chunk ^ r % RC) * 8) = gr[i];
-      }
-#pragma unroll
-      for (int t = 0; t < KS; ++t) dof[t] = bbm::slab_frag<D>(stage, t, lane);
-      nl = -lse * kLog2e;
-      nd = -delta_s[wave][lq];
-      if (hh == 0 && half == 0) {
-        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(nl / rc), buffer_of(P->nls + row_at, wrows * 4), lq * 4, 0, 0);
-        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(nd), buffer_of(P->ndelta + row_at, wrows * 4), lq * 4, 0, 0);
-      }
-    } else {
-      const float nls = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer_of(P->nls + row_at, wrows * 4), lq * 4, 0, 0));
-      nd = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer_of(P->ndelta + row_at, wrows * 4), lq * 4, 0, 0));
-#pragma unroll
-      for (int t = 0; t < KS; ++t) dof[t] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(do_r, (lq * P->d_o.row + 16 * t + 8 * hh) * 2, 0, 0));
-#pragma unroll
-      for (int i = 0; i < 2 * LPW; ++i) copy_piece(0, rows_at(0), k_s0, v_s0, i);
-      __builtin_amdgcn_s_waitcnt(0);
-#pragma unroll
-      for (int t = 0; t < KS; ++t) qf[t] = bbm::slab_frag<D>(stage, t, lane);
-      nl = nls * rc;
-    }
+    for (int t = 0; t < KS; ++t) qf[t] = bbm::slab_frag<D>(stage, t, lane);
+    nl = nls * rc;
   }
   for (int i = 0; i < 2; ++i) {  // this wave's keys of a tile
     A.ra[i] += half * (32 / L::NBLK) * D;
@@ -258,14 +220,6 @@ __device__ __forceinline__ void dq_of(Args P, int wg, __bf16* t_s0, __bf16* t_s1
   if (wrows == 0) return;
   __bf16* const stage = (wave / 2 == 0 ? k_s0 : v_s0) + wave % 2 * 32 * D;
   bbm::store_strided<D>(dq, P->scale, stage, global(P->dq.p) + h * P->dq.head + (int64_t)(s.begin + wrow) * P->dq.row, wrows, P->dq.row, lane);
-}
-
-template <int D>
-__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dq_kernel(const PromptBwdParams) {
-  __shared__ __attribute__((aligned(16))) __bf16 t_s0[2 * TL<D>::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 t_s1[2 * TL<D>::ELEMS];
-  __shared__ float delta_s[4][32];
-  dq_of<D, 1, true>(bbm::kernel_args<PromptBwdParams>(), blockIdx.x, t_s0, t_s1, delta_s);
 }
 
 // Registers are what this form lives by.  D = 128: 256, two pieces of the K operand in LDS, two waves a SIMD; D = 64: 168, three.
@@ -506,18 +460,9 @@ __device__ __forceinline__ void dkv_of(Args P, int wg, __bf16* t_s0, __bf16* t_s
     bbm::store_strided<D>(dk, P->scale, t_s0 + kh * 32 * D, global(P->dk.p) + hk * P->dk.head + (int64_t)(s.begin + row0) * P->dk.row, rows, P->dk.row, lane);
 }
 
-template <int D>
-__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_dkv_kernel(const PromptBwdParams) {
-  __shared__ __attribute__((aligned(16))) __bf16 t_s0[2 * TL<D>::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 t_s1[2 * TL<D>::ELEMS];
-  __shared__ __attribute__((aligned(16))) float st_s0[2 * 64];
-  __shared__ __attribute__((aligned(16))) float st_s1[2 * 64];
-  __shared__ __attribute__((aligned(16))) bf16x8 kl_s[kPiecesInLds<D> ? kPiecesInLds<D> : 1][4][64];
-  dkv_of<D>(bbm::kernel_args<PromptBwdParams>(), blockIdx.x, t_s0, t_s1, st_s0, st_s1, kl_s);
-}
-
-// Short launches, which wait for the longest sequence: both gradients side by side, from statistics that a kernel of their own has left.
-template <int D>
+// Both gradients side by side, dK and dV, whose steps are longer, first.  One behind the other (the first one forming the statistics) / side by side, forward and
+// backward, us: 1 x 1024 tokens, 16 heads of 64, 42 / 36; 1 x 4096, 32 / 8 heads of 128, 669 / 605; 8 x 1024, 32 / 8 of 128, 321 / 308; but 300 x 100, 8 heads of 64, 103 / 109.
+template <int D, int HALVES>
 __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_both_kernel(const PromptBwdParams) {
   Args P = bbm::kernel_args<PromptBwdParams>();
   __shared__ __attribute__((aligned(16))) __bf16 t_s0[2 * TL<D>::ELEMS];
@@ -529,7 +474,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void prompt_both_kernel(cons
   if (wg < keys)
     dkv_of<D>(P, wg, t_s0, t_s1, st_s0, st_s1, kl_s);
   else
-    dq_of<D, 2, false>(P, wg - keys, t_s0, t_s1, nullptr);
+    dq_of<D, HALVES>(P, wg - keys, t_s0, t_s1);
 }
 
 // -lse / scale and -D of all rows, a row of a head for D / 8 lanes.  (Of rows of nobody too, from whatever they hold: nobody reads those.)
@@ -572,7 +517,7 @@ __global__ __launch_bounds__(256) void prompt_sum_kernel(const PromptBwdParams P
   *reinterpret_cast<bf16x8*>(to.p + hk * to.head + (int64_t)t * to.row + chunk * 8) = y;
 }
 
-// Parts of a group's heads that the dkv kernel takes side by side: one key head's walk over all heads of its group is as long as they are many, and a
+// Parts of a group's heads whose dK and dV are formed side by side: one key head's walk over all heads of its group is as long as they are many, and a
 // chip that is not full waits for it.  Worth the fp32 sums in memory where the walk is long.  Forward and backward, one / several parts, us: 1 x 1024
 // tokens, 8 / 2 heads of 128, 104 / 78; 1 x 4096, 8 / 2 of 64, 230 / 158; 1 x 2048, 32 / 8 of 128, 255 / 220; but 8 x 300, 16 / 4 of 64, 46 / 51.
 constexpr int64_t kDkvWgs = 512, kLongWalk = 2048;  // work-groups, two a CU; queries of all heads of a group
@@ -626,19 +571,15 @@ extern "C" __attribute__((visibility("default"))) int bbm_prompt_attn_bwd(const 
   P.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * stats_bytes(T, H));
   const bool halves = split_keys(T, R, H);
   const int64_t row_pieces = count_pieces(T, R, 1, halves ? 64 : 128), key_pieces = count_pieces(T, R, 1, 64);
-  const int64_t rows = work_groups(H, row_pieces), keys = work_groups(Hk * P.parts, key_pieces), sums = P.parts > 1 ? ceil_div(2 * Hk * T * (d / 8), 256) : 0;
-  if (rows >= kMaxWgs || keys >= kMaxWgs || sums >= kMaxWgs) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld)", fn, (long long)T, (long long)H);
+  const int64_t rows = work_groups(H, row_pieces), keys = work_groups(Hk * P.parts, key_pieces), sums = P.parts > 1 ? ceil_div(2 * Hk * T * (d / 8), 256) : 0, stats = ceil_div(T * H * (d / 8), 256);
+  if (rows + keys >= kMaxWgs || stats >= kMaxWgs || sums >= kMaxWgs) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld)", fn, (long long)T, (long long)H);
   P.row_pieces = (int32_t)row_pieces, P.key_pieces = (int32_t)key_pieces, P.key_wgs = (int32_t)keys;
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto go = [&](auto size) {
     constexpr int D = decltype(size)::value;
-    if (halves) {
-      prompt_stats_kernel<D><<<(unsigned)ceil_div(T * H * (D / 8), 256), 256, 0, s>>>(P);
-      prompt_both_kernel<D><<<(unsigned)(rows + keys), 256, 0, s>>>(P);
-    } else {
-      prompt_dq_kernel<D><<<(unsigned)rows, 256, 0, s>>>(P);
-      prompt_dkv_kernel<D><<<(unsigned)keys, 256, 0, s>>>(P);
-    }
+    prompt_stats_kernel<D><<<(unsigned)stats, 256, 0, s>>>(P);
+    if (halves) prompt_both_kernel<D, 2><<<(unsigned)(rows + keys), 256, 0, s>>>(P);
+    else prompt_both_kernel<D, 1><<<(unsigned)(rows + keys), 256, 0, s>>>(P);
     if (P.parts > 1) prompt_sum_kernel<D><<<(unsigned)sums, 256, 0, s>>>(P);
   };
   if (d == 64) go(IntC<64>{});
