@@ -34,9 +34,9 @@ __device__ __forceinline__ Work work_of(int wg, int planes) {
 inline int64_t work_groups(int64_t planes, int64_t pieces) { return 8 * planes * ceil_div(pieces, 8); }
 
 // With few pieces the longest sequence is what a launch waits for: two waves then share the keys of every tile (HALVES of the kernels), which makes twice as
-// many work-groups of steps half as long.  Whole / halved, us, both directions: 1 x 1024 tokens, 8 / 2 heads of 128 (64 pieces of 128 rows), 77 / 64; 13 packed
-// sequences of 213 on average, 16 heads of 64 (352), 62 / 55; but 3 x 867, 24 / 8 heads of 128 (504), 129 / 136; forward alone: 37 sequences of 59,
-// 16 heads (288), 10.5 / 12.0; 1 x 4096, 32 heads of 128 (1024), 153 / 179.
+// many work-groups of steps half as long.  Whole / halved, us, a training step with the backward pass either way: 13 packed sequences of 213 on average, 16 heads of
+// 64 (352 pieces of 128 rows), 54 / 50; 1 x 2048, 16 heads of 64 (256), 74 / 67; but 4096 and 3277, 32 / 8 heads of 128 (1856), 962 / 989; 200 x 22, 8 / 2 of 128, 59 / 61.
+// Forward alone: 37 sequences of 59, 16 heads of 64 (288), 10.5 / 12.0; 1 x 4096, 32 heads of 128 (1024), 153 / 179.
 inline bool split_keys(int64_t T, int64_t R, int64_t H) { return ceil_div(T, 128) * H <= 384 && T >= 128 * R; }
 
 // Asynchronous copies of up to 64 strided rows to a tile in LDS (layout TL), NBLK / NW instructions a wave; rows from `rows` on come as zeros.

@@ -519,8 +519,9 @@ __global__ __launch_bounds__(256) void prompt_sum_kernel(const PromptBwdParams P
 
 // Parts of a group's heads whose dK and dV are formed side by side: one key head's walk over all heads of its group is as long as they are many, and a
 // chip that is not full waits for it.  Worth the fp32 sums in memory where the walk is long.  Forward and backward, one / several parts, us: 1 x 1024
-// tokens, 8 / 2 heads of 128, 104 / 78; 1 x 4096, 8 / 2 of 64, 230 / 158; 1 x 2048, 32 / 8 of 128, 255 / 220; but 8 x 300, 16 / 4 of 64, 46 / 51.
-constexpr int64_t kDkvWgs = 512, kLongWalk = 2048;  // work-groups, two a CU; queries of all heads of a group
+// tokens, 8 / 2 heads of 128, 90 / 53; 1 x 4096, 8 / 2 of 64, 237 / 126; 1 x 2048, 32 / 8 of 128, 221 / 198; 12 x 214 on average and 1000 at most, 12 / 4 of 128, 85 / 76;
+// 6 x 125, 8 / 1 of 64, 30 / 21; but 8 x 248, 16 / 4 of 128, 52 / 60; 30 x 81, 8 / 2 of 64, 23 / 29 (not cut up).
+constexpr int64_t kDkvWgs = 512, kLongWalk = 512;  // work-groups, two a CU; queries of all heads of a group
 inline int64_t head_parts(int64_t T, int64_t R, int64_t H, int64_t Hk) {
   if (H / Hk * T < kLongWalk * R) return 1;
   return std::min(H / Hk, std::max<int64_t>(1, kDkvWgs / (bbm::ceil_div(T, 64) * Hk)));
