@@ -114,7 +114,7 @@ int bbm_kv4_read(const int32_t* slots, int64_t T, const bbm_kv4_cache* cache, co
                  void* stream);
 
 /*
- * Attention of new tokens over the cache.  Request r has lens[r] keys in it, the n = cu[r+1] - cu[r] new tokens' the last of
+ * Attention of new tokens over the cache.  Request r has lens[r] keys in it, the n = cu[r+1] - cu[r] new tokens' (rows outside 0 .. T counted) the last of
  * them; key p lies on page block_table[r * table_stride + p / page].  Query i of the request sees the keys 0 .. lens[r] - n + i,
  * or, with `mask`, keys 0 .. lens[r] - n - 1 and new key j where bit j % 64 of mask[t * mask_words + j / 64] is set (t the query's
  * row; bits from n or 64 * mask_words on count as not set).  Keys on a page outside the cache (-1) or behind max_pages * page are not seen.  A query that sees no

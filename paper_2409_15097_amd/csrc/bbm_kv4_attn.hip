@@ -45,16 +45,17 @@ struct Kv4AttnParams {
 struct Piece {
   bbm::Span s;
   int cols, col0;    // columns of the request; the piece's first
-  int len, prefix;   // keys that can be seen at all; keys in front of the new tokens
+  int len, prefix;   // keys that can be seen at all; keys in front of the new tokens (causal: of the first one that has a row here)
   int parts, keys;   // parts of this request, keys of one
 };
 __device__ __forceinline__ Piece piece_of(const Kv4AttnParams& P, int number, int width) {
   Piece x;
   x.s = bbm::find_piece(P.cu, P.R, P.T, P.G, width, number);
   const int n = x.s.end - x.s.begin, len = (int)scalar(P.lens[x.s.r]);
+  const int c0 = (int)scalar(P.cu[x.s.r]), c1 = (int)scalar(P.cu[x.s.r + 1]);  // (rows outside 0 .. T are not here, but their tokens are in the cache)
   x.cols = n * P.G;
   x.col0 = x.s.piece * width;
-  x.prefix = len - n;
+  x.prefix = (int)((uint32_t)len - (uint32_t)max(0, c1 - c0) + (P.mask ? 0u : (uint32_t)x.s.begin - (uint32_t)c0));
   x.len = (int)max((int64_t)0, min((int64_t)len, (int64_t)P.max_pages << P.c.page_shift));
   x.keys = max(P.part_keys, (int)(((int64_t)x.len + P.parts - 1) / P.parts + kStep - 1) / kStep * kStep);
   x.parts = x.len > 0 ? (x.len - 1) / x.keys + 1 : 1;

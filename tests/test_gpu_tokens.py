@@ -322,24 +322,23 @@ def check_cached(bbm, c, table, lens, cu, T, q, words, H, Hk, d, page, **kw):
     out, lse = torch.full((T, H, d), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((H, T), 7.0, device="cuda")
     bbm.bbm_kv4_attn(q, c, i32(table), i32(lens), i32(cu), mask=None if words is None else torch.from_numpy(words).cuda(), out=out, lse=lse, **kw)
     real = np.zeros(T, bool)
-    real[cu[0]:cu[-1]] = True
+    real[max(0, cu[0]):cu[-1]] = True
     assert (f64(out)[~real] == 7.0).all() and (f64(lse)[:, ~real] == 7.0).all()
     hk, hv = host_cache(c)
     nq, G = f64(q), H // Hk
     for r, n in enumerate(lens):
-        a, b = int(cu[r]), int(cu[r + 1])
-        new = b - a
-        if not new:
+        a, b, new = max(0, int(cu[r])), min(T, int(cu[r + 1])), int(cu[r + 1] - cu[r])
+        if b <= a:
             continue
         m = min(max(n, 0), table.shape[1] * page)
         pg = table[r, np.arange(m) // page]
         ok = (pg >= 0) & (pg < c.k.shape[0])
-        j, i = np.arange(m), np.arange(new)[:, None]
+        j, i = np.arange(m), np.arange(a, b)[:, None] - int(cu[r])
         if words is None:
             seen = (j <= n - new + i) & ok
         else:
             nj = j - (n - new)
-            bit = np.zeros((new, m), bool)
+            bit = np.zeros((b - a, m), bool)
             inside = (nj >= 0) & (nj < 64 * words.shape[1])
             bit[:, inside] = (words[a:b][:, nj[inside] // 64] >> (nj[inside] % 64)) & 1 != 0
             seen = ((nj < 0) | bit) & ok
@@ -373,6 +372,15 @@ def test_cached_pages_outside_and_a_narrow_table(bbm):
     check_cached(bbm, c, table, lens, cu, T, q, None, H, Hk, d, page)
     check_cached(bbm, c, table[:, :5], lens, cu, T, q, None, H, Hk, d, page)
     check_cached(bbm, c, table[:, :5], [700, -4, 1 << 30], cu, T, q, None, H, Hk, d, page)
+
+
+@pytest.mark.parametrize("H, lens, news, tree", [(4, [300, 90, 70], [40, 30, 60], None), (4, [300, 90, 70], [40, 30, 60], 1), (40, [700, 900, 700], [240, 230, 260], None)])
+@pytest.mark.parametrize("front, rows", [(0, 3), (17, 5)])
+def test_cached_rows_that_are_not_there(bbm, H, lens, news, tree, front, rows):
+    """Offsets that begin in front of the first row or end behind the last: the tokens without a row are in the cache all the same."""
+    c, table, cu, T, q, words = cached_case(bbm, lens, news, H, 2, 64, 32, seed=11, tree=tree)
+    a, b = front, news[0] + news[1] + rows
+    check_cached(bbm, c, table, lens, cu - a, b - a, q[a:b].contiguous(), None if words is None else words[a:b].copy(), H, 2, 64, 32)
 
 
 @pytest.mark.parametrize("max_len", [1, 300, 5000, 1 << 40])
