@@ -11,7 +11,7 @@
  * operator writes them (bbm_build_slots and bbm_kv4_read, which write all T rows, say what they write there).  Offsets outside
  * 0 .. T are cut to that range.
  *
- * Unless a function says otherwise, outputs overlap neither inputs nor each other.  What rows of nobody hold does not matter (it may be
+ * Unless a function says otherwise, outputs overlap neither inputs nor each other (the same pointer is refused).  What rows of nobody hold does not matter (it may be
  * an infinity or a NaN); the rows of requests are taken to be finite, as are the cache's groups: an infinity or a NaN among them may reach any
  * row of its own request.  Scores are fp32 numbers: a softmax_scale lies within 2^-100 .. 2^100, and sums of products of q and k stay within fp32's range.
  *

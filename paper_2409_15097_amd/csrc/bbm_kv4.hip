@@ -112,6 +112,7 @@ int kv4_move(const char* fn, const bbm_packed* k, const bbm_packed* v, int64_t T
   const int64_t per_token = cache->Hk * (cache->d / 8), items = T > kMaxTokens ? 1ll << 40 : T * per_token;
   if (items > 0x7fffff00ll) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, Hk=%lld)", fn, (long long)T, (long long)cache->Hk);
   if (T == 0) return BBM_OK;
+  if (!write && k->ptr == v->ptr) return fail(BBM_EINVAL, "%s: two outputs must not be the same", fn);
   Kv4Params P;
   P.c = kv4_of(cache);
   P.k = static_cast<__bf16*>(k->ptr), P.v = static_cast<__bf16*>(v->ptr);

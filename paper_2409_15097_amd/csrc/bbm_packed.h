@@ -3,6 +3,8 @@
 #include "bbm_internal.h"
 #include "bbm_tokens.h"
 
+#include <initializer_list>
+
 namespace bbm {
 
 constexpr int64_t kMaxTokens = 1ll << 30;
@@ -23,6 +25,17 @@ inline int check_packed(const char* fn, const char* name, const bbm_packed* x, i
     const int64_t outer = rows_first ? x->row_stride : x->head_stride, n_outer = rows_first ? rows : heads;
     if ((n_inner > 1 && inner < d) || (n_outer > 1 && outer < (n_inner > 1 ? (n_inner - 1) * inner : 0) + d))
       return fail(BBM_EINVAL, "%s: rows or heads of %s overlap (strides %lld, %lld)", fn, name, (long long)x->row_stride, (long long)x->head_stride);
+  }
+  return BBM_OK;
+}
+
+// The overlap that a caller is most likely to ask for: an output in the place of an input or of another output.
+inline int check_apart(const char* fn, std::initializer_list<const bbm_packed*> outputs, std::initializer_list<const bbm_packed*> inputs) {
+  for (auto a = outputs.begin(); a != outputs.end(); ++a) {
+    for (const bbm_packed* x : inputs)
+      if (x->ptr == (*a)->ptr) return fail(BBM_EINVAL, "%s: an output must not be an input", fn);
+    for (auto b = outputs.begin(); b != a; ++b)
+      if ((*b)->ptr == (*a)->ptr) return fail(BBM_EINVAL, "%s: two outputs must not be the same", fn);
   }
   return BBM_OK;
 }

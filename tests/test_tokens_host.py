@@ -70,6 +70,8 @@ def test_rope_refuses(bbm):
     for kw in (dict(d=72, rot=2), dict(d=528), dict(d=0), dict(T=1 << 31), dict(q=pk(row=(1 << 22) + 8)), dict(T=1 << 30)):
         assert rope(bbm, **kw) == bbm.BBM_EUNSUPPORTED, kw
     assert rope(bbm, T=0) == bbm.BBM_OK
+    for kw in (dict(k=pk(2 * P)), dict(ko=pk(2 * P)), dict(q=pk(2 * P), qo=pk(2 * P), k=pk(3 * P), ko=pk(2 * P))):
+        assert rope(bbm, **kw) == bbm.BBM_EINVAL, kw
 
 
 def fwd(bbm, q=pk, k=pk, v=pk, o=pk, lse=P, T=3, R=2, cu=P, H=4, Hk=2, d=64, scale=0.125):
@@ -95,6 +97,10 @@ def test_prompt_attention_refuses(bbm):
         assert call(bbm, T=0) == bbm.BBM_OK
     for bad in OVERLAP:
         assert fwd(bbm, o=pk(**bad)) == bbm.BBM_EINVAL and bwd(bbm, dk=pk(**bad)) == bbm.BBM_EINVAL
+    apart = {n: pk((i + 1) * P) for i, n in enumerate(("q", "k", "v", "o", "d_o", "dq", "dk", "dv"))}
+    for out, other in (("dq", "q"), ("dk", "k"), ("dv", "d_o"), ("dv", "dk")):
+        assert bwd(bbm, **apart | {out: apart[other]}) == bbm.BBM_EINVAL
+    assert fwd(bbm, k=pk(2 * P), v=pk(3 * P)) == bbm.BBM_EINVAL and fwd(bbm, q=pk(2 * P), v=pk(3 * P)) == bbm.BBM_EINVAL
     assert bwd(bbm, lse=None) == bbm.BBM_EINVAL and bwd(bbm, ws=P + 8) == bbm.BBM_EINVAL
     assert bbm.bbm_prompt_attn_bwd_workspace_bytes(0, 1, 4, 2, 64) == 0 and bbm.bbm_prompt_attn_bwd_workspace_bytes(3, 1, 4, 3, 64) == 0
     need = bbm.bbm_prompt_attn_bwd_workspace_bytes(3, 2, 4, 2, 64)
@@ -135,7 +141,7 @@ def test_cache_refuses(bbm):
         assert attn(bbm, **kw) == bbm.BBM_EINVAL, kw
     for kw in (dict(T=1 << 31), dict(T=1 << 30), dict(scale=2.0 ** -101), dict(width=(1 << 24) + 1, stride=1 << 26), dict(mask=P, words=(1 << 20) + 1)):
         assert attn(bbm, **kw) == bbm.BBM_EUNSUPPORTED, kw
-    assert attn(bbm, T=0) == bbm.BBM_OK
+    assert attn(bbm, T=0) == bbm.BBM_OK and attn(bbm) == bbm.BBM_EINVAL and bbm.lib.bbm_kv4_read(P, 3, cache(), pk(), pk(), None) == bbm.BBM_EINVAL
     need = bbm.bbm_kv4_attn_workspace_bytes(1, 1, 8, 1, 128, 1 << 16)
     long = dict(T=1, R=1, H=8, c=cache(Hk=1, d=128), max_len=1 << 16)
     assert need > 0 and attn(bbm, **long, ws_bytes=need - 1) == bbm.BBM_EWORKSPACE and attn(bbm, **long, ws=None) == bbm.BBM_EWORKSPACE
