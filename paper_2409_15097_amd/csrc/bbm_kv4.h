@@ -18,7 +18,8 @@ inline int check_kv4(const char* fn, const bbm_kv4_cache* c) {
   if (c->pages < 1 || c->Hk < 1) return fail(BBM_EINVAL, "%s: pages=%lld, Hk=%lld must be >= 1", fn, (long long)c->pages, (long long)c->Hk);
   if (c->d != 64 && c->d != 128) return fail(BBM_EUNSUPPORTED, "%s: d=%d has no kernel instance (64, 128)", fn, c->d);
   if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return fail(BBM_EUNSUPPORTED, "%s: page=%d is none of 16, 32, 64, 128", fn, c->page);
-  if (c->pages * c->page >= (1ll << 31) || c->Hk > 65535) return fail(BBM_EUNSUPPORTED, "%s: cache too large (%lld pages of %d, %lld heads)", fn, (long long)c->pages, c->page, (long long)c->Hk);
+  if (c->pages > 0x7fffffffll / c->page || c->Hk > 65535)  // (by division: a product of the caller's may wrap)
+    return fail(BBM_EUNSUPPORTED, "%s: cache too large (%lld pages of %d, %lld heads)", fn, (long long)c->pages, c->page, (long long)c->Hk);
   return BBM_OK;
 }
 inline Kv4 kv4_of(const bbm_kv4_cache* c) {

@@ -106,11 +106,12 @@ int kv4_move(const char* fn, const bbm_packed* k, const bbm_packed* v, int64_t T
   clear_error();
   if (int rc = check_kv4(fn, cache)) return rc;
   if (T < 0) return fail(BBM_EINVAL, "%s: T=%lld must be >= 0", fn, (long long)T);
+  const int64_t per_token = cache->Hk * (cache->d / 8);
+  if (T > 0x7fffff00ll / per_token) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, Hk=%lld)", fn, (long long)T, (long long)cache->Hk);
   if (int rc = check_packed(fn, "k", k, T, cache->Hk, cache->d, !write)) return rc;
   if (int rc = check_packed(fn, "v", v, T, cache->Hk, cache->d, !write)) return rc;
   if ((T > 0 && !slots) || !aligned(slots, 4)) return fail(BBM_EINVAL, "%s: slots must be a non-NULL 4-byte aligned pointer", fn);
-  const int64_t per_token = cache->Hk * (cache->d / 8), items = T > kMaxTokens ? 1ll << 40 : T * per_token;
-  if (items > 0x7fffff00ll) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, Hk=%lld)", fn, (long long)T, (long long)cache->Hk);
+  const int64_t items = T * per_token;
   if (T == 0) return BBM_OK;
   if (!write && k->ptr == v->ptr) return fail(BBM_EINVAL, "%s: two outputs must not be the same", fn);
   Kv4Params P;

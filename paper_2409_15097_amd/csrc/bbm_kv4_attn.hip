@@ -621,7 +621,7 @@ extern "C" __attribute__((visibility("default"))) int bbm_kv4_attn(const bbm_pac
     return fail(BBM_EINVAL, "%s: max_pages=%lld, max_len=%lld must be >= 1, table_stride=%lld no less than max_pages", fn, (long long)max_pages, (long long)max_len, (long long)table_stride);
   if (mask ? mask_words < 1 : mask_words != 0) return fail(BBM_EINVAL, "%s: mask_words=%lld does not fit the mask", fn, (long long)mask_words);
   if (T * (H / cache->Hk) > kMaxTokens) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld)", fn, (long long)T, (long long)H);
-  if (max_pages * cache->page > kMaxTokens || mask_words > (1 << 20)) return fail(BBM_EUNSUPPORTED, "%s: max_pages=%lld or mask_words=%lld is too large", fn, (long long)max_pages, (long long)mask_words);
+  if (max_pages > kMaxTokens / cache->page || mask_words > (1 << 20)) return fail(BBM_EUNSUPPORTED, "%s: max_pages=%lld or mask_words=%lld is too large", fn, (long long)max_pages, (long long)mask_words);
   if (int rc = check_scale(fn, softmax_scale)) return rc;
   const size_t need = bbm_kv4_attn_workspace_bytes(T, R, H, cache->Hk, cache->d, max_len);
   if (need > 0 && (!workspace || workspace_bytes < need))

@@ -147,7 +147,7 @@ extern "C" __attribute__((visibility("default"))) int bbm_rope(const bbm_packed*
   if (T < 0 || H < 1 || Hk < 0) return fail(BBM_EINVAL, "%s: T=%lld, Hk=%lld must be >= 0, H=%lld >= 1", fn, (long long)T, (long long)Hk, (long long)H);
   if (d < 16 || d > 512 || d % 16) return fail(BBM_EUNSUPPORTED, "%s: d=%d is no multiple of 16 up to 512", fn, d);
   if (rot < 2 || rot > d || rot % 2) return fail(BBM_EINVAL, "%s: rot=%d must be even, 2 .. d=%d", fn, rot, d);
-  if (T > kMaxTokens || H + Hk > 65535) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld, Hk=%lld)", fn, (long long)T, (long long)H, (long long)Hk);
+  if (T > kMaxTokens || H > 65535 || Hk > 65535 - H) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld, Hk=%lld)", fn, (long long)T, (long long)H, (long long)Hk);
   if (T > 0 && (!positions || !freqs)) return fail(BBM_EINVAL, "%s: positions and freqs must not be NULL", fn);
   if (!aligned(positions, 4) || !aligned(freqs, 4)) return fail(BBM_EINVAL, "%s: positions and freqs must be 4-byte aligned", fn);
   if (!(mscale > -INFINITY && mscale < INFINITY)) return fail(BBM_EINVAL, "%s: mscale must be finite", fn);

@@ -129,7 +129,8 @@ extern "C" __attribute__((visibility("default"))) int bbm_build_slots(const int3
   if (table_stride < max_pages) return fail(BBM_EINVAL, "%s: table_stride=%lld is less than max_pages=%lld", fn, (long long)table_stride, (long long)max_pages);
   if (page != 16 && page != 32 && page != 64 && page != 128) return fail(BBM_EUNSUPPORTED, "%s: page=%d is none of 16, 32, 64, 128", fn, page);
   if (R > BBM_SLOTS_MAX_REQUESTS) return fail(BBM_EUNSUPPORTED, "%s: R=%lld requests, more than %d", fn, (long long)R, BBM_SLOTS_MAX_REQUESTS);
-  if (T > kMaxTokens || R * max_pages >= (1ll << 31)) return fail(BBM_EUNSUPPORTED, "%s: T=%lld or R * max_pages=%lld is too large", fn, (long long)T, (long long)(R * max_pages));
+  if (T > kMaxTokens || max_pages > 0x7fffffffll / R)  // (by division: a product of the caller's may wrap)
+    return fail(BBM_EUNSUPPORTED, "%s: T=%lld or R=%lld times max_pages=%lld is too large", fn, (long long)T, (long long)R, (long long)max_pages);
   SlotParams P;
   P.ctx = ctx_lens, P.add = new_lens, P.table = block_table, P.free_pages = free_pages, P.free_at = free_at;
   P.cu = cu_new, P.lens = lens, P.positions = positions, P.slots = slots, P.free_next = free_next;

@@ -202,3 +202,21 @@ def test_oracle_of_the_cache_format():
     assert s[0, 0] == 127 and list(ot.kv4_decode(c, s)[0, :12]) == [0, 1, 1, 2, 2, 4, 4, 6, -0.5, -6, 6, 0.5]
     x[0, 7] = 7.01
     assert ot.kv4_encode(x)[1][0, 0] == 128
+
+
+APART = {n: pk((i + 20) * P) for i, n in enumerate(("q", "qo", "k", "ko", "v", "o"))}
+
+
+def test_refuses_sizes_whose_product_wraps(bbm):
+    """Products of two arguments that pass 2^64 and come out small are refused like those just above a limit."""
+    for kw in (dict(R=16384, width=1 << 50, stride=1 << 50), dict(R=4, width=1 << 62, stride=1 << 62), dict(R=16384, width=1 << 17, stride=1 << 17)):
+        assert slots(bbm, ctx=11 * P, new=12 * P, table=13 * P, free=14 * P, at=15 * P, **kw) == bbm.BBM_EUNSUPPORTED, kw
+    for kw in (dict(width=1 << 58, stride=1 << 58), dict(c=cache(pages=1 << 58)), dict(c=cache(pages=1 << 57, page=128)), dict(c=cache(pages=(1 << 60) + 1, page=16)),
+               dict(c=cache(Hk=1 << 62), H=1 << 62)):
+        assert attn(bbm, q=APART["q"], o=APART["o"], **kw) == bbm.BBM_EUNSUPPORTED, kw
+    a = APART
+    for pages, T in ((1 << 58, 3), (8, 1 << 62), (8, (1 << 63) - 1)):
+        assert bbm.lib.bbm_kv4_append(a["k"], a["v"], T, P, cache(pages=pages), None) == bbm.BBM_EUNSUPPORTED
+        assert bbm.lib.bbm_kv4_read(P, T, cache(pages=pages), a["k"], a["v"], None) == bbm.BBM_EUNSUPPORTED
+    for H, Hk in ((1 << 62, 1 << 62), ((1 << 63) - 1, 2), (65535, 1), (1, 65535)):
+        assert rope(bbm, **{n: a[n] for n in ("q", "qo", "k", "ko")}, H=H, Hk=Hk) == bbm.BBM_EUNSUPPORTED, (H, Hk)
