@@ -11,9 +11,9 @@
  * operator writes them (bbm_build_slots and bbm_kv4_read, which write all T rows, say what they write there).  Offsets outside
  * 0 .. T are cut to that range.
  *
- * Unless a function says otherwise, outputs overlap neither inputs nor each other (the same pointer is refused).  What rows of nobody hold does not matter (it may be
- * an infinity or a NaN); the rows of requests are taken to be finite, as are the cache's groups: an infinity or a NaN among them may reach any
- * row of its own request.  Scores are fp32 numbers: a softmax_scale lies within 2^-100 .. 2^100, and sums of products of q and k stay within fp32's range.
+ * Unless a function says otherwise, outputs and workspaces overlap neither inputs nor each other (the same pointer is refused).  What rows
+ * of nobody hold does not matter (it may be an infinity or a NaN); the rows of requests are taken to be finite, as are the cache's groups: an
+ * infinity or a NaN among them may reach any row of its own request.  Scores are fp32 numbers: a softmax_scale lies within 2^-100 .. 2^100, and sums of products of q and k stay within fp32's range.
  *
  * A packed tensor is bf16 [T][heads][d] with any row and head strides (in elements, multiples of 8; the d elements of a head
  * are contiguous and 16-byte aligned), so the q, k and v parts of one projection's output, or [heads][T][d], need no copy.
@@ -44,8 +44,8 @@ typedef struct bbm_packed {
  *   positions [T], slots [T] of every new token; slot -1 where it has no page.  Rows from cu_new[R] on: position 0, slot -1.
  *                            Of more than T new tokens the first T are written.
  *   free_next [1]            *free_at + the pages asked for; beyond n_free, the list was too short
- * Nothing but block_table may overlap an input, and of it only entries behind a request's last page are written, so that a call
- * may be repeated.  1 <= R <= BBM_SLOTS_MAX_REQUESTS; page 16, 32, 64 or 128; totals fit 31 bits.
+ * block_table is read and written, but only entries behind a request's last page are written, so that a call may be repeated.
+ * 1 <= R <= BBM_SLOTS_MAX_REQUESTS; page 16, 32, 64 or 128; totals fit 31 bits.
  */
 #define BBM_SLOTS_MAX_REQUESTS 16384
 int bbm_build_slots(const int32_t* ctx_lens, const int32_t* new_lens, int64_t R, int32_t* block_table, int64_t table_stride,

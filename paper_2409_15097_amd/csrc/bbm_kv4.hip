@@ -113,7 +113,9 @@ int kv4_move(const char* fn, const bbm_packed* k, const bbm_packed* v, int64_t T
   if ((T > 0 && !slots) || !aligned(slots, 4)) return fail(BBM_EINVAL, "%s: slots must be a non-NULL 4-byte aligned pointer", fn);
   const int64_t items = T * per_token;
   if (T == 0) return BBM_OK;
-  if (!write && k->ptr == v->ptr) return fail(BBM_EINVAL, "%s: two outputs must not be the same", fn);
+  const bbm_kv4_cache& c = *cache;
+  if (int rc = write ? check_apart(fn, {c.k, c.k_scale, c.v, c.v_scale}, {k->ptr, v->ptr, slots}) : check_apart(fn, {k->ptr, v->ptr}, {slots, c.k, c.k_scale, c.v, c.v_scale}))
+    return rc;
   Kv4Params P;
   P.c = kv4_of(cache);
   P.k = static_cast<__bf16*>(k->ptr), P.v = static_cast<__bf16*>(v->ptr);

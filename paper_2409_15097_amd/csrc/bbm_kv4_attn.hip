@@ -628,7 +628,7 @@ extern "C" __attribute__((visibility("default"))) int bbm_kv4_attn(const bbm_pac
     return fail(BBM_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, workspace ? workspace_bytes : (size_t)0);
   if (!aligned(workspace, 16)) return fail(BBM_EINVAL, "%s: workspace must be 16-byte aligned", fn);
   if (T == 0) return BBM_OK;
-  if (int rc = check_apart(fn, {o}, {q})) return rc;
+  if (int rc = check_apart(fn, {o->ptr, lse, need > 0 ? workspace : nullptr}, {q->ptr, cu, lens, block_table, mask, cache->k, cache->k_scale, cache->v, cache->v_scale})) return rc;
   Kv4AttnParams P;
   P.c = kv4_of(cache);
   P.q = static_cast<const __bf16*>(q->ptr), P.o = static_cast<__bf16*>(o->ptr), P.lse = lse;

@@ -29,13 +29,14 @@ inline int check_packed(const char* fn, const char* name, const bbm_packed* x, i
   return BBM_OK;
 }
 
-// The overlap that a caller is most likely to ask for: an output in the place of an input or of another output.
-inline int check_apart(const char* fn, std::initializer_list<const bbm_packed*> outputs, std::initializer_list<const bbm_packed*> inputs) {
+// The overlap that a caller is most likely to ask for: an output (or a workspace) in the place of an input or of another output.  NULL: not there.
+inline int check_apart(const char* fn, std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs) {
   for (auto a = outputs.begin(); a != outputs.end(); ++a) {
-    for (const bbm_packed* x : inputs)
-      if (x->ptr == (*a)->ptr) return fail(BBM_EINVAL, "%s: an output must not be an input", fn);
+    if (!*a) continue;
+    for (const void* x : inputs)
+      if (x == *a) return fail(BBM_EINVAL, "%s: an output must not be an input", fn);
     for (auto b = outputs.begin(); b != a; ++b)
-      if ((*b)->ptr == (*a)->ptr) return fail(BBM_EINVAL, "%s: two outputs must not be the same", fn);
+      if (*b == *a) return fail(BBM_EINVAL, "%s: two outputs must not be the same", fn);
   }
   return BBM_OK;
 }

@@ -235,7 +235,7 @@ extern "C" __attribute__((visibility("default"))) int bbm_prompt_attn_fwd(const 
   if (!aligned(lse, 4)) return fail(BBM_EINVAL, "%s: lse must be 4-byte aligned", fn);
   if (int rc = check_scale(fn, softmax_scale)) return rc;
   if (T == 0) return BBM_OK;
-  if (int rc = check_apart(fn, {o}, {q, k, v})) return rc;
+  if (int rc = check_apart(fn, {o->ptr, lse}, {q->ptr, k->ptr, v->ptr, cu})) return rc;
   PromptParams P;
   P.q = rows_of(q, T, d), P.k = rows_of(k, T, d), P.v = rows_of(v, T, d), P.o = rows_of(o, T, d);
   P.lse = lse, P.cu = cu, P.T = (int32_t)T, P.R = (int32_t)R, P.G = (int32_t)(H / Hk), P.H = (int32_t)H, P.rc = softmax_scale * kLog2e;

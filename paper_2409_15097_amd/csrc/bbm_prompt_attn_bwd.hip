@@ -563,7 +563,7 @@ extern "C" __attribute__((visibility("default"))) int bbm_prompt_attn_bwd(const 
     return fail(BBM_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, workspace ? workspace_bytes : (size_t)0);
   if (!aligned(workspace, 16)) return fail(BBM_EINVAL, "%s: workspace must be 16-byte aligned", fn);
   if (T == 0) return BBM_OK;
-  if (int rc = check_apart(fn, {dq, dk, dv}, {q, k, v, o, d_o})) return rc;
+  if (int rc = check_apart(fn, {dq->ptr, dk->ptr, dv->ptr, workspace}, {q->ptr, k->ptr, v->ptr, o->ptr, d_o->ptr, lse, cu})) return rc;
   PromptBwdParams P;
   Rows* const to[] = {&P.q, &P.k, &P.v, &P.o, &P.d_o, &P.dq, &P.dk, &P.dv};
   for (int i = 0; i < 8; ++i) *to[i] = rows_of(all[i].x, T, d);

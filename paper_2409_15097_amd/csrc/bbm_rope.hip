@@ -174,7 +174,9 @@ extern "C" __attribute__((visibility("default"))) int bbm_rope(const bbm_packed*
   while (tokens * items < 4 * NT && 2 * tokens * (rot / 2) <= 2048 && ceil_div(T, 2 * tokens) >= 1024) tokens *= 2;
   P.tokens = (int32_t)tokens;
   if (ceil_div(T, tokens) >= kMaxWgs) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld)", fn, (long long)T, (long long)H);
-  if (Hk > 0 && (q_out->ptr == k_out->ptr || q_out->ptr == k->ptr || k_out->ptr == q->ptr)) return fail(BBM_EINVAL, "%s: the outputs must not be the same, nor the other tensor's input", fn);
+  // (a tensor is turned in place, or into a place that is no input)
+  if (int rc = check_apart(fn, {q_out->ptr, Hk > 0 ? k_out->ptr : nullptr}, {positions, freqs})) return rc;
+  if (Hk > 0 && (q_out->ptr == k->ptr || k_out->ptr == q->ptr)) return fail(BBM_EINVAL, "%s: an output must not be the other tensor's input", fn);
   const unsigned wgs = (unsigned)ceil_div(T, tokens);
   const size_t lds = (size_t)(tokens * (rot / 2) + 1) / 2 * 2 * sizeof(float2);
   hipStream_t s = static_cast<hipStream_t>(stream);

@@ -125,12 +125,14 @@ extern "C" __attribute__((visibility("default"))) int bbm_build_slots(const int3
   for (const void* p : {(const void*)ctx_lens, (const void*)new_lens, (const void*)block_table, (const void*)free_pages, (const void*)free_at, (const void*)cu_new,
                         (const void*)lens, (const void*)positions, (const void*)slots, (const void*)free_next})
     if (!aligned(p, 4)) return fail(BBM_EINVAL, "%s: pointers must be 4-byte aligned", fn);
-  if (free_next == free_at || lens == ctx_lens || lens == new_lens) return fail(BBM_EINVAL, "%s: an output other than block_table must not be an input", fn);
   if (table_stride < max_pages) return fail(BBM_EINVAL, "%s: table_stride=%lld is less than max_pages=%lld", fn, (long long)table_stride, (long long)max_pages);
   if (page != 16 && page != 32 && page != 64 && page != 128) return fail(BBM_EUNSUPPORTED, "%s: page=%d is none of 16, 32, 64, 128", fn, page);
   if (R > BBM_SLOTS_MAX_REQUESTS) return fail(BBM_EUNSUPPORTED, "%s: R=%lld requests, more than %d", fn, (long long)R, BBM_SLOTS_MAX_REQUESTS);
   if (T > kMaxTokens || max_pages > 0x7fffffffll / R)  // (by division: a product of the caller's may wrap)
     return fail(BBM_EUNSUPPORTED, "%s: T=%lld or R=%lld times max_pages=%lld is too large", fn, (long long)T, (long long)R, (long long)max_pages);
+  // (Every work-group reads the inputs while others write.  The pointers of no tokens or no pages may be anything.)
+  if (int rc = check_apart(fn, {cu_new, lens, T > 0 ? positions : nullptr, T > 0 ? slots : nullptr, free_next, block_table}, {ctx_lens, new_lens, n_free > 0 ? free_pages : nullptr, free_at}))
+    return rc;
   SlotParams P;
   P.ctx = ctx_lens, P.add = new_lens, P.table = block_table, P.free_pages = free_pages, P.free_at = free_at;
   P.cu = cu_new, P.lens = lens, P.positions = positions, P.slots = slots, P.free_next = free_next;

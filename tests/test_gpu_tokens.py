@@ -603,3 +603,15 @@ def test_binding_refuses(bbm):
         bbm.bbm_prompt_attn_fwd(normal(1, 4, 3, 64), k, k, cu)
     with pytest.raises(bbm.BbmError):
         bbm.bbm_rope(normal(1, 4, 4, 72), None, pos, f)
+
+
+def test_slots_of_a_step_without_tokens_or_free_pages(bbm):
+    """Outputs of no elements, and an empty list of pages, may lie where the next one begins."""
+    ctx, new = i32([40, 16]), i32([3, 0])
+    table = i32([[7, 8, 9, -2], [5, -2, -2, -2]])
+    for T, free in ((0, i32([3, 4])), (5, table.flatten()[:0]), (0, i32([]))):
+        mine = table.clone()
+        free = mine.flatten()[:0] if T else free
+        r = bbm.bbm_build_slots(ctx, new, mine, free, i32([0]), T, 16)
+        assert r.cu_new.tolist() == [0, 3, 3] and r.lens.tolist() == [43, 16] and r.free_next.tolist() == [0] and torch.equal(mine, table)
+        assert r.positions.tolist() == [40, 41, 42, 0, 0][:T] and r.slots.tolist() == [9 * 16 + 8, 9 * 16 + 9, 9 * 16 + 10, -1, -1][:T]

@@ -220,3 +220,28 @@ def test_refuses_sizes_whose_product_wraps(bbm):
         assert bbm.lib.bbm_kv4_read(P, T, cache(pages=pages), a["k"], a["v"], None) == bbm.BBM_EUNSUPPORTED
     for H, Hk in ((1 << 62, 1 << 62), ((1 << 63) - 1, 2), (65535, 1), (1, 65535)):
         assert rope(bbm, **{n: a[n] for n in ("q", "qo", "k", "ko")}, H=H, Hk=Hk) == bbm.BBM_EUNSUPPORTED, (H, Hk)
+
+
+def test_refuses_outputs_at_the_address_of_anything_else(bbm):
+    """Every output and workspace against every input and every other output, each of which has an address of its own otherwise."""
+    def check(call, outputs, inputs, allowed=()):
+        at = {n: (i + 50) * P for i, n in enumerate(outputs + inputs)}
+        for out in outputs:
+            for other in outputs + inputs:
+                if other != out and (out, other) not in allowed and (other, out) not in allowed:
+                    assert call(at | {out: at[other]}) == bbm.BBM_EINVAL, (out, other)
+                    assert "must not be" in bbm.bbm_last_error(), (out, other, bbm.bbm_last_error())
+    check(lambda a: slots(bbm, **a), ["cu", "lens", "pos", "sl", "nxt", "table"], ["ctx", "new", "free", "at"])
+    tensors = lambda a, *names: {n: pk(a[n]) for n in names}  # noqa: E731
+    check(lambda a: rope(bbm, **tensors(a, "q", "qo", "k", "ko"), pos=a["pos"], freqs=a["freqs"]), ["qo", "ko"], ["q", "k", "pos", "freqs"], [("qo", "q"), ("ko", "k")])
+    check(lambda a: fwd(bbm, **tensors(a, "q", "k", "v", "o"), lse=a["lse"], cu=a["cu"]), ["o", "lse"], ["q", "k", "v", "cu"])
+    names = ("q", "k", "v", "o", "d_o", "dq", "dk", "dv")
+    check(lambda a: bwd(bbm, **tensors(a, *names), lse=a["lse"], cu=a["cu"], ws=a["ws"]), ["dq", "dk", "dv", "ws"], ["q", "k", "v", "o", "d_o", "lse", "cu"])
+    parts = ["k", "ks", "v", "vs"]
+    c = lambda a: cache(**{n: a["c" + n] for n in parts})  # noqa: E731
+    in_cache = ["c" + n for n in parts]
+    check(lambda a: bbm.lib.bbm_kv4_append(pk(a["k"]), pk(a["v"]), 3, a["slots"], c(a), None), in_cache, ["k", "v", "slots"])
+    check(lambda a: bbm.lib.bbm_kv4_read(a["slots"], 3, c(a), pk(a["k"]), pk(a["v"]), None), ["k", "v"], ["slots"] + in_cache)
+    long = dict(T=1, R=1, H=2, max_len=1 << 16, mask=None)
+    check(lambda a: attn(bbm, **long | dict(q=pk(a["q"]), o=pk(a["o"]), lse=a["lse"], cu=a["cu"], lens=a["lens"], table=a["table"], ws=a["ws"], c=c(a), mask=a["mask"], words=1)),
+          ["o", "lse", "ws"], ["q", "cu", "lens", "table", "mask"] + in_cache)
