@@ -164,6 +164,8 @@ def rope_freqs(rot: int, base: float = 10000.0, factor: float = 1.0, method: Opt
     those between in proportion, and scales both sine and cosine by 0.1 ln(factor) + 1 (published as YaRN, arXiv 2309.00071)."""
     if rot < 2 or rot % 2 or not base > 0 or not factor >= 1:
         raise ValueError(f"rot={rot} must be even and positive, base={base} positive, factor={factor} no less than 1")
+    if method is None and factor != 1:
+        raise ValueError(f"factor={factor} needs a method: linear, ntk or yarn")
     j = torch.arange(0, rot, 2, dtype=torch.float64)
     mscale = 1.0
     if method == "ntk":

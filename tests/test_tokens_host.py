@@ -245,3 +245,9 @@ def test_refuses_outputs_at_the_address_of_anything_else(bbm):
     long = dict(T=1, R=1, H=2, max_len=1 << 16, mask=None)
     check(lambda a: attn(bbm, **long | dict(q=pk(a["q"]), o=pk(a["o"]), lse=a["lse"], cu=a["cu"], lens=a["lens"], table=a["table"], ws=a["ws"], c=c(a), mask=a["mask"], words=1)),
           ["o", "lse", "ws"], ["q", "cu", "lens", "table", "mask"] + in_cache)
+
+
+def test_frequencies_of_a_longer_context_need_a_method(bbm):
+    with pytest.raises(ValueError, match="method"):
+        bbm.rope_freqs(64, factor=8.0, device="cpu")
+    assert bbm.rope_freqs(64, factor=1, device="cpu")[0].equal(bbm.rope_freqs(64, device="cpu")[0])
