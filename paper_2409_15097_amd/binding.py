@@ -87,6 +87,24 @@ def _load():
     L.bbm_probe_mfma_bf16.argtypes = [ci, i64, vp, vp]
     L.bbm_probe_mfma_bf16_flop.restype = C.c_double
     L.bbm_probe_mfma_bf16_flop.argtypes = [i64]
+    # include/bbm_tokens.h; the packed tensors and caches go in by their addresses (tokens.py fills one array with all packed tensors of a call)
+    pk = cache = vp
+    cf, size = C.c_float, C.c_size_t
+    for name, args in {
+        "bbm_build_slots": [vp, vp, i64, vp, i64, i64, ci, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp],
+        "bbm_rope": [pk, pk, i64, pk, pk, i64, i64, ci, ci, ci, ci, vp, vp, cf, vp],
+        "bbm_prompt_attn_fwd": [pk, pk, pk, pk, vp, i64, i64, vp, i64, i64, ci, cf, vp],
+        "bbm_prompt_attn_bwd": [pk, pk, pk, pk, pk, vp, pk, pk, pk, i64, i64, vp, i64, i64, ci, cf, vp, size, vp],
+        "bbm_kv4_append": [pk, pk, i64, vp, cache, vp],
+        "bbm_kv4_read": [vp, i64, cache, pk, pk, vp],
+        "bbm_kv4_attn": [pk, pk, vp, i64, i64, vp, vp, vp, i64, i64, vp, i64, cache, i64, cf, i64, vp, size, vp],
+    }.items():
+        f = getattr(L, name)
+        f.restype, f.argtypes = ci, args
+    L.bbm_prompt_attn_bwd_workspace_bytes.restype = size
+    L.bbm_prompt_attn_bwd_workspace_bytes.argtypes = [i64, i64, i64, i64, ci]
+    L.bbm_kv4_attn_workspace_bytes.restype = size
+    L.bbm_kv4_attn_workspace_bytes.argtypes = [i64, i64, i64, i64, ci, i64]
     return L
 
 

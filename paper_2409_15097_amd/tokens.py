@@ -21,29 +21,6 @@ class _CCache(C.Structure):
                 ("pages", C.c_int64), ("Hk", C.c_int64), ("page", C.c_int32), ("d", C.c_int32)]
 
 
-def _declare(L):
-    i64, vp, ci, cf = C.c_int64, C.c_void_p, C.c_int, C.c_float
-    pk = cache = vp  # (addresses of structures: a call fills one array with all of its packed tensors)
-    for name, args in {
-        "bbm_build_slots": [vp, vp, i64, vp, i64, i64, ci, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp],
-        "bbm_rope": [pk, pk, i64, pk, pk, i64, i64, ci, ci, ci, ci, vp, vp, cf, vp],
-        "bbm_prompt_attn_fwd": [pk, pk, pk, pk, vp, i64, i64, vp, i64, i64, ci, cf, vp],
-        "bbm_prompt_attn_bwd": [pk, pk, pk, pk, pk, vp, pk, pk, pk, i64, i64, vp, i64, i64, ci, cf, vp, C.c_size_t, vp],
-        "bbm_kv4_append": [pk, pk, i64, vp, cache, vp],
-        "bbm_kv4_read": [vp, i64, cache, pk, pk, vp],
-        "bbm_kv4_attn": [pk, pk, vp, i64, i64, vp, vp, vp, i64, i64, vp, i64, cache, i64, cf, i64, vp, C.c_size_t, vp],
-    }.items():
-        f = getattr(L, name)
-        f.restype, f.argtypes = ci, args
-    L.bbm_prompt_attn_bwd_workspace_bytes.restype = C.c_size_t
-    L.bbm_prompt_attn_bwd_workspace_bytes.argtypes = [i64, i64, i64, i64, ci]
-    L.bbm_kv4_attn_workspace_bytes.restype = C.c_size_t
-    L.bbm_kv4_attn_workspace_bytes.argtypes = [i64, i64, i64, i64, ci, i64]
-
-
-_declare(lib)
-
-
 # A small call is all submission: of 10.8 us that a rotation of 33 tokens took the host, the launch is 3.2, allocating two results 2.9; structures a tensor,
 # contexts, devices compared as objects were the rest.  So: the current device's stream is asked for by its number, packed tensors go into one
 # array, and only a call for another device or stream enters a context (and then calls itself).

@@ -251,3 +251,20 @@ def test_frequencies_of_a_longer_context_need_a_method(bbm):
     with pytest.raises(ValueError, match="method"):
         bbm.rope_freqs(64, factor=8.0, device="cpu")
     assert bbm.rope_freqs(64, factor=1, device="cpu")[0].equal(bbm.rope_freqs(64, device="cpu")[0])
+
+
+def test_signatures_are_declared_with_the_library(bbm):
+    """`lib` alone, before any name of the operators on packed tokens is used: 64-bit arguments arrive as such."""
+    code = """
+import re
+import paper_2409_15097_amd as bbm
+L = bbm.lib
+for h in ("bbm.h", "bbm_mask_index.h", "bbm_tokens.h"):
+    hdr = re.sub(r"/\\*.*?\\*/", "", open("include/" + h).read(), flags=re.S)
+    for name in set(re.findall(r"\\b(bbm_[a-z0-9_]+)\\s*\\(", hdr)):
+        assert getattr(L, name).argtypes is not None, name
+assert L.bbm_build_slots(1, 1, 4, 1, 8, 8, 64, 1, 9, 1, -(1 << 40), 1, 1, 1, 1, 1, None) == bbm.BBM_EINVAL
+assert "T=-1099511627776" in bbm.bbm_last_error(), bbm.bbm_last_error()
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout[-2000:]
