@@ -13,7 +13,12 @@
  *
  * Unless a function says otherwise, outputs and workspaces overlap neither inputs nor each other (the same pointer is refused).  What rows
  * of nobody hold does not matter (it may be an infinity or a NaN); the rows of requests are taken to be finite, as are the cache's groups: an
- * infinity or a NaN among them may reach any row of its own request.  Scores are fp32 numbers: a softmax_scale lies within 2^-100 .. 2^100, and sums of products of q and k stay within fp32's range.
+ * infinity or a NaN among them may reach any row of its own request.
+ *
+ * Scores, their sums and the log-sum-exp are fp32 numbers: a softmax_scale lies within 2^-100 .. 2^100, sums of products of q and k stay below
+ * 2^126 before and after it, as do 2^16 times the sums of |v| over a request's keys.  Within that, attention is as exact for large scores as fp32
+ * scores allow: equal ones share a row, however large.  The gradients form their probabilities again from the fp32 log-sum-exp, half a step of which is a relative error of
+ * 2^-24 times its size in all of a row's: they are meant for scores (times softmax_scale) up to 2^12, and from 2^20 on say nothing.
  *
  * A packed tensor is bf16 [T][heads][d] with any row and head strides (in elements, multiples of 8; the d elements of a head
  * are contiguous and 16-byte aligned), so the q, k and v parts of one projection's output, or [heads][T][d], need no copy.

@@ -13,6 +13,7 @@
 // Measured: one token each of 64 requests of 9.8 to 16 thousand keys, 32 / 8 heads of 128 (861 MB), narrow, 163 - 176 us, 4.9 - 5.3 TB/s (a large copy reaches
 // 4.8), and 5.4 for the join; trees of 256 nodes of 8 requests, 32 heads, over 805 to 1280 keys, wide, 53 us, 0.64 PFLOP/s counted as the products of all pairs.
 #include "bbm_kv4.h"
+#include "bbm_softmax.h"
 #include "bbm_tile.h"
 
 #include <algorithm>
@@ -23,7 +24,6 @@ using bbm::bf16x8, bbm::f32x16, bbm::Kv4, bbm::scalar;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLazy = 8.0f;
 constexpr int NW = 4;
 constexpr int kStep = 32 * NW;  // keys of a work-group's step
@@ -38,7 +38,8 @@ struct Kv4AttnParams {
   const uint64_t* mask;
   float* partials;  // [piece][key head][part]: `width` rows of D sums, then as many (maximum, sum) pairs
   int32_t T, R, G, max_pages, mask_words, width, pieces, parts, part_keys;
-  float rc;  // softmax_scale * log2(e)
+  float rc;    // softmax_scale * log2(e)
+  float lazy;  // kLazy as a difference of scores
 };
 
 // What a work-group and the one that joins its parts both need to know.
@@ -107,7 +108,7 @@ __device__ __forceinline__ void put_column(const Kv4AttnParams& P, const Piece& 
 #pragma unroll
   for (int e = 0; e < D / 16; ++e) y[e] = (__bf16)(v[e] * inv);
   *reinterpret_cast<out_t*>(P.o + (int64_t)t * P.o_row + h * P.o_head + e0) = y;
-  if (P.lse && e0 == 0) P.lse[(int64_t)h * P.T + t] = l > 0.0f ? (m + __log2f(l)) * kLn2 : -INFINITY;
+  if (P.lse && e0 == 0) P.lse[(int64_t)h * P.T + t] = l > 0.0f ? bbm::log_sum(m, l, P.rc) : -INFINITY;
 }
 
 template <int D>
@@ -131,7 +132,8 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 3 : 5) void kv4_narrow_kernel(c
   const int my_i = min(x.col0 + n, x.cols - 1) / P.G, my_h = hk * P.G + (min(x.col0 + n, x.cols - 1) - my_i * P.G), my_t = x.s.begin + my_i;
   bf16x8 qf[KS];
   f32x4 acc[VD];
-  float m_run = -INFINITY, l_run = 0.0f, nm = 0.0f;
+  bbm::RunningMax top;
+  float l_run = 0.0f;
   {
     const __bf16* const row = P.q + (int64_t)my_t * P.q_row + my_h * P.q_head + kq * KD;
 #pragma unroll
@@ -198,20 +200,18 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 3 : 5) void kv4_narrow_kernel(c
       there(b, sb, j0 + 16);
     }
     float mx = fmaxf(fmaxf(fmaxf(sa[0], sa[1]), fmaxf(sa[2], sa[3])), fmaxf(fmaxf(sb[0], sb[1]), fmaxf(sb[2], sb[3])));
-    mx = other_max<16>(other_max<32>(mx)) * P.rc;
-    if (__any(mx > m_run + kLazy ? 1 : 0)) {
-      const float m_new = fmaxf(m_run, mx), m_fin = m_new == -INFINITY ? 0.0f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f(m_run - m_fin);
+    top.update(other_max<16>(other_max<32>(mx)), P.lazy, P.rc, [&](float alpha) __attribute__((always_inline)) {
       l_run *= alpha;
-      m_run = m_new;
-      nm = -m_fin;
 #pragma unroll
       for (int j = 0; j < VD; ++j) acc[j] *= alpha;
-    }
+    });
+    // The far form for all rows (bbm_softmax.h): the test for it and the two forms behind it cost the kernel of D = 64 registers in scratch memory.  One token each of 64
+    // requests of 8 to 16 thousand keys, 32 / 8 heads of 64: 104 us, as with the near form alone; with the test 117.
+    const float off = top.m == -INFINITY ? 0.0f : top.m;
     bf16x8 pf;
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
-      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(r < 4 ? sa[r & 3] : sb[r & 3], P.rc, nm));
+      const float p = __builtin_amdgcn_exp2f(((r < 4 ? sa[r & 3] : sb[r & 3]) - off) * P.rc);
       l_run += p;
       pf[r] = (__bf16)p;
     }
@@ -270,7 +270,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 3 : 5) void kv4_narrow_kernel(c
 
   // The waves' results meet: columns on threads, 16 threads a column.
   const float l = other_sum<16>(other_sum<32>(l_run));
-  if (kq == 0) m_s[wave][n] = m_run, l_s[wave][n] = l;
+  if (kq == 0) m_s[wave][n] = top.m, l_s[wave][n] = l;
   // lane (n, kq): rows 4 kq + r of instruction j, element (4 kq + r) * VD + j
 #pragma unroll
   for (int r = 0; r < 4; ++r)
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 3 : 5) void kv4_narrow_kernel(c
   float sum = 0.0f, v[VD] = {};
 #pragma unroll
   for (int w = 0; w < NW; ++w) {
-    const float f = __builtin_amdgcn_exp2f(m_s[w][c] - m_fin);
+    const float f = bbm::weight(m_s[w][c], m_fin, P.rc);
     sum += f * l_s[w][c];
 #pragma unroll
     for (int e = 0; e < VD; ++e) v[e] += f * o_s[w][c][e0 + e];
@@ -336,7 +336,8 @@ __global__ __launch_bounds__(64 * NW, 2) void kv4_wide_kernel(const Kv4AttnParam
 #pragma unroll
   for (int db = 0; db < DB; ++db)
     for (int e = 0; e < 16; ++e) oacc[db][e] = 0.0f;
-  float m_run = -INFINITY, l_run = 0.0f, nm = 0.0f;
+  bbm::RunningMax top;
+  float l_run = 0.0f;
   bbm::TileAddr<D> A;
   A.init(lane);
 
@@ -422,22 +423,23 @@ __global__ __launch_bounds__(64 * NW, 2) void kv4_wide_kernel(const Kv4AttnParam
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
         for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[kb][e]);
-      mx = other_max<32>(mx) * P.rc;
-      if (__any(mx > m_run + kLazy ? 1 : 0)) {
-        const float m_new = fmaxf(m_run, mx), m_fin = m_new == -INFINITY ? 0.0f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m_run - m_fin);
+      top.update(other_max<32>(mx), P.lazy, P.rc, [&](float alpha) __attribute__((always_inline)) {
         l_run *= alpha;
-        m_run = m_new;
-        nm = -m_fin;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
           for (int e = 0; e < 16; ++e) oacc[db][e] *= alpha;
+      });
+      if (top.far) {
+        const float off = top.offset(P.rc);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+          for (int e = 0; e < 16; ++e) sc[kb][e] -= off;
       }
       bf16x8 pf[2];
       auto exps = [&](int u, int e0, int e1) {
 #pragma unroll
         for (int e = e0; e < e1; ++e) {
-          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[u / 2][8 * (u % 2) + e], P.rc, nm));
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[u / 2][8 * (u % 2) + e], P.rc, top.nm));
           l_run += p;
           pf[u & 1][e] = (__bf16)p;
         }
@@ -485,7 +487,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv4_wide_kernel(const Kv4AttnParam
 #pragma unroll
         for (int g = 0; g < 4; ++g)
           *reinterpret_cast<f32x4*>(rec + c * D + 32 * db + 8 * g + 4 * hh) = f32x4{oacc[db][4 * g], oacc[db][4 * g + 1], oacc[db][4 * g + 2], oacc[db][4 * g + 3]};
-      if (hh == 0) *reinterpret_cast<float2*>(rec + P.width * D + 2 * c) = make_float2(m_run, l);
+      if (hh == 0) *reinterpret_cast<float2*>(rec + P.width * D + 2 * c) = make_float2(top.m, l);
     }
     return;
   }
@@ -505,7 +507,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv4_wide_kernel(const Kv4AttnParam
     if (r < wcols)
       *reinterpret_cast<bf16x8*>(P.o + (int64_t)(x.s.begin + tok) * P.o_row + h * P.o_head + lane % RC * 8) = *reinterpret_cast<const bf16x8*>(stage + r * D + (lane % RC ^ r % RC) * 8);
   }
-  if (P.lse && hh == 0 && lq < wcols) P.lse[(int64_t)my_h * P.T + x.s.begin + my_i] = l > 0.0f ? (m_run + __log2f(l)) * kLn2 : -INFINITY;
+  if (P.lse && hh == 0 && lq < wcols) P.lse[(int64_t)my_h * P.T + x.s.begin + my_i] = l > 0.0f ? bbm::log_sum(top.m, l, P.rc) : -INFINITY;
 }
 
 // Joins the parts of a piece's columns in a fixed order, 16 lanes a column.  With many parts (SIDE = 4) a wave takes one column and four parts side by
@@ -533,21 +535,21 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(const Kv4AttnParams P) {
       for (int e = 0; e < VD / 4; ++e) y[i][e] = *reinterpret_cast<const f32x4*>(r + c * D + e0 + 4 * e);
     }
     const float m_new = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m), m_fin = m_new == -INFINITY ? 0.0f : m_new;
-    const float keep = __builtin_amdgcn_exp2f(m - m_fin);
+    const float keep = bbm::weight(m, m_fin, P.rc);
     m = m_new;
     l *= keep;
 #pragma unroll
     for (int e = 0; e < VD; ++e) v[e] *= keep;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float f = __builtin_amdgcn_exp2f(ml[i].x - m_fin);
+      const float f = bbm::weight(ml[i].x, m_fin, P.rc);
       l += f * ml[i].y;
 #pragma unroll
       for (int e = 0; e < VD; ++e) v[e] += f * y[i][e / 4][e % 4];
     }
   }
   if constexpr (SIDE == 4) {
-    const float m_all = other_max<16>(other_max<32>(m)), f = __builtin_amdgcn_exp2f(m - (m_all == -INFINITY ? 0.0f : m_all));
+    const float m_all = other_max<16>(other_max<32>(m)), f = bbm::weight(m, m_all == -INFINITY ? 0.0f : m_all, P.rc);
     l = other_sum<16>(other_sum<32>(l * f));
 #pragma unroll
     for (int e = 0; e < VD; ++e) v[e] = other_sum<16>(other_sum<32>(v[e] * f));
@@ -635,7 +637,7 @@ extern "C" __attribute__((visibility("default"))) int bbm_kv4_attn(const bbm_pac
   P.q_row = q->row_stride, P.q_head = q->head_stride, P.o_row = o->row_stride, P.o_head = o->head_stride, P.table_stride = table_stride;
   P.cu = cu, P.lens = lens, P.table = block_table, P.mask = mask;
   P.T = (int32_t)T, P.R = (int32_t)R, P.G = (int32_t)(H / cache->Hk), P.max_pages = (int32_t)max_pages, P.mask_words = (int32_t)mask_words;
-  P.rc = softmax_scale * kLog2e;
+  P.rc = softmax_scale * kLog2e, P.lazy = kLazy / P.rc;
   const Plan p = plan_of(T, R, P.G, cache->Hk, std::min<int64_t>(max_len, bbm::kMaxTokens));
   if (p.pieces >= kMaxWgs || p.pieces * cache->Hk * p.parts >= kMaxWgs) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, R=%lld, H=%lld)", fn, (long long)T, (long long)R, (long long)H);
   P.partials = static_cast<float*>(workspace);

@@ -11,13 +11,13 @@
 // 37 of 1 to 300 tokens, 16 heads of 64, 9.8 us.
 #include "bbm_mfma.h"
 #include "bbm_prompt.h"
+#include "bbm_softmax.h"
 
 namespace {
 
 using bbm::bf16x8, bbm::f32x16, bbm::global, bbm::IntC, bbm::mfma_ring, bbm::partner_sum, bbm::scalar, bbm::TileAddr, bbm::TL;
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLazy = 8.0f;  // the running maximum moves when a row exceeds it by a factor of 2^8: P and its sum keep their relative precision
 
 struct PromptParams {
@@ -25,7 +25,8 @@ struct PromptParams {
   float* lse;
   const int32_t* cu;
   int32_t T, R, G, H, pieces;
-  float rc;  // softmax_scale * log2(e)
+  float rc;    // softmax_scale * log2(e)
+  float lazy;  // kLazy as a difference of scores
 };
 typedef bbm::InPlace<PromptParams> Args;
 
@@ -59,7 +60,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void prompt_fwd_kernel(const 
   if (n <= 0) return;
   const int wrow = row0 + 32 * (wave / HALVES), wrows = max(0, min(32, n - wrow));  // this wave's rows
   const int n_tiles = (min(n, row0 + BR) + 63) / 64, n_full = row0 / 64 & ~1;
-  const float rc = P->rc;
+  const float rc = P->rc, lazy = P->lazy;
 
   const int k_row = P->k.row, v_row = P->v.row;
   const __bf16* const kg = global(P->k.p) + h / P->G * P->k.head + (int64_t)s.begin * k_row;
@@ -92,7 +93,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void prompt_fwd_kernel(const 
 #pragma unroll
   for (int db = 0; db < DB; ++db)
     for (int e = 0; e < 16; ++e) oacc[db][e] = 0.0f;
-  float m_run = -INFINITY, nm = 0.0f, l_run = 0.0f;  // running maximum in exponent units; what is added to exponents: its negative, or 0
+  bbm::RunningMax top;
+  float l_run = 0.0f;
   __builtin_amdgcn_s_waitcnt(0);
 #pragma unroll
   for (int t = 0; t < KS; ++t) qf[t] = bbm::slab_frag<D>(q_stage, t, lane);
@@ -143,16 +145,17 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void prompt_fwd_kernel(const 
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
       for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[kb][e]);
-    mx = partner_max(mx) * rc;
-    if (__any(mx > m_run + kLazy ? 1 : 0)) {
-      const float m_new = fmaxf(m_run, mx), m_fin = m_new == -INFINITY ? 0.0f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f(m_run - m_fin);
+    top.update(partner_max(mx), lazy, rc, [&](float alpha) __attribute__((always_inline)) {
       l_run *= alpha;
-      m_run = m_new;
-      nm = -m_fin;
 #pragma unroll
       for (int db = 0; db < DB; ++db)
         for (int e = 0; e < 16; ++e) oacc[db][e] *= alpha;
+    });
+    if (top.far) {
+      const float off = top.offset(rc);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+        for (int e = 0; e < 16; ++e) sc[kb][e] -= off;
     }
     __builtin_amdgcn_s_setprio(1);
     // the exponentials of 16 keys behind the matrix instructions of the 16 before
@@ -160,7 +163,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void prompt_fwd_kernel(const 
     auto exps = [&](int u, int e0, int e1) {
 #pragma unroll
       for (int e = e0; e < e1; ++e) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[u / 2][8 * (u % 2) + e], rc, nm));
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[u / 2][8 * (u % 2) + e], rc, top.nm));
         l_run += p;  // (before it is rounded: the log-sum-exp is an fp32 result)
         pf[u & 1][e] = (__bf16)p;
       }
@@ -196,15 +199,15 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void prompt_fwd_kernel(const 
     if (half == 1) {
 #pragma unroll
       for (int i = 0; i < 4 * DB; ++i) sums[i * 64] = f32x4{oacc[i / 4][i % 4 * 4], oacc[i / 4][i % 4 * 4 + 1], oacc[i / 4][i % 4 * 4 + 2], oacc[i / 4][i % 4 * 4 + 3]};
-      *stats = make_float2(m_run, l_run);
+      *stats = make_float2(top.m, l_run);
     }
     __syncthreads();
     if (half == 1) return;
     const float2 other = *stats;
-    const float m_new = fmaxf(m_run, other.x), m_fin = m_new == -INFINITY ? 0.0f : m_new;
-    const float w0 = __builtin_amdgcn_exp2f(m_run - m_fin), w1 = __builtin_amdgcn_exp2f(other.x - m_fin);
+    const float m_new = fmaxf(top.m, other.x), m_fin = m_new == -INFINITY ? 0.0f : m_new;
+    const float w0 = bbm::weight(top.m, m_fin, rc), w1 = bbm::weight(other.x, m_fin, rc);
     l_run = w0 * l_run + w1 * other.y;
-    m_run = m_new;
+    top.m = m_new;
 #pragma unroll
     for (int i = 0; i < 4 * DB; ++i) {
       const f32x4 y = sums[i * 64];
@@ -215,7 +218,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void prompt_fwd_kernel(const 
   const float l_tot = partner_sum(l_run);
   __bf16* const stage = (wave / 2 == 0 ? k_s0 : v_s0) + wave % 2 * 32 * D;
   bbm::store_strided<D>(oacc, 1.0f / l_tot, stage, global(P->o.p) + h * P->o.head + (int64_t)(s.begin + wrow) * P->o.row, wrows, P->o.row, lane);
-  if (global(P->lse) && hh == 0 && lq < wrows) global(P->lse)[(int64_t)h * P->T + s.begin + wrow + lq] = (m_run + __log2f(l_tot)) * kLn2;
+  if (global(P->lse) && hh == 0 && lq < wrows) global(P->lse)[(int64_t)h * P->T + s.begin + wrow + lq] = bbm::log_sum(top.m, l_tot, rc);
 }
 
 }  // namespace
@@ -238,7 +241,7 @@ extern "C" __attribute__((visibility("default"))) int bbm_prompt_attn_fwd(const 
   if (int rc = check_apart(fn, {o->ptr, lse}, {q->ptr, k->ptr, v->ptr, cu})) return rc;
   PromptParams P;
   P.q = rows_of(q, T, d), P.k = rows_of(k, T, d), P.v = rows_of(v, T, d), P.o = rows_of(o, T, d);
-  P.lse = lse, P.cu = cu, P.T = (int32_t)T, P.R = (int32_t)R, P.G = (int32_t)(H / Hk), P.H = (int32_t)H, P.rc = softmax_scale * kLog2e;
+  P.lse = lse, P.cu = cu, P.T = (int32_t)T, P.R = (int32_t)R, P.G = (int32_t)(H / Hk), P.H = (int32_t)H, P.rc = softmax_scale * kLog2e, P.lazy = kLazy / P.rc;
   const bool halves = split_keys(T, R, H);
   const int64_t pieces = count_pieces(T, R, 1, halves ? 64 : 128), wgs = work_groups(H, pieces);
   if (wgs >= kMaxWgs) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld)", fn, (long long)T, (long long)H);

@@ -615,3 +615,111 @@ def test_slots_of_a_step_without_tokens_or_free_pages(bbm):
         r = bbm.bbm_build_slots(ctx, new, mine, free, i32([0]), T, 16)
         assert r.cu_new.tolist() == [0, 3, 3] and r.lens.tolist() == [43, 16] and r.free_next.tolist() == [0] and torch.equal(mine, table)
         assert r.positions.tolist() == [40, 41, 42, 0, 0][:T] and r.slots.tolist() == [9 * 16 + 8, 9 * 16 + 9, 9 * 16 + 10, -1, -1][:T]
+
+
+# ---- scores of any size
+
+
+# Scores of 2^base + j 2^gap (j of 0 .. 6, exact in fp32) times 2^scale: small ones, where one step of the running maximum's exponent begins to count, and so on up
+# to fp32's range; the later ones are ties of the largest j.
+SIZES = [(10, -1, 0), (16, -4, 3), (20, -2, -1), (30, 8, -8), (30, 8, -5), (30, 8, 4), (60, 38, -20), (100, 78, -20), (20, -2, 95), (20, -2, 99), (-80, -100, 99), (100, 78, -100)]
+
+
+def sized_rows(seed, T, heads, d, sign, base, gap):
+    """Keys whose product with sized_query is sign * 2^base + j * 2^gap: two groups of 32 elements that the 4-bit cache holds exactly."""
+    g = torch.Generator().manual_seed(seed)
+    k = torch.zeros(T, heads, d)
+    k[..., 1] = sign * 2.0 ** (base - base // 2)
+    k[..., 33] = torch.tensor([0.0, 1, 2, 3, 4, 6])[torch.randint(0, 6, (T, heads), generator=g)] * 2.0 ** gap
+    return k.to(torch.bfloat16).cuda()
+
+
+def sized_query(T, heads, d, base):
+    q = torch.zeros(T, heads, d)
+    q[..., 1], q[..., 33] = 2.0 ** (base // 2), 1.0
+    q[1::3] *= 2.0 ** -20                                                  # rows of other sizes side by side
+    return q.to(torch.bfloat16).cuda()
+
+
+def sized_bounds(seen, p, v, o, lse):
+    """Differences of these scores are exact, so an exponent is off by its product's rounding (2^-16 at 2^8, where probabilities end), or by the running maximum's (2^-13 where
+    that is kept as a rounded product); the rest as in ot.bounds: P rounded to bf16, sums of n terms, five roundings of the log-sum-exp's own size."""
+    n = max(1, int(seen.sum(1).max(initial=0)))
+    e_p = 2.0 ** -12 + (n + 32) * ot.F
+    return ot.U + ot.B * np.abs(o) + (ot.B * (1 + ot.B) + e_p) * (p @ np.abs(v)), e_p + 8 * ot.F * np.abs(np.where(np.isfinite(lse), lse, 0.0))
+
+
+@pytest.mark.parametrize("base, gap, scale", SIZES)
+@pytest.mark.parametrize("name, H, Hk, d, sign", [("long", 2, 1, 64, 1), ("tiles", 2, 2, 128, -1), ("ragged", 64, 64, 64, 1), ("ragged", 24, 24, 128, -1)])
+def test_prompt_scores_of_any_size(bbm, name, H, Hk, d, sign, base, gap, scale):
+    lens = LENS[name]
+    cu, T = np.concatenate([[0], np.cumsum(lens)]), sum(lens)
+    q, k, v = sized_query(T, H, d, base), sized_rows(1, T, Hk, d, sign, base, gap), normal(2, T, Hk, d)
+    o, lse = bbm.bbm_prompt_attn_fwd(q, k, v, i32(cu), softmax_scale=2.0 ** scale)
+    q, k, v = f64(q), f64(k), f64(v)
+    for a, b in zip(cu, cu[1:]):
+        seen = np.tril(np.ones((b - a, b - a), bool))
+        for h in range(0, H, max(1, H // 6)):
+            kk, vv = k[a:b, h * Hk // H], v[a:b, h * Hk // H]
+            wo, wl, p = ot.attention(q[a:b, h], kk, vv, seen, 2.0 ** scale)
+            e_o, e_l = sized_bounds(seen, p, vv, wo, wl)
+            close(f"rows {a}..{b}, head {h}: O", o[a:b, h], wo, e_o), close(f"rows {a}..{b}, head {h}: lse", lse[h, a:b], wl, e_l)
+
+
+@pytest.mark.parametrize("base, gap, scale", SIZES)
+@pytest.mark.parametrize("lens, news, H, Hk, d, sign", [([70, 200], [3, 1], 4, 2, 64, 1), ([2300, 40, 900], [1, 1, 2], 8, 2, 128, -1), ([300, 150], [140, 130], 64, 64, 64, 1),
+                                                        ([2500, 2100], [130, 130], 64, 8, 128, -1)])
+def test_cached_scores_of_any_size(bbm, lens, news, H, Hk, d, sign, base, gap, scale):
+    """The narrow and the wide kernel, whole and in parts."""
+    page, n = 32, sum(lens)
+    c = bbm.kv4_cache(-(-n // page) + len(lens), Hk, d, page)
+    width = max(-(-m // page) for m in lens)
+    table, slots, at = np.full((len(lens), width), -1), [], 0
+    for r, m in enumerate(lens):
+        pages = -(-m // page)
+        table[r, :pages] = np.arange(at, at + pages)
+        slots += list(at * page + np.arange(m))
+        at += pages
+    v = normal(2, n, Hk, d)
+    bbm.bbm_kv4_append(sized_rows(1, n, Hk, d, sign, base, gap), v, i32(slots), c)
+    hk, hv = host_cache(c)
+    cu, T = np.concatenate([[0], np.cumsum(news)]), sum(news)
+    q = sized_query(T, H, d, base)
+    o, lse = bbm.bbm_kv4_attn(q, c, i32(table), i32(lens), i32(cu), softmax_scale=2.0 ** scale, max_len=max(lens))
+    q = f64(q)
+    for r, m in enumerate(lens):
+        a, b = cu[r], cu[r + 1]
+        seen = np.arange(m) <= m - news[r] + np.arange(b - a)[:, None]
+        pg, j = table[r, np.arange(m) // page], np.arange(m) % page
+        for h in range(0, H, max(1, H // 6)):
+            kk, vv = hk[pg, h * Hk // H, j], hv[pg, h * Hk // H, j]
+            assert np.abs(kk).max() >= 2.0 ** (base // 2)
+            wo, wl, p = ot.attention(q[a:b, h], kk, vv, seen, 2.0 ** scale)
+            e_o, e_l = sized_bounds(seen, p, vv, wo, wl)
+            close(f"request {r}, head {h}: O", o[a:b, h], wo, e_o), close(f"request {r}, head {h}: lse", lse[h, a:b], wl, e_l)
+
+
+def test_prompt_rows_that_see_keys_of_1e30(bbm):
+    """Keys of 1e30 share a row among themselves where their scores are positive, and leave it to the others where they are not."""
+    cu, T, x = prompt_case("long", 1, 1, 64, "plain", seed=4)
+    a, b, m = int(cu[0]), int(cu[1]), 40
+    x["k"][b - m:b], x["v"][b - m:b] = 1e30, -1e30
+    o, lse = bbm.bbm_prompt_attn_fwd(x["q"], x["k"], x["v"], i32(cu))
+    n = {t: f64(y)[a:b, 0] for t, y in x.items()}
+    rows = np.arange(b - m, b) - a
+    large = n["q"][rows].sum(1) > 0
+    assert 5 < large.sum() < m - 5
+    seen = (np.arange(b - a) <= rows[:, None]) & ((np.arange(b - a) >= b - m - a) == large[:, None])     # (the weight of the other keys is an exact zero)
+    q = n["q"][rows]
+    wo, wl, p = ot.attention(q, n["k"], n["v"], seen, 0.125)
+    e_o, e_l = ot.bounds(q, n["k"], n["v"], seen, 0.125, p, wo, wl)
+    got_o, got_l = o[a + rows, 0], lse[0, a + rows]
+    close("O, others", got_o[torch.from_numpy(~large).cuda()], wo[~large], e_o[~large]), close("lse, others", got_l[torch.from_numpy(~large).cuda()], wl[~large], e_l[~large])
+    # equal scores, an average of equal values: P is 1 or a power of two's neighbour, rounded once, and so is the result
+    close("O", got_o[torch.from_numpy(large).cuda()], wo[large], (2 * ot.B + 2.0 ** -12) * np.abs(wo[large]))
+    close("lse", got_l[torch.from_numpy(large).cuda()], wl[large], e_l[large])
+
+
+def test_gradients_of_scores_up_to_2000(bbm):
+    cu, T, x = prompt_case("ragged", 4, 2, 64, "plain", seed=12, scale=8.0)
+    check_prompt(bbm, cu, T, x, 4, 2, 64, scale=1.0)
