@@ -723,3 +723,109 @@ def test_prompt_rows_that_see_keys_of_1e30(bbm):
 def test_gradients_of_scores_up_to_2000(bbm):
     cu, T, x = prompt_case("ragged", 4, 2, 64, "plain", seed=12, scale=8.0)
     check_prompt(bbm, cu, T, x, 4, 2, 64, scale=1.0)
+
+
+# ---- outputs in other layouts, and without a log-sum-exp
+
+
+def output_in(layout, T, H, d):
+    """(packed output, the memory that it is a part of), all sevens."""
+    if layout == "fused":
+        whole = torch.full((T, (H + 3) * d + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+        return whole[:, d:(H + 1) * d].unflatten(1, (H, d)), whole
+    whole = torch.full((H + 2, T + 3, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    return whole[1:H + 1, 2:T + 2].transpose(0, 1), whole
+
+
+def same_and_nothing_else(part, whole, want, rows):
+    """`want` in these rows of the part, and sevens in the rest of what it is a part of."""
+    assert torch.equal(part[rows], want[rows])
+    part[rows] = 7.0
+    assert (whole == 7.0).all(), "written outside the output's rows"
+
+
+OUT_LAYOUTS = pytest.mark.parametrize("layout", ["fused", "heads"])
+
+
+@OUT_LAYOUTS
+@pytest.mark.parametrize("name, H, Hk, d", [("ragged", 4, 2, 64), ("longer", 5, 1, 64), ("longer", 5, 1, 128), ("tiles", 3, 1, 128), ("longer", 40, 8, 128), ("longer", 64, 16, 64), ("many", 2, 2, 64)])
+def test_prompt_outputs_in_other_layouts(bbm, name, H, Hk, d, layout):
+    """Whole and halved tiles, dK and dV whole and in parts."""
+    cu, T, x = prompt_case(name, H, Hk, d, "plain", seed=14)
+    rows = slice(int(cu[0]), int(cu[-1]))
+    args = x["q"], x["k"], x["v"]
+    wo, wl = bbm.bbm_prompt_attn_fwd(*args, i32(cu))
+    wg = bbm.bbm_prompt_attn_bwd(*args, wo, x["d_o"], wl, i32(cu))
+    o, o_all = output_in(layout, T, H, d)
+    grads = [output_in(layout, T, h, d) for h in (H, Hk, Hk)]
+    got, _ = bbm.bbm_prompt_attn_fwd(*args, i32(cu), out=o)
+    assert got is o
+    bbm.bbm_prompt_attn_bwd(*args, o, x["d_o"], wl, i32(cu), **{n: g[0] for n, g in zip(("dq", "dk", "dv"), grads)})
+    same_and_nothing_else(o, o_all, wo, rows)
+    for (part, whole), want in zip(grads, wg):
+        same_and_nothing_else(part, whole, want, rows)
+
+
+CACHED = [([63, 200, 1, 0], [1, 3, 1, 1], 8, 2, 64), ([63, 200, 1, 0], [1, 3, 1, 1], 3, 1, 128), ([2900, 9, 1700], [1, 1, 2], 12, 4, 64), ([9000, 40], [1, 2], 4, 2, 128),
+          ([300, 150], [140, 130], 64, 64, 64), ([300, 150], [140, 130], 64, 64, 128), ([2500, 2100], [130, 130], 64, 8, 64), ([2500, 2100], [130, 130], 64, 8, 128)]
+
+
+@OUT_LAYOUTS
+@pytest.mark.parametrize("lens, news, H, Hk, d", CACHED)
+def test_cached_outputs_in_other_layouts(bbm, lens, news, H, Hk, d, layout):
+    """Few columns and many, whole, in a few parts and in more than four."""
+    c, table, cu, T, q, _ = cached_case(bbm, lens, news, H, Hk, d, 32, seed=15, before=2, behind=3)
+    args = q, c, i32(table), i32(lens), i32(cu)
+    want, _ = bbm.bbm_kv4_attn(*args, max_len=max(lens))
+    o, o_all = output_in(layout, T, H, d)
+    bbm.bbm_kv4_attn(*args, max_len=max(lens), out=o)
+    same_and_nothing_else(o, o_all, want, slice(int(cu[0]), int(cu[-1])))
+
+
+@OUT_LAYOUTS
+@pytest.mark.parametrize("rot, interleaved", [(64, False), (62, False), (40, True)])
+def test_rope_and_read_into_other_layouts(bbm, rot, interleaved, layout):
+    T, H, Hk, d, page = 70, 6, 2, 64, 16
+    q, k, pos, f = normal(1, T, H, d), normal(2, T, Hk, d), i32(np.arange(T) * 3), bbm.rope_freqs(rot)[0]
+    want = bbm.bbm_rope(q, k, pos, f, interleaved=interleaved)
+    (oq, q_all), (ok, k_all) = output_in(layout, T, H, d), output_in(layout, T, Hk, d)
+    bbm.bbm_rope(q, k, pos, f, interleaved=interleaved, out_q=oq, out_k=ok)
+    c = bbm.kv4_cache(6, Hk, d, page)
+    slots = i32(np.arange(T))
+    bbm.bbm_kv4_append(k, q[:, :Hk], slots, c)
+    read = bbm.bbm_kv4_read(slots, c)
+    (rk, rk_all), (rv, rv_all) = output_in(layout, T, Hk, d), output_in(layout, T, Hk, d)
+    bbm.bbm_kv4_read(slots, c, out_k=rk, out_v=rv)
+    for part, whole, x in ((oq, q_all, want[0]), (ok, k_all, want[1]), (rk, rk_all, read[0]), (rv, rv_all, read[1])):
+        same_and_nothing_else(part, whole, x, slice(0, T))
+
+
+def c_packed(x):
+    """The C structure of a packed tensor."""
+    import ctypes
+    from paper_2409_15097_amd.tokens import _CPacked
+    return ctypes.byref(_CPacked(x.data_ptr(), x.stride(0), x.stride(1)))
+
+
+@pytest.mark.parametrize("name, H, Hk, d", [("ragged", 4, 2, 64), ("longer", 40, 8, 128)])
+def test_prompt_without_a_log_sum_exp(bbm, name, H, Hk, d):
+    cu, T, x = prompt_case(name, H, Hk, d, "plain", seed=16)
+    want, _ = bbm.bbm_prompt_attn_fwd(x["q"], x["k"], x["v"], i32(cu))
+    o, offsets = torch.full_like(want, 7.0), i32(cu)
+    stream = torch.cuda.current_stream().cuda_stream
+    assert bbm.lib.bbm_prompt_attn_fwd(*(c_packed(x[n]) for n in "qkv"), c_packed(o), None, T, len(cu) - 1, offsets.data_ptr(), H, Hk, d, d ** -0.5, stream) == bbm.BBM_OK
+    rows = slice(int(cu[0]), int(cu[-1]))
+    assert torch.equal(o[rows], want[rows])
+
+
+@pytest.mark.parametrize("lens, news, H, Hk, d", CACHED)
+def test_cached_without_a_log_sum_exp(bbm, lens, news, H, Hk, d):
+    import ctypes
+    c, table, cu, T, q, _ = cached_case(bbm, lens, news, H, Hk, d, 32, seed=17)
+    tab, ln, offsets, R = i32(table), i32(lens), i32(cu), len(lens)
+    want, _ = bbm.bbm_kv4_attn(q, c, tab, ln, offsets, max_len=max(lens))
+    need = bbm.bbm_kv4_attn_workspace_bytes(T, R, H, Hk, d, max(lens))
+    ws, o = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda"), torch.full_like(want, 7.0)
+    assert bbm.lib.bbm_kv4_attn(c_packed(q), c_packed(o), None, T, R, offsets.data_ptr(), ln.data_ptr(), tab.data_ptr(), tab.stride(0), tab.shape[1], None, 0,
+                                ctypes.byref(c.c_struct), H, d ** -0.5, max(lens), ws.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == bbm.BBM_OK
+    assert torch.equal(o, want)
