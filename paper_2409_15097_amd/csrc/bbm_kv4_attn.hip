@@ -10,8 +10,8 @@
 //   O^T += V^T P^T    over 32 keys: lane (n, q) loads elements n * D / 16 .. of the keys 4 q .. 4 q + 3 of both blocks of 16, converts pairs of elements,
 //                     and pairs the keys by byte permutes; row n of instruction j is element n * D / 16 + j.  The lane's scores are of the same eight keys
 //                     (the layout of the first product's result), so P goes from one product to the other in place.
-// Measured: one token each of 64 requests of 9.8 to 16 thousand keys, 32 / 8 heads of 128 (861 MB), narrow, 163 - 176 us, 4.9 - 5.3 TB/s (a large copy reaches
-// 4.8), and 5.4 for the join; trees of 256 nodes of 8 requests, 32 heads, over 805 to 1280 keys, wide, 53 us, 0.64 PFLOP/s counted as the products of all pairs.
+// Measured: one token each of 64 requests of 9.8 to 16 thousand keys, 32 / 8 heads of 128 (861 MB), narrow, 162 - 176 us, 4.9 - 5.3 TB/s (a large copy reaches
+// 4.8), and 5.2 for the join; trees of 256 nodes of 8 requests, 32 heads, over 805 to 1280 keys, wide, 52 us, 0.65 PFLOP/s counted as the products of all pairs.
 #include "bbm_kv4.h"
 #include "bbm_softmax.h"
 #include "bbm_tile.h"

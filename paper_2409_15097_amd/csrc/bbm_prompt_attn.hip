@@ -7,8 +7,8 @@
 // Scores are not rounded between the products: the scale multiplies them inside the exponential, in fp32, one fused multiply-add an
 // element.  P is rounded to bf16 for the second product, half a step each, and summed before that.
 // Bound by the matrix instructions with the exponentials between them: two prompts of 8192 and 6554 tokens, 32 heads of 128, 0.90 TFLOP counted as
-// the pairs that are seen, 820 - 880 us, 1.0 - 1.1 PFLOP/s (a large bf16 product reaches 1.14 on this card); short prompts by one chain of tiles:
-// 37 of 1 to 300 tokens, 16 heads of 64, 9.8 us.
+// the pairs that are seen, 800 - 850 us a call, 1.06 - 1.13 PFLOP/s (a large bf16 product reaches 1.14 on this card; the matrix pipe is busy for 60 % of the cycles of a
+// clock that falls to 1.5 GHz); 4096 tokens, 32 / 8 heads of 64, 87 us, 0.79 PFLOP/s; short prompts by one chain of tiles: 37 of 1 to 300 tokens, 16 heads of 64, 9.5 us.
 #include "bbm_mfma.h"
 #include "bbm_prompt.h"
 #include "bbm_softmax.h"

@@ -10,8 +10,8 @@
 // Each step is one chain of matrix instructions with the copies of the next tile, the exponentials and the roundings behind them.  As in the forward
 // the scale multiplies the scores inside the exponential in fp32; P and dS are rounded to bf16 for the products that they enter, and D is formed from the
 // O that the forward rounded, which is the O that was used: <dO, O> as a program would form it.
-// Bound by the matrix instructions: sequences of 4096 and 3277 tokens, 32 / 8 heads of 128, forward and backward, 0.79 TFLOP (pairs that are seen) in 930 - 960 us;
-// with the scores and dP that dQ and dK, dV both form, 9 products are multiplied where 7 are counted, 1.06 PFLOP/s.  Short sequences by a chain of steps of
+// Bound by the matrix instructions: sequences of 4096 and 3277 tokens, 32 / 8 heads of 128, forward and backward, 0.79 TFLOP (pairs that are seen) in 945 - 985 us;
+// with the scores and dP that dQ and dK, dV both form, 9 products are multiplied where 7 are counted, 1.03 - 1.07 PFLOP/s.  Short sequences by a chain of steps of
 // 0.5 to 1 us: 13 of 1 to 1024, 16 heads of 64, 34 us.
 #include "bbm_mfma.h"
 #include "bbm_prompt.h"
@@ -520,7 +520,7 @@ __global__ __launch_bounds__(256) void prompt_sum_kernel(const PromptBwdParams P
 // Parts of a group's heads whose dK and dV are formed side by side: one key head's walk over all heads of its group is as long as they are many, and a
 // chip that is not full waits for it.  Worth the fp32 sums in memory where the walk is long.  Forward and backward, one / several parts, us: 1 x 1024
 // tokens, 8 / 2 heads of 128, 90 / 53; 1 x 4096, 8 / 2 of 64, 237 / 126; 1 x 2048, 32 / 8 of 128, 221 / 198; 12 x 214 on average and 1000 at most, 12 / 4 of 128, 85 / 76;
-// 6 x 125, 8 / 1 of 64, 30 / 21; but 8 x 248, 16 / 4 of 128, 52 / 60; 30 x 81, 8 / 2 of 64, 23 / 29 (not cut up).
+// 6 x 125, 8 / 1 of 64, 30 / 21; but 8 x 248, 16 / 4 of 128, 52 / 60 (cut up by this rule all the same, the slower side there); 30 x 81, 8 / 2 of 64, 23 / 29 (not cut up).
 constexpr int64_t kDkvWgs = 512, kLongWalk = 512;  // work-groups, two a CU; queries of all heads of a group
 inline int64_t head_parts(int64_t T, int64_t R, int64_t H, int64_t Hk) {
   if (H / Hk * T < kLongWalk * R) return 1;
