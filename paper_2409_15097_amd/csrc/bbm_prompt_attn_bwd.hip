@@ -8,10 +8,11 @@
 //   dK and dV   a work-group takes 64 keys of one key head and walks the tiles of 64 queries of every head of the group, a wave 32 keys and
 //               32 queries of a tile: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS, all in its registers.
 // Each step is one chain of matrix instructions with the copies of the next tile, the exponentials and the roundings behind them.  As in the forward
-// the scale multiplies the scores inside the exponential in fp32; P and dS are rounded to bf16 for the products that they enter, and D is formed from the
+// the scale multiplies the scores inside the exponential in fp32; P and dS are rounded to bf16 for the products that they enter, dS once, from the
+// fp32 P (from the rounded one the gradients are no faster, 570 against 568 us for 1 x 4096 tokens, 32 / 8 heads of 128, and dK off by 0.0030 instead of 0.0025), and D is formed from the
 // O that the forward rounded, which is the O that was used: <dO, O> as a program would form it.
-// Bound by the matrix instructions: sequences of 4096 and 3277 tokens, 32 / 8 heads of 128, forward and backward, 0.79 TFLOP (pairs that are seen) in 945 - 985 us;
-// with the scores and dP that dQ and dK, dV both form, 9 products are multiplied where 7 are counted, 1.03 - 1.07 PFLOP/s.  Short sequences by a chain of steps of
+// Bound by the matrix instructions: sequences of 4096 and 3277 tokens, 32 / 8 heads of 128, forward and backward, 0.79 TFLOP (pairs that are seen) in 920 - 985 us;
+// with the scores and dP that dQ and dK, dV both form, 9 products are multiplied where 7 are counted, 1.03 - 1.10 PFLOP/s.  Short sequences by a chain of steps of
 // 0.5 to 1 us: 13 of 1 to 1024, 16 heads of 64, 34 us.
 #include "bbm_mfma.h"
 #include "bbm_prompt.h"
@@ -337,7 +338,6 @@ __device__ __forceinline__ void dkv_of(Args P, int wg, __bf16* t_s0, __bf16* t_s
     }
     if (live) {
       f32x16 sc, dp;
-      constexpr bool P32 = D == 64;  // at D = 128 the fp32 probabilities do not outlive dP (registers): dS is formed from P as dV's product takes it
       constexpr int N1 = KS, N2 = 2 * KS, N3 = N2 + 2 * DB, N4 = N3 + 2 * DB;
       constexpr int PER = D == 128 ? 4 : 8;
       static_assert(PER * (KS - 2) >= 16 && PER * (2 * DB - 2) >= 16, "all 16 must find room");
@@ -397,16 +397,12 @@ __device__ __forceinline__ void dkv_of(Args P, int wg, __bf16* t_s0, __bf16* t_s
                 sc[e] = __builtin_amdgcn_exp2f(sc[e] * rc);
                 sc[e + 1] = __builtin_amdgcn_exp2f(sc[e + 1] * rc);
                 pf[e / 8][e % 8 / 2] = pack(sc[e], sc[e + 1]);
-                // (hides the pair's origin: the compiler otherwise rounds each of the two once more where dS takes it apart)
-                if constexpr (!P32) asm("" : "+v"(pf[e / 8][e % 8 / 2]));
               }
             }
             if constexpr (x >= N2 + 2 && x < N3) {
 #pragma unroll
               for (int e = (x - N2 - 2) * PER; e < min(16, (x - N2 - 1) * PER); e += 2) {
-                const uint32_t w = pf[e / 8][e % 8 / 2];
-                const float p0 = P32 ? sc[e] : __uint_as_float(w << 16), p1 = P32 ? sc[e + 1] : __uint_as_float(w & 0xffff0000u);
-                dsf[e / 8][e % 8 / 2] = pack(p0 * dp[e], p1 * dp[e + 1]);
+                dsf[e / 8][e % 8 / 2] = pack(sc[e] * dp[e], sc[e + 1] * dp[e + 1]);
               }
             }
           });

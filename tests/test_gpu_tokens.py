@@ -829,3 +829,32 @@ def test_cached_without_a_log_sum_exp(bbm, lens, news, H, Hk, d):
     assert bbm.lib.bbm_kv4_attn(c_packed(q), c_packed(o), None, T, R, offsets.data_ptr(), ln.data_ptr(), tab.data_ptr(), tab.stride(0), tab.shape[1], None, 0,
                                 ctypes.byref(c.c_struct), H, d ** -0.5, max(lens), ws.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == bbm.BBM_OK
     assert torch.equal(o, want)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_gradients_round_the_score_gradient_once(bbm, d):
+    """Pairs of tokens: a row of dK (and dQ) is one or two terms, so a second rounding on the way to it shows.  The bound is that of ot.bounds with one rounding of dS to bf16, from
+    an fp32 probability, and one of the result."""
+    pairs, H = 300, 4
+    cu, T = np.arange(pairs + 1) * 2, 2 * pairs
+    q, k, v, d_o = (normal(30 + i, T, H, d) for i in range(4))
+    o, lse = bbm.bbm_prompt_attn_fwd(q, k, v, i32(cu))
+    dq, dk, _ = bbm.bbm_prompt_attn_bwd(q, k, v, o, d_o, lse, i32(cu))
+    q, k, v, d_o, o = (f64(t) for t in (q, k, v, d_o, o))
+    want, tol = ([np.zeros((T, H, d)) for _ in range(2)] for _ in range(2))
+    sm, seen = d ** -0.5, np.tril(np.ones((2, 2), bool))
+    for a in cu[:-1]:
+        for h in range(H):
+            at = slice(a, a + 2), h
+            wo, wl, p = ot.attention(q[at], k[at], v[at], seen, sm)
+            delta = (d_o[at] * o[at]).sum(1)
+            g = ot.attention_bwd(q[at], k[at], v[at], d_o[at], p, sm, delta)
+            e_l = ot.bounds(q[at], k[at], v[at], seen, sm, p, wo, wl)[1]
+            e_s = ((d + 8) * ot.F + 32 * ot.F) * sm * (np.abs(q[at]) @ np.abs(k[at]).T) + 32 * ot.F
+            dp_mag = np.abs(d_o[at]) @ np.abs(v[at]).T + (np.abs(d_o[at]) * np.abs(o[at])).sum(1)[:, None]
+            ds = p * np.abs(d_o[at] @ v[at].T - delta[:, None])
+            e_ds = (ot.B + e_s + e_l[:, None] + 32 * ot.F) * ds + p * (d + 8) * ot.F * dp_mag
+            for i, (x, e) in enumerate(((k[at], e_ds), (q[at], e_ds.T))):
+                want[i][at] = g[i]
+                tol[i][at] = ot.U + ot.B * np.abs(g[i]) + (1 + ot.B) * sm * (e @ np.abs(x)) + 4 * ot.F * sm * ((ds if i == 0 else ds.T) @ np.abs(x))
+    close("dQ", dq, want[0], tol[0]), close("dK", dk, want[1], tol[1])
