@@ -1,6 +1,6 @@
 """Binary Block Masking flash attention (forward and backward) for AMD MI355X: thin Python binding over libbbm.so.
 
-The names below are those of the C ABI (include/bbm.h); the functions only marshal arguments: device memory and the
+The names below are those of the C ABI (include/bbm.h, bbm_tokens.h, bbm_cache.h); the functions only marshal arguments: device memory and the
 stream come from PyTorch, every computation runs in the library's HIP kernels.  There is no CPU fallback: the
 binding is loaded at the first use of any of these names and raises ImportError if the library is not built (the
 package itself imports without it, so that `python -m paper_2409_15097_amd.build` can build it).
@@ -20,7 +20,9 @@ _TOKEN_NAMES = (
     "Slots", "KV4Cache", "kv4_cache", "rope_freqs", "bbm_build_slots", "bbm_rope", "bbm_prompt_attn_fwd",
     "bbm_prompt_attn_bwd_workspace_bytes", "bbm_prompt_attn_bwd", "bbm_kv4_append", "bbm_kv4_read", "bbm_kv4_attn_workspace_bytes", "bbm_kv4_attn",
 )
-__all__ = list(_NAMES + _TOKEN_NAMES)
+# operators on the cache of many and long answers (include/bbm_cache.h)
+_CACHE_NAMES = ("bbm_kv4_shared_attn_workspace_bytes", "bbm_kv4_shared_attn")
+__all__ = list(_NAMES + _TOKEN_NAMES + _CACHE_NAMES)
 
 
 def __getattr__(name):
@@ -34,8 +36,13 @@ def __getattr__(name):
         value = getattr(tokens, name)
         globals()[name] = value
         return value
+    if name in _CACHE_NAMES:
+        from . import cache
+        value = getattr(cache, name)
+        globals()[name] = value
+        return value
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
 def __dir__():
-    return sorted(list(globals()) + list(_NAMES + _TOKEN_NAMES))
+    return sorted(list(globals()) + list(_NAMES + _TOKEN_NAMES + _CACHE_NAMES))

@@ -98,6 +98,8 @@ def _load():
         "bbm_kv4_append": [pk, pk, i64, vp, cache, vp],
         "bbm_kv4_read": [vp, i64, cache, pk, pk, vp],
         "bbm_kv4_attn": [pk, pk, vp, i64, i64, vp, vp, vp, i64, i64, vp, i64, cache, i64, cf, i64, vp, size, vp],
+        # include/bbm_cache.h
+        "bbm_kv4_shared_attn": [pk, pk, vp, i64, i64, vp, vp, vp, i64, i64, i64, vp, vp, vp, i64, cache, i64, cf, i64, i64, vp, size, vp],
     }.items():
         f = getattr(L, name)
         f.restype, f.argtypes = ci, args
@@ -105,6 +107,8 @@ def _load():
     L.bbm_prompt_attn_bwd_workspace_bytes.argtypes = [i64, i64, i64, i64, ci]
     L.bbm_kv4_attn_workspace_bytes.restype = size
     L.bbm_kv4_attn_workspace_bytes.argtypes = [i64, i64, i64, i64, ci, i64]
+    L.bbm_kv4_shared_attn_workspace_bytes.restype = size
+    L.bbm_kv4_shared_attn_workspace_bytes.argtypes = [i64, i64, i64, i64, i64, ci, i64, i64]
     return L
 
 

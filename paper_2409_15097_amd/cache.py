@@ -1,0 +1,64 @@
+"""ctypes binding of the operators on the 4-bit cache of many and long answers.  Argument marshalling only; see include/bbm_cache.h for the contract.
+
+Devices, streams and what a call allocates are as in tokens.py."""
+from typing import Optional
+
+import torch
+
+from .binding import _check, lib
+from .tokens import KV4Cache, _address, _context, _elsewhere, _gpu, _here, _I64x6, _ints, _lse_out, _out, _packed, _table, _workspace
+
+
+def _mask(mask: Optional[torch.Tensor], device: int, T: int):
+    """(address, words of a row) of a mask over new tokens."""
+    if mask is None:
+        return None, 0
+    assert mask.dtype is torch.int64 and mask.is_contiguous() and mask.dim() == 2 and mask.shape[0] == T and mask.get_device() == device, "an int64 mask of words for every row"
+    return mask.data_ptr(), mask.shape[1]
+
+
+def _groups(group_cu: Optional[torch.Tensor], shared_lens: Optional[torch.Tensor], device: int):
+    """(number, addresses) of the groups that share prefixes."""
+    assert (group_cu is None) == (shared_lens is None), "groups have offsets and shared lengths"
+    if group_cu is None:
+        return 0, None, None
+    S = shared_lens.shape[0]
+    return S, _ints(group_cu, device, S + 1), _ints(shared_lens, device, S)
+
+
+def bbm_kv4_shared_attn_workspace_bytes(T: int, R: int, S: int, H: int, Hk: int, d: int, max_shared: int, max_own: int) -> int:
+    return int(lib.bbm_kv4_shared_attn_workspace_bytes(T, R, S, H, Hk, d, max_shared, max_own))
+
+
+def bbm_kv4_shared_attn(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor, lens: torch.Tensor, cu: torch.Tensor, group_cu: Optional[torch.Tensor],
+                        shared_lens: Optional[torch.Tensor], mask: Optional[torch.Tensor] = None, max_shared: Optional[int] = None, max_own: Optional[int] = None,
+                        softmax_scale: Optional[float] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None, stream=None):
+    """bbm_kv4_attn where requests group_cu[g] .. group_cu[g+1] - 1 (int32 [S + 1]) have their first shared_lens[g] (int32 [S]) keys in common, which are read once for all of them;
+    max_shared, max_own: upper bounds of shared_lens and of the keys behind them, for the work split (None: what the table holds).  Returns (O bf16 [T, H, d], lse fp32 [H, T])."""
+    dev = _gpu(q)
+    if _elsewhere(dev, stream):
+        with _context(dev, stream):
+            return _kv4_shared_attn(dev, q, cache, block_table, lens, cu, group_cu, shared_lens, mask, max_shared, max_own, softmax_scale, out, lse, workspace)
+    return _kv4_shared_attn(dev, q, cache, block_table, lens, cu, group_cu, shared_lens, mask, max_shared, max_own, softmax_scale, out, lse, workspace)
+
+
+def _kv4_shared_attn(dev, q, cache, block_table, lens, cu, group_cu, shared_lens, mask, max_shared, max_own, softmax_scale, out, lse, workspace):
+    T, H, d = q.shape
+    R, c = lens.shape[0], cache.c_struct
+    assert d == c.d and cache.device == dev, "the cache has another head size, or lies elsewhere"
+    table, stride, width = _table(block_table, dev, R)
+    S, group_at, shared_at = _groups(group_cu, shared_lens, dev)
+    most = width * c.page
+    max_shared, max_own = most if max_shared is None else max(1, max_shared), most if max_own is None else max(1, max_own)
+    packed = _packed(q, dev, T, H, d)
+    out, to = _out(out, q, dev, T, H, d)
+    lse, lse_at = _lse_out(lse, q, dev, H, T)
+    if workspace is None:
+        need = lib.bbm_kv4_shared_attn_workspace_bytes(T, R, S, H, c.Hk, d, max_shared, max_own)
+        workspace = q.new_empty(need, dtype=torch.uint8) if need else None
+    keep = _I64x6(*packed, *to)
+    at = _address(keep)
+    _check(lib.bbm_kv4_shared_attn(at, at + 24, lse_at, T, R, _ints(cu, dev, R + 1), _ints(lens, dev, R), table, stride, width, S, group_at, shared_at, *_mask(mask, dev, T),
+                                   _address(c), H, d ** -0.5 if softmax_scale is None else softmax_scale, max_shared, max_own, *_workspace(workspace, dev), _here(dev)))
+    return out, lse

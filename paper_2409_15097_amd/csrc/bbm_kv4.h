@@ -26,6 +26,27 @@ inline Kv4 kv4_of(const bbm_kv4_cache* c) {
   return Kv4{c->k, c->k_scale, c->v, c->v_scale, (int32_t)c->pages, (int32_t)c->Hk, c->page == 16 ? 4 : c->page == 32 ? 5 : c->page == 64 ? 6 : 7, c->page};
 }
 
+// Lengths and block table of requests, the mask over their new tokens, and the groups that share prefixes.
+inline int check_table(const char* fn, const int32_t* lens, const int32_t* table, int64_t stride, int64_t max_pages, int page) {
+  if (!lens || !aligned(lens, 4) || !table || !aligned(table, 4)) return fail(BBM_EINVAL, "%s: lens and block_table must be non-NULL 4-byte aligned pointers", fn);
+  if (max_pages < 1 || stride < max_pages) return fail(BBM_EINVAL, "%s: max_pages=%lld must be >= 1, table_stride=%lld no less than it", fn, (long long)max_pages, (long long)stride);
+  if (max_pages > kMaxTokens / page) return fail(BBM_EUNSUPPORTED, "%s: max_pages=%lld is too large", fn, (long long)max_pages);
+  return BBM_OK;
+}
+inline int check_mask(const char* fn, const uint64_t* mask, int64_t mask_words) {
+  if (!aligned(mask, 8)) return fail(BBM_EINVAL, "%s: mask must be 8-byte aligned", fn);
+  if (mask ? mask_words < 1 : mask_words != 0) return fail(BBM_EINVAL, "%s: mask_words=%lld does not fit the mask", fn, (long long)mask_words);
+  if (mask_words > (1 << 20)) return fail(BBM_EUNSUPPORTED, "%s: mask_words=%lld is too large", fn, (long long)mask_words);
+  return BBM_OK;
+}
+inline int check_groups(const char* fn, int64_t R, int64_t S, const int32_t* group_cu, const int32_t* shared_lens, int64_t max_shared, int64_t max_own) {
+  if (S < 0 || S > R) return fail(BBM_EINVAL, "%s: S=%lld is outside 0 .. R=%lld", fn, (long long)S, (long long)R);
+  if (S > 0 && (!group_cu || !shared_lens || !aligned(group_cu, 4) || !aligned(shared_lens, 4)))
+    return fail(BBM_EINVAL, "%s: group_cu and shared_lens must be non-NULL 4-byte aligned pointers", fn);
+  if (max_shared < 1 || max_own < 1) return fail(BBM_EINVAL, "%s: max_shared=%lld and max_own=%lld must be >= 1", fn, (long long)max_shared, (long long)max_own);
+  return BBM_OK;
+}
+
 // A scale byte as the conversion takes it: in the exponent's place of a float.  It looks at nothing else (sign and fraction may be anything), 255
 // gives NaNs, 0 gives 2^-127.
 __device__ __forceinline__ float scale_of(uint32_t s) { return __uint_as_float(s << 23); }

@@ -12,6 +12,7 @@
 //                     (the layout of the first product's result), so P goes from one product to the other in place.
 // Measured: one token each of 64 requests of 9.8 to 16 thousand keys, 32 / 8 heads of 128 (861 MB), narrow, 162 - 176 us, 4.9 - 5.3 TB/s (a large copy reaches
 // 4.8), and 5.2 for the join; trees of 256 nodes of 8 requests, 32 heads, over 805 to 1280 keys, wide, 52 us, 0.65 PFLOP/s counted as the products of all pairs.
+#include "bbm_cache.h"
 #include "bbm_kv4.h"
 #include "bbm_softmax.h"
 #include "bbm_tile.h"
@@ -40,15 +41,76 @@ struct Kv4AttnParams {
   int32_t T, R, G, max_pages, mask_words, width, pieces, parts, part_keys;
   float rc;    // softmax_scale * log2(e)
   float lazy;  // kLazy as a difference of scores
+  // Of calls with shared prefixes (SHARED of what follows); partials then are [part of a group, then part of a request][key head][column of all T * G],
+  // D sums each, and behind all of them the (maximum, sum) pairs in the same order.
+  const int32_t *group_cu, *shared_lens;
+  int32_t S, group_pieces, group_parts, group_part_keys;
+  int32_t group_wgs, own_wgs;  // work-groups of this launch for pieces of groups (they come first, up to a multiple of 8) and of requests
 };
+
+// Which piece, part and key head a work-group has; `group`: of a group's shared keys.
+struct Item {
+  int number, part, hk;
+  bool group, none;
+};
+template <bool SHARED>
+__device__ __forceinline__ Item item_of(const Kv4AttnParams& P) {
+  const int ahead = SHARED ? (P.group_wgs + 7) & ~7 : 0;  // (a multiple of 8, so that both kinds spread over the XCDs alike)
+  const bool group = SHARED && (int)blockIdx.x < ahead;
+  const int wg = (int)blockIdx.x - (group ? 0 : ahead), total = !SHARED ? (int)gridDim.x : group ? P.group_wgs : P.own_wgs;
+  const int pieces = group ? P.group_pieces : P.pieces, parts = group ? P.group_parts : P.parts;
+  Item x;
+  x.none = wg >= total;
+  const int at = x.none ? 0 : bbm::logical_wg(wg, total), rest = at / pieces;
+  x.number = at % pieces, x.part = rest % parts, x.hk = rest / parts, x.group = group;
+  return x;
+}
 
 // What a work-group and the one that joins its parts both need to know.
 struct Piece {
   bbm::Span s;
   int cols, col0;    // columns of the request; the piece's first
   int len, prefix;   // keys that can be seen at all; keys in front of the new tokens (causal: of the first one that has a row here)
+  int from;          // the first key that is this piece's: those in front of it are its group's
   int parts, keys;   // parts of this request, keys of one
+  int group_parts;   // parts of the keys that its group shares
 };
+template <bool SHARED>
+__device__ __forceinline__ void cut_keys(const Kv4AttnParams& P, Piece& x, int parts, int part_keys) {
+  const int n = x.len - (SHARED ? x.from : 0);
+  x.keys = max(part_keys, (int)(((int64_t)n + parts - 1) / parts + kStep - 1) / kStep * kStep);
+  x.parts = n > 0 ? (n - 1) / x.keys + 1 : 1;
+}
+// The keys that group g shares, in whole blocks of 16: what is left over is each request's own.
+__device__ __forceinline__ int shared_of(const Kv4AttnParams& P, int g) {
+  return (int)scalar((int)max((int64_t)0, min((int64_t)P.shared_lens[g], (int64_t)P.max_pages << P.c.page_shift)) & ~15);
+}
+__device__ __forceinline__ int request_at(const Kv4AttnParams& P, int g) { return min(max(P.group_cu[g], 0), P.R); }
+__device__ __forceinline__ Piece group_piece_of(const Kv4AttnParams& P, int number, int width) {
+  Piece x;
+  x.s = bbm::find_piece_of([&](int g) __attribute__((always_inline)) { return P.cu[request_at(P, g)]; }, P.S, P.T, P.G, width, number);
+  x.len = x.s.end > x.s.begin ? shared_of(P, x.s.r) : 0;
+  x.s.r = min((int)scalar(request_at(P, x.s.r)), P.R - 1);  // (the first request's row of the table)
+  x.cols = (x.s.end - x.s.begin) * P.G;
+  x.col0 = x.s.piece * width;
+  x.prefix = x.len;
+  x.from = 0;
+  x.group_parts = 0;
+  cut_keys<true>(P, x, P.group_parts, P.group_part_keys);
+  if (x.len == 0) x.s.end = x.s.begin;  // nothing to do
+  return x;
+}
+// The group of request r, -1 if it has none; 64 groups at a time.
+__device__ __forceinline__ int group_of(const Kv4AttnParams& P, int r) {
+  const int lane = threadIdx.x & 63;
+  for (int g0 = 0; g0 < P.S; g0 += 64) {
+    const int g = min(g0 + lane, P.S - 1);
+    const uint64_t has = __ballot(P.group_cu[g] <= r && r < P.group_cu[g + 1]);
+    if (has) return min(g0 + __ffsll((unsigned long long)has) - 1, P.S - 1);
+  }
+  return -1;
+}
+template <bool SHARED>
 __device__ __forceinline__ Piece piece_of(const Kv4AttnParams& P, int number, int width) {
   Piece x;
   x.s = bbm::find_piece(P.cu, P.R, P.T, P.G, width, number);
@@ -58,8 +120,19 @@ __device__ __forceinline__ Piece piece_of(const Kv4AttnParams& P, int number, in
   x.col0 = x.s.piece * width;
   x.prefix = (int)((uint32_t)len - (uint32_t)max(0, c1 - c0) + (P.mask ? 0u : (uint32_t)x.s.begin - (uint32_t)c0));
   x.len = (int)max((int64_t)0, min((int64_t)len, (int64_t)P.max_pages << P.c.page_shift));
-  x.keys = max(P.part_keys, (int)(((int64_t)x.len + P.parts - 1) / P.parts + kStep - 1) / kStep * kStep);
-  x.parts = x.len > 0 ? (x.len - 1) / x.keys + 1 : 1;
+  x.from = 0;
+  x.group_parts = 0;
+  if constexpr (SHARED) {
+    const int g = group_of(P, x.s.r), shared = g >= 0 ? shared_of(P, g) : 0;
+    if (shared > 0) {
+      Piece all;
+      all.len = shared, all.from = 0;
+      cut_keys<true>(P, all, P.group_parts, P.group_part_keys);
+      x.group_parts = all.parts;
+      x.from = min(shared, x.len);
+    }
+  }
+  cut_keys<SHARED>(P, x, P.parts, P.part_keys);
   return x;
 }
 
@@ -81,10 +154,25 @@ __device__ __forceinline__ float other_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-template <int D>
-__device__ __forceinline__ float* record_of(const Kv4AttnParams& P, int number, int hk, int part) {
-  return P.partials + (((int64_t)number * P.c.Hk + hk) * P.parts + part) * (P.width * (D + 2));
+// Where a part's sums of column c of its piece lie, and their (maximum, sum).
+struct Record {
+  float *sums, *pair;
+};
+template <int D, bool SHARED>
+__device__ __forceinline__ Record record_of(const Kv4AttnParams& P, const Piece& x, int number, int hk, int part, int c) {
+  if constexpr (SHARED) {  // (part: a group's parts, then the request's)
+    const int64_t all = (int64_t)P.T * P.G, at = ((int64_t)part * P.c.Hk + hk) * all + (int64_t)x.s.begin * P.G + x.col0 + c;
+    return {P.partials + at * D, P.partials + (P.group_parts + P.parts) * P.c.Hk * all * D + 2 * at};
+  }
+  float* const rec = P.partials + (((int64_t)number * P.c.Hk + hk) * P.parts + part) * (P.width * (D + 2));
+  return {rec + c * D, rec + P.width * D + 2 * c};
 }
+
+// Whether a piece's columns are done with this part; the place of its record among the others of a column.
+template <bool SHARED>
+__device__ __forceinline__ bool alone(const Piece& x, const Item& item) { return x.parts == 1 && !(SHARED && (item.group || x.group_parts > 0)); }
+template <bool SHARED>
+__device__ __forceinline__ int slot_of(const Kv4AttnParams& P, const Item& item) { return item.part + (SHARED && !item.group ? P.group_parts : 0); }
 
 // Which of the keys j0 .. j0 + 63 new token i of the request may see, as far as its order or the mask goes.
 __device__ __forceinline__ uint64_t seen_from(const Kv4AttnParams& P, const Piece& x, int i, int j0) {
@@ -111,7 +199,7 @@ __device__ __forceinline__ void put_column(const Kv4AttnParams& P, const Piece& 
   if (P.lse && e0 == 0) P.lse[(int64_t)h * P.T + t] = l > 0.0f ? bbm::log_sum(m, l, P.rc) : -INFINITY;
 }
 
-template <int D>
+template <int D, bool SHARED>
 __global__ __launch_bounds__(64 * NW, D == 128 ? 3 : 5) void kv4_narrow_kernel(const Kv4AttnParams P) {
   constexpr int KD = D / 4;        // elements of K a lane loads of its key
   constexpr int KS = D / 32;       // steps of the first product
@@ -122,11 +210,12 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 3 : 5) void kv4_narrow_kernel(c
 
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, kq = lane >> 4;
   const int wave = (int)scalar(tid >> 6);
-  const int at = bbm::logical_wg(blockIdx.x, gridDim.x);
-  const int number = at % P.pieces, rest = at / P.pieces, part = rest % P.parts, hk = rest / P.parts;
-  const Piece x = piece_of(P, number, 16);
+  const Item item = item_of<SHARED>(P);
+  if (SHARED && item.none) return;
+  const int number = item.number, part = item.part, hk = item.hk;
+  const Piece x = SHARED && item.group ? group_piece_of(P, number, 16) : piece_of<SHARED>(P, number, 16);
   if (x.s.end <= x.s.begin || part >= x.parts) return;
-  const int first = part * x.keys, last = first + min(x.keys, x.len - first);
+  const int first = (SHARED ? x.from : 0) + part * x.keys, last = first + min(x.keys, x.len - first);
 
   // this lane's column: Q as operands, how far it sees (columns behind the last repeat it; they are not written)
   const int my_i = min(x.col0 + n, x.cols - 1) / P.G, my_h = hk * P.G + (min(x.col0 + n, x.cols - 1) - my_i * P.G), my_t = x.s.begin + my_i;
@@ -291,19 +380,19 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 3 : 5) void kv4_narrow_kernel(c
 #pragma unroll
     for (int e = 0; e < VD; ++e) v[e] += f * o_s[w][c][e0 + e];
   }
-  if (x.parts == 1) {
+  if (alone<SHARED>(x, item)) {
     put_column<D>(P, x, hk, col, e0, v, m, sum);
   } else {
-    float* const rec = record_of<D>(P, number, hk, part);
+    const Record rec = record_of<D, SHARED>(P, x, number, hk, slot_of<SHARED>(P, item), c);
 #pragma unroll
-    for (int e = 0; e < VD; e += 4) *reinterpret_cast<f32x4*>(rec + c * D + e0 + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
-    if (e0 == 0) *reinterpret_cast<float2*>(rec + P.width * D + 2 * c) = make_float2(m, sum);
+    for (int e = 0; e < VD; e += 4) *reinterpret_cast<f32x4*>(rec.sums + e0 + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+    if (e0 == 0) *reinterpret_cast<float2*>(rec.pair) = make_float2(m, sum);
   }
 }
 
 // 128 columns of a piece, a wave 32 of them, one lane a column, with the products of the kernels for prompts: the codes of 64 keys at a time are converted once
 // for all of them, on their way to LDS, where the tile is read as keys and values in bf16 are.
-template <int D>
+template <int D, bool SHARED>
 __global__ __launch_bounds__(64 * NW, 2) void kv4_wide_kernel(const Kv4AttnParams P) {
   using L = bbm::TL<D>;
   constexpr int KS = D / 16, DB = D / 32, RC = D / 8, RPB = 64 / RC;
@@ -316,11 +405,12 @@ __global__ __launch_bounds__(64 * NW, 2) void kv4_wide_kernel(const Kv4AttnParam
 
   const int tid = threadIdx.x, lane = tid & 63, lq = lane & 31, hh = lane >> 5;
   const int wave = (int)scalar(tid >> 6);
-  const int at = bbm::logical_wg(blockIdx.x, gridDim.x);
-  const int number = at % P.pieces, rest = at / P.pieces, part = rest % P.parts, hk = rest / P.parts;
-  const Piece x = piece_of(P, number, 128);
+  const Item item = item_of<SHARED>(P);
+  if (SHARED && item.none) return;
+  const int number = item.number, part = item.part, hk = item.hk;
+  const Piece x = SHARED && item.group ? group_piece_of(P, number, 128) : piece_of<SHARED>(P, number, 128);
   if (x.s.end <= x.s.begin || part >= x.parts) return;
-  const int first = part * x.keys, last = first + min(x.keys, x.len - first);
+  const int first = (SHARED ? x.from : 0) + part * x.keys, last = first + min(x.keys, x.len - first);
   const int n_tiles = (last - first + 63) / 64;
 
   const int wcol = x.col0 + 32 * wave, my_col = min(wcol + lq, x.cols - 1), my_i = my_col / P.G, my_h = hk * P.G + (my_col - my_i * P.G);
@@ -478,16 +568,15 @@ __global__ __launch_bounds__(64 * NW, 2) void kv4_wide_kernel(const Kv4AttnParam
   __syncthreads();  // the result is staged in the tile buffers
   if (wcols == 0) return;
   const float l = other_sum<32>(l_run);
-  if (x.parts > 1) {
-    float* const rec = record_of<D>(P, number, hk, part);
+  if (!alone<SHARED>(x, item)) {
     if (lq < wcols) {
-      const int c = 32 * wave + lq;
+      const Record rec = record_of<D, SHARED>(P, x, number, hk, slot_of<SHARED>(P, item), 32 * wave + lq);
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<f32x4*>(rec + c * D + 32 * db + 8 * g + 4 * hh) = f32x4{oacc[db][4 * g], oacc[db][4 * g + 1], oacc[db][4 * g + 2], oacc[db][4 * g + 3]};
-      if (hh == 0) *reinterpret_cast<float2*>(rec + P.width * D + 2 * c) = make_float2(top.m, l);
+          *reinterpret_cast<f32x4*>(rec.sums + 32 * db + 8 * g + 4 * hh) = f32x4{oacc[db][4 * g], oacc[db][4 * g + 1], oacc[db][4 * g + 2], oacc[db][4 * g + 3]};
+      if (hh == 0) *reinterpret_cast<float2*>(rec.pair) = make_float2(top.m, l);
     }
     return;
   }
@@ -512,27 +601,30 @@ __global__ __launch_bounds__(64 * NW, 2) void kv4_wide_kernel(const Kv4AttnParam
 
 // Joins the parts of a piece's columns in a fixed order, 16 lanes a column.  With many parts (SIDE = 4) a wave takes one column and four parts side by
 // side, whose sums meet at the end; with few, a column for every 16 lanes: a wave costs more to start than to add up four records.
-template <int D, int SIDE>
+template <int D, int SIDE, bool SHARED>
 __global__ __launch_bounds__(256) void kv4_join_kernel(const Kv4AttnParams P) {
   constexpr int VD = D / 16;
   const int lane = threadIdx.x & 63, number = blockIdx.x, hk = blockIdx.y, e0 = (lane & 15) * VD;
   const int c = SIDE == 4 ? 4 * blockIdx.z + (threadIdx.x >> 6) : 16 * blockIdx.z + (threadIdx.x >> 4);
-  const Piece x = piece_of(P, number, P.width);
-  if (x.s.end <= x.s.begin || x.parts == 1 || x.col0 + c >= x.cols) return;
-  const int64_t stride = (int64_t)P.width * (D + 2);
-  const float* const rec = record_of<D>(P, number, hk, 0);
+  const Piece x = piece_of<SHARED>(P, number, SHARED ? (SIDE == 4 ? 4 : 16) : P.width);
+  const int parts = x.parts + x.group_parts;
+  if (x.s.end <= x.s.begin || parts == 1 || x.col0 + c >= x.cols) return;
+  // (a part's records are `stride` apart, its pairs `pairs`; a request's own lie behind all that a group may have)
+  const Record rec = record_of<D, SHARED>(P, x, number, hk, 0, c);
+  const int64_t stride = SHARED ? P.c.Hk * ((int64_t)P.T * P.G) * D : (int64_t)P.width * (D + 2), pairs = SHARED ? P.c.Hk * ((int64_t)P.T * P.G) * 2 : stride;
+  auto slot = [&](int p) { return SHARED && p >= x.group_parts ? p - x.group_parts + P.group_parts : p; };
   float m = -INFINITY, l = 0.0f, v[VD] = {};
 #pragma unroll 1
-  for (int p = SIDE == 4 ? lane >> 4 : 0; p < x.parts; p += 4 * SIDE) {  // four records' loads in flight
+  for (int p = SIDE == 4 ? lane >> 4 : 0; p < parts; p += 4 * SIDE) {  // four records' loads in flight
     float2 ml[4];
     f32x4 y[4][VD / 4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float* const r = rec + min(p + SIDE * i, x.parts - 1) * stride;
-      ml[i] = *reinterpret_cast<const float2*>(r + P.width * D + 2 * c);
-      if (p + SIDE * i >= x.parts) ml[i] = make_float2(-INFINITY, 0.0f);
+      const int at = slot(min(p + SIDE * i, parts - 1));
+      ml[i] = *reinterpret_cast<const float2*>(rec.pair + at * pairs);
+      if (p + SIDE * i >= parts) ml[i] = make_float2(-INFINITY, 0.0f);
 #pragma unroll
-      for (int e = 0; e < VD / 4; ++e) y[i][e] = *reinterpret_cast<const f32x4*>(r + c * D + e0 + 4 * e);
+      for (int e = 0; e < VD / 4; ++e) y[i][e] = *reinterpret_cast<const f32x4*>(rec.sums + at * stride + e0 + 4 * e);
     }
     const float m_new = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m), m_fin = m_new == -INFINITY ? 0.0f : m_new;
     const float keep = bbm::weight(m, m_fin, P.rc);
@@ -592,10 +684,10 @@ inline bool sizes_ok(int64_t T, int64_t R, int64_t H, int64_t Hk, int64_t max_le
 template <int D>
 void launch(const Kv4AttnParams& P, hipStream_t s) {
   const unsigned wgs = (unsigned)((int64_t)P.pieces * P.c.Hk * P.parts);
-  if (P.width == 16) kv4_narrow_kernel<D><<<wgs, 64 * NW, 0, s>>>(P);
-  else kv4_wide_kernel<D><<<wgs, 64 * NW, 0, s>>>(P);
-  if (P.parts > 4) kv4_join_kernel<D, 4><<<dim3((unsigned)P.pieces, (unsigned)P.c.Hk, (unsigned)P.width / 4), 256, 0, s>>>(P);
-  else if (P.parts > 1) kv4_join_kernel<D, 1><<<dim3((unsigned)P.pieces, (unsigned)P.c.Hk, (unsigned)P.width / 16), 256, 0, s>>>(P);
+  if (P.width == 16) kv4_narrow_kernel<D, false><<<wgs, 64 * NW, 0, s>>>(P);
+  else kv4_wide_kernel<D, false><<<wgs, 64 * NW, 0, s>>>(P);
+  if (P.parts > 4) kv4_join_kernel<D, 4, false><<<dim3((unsigned)P.pieces, (unsigned)P.c.Hk, (unsigned)P.width / 4), 256, 0, s>>>(P);
+  else if (P.parts > 1) kv4_join_kernel<D, 1, false><<<dim3((unsigned)P.pieces, (unsigned)P.c.Hk, (unsigned)P.width / 16), 256, 0, s>>>(P);
 }
 
 }  // namespace
@@ -606,6 +698,56 @@ extern "C" __attribute__((visibility("default"))) size_t bbm_kv4_attn_workspace_
   return p.parts == 1 ? 0 : (size_t)(p.pieces * Hk * p.parts * p.width * (d + 2)) * sizeof(float);
 }
 
+namespace {
+
+// A call's arguments as both entry points have them.
+struct Call {
+  const bbm_packed *q, *o;
+  float* lse;
+  int64_t T, R;
+  const int32_t *cu, *lens, *table;
+  int64_t table_stride, max_pages;
+  const uint64_t* mask;
+  int64_t mask_words;
+  const bbm_kv4_cache* cache;
+  int64_t H;
+  float softmax_scale;
+  void* workspace;
+  size_t workspace_bytes;
+};
+int check_call(const char* fn, const Call& a) {
+  using namespace bbm;
+  if (int rc = check_kv4(fn, a.cache)) return rc;
+  if (int rc = check_tokens(fn, a.T, a.R, a.cu, a.H, a.cache->Hk)) return rc;
+  if (int rc = check_packed(fn, "q", a.q, a.T, a.H, a.cache->d, false)) return rc;
+  if (int rc = check_packed(fn, "o", a.o, a.T, a.H, a.cache->d, true)) return rc;
+  if (!aligned(a.lse, 4)) return fail(BBM_EINVAL, "%s: lse must be 4-byte aligned", fn);
+  if (int rc = check_table(fn, a.lens, a.table, a.table_stride, a.max_pages, a.cache->page)) return rc;
+  if (int rc = check_mask(fn, a.mask, a.mask_words)) return rc;
+  if (a.T * (a.H / a.cache->Hk) > kMaxTokens) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld)", fn, (long long)a.T, (long long)a.H);
+  return check_scale(fn, a.softmax_scale);
+}
+int check_workspace(const char* fn, const Call& a, size_t need) {
+  using namespace bbm;
+  if (need > 0 && (!a.workspace || a.workspace_bytes < need))
+    return fail(BBM_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, a.workspace ? a.workspace_bytes : (size_t)0);
+  if (!aligned(a.workspace, 16)) return fail(BBM_EINVAL, "%s: workspace must be 16-byte aligned", fn);
+  return BBM_OK;
+}
+Kv4AttnParams params_of(const Call& a) {
+  using namespace bbm;
+  Kv4AttnParams P = {};
+  P.c = kv4_of(a.cache);
+  P.q = static_cast<const __bf16*>(a.q->ptr), P.o = static_cast<__bf16*>(a.o->ptr), P.lse = a.lse;
+  P.q_row = a.q->row_stride, P.q_head = a.q->head_stride, P.o_row = a.o->row_stride, P.o_head = a.o->head_stride, P.table_stride = a.table_stride;
+  P.cu = a.cu, P.lens = a.lens, P.table = a.table, P.mask = a.mask, P.partials = static_cast<float*>(a.workspace);
+  P.T = (int32_t)a.T, P.R = (int32_t)a.R, P.G = (int32_t)(a.H / a.cache->Hk), P.max_pages = (int32_t)a.max_pages, P.mask_words = (int32_t)a.mask_words;
+  P.rc = a.softmax_scale * kLog2e, P.lazy = kLazy / P.rc;
+  return P;
+}
+
+}  // namespace
+
 extern "C" __attribute__((visibility("default"))) int bbm_kv4_attn(const bbm_packed* q, const bbm_packed* o, float* lse, int64_t T, int64_t R, const int32_t* cu,
                                                                    const int32_t* lens, const int32_t* block_table, int64_t table_stride, int64_t max_pages,
                                                                    const uint64_t* mask, int64_t mask_words, const bbm_kv4_cache* cache, int64_t H,
@@ -613,37 +755,93 @@ extern "C" __attribute__((visibility("default"))) int bbm_kv4_attn(const bbm_pac
   using namespace bbm;
   const char* fn = "bbm_kv4_attn";
   clear_error();
-  if (int rc = check_kv4(fn, cache)) return rc;
-  if (int rc = check_tokens(fn, T, R, cu, H, cache->Hk)) return rc;
-  if (int rc = check_packed(fn, "q", q, T, H, cache->d, false)) return rc;
-  if (int rc = check_packed(fn, "o", o, T, H, cache->d, true)) return rc;
-  if (!lens || !aligned(lens, 4) || !block_table || !aligned(block_table, 4)) return fail(BBM_EINVAL, "%s: lens and block_table must be non-NULL 4-byte aligned pointers", fn);
-  if (!aligned(lse, 4) || !aligned(mask, 8)) return fail(BBM_EINVAL, "%s: lse must be 4-byte aligned, mask 8-byte aligned", fn);
-  if (max_pages < 1 || table_stride < max_pages || max_len < 1)
-    return fail(BBM_EINVAL, "%s: max_pages=%lld, max_len=%lld must be >= 1, table_stride=%lld no less than max_pages", fn, (long long)max_pages, (long long)max_len, (long long)table_stride);
-  if (mask ? mask_words < 1 : mask_words != 0) return fail(BBM_EINVAL, "%s: mask_words=%lld does not fit the mask", fn, (long long)mask_words);
-  if (T * (H / cache->Hk) > kMaxTokens) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld)", fn, (long long)T, (long long)H);
-  if (max_pages > kMaxTokens / cache->page || mask_words > (1 << 20)) return fail(BBM_EUNSUPPORTED, "%s: max_pages=%lld or mask_words=%lld is too large", fn, (long long)max_pages, (long long)mask_words);
-  if (int rc = check_scale(fn, softmax_scale)) return rc;
+  const Call a{q, o, lse, T, R, cu, lens, block_table, table_stride, max_pages, mask, mask_words, cache, H, softmax_scale, workspace, workspace_bytes};
+  if (int rc = check_call(fn, a)) return rc;
+  if (max_len < 1) return fail(BBM_EINVAL, "%s: max_len=%lld must be >= 1", fn, (long long)max_len);
   const size_t need = bbm_kv4_attn_workspace_bytes(T, R, H, cache->Hk, cache->d, max_len);
-  if (need > 0 && (!workspace || workspace_bytes < need))
-    return fail(BBM_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, workspace ? workspace_bytes : (size_t)0);
-  if (!aligned(workspace, 16)) return fail(BBM_EINVAL, "%s: workspace must be 16-byte aligned", fn);
+  if (int rc = check_workspace(fn, a, need)) return rc;
   if (T == 0) return BBM_OK;
   if (int rc = check_apart(fn, {o->ptr, lse, need > 0 ? workspace : nullptr}, {q->ptr, cu, lens, block_table, mask, cache->k, cache->k_scale, cache->v, cache->v_scale})) return rc;
-  Kv4AttnParams P;
-  P.c = kv4_of(cache);
-  P.q = static_cast<const __bf16*>(q->ptr), P.o = static_cast<__bf16*>(o->ptr), P.lse = lse;
-  P.q_row = q->row_stride, P.q_head = q->head_stride, P.o_row = o->row_stride, P.o_head = o->head_stride, P.table_stride = table_stride;
-  P.cu = cu, P.lens = lens, P.table = block_table, P.mask = mask;
-  P.T = (int32_t)T, P.R = (int32_t)R, P.G = (int32_t)(H / cache->Hk), P.max_pages = (int32_t)max_pages, P.mask_words = (int32_t)mask_words;
-  P.rc = softmax_scale * kLog2e, P.lazy = kLazy / P.rc;
+  Kv4AttnParams P = params_of(a);
   const Plan p = plan_of(T, R, P.G, cache->Hk, std::min<int64_t>(max_len, bbm::kMaxTokens));
   if (p.pieces >= kMaxWgs || p.pieces * cache->Hk * p.parts >= kMaxWgs) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, R=%lld, H=%lld)", fn, (long long)T, (long long)R, (long long)H);
-  P.partials = static_cast<float*>(workspace);
   P.width = p.width, P.pieces = (int32_t)p.pieces, P.parts = (int32_t)p.parts, P.part_keys = (int32_t)p.part_keys;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (cache->d == 64) launch<64>(P, s);
   else launch<128>(P, s);
+  return launch_status(fn);
+}
+
+namespace {
+
+// Of a call with shared prefixes: the groups' cut and the requests'.
+struct SharedPlan {
+  Plan group, own;
+};
+inline SharedPlan shared_plan_of(int64_t T, int64_t R, int64_t S, int64_t G, int64_t Hk, int64_t max_shared, int64_t max_own) {
+  SharedPlan p;
+  p.own = plan_of(T, R, G, Hk, max_own);
+  p.group = plan_of(T, std::max<int64_t>(S, 1), G, Hk, max_shared);
+  if (S == 0) p.group.pieces = 0, p.group.parts = 0;
+  return p;
+}
+inline size_t shared_workspace(const SharedPlan& p, int64_t T, int64_t H, int d) {
+  return p.group.parts + p.own.parts <= 1 ? 0 : (size_t)((p.group.parts + p.own.parts) * T * H) * (size_t)(d + 2) * sizeof(float);
+}
+
+template <int D>
+void launch_shared(Kv4AttnParams P, const SharedPlan& p, hipStream_t s) {
+  const int64_t group = p.group.pieces * P.c.Hk * p.group.parts, own = p.own.pieces * P.c.Hk * p.own.parts;
+  auto go = [&](int width, int64_t group_wgs, int64_t own_wgs) {
+    P.group_wgs = (int32_t)group_wgs, P.own_wgs = (int32_t)own_wgs;
+    const unsigned wgs = (unsigned)(((group_wgs + 7) & ~7ll) + own_wgs);
+    if (width == 16) kv4_narrow_kernel<D, true><<<wgs, 64 * NW, 0, s>>>(P);
+    else kv4_wide_kernel<D, true><<<wgs, 64 * NW, 0, s>>>(P);
+  };
+  if (group > 0 && p.group.width != p.own.width) go(p.group.width, group, 0), go(p.own.width, 0, own);
+  else go(p.own.width, group, own);
+  if (p.group.parts + p.own.parts > 4)
+    kv4_join_kernel<D, 4, true><<<dim3((unsigned)bbm::count_pieces(P.T, P.R, P.G, 4), (unsigned)P.c.Hk), 256, 0, s>>>(P);
+  else if (p.group.parts + p.own.parts > 1)
+    kv4_join_kernel<D, 1, true><<<dim3((unsigned)bbm::count_pieces(P.T, P.R, P.G, 16), (unsigned)P.c.Hk), 256, 0, s>>>(P);
+}
+
+}  // namespace
+
+extern "C" __attribute__((visibility("default"))) size_t bbm_kv4_shared_attn_workspace_bytes(int64_t T, int64_t R, int64_t S, int64_t H, int64_t Hk, int d, int64_t max_shared,
+                                                                                             int64_t max_own) {
+  if (!sizes_ok(T, R, H, Hk, std::min(max_shared, max_own)) || S < 0 || S > R || (d != 64 && d != 128)) return 0;
+  return shared_workspace(shared_plan_of(T, R, S, H / Hk, Hk, std::min<int64_t>(max_shared, bbm::kMaxTokens), std::min<int64_t>(max_own, bbm::kMaxTokens)), T, H, d);
+}
+
+extern "C" __attribute__((visibility("default"))) int bbm_kv4_shared_attn(const bbm_packed* q, const bbm_packed* o, float* lse, int64_t T, int64_t R, const int32_t* cu,
+                                                                          const int32_t* lens, const int32_t* block_table, int64_t table_stride, int64_t max_pages, int64_t S,
+                                                                          const int32_t* group_cu, const int32_t* shared_lens, const uint64_t* mask, int64_t mask_words,
+                                                                          const bbm_kv4_cache* cache, int64_t H, float softmax_scale, int64_t max_shared, int64_t max_own,
+                                                                          void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace bbm;
+  const char* fn = "bbm_kv4_shared_attn";
+  clear_error();
+  const Call a{q, o, lse, T, R, cu, lens, block_table, table_stride, max_pages, mask, mask_words, cache, H, softmax_scale, workspace, workspace_bytes};
+  if (int rc = check_call(fn, a)) return rc;
+  if (int rc = check_groups(fn, R, S, group_cu, shared_lens, max_shared, max_own)) return rc;
+  const size_t need = bbm_kv4_shared_attn_workspace_bytes(T, R, S, H, cache->Hk, cache->d, max_shared, max_own);
+  if (int rc = check_workspace(fn, a, need)) return rc;
+  if (T == 0) return BBM_OK;
+  if (int rc = check_apart(fn, {o->ptr, lse, need > 0 ? workspace : nullptr},
+                           {q->ptr, cu, lens, block_table, mask, cache->k, cache->k_scale, cache->v, cache->v_scale, S > 0 ? group_cu : nullptr, S > 0 ? shared_lens : nullptr}))
+    return rc;
+  Kv4AttnParams P = params_of(a);
+  const SharedPlan p = shared_plan_of(T, R, S, P.G, cache->Hk, std::min<int64_t>(max_shared, kMaxTokens), std::min<int64_t>(max_own, kMaxTokens));
+  for (const Plan& x : {p.group, p.own})
+    if (x.pieces >= kMaxWgs || x.pieces * cache->Hk * std::max<int64_t>(x.parts, 1) >= kMaxWgs / 2)
+      return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, R=%lld, H=%lld)", fn, (long long)T, (long long)R, (long long)H);
+  if (count_pieces(T, R, P.G, 4) * cache->Hk >= kMaxWgs) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, R=%lld, H=%lld)", fn, (long long)T, (long long)R, (long long)H);
+  P.width = p.own.width, P.pieces = (int32_t)p.own.pieces, P.parts = (int32_t)p.own.parts, P.part_keys = (int32_t)p.own.part_keys;
+  P.S = (int32_t)S, P.group_cu = group_cu, P.shared_lens = shared_lens;
+  P.group_pieces = (int32_t)p.group.pieces, P.group_parts = (int32_t)p.group.parts, P.group_part_keys = (int32_t)p.group.part_keys;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (cache->d == 64) launch_shared<64>(P, p, s);
+  else launch_shared<128>(P, p, s);
   return launch_status(fn);
 }

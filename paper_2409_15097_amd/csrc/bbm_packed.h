@@ -82,7 +82,9 @@ __device__ __forceinline__ int wave_prefix_sum(int x) {
 // factor of 64 in R, and there are holes.  Counted / searched, us: one token each of 200 requests of up to 300 keys 19.5 / 20.7; forward over 100, 300, 500 sequences of
 // up to 100 tokens 11.9 / 12.6, 27.6 / 27.8, 44.3 / 43.3, over 600 and 1000 54.6 / 50.2, 93 / 79.
 constexpr int kCounted = 512;
-__device__ __forceinline__ Span find_piece(const int32_t* __restrict__ cu, int R, int T, int mul, int unit, int at) {
+// `cu` gives offset r of R + 1, by cu(r).
+template <typename Offsets>
+__device__ __forceinline__ Span find_piece_of(Offsets cu, int R, int T, int mul, int unit, int at) {
   const int lane = threadIdx.x & 63;
   auto cut = [&](int c) { return min(max(c, 0), T); };
   Span s;
@@ -107,7 +109,7 @@ __device__ __forceinline__ Span find_piece(const int32_t* __restrict__ cu, int R
     };
     if (R <= 64) {
       const int r = min(lane, R - 1);
-      among(0, cu[r], cu[r + 1]);
+      among(0, cu(r), cu(r + 1));
       return s;
     }
     for (int r0 = 0; r0 < R; r0 += 256) {  // (four times 64 in one trip to memory)
@@ -115,7 +117,7 @@ __device__ __forceinline__ Span find_piece(const int32_t* __restrict__ cu, int R
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int r = min(r0 + 64 * i + lane, R - 1);
-        c0[i] = cu[r], c1[i] = cu[r + 1];
+        c0[i] = cu(r), c1[i] = cu(r + 1);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -128,13 +130,13 @@ __device__ __forceinline__ Span find_piece(const int32_t* __restrict__ cu, int R
   while (n > 1) {
     const int step = (n + 63) / 64;
     const int r = lo + lane * step;
-    const bool ok = lane * step < n && first(cu[min(r, R)], r) <= at;
+    const bool ok = lane * step < n && first(cu(min(r, R)), r) <= at;
     const int hits = __popcll(__ballot(ok));
     const int k = max(0, hits - 1) * step;
     lo += k;
     n = min(step, n - k);
   }
-  const int c0 = cu[lo], c1 = cu[lo + 1];
+  const int c0 = cu(lo), c1 = cu(lo + 1);
   s.r = __builtin_amdgcn_readfirstlane(lo);
   s.begin = __builtin_amdgcn_readfirstlane(cut(c0));
   s.end = __builtin_amdgcn_readfirstlane(max(cut(c0), cut(c1)));
@@ -143,6 +145,9 @@ __device__ __forceinline__ Span find_piece(const int32_t* __restrict__ cu, int R
   s.piece = __builtin_amdgcn_readfirstlane(real ? (int)piece : 0);
   if (__builtin_amdgcn_readfirstlane(real) == 0) s.end = s.begin;
   return s;
+}
+__device__ __forceinline__ Span find_piece(const int32_t* __restrict__ cu, int R, int T, int mul, int unit, int at) {
+  return find_piece_of([=](int r) __attribute__((always_inline)) { return cu[r]; }, R, T, mul, unit, at);
 }
 inline int64_t count_pieces(int64_t T, int64_t R, int64_t mul, int64_t unit) { return T * mul / unit + R; }
 

@@ -1,0 +1,135 @@
+"""GPU: the operators on the cache of many and long answers against their definitions in 64 bits (oracle/tokens.py), at the sizes, groups and masks where they can go wrong.
+Tolerances are the bounds derived there from the roundings that the kernels make."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_tokens import cached_case, check_cached, f64, i32
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def bbm():
+    import paper_2409_15097_amd as m
+    return m
+
+
+# ---- attention behind shared prefixes
+
+
+class Behind:
+    """bbm_kv4_attn by way of the groups."""
+
+    def __init__(self, bbm, group_cu, shared):
+        self.bbm, self.groups = bbm, (None if group_cu is None else i32(group_cu), None if shared is None else i32(shared))
+        self.kv4_cache = bbm.kv4_cache
+
+    def bbm_kv4_attn(self, q, cache, table, lens, cu, **kw):
+        return self.bbm.bbm_kv4_shared_attn(q, cache, table, lens, cu, *self.groups, **kw)
+
+
+def grouped_case(bbm, group_cu, shared, lens, news, H, Hk, d, page, **kw):
+    """cached_case whose groups have the pages of their shared keys in common (a page that they share in part is each request's own)."""
+    case = cached_case(bbm, lens, news, H, Hk, d, page, **kw)
+    table = case[1]
+    for g, n in enumerate(shared):
+        first = group_cu[g]
+        for r in range(first + 1, group_cu[g + 1]):
+            table[r, :max(0, n) // page] = table[first, :max(0, n) // page]
+    return case
+
+
+def check_grouped(bbm, group_cu, shared, lens, news, H, Hk, d, page, hints=({},), **kw):
+    c, table, cu, T, q, words = grouped_case(bbm, group_cu, shared, lens, news, H, Hk, d, page, **kw)
+    by = Behind(bbm, group_cu, shared)
+    for hint in hints:
+        a = check_cached(by, c, table, lens, cu, T, q, words, H, Hk, d, page, **hint)
+        b = check_cached(by, c, table, lens, cu, T, q, words, H, Hk, d, page, **hint)
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+    return c, table, cu, T, q, words
+
+
+NEAR = [{}, dict(max_shared=300, max_own=40)]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("group_cu, shared, lens, news, H, Hk, page, layout, tree", [
+    ([0, 1], [16], [17], [1], 1, 1, 16, "plain", None),
+    ([0, 4], [48], [49, 60, 52, 100], [1] * 4, 8, 2, 16, "fused", None),
+    ([1, 3, 3, 6], [37, 500, 130], [20, 40, 38, 131, 150, 300, 9], [1, 2, 1, 1, 0, 5, 3], 6, 2, 32, "heads", None),     # alone in front and behind, a group of nobody, keys that end inside a page
+    ([0, 2, 5], [0, -3], [30, 1, 70, 0, 2], [1, 1, 9, 0, 2], 4, 4, 16, "plain", None),                                     # nothing is shared
+    ([0, 3], [15], [20, 19, 16], [1, 4, 1], 4, 1, 16, "plain", None),                                                        # less than a block
+    ([0, 3], [200], [206, 230, 204], [6, 30, 4], 3, 1, 64, "plain", 1),
+    ([0, 2, 4], [128, 64], [200, 270, 150, 64], [70, 129, 66, 0], 5, 1, 128, "heads", 2),
+    ([0, 30], [96], [100 + i for i in range(30)], [1 + i % 3 for i in range(30)], 16, 2, 32, "plain", None),
+    ([0, 2], [2304], [2400, 2310], [3, 1], 12, 4, 64, "fused", None)])
+def test_shared(bbm, group_cu, shared, lens, news, H, Hk, d, page, layout, tree):
+    check_grouped(bbm, group_cu, shared, lens, news, H, Hk, d, page, hints=NEAR, layout=layout, tree=tree, seed=len(lens), before=2, behind=3)
+
+
+@pytest.mark.parametrize("d, H, Hk, tree", [(64, 64, 8, None), (128, 64, 8, None), (128, 64, 16, 1), (64, 40, 40, None)])
+def test_shared_by_many_columns(bbm, d, H, Hk, tree):
+    """The kernel of many columns for the groups, in parts; alone and beside requests of few and of many."""
+    for lens, news in (([2100, 2088], [60, 70]), ([1100 + i for i in range(40)], [1 + i % 15 for i in range(40)])):
+        check_grouped(bbm, [0, len(lens)], [1072 if len(lens) > 2 else 2016], lens, news, H, Hk, d, 16, hints=[{}, dict(max_shared=2048, max_own=100)], tree=tree, seed=9, before=1, behind=2)
+
+
+def test_shared_by_one_and_by_many_requests(bbm):
+    """More requests, and more groups, than are counted or read at once."""
+    R = 600
+    check_grouped(bbm, [0, R], [32], [33 + i % 9 for i in range(R)], [1] * R, 2, 1, 64, 16)
+    check_grouped(bbm, list(range(0, R + 1, 8)), [16 * (i % 3) for i in range(75)], [33 + i % 9 for i in range(R)], [1] * R, 2, 1, 64, 16)
+    check_grouped(bbm, list(range(R + 1)), [16 * (i % 3) for i in range(R)], [33 + i % 9 for i in range(R)], [1] * R, 2, 1, 64, 16)
+
+
+def test_shared_pages_outside_and_a_narrow_table(bbm):
+    group_cu, shared, lens, news, H, Hk, d, page = [0, 2, 4], [256, 64], [500, 300, 90, 70], [1, 3, 2, 1], 4, 2, 128, 32
+    c, table, cu, T, q, _ = grouped_case(bbm, group_cu, shared, lens, news, H, Hk, d, page, seed=3)
+    table[:2, 3], table[0, 15], table[2:, 0], table[3, 2] = -1, 1 << 30, c.k.shape[0], -5
+    by = Behind(bbm, group_cu, shared)
+    check_cached(by, c, table, lens, cu, T, q, None, H, Hk, d, page)
+    check_cached(by, c, table[:, :9], lens, cu, T, q, None, H, Hk, d, page)
+    # a prefix that ends behind the table, and one of which no page is there: the queries behind it see what is left, or nothing
+    check_cached(by, c, table[:, :5], [700, 600, 90, 70], cu, T, q, None, H, Hk, d, page)
+    gone = table.copy()
+    gone[2:] = -1
+    check_cached(by, c, gone, lens, cu, T, q, None, H, Hk, d, page)
+
+
+@pytest.mark.parametrize("tree", [None, 1])
+@pytest.mark.parametrize("front, rows", [(0, 3), (17, 5)])
+def test_shared_rows_that_are_not_there(bbm, tree, front, rows):
+    """Offsets that begin in front of the first row or end behind the last: the tokens without a row are in the cache all the same."""
+    lens, news, H = [300, 290, 170], [40, 30, 60], 4
+    c, table, cu, T, q, words = grouped_case(bbm, [0, 3], [96], lens, news, H, 2, 64, 32, seed=11, tree=tree)
+    a, b = front, news[0] + news[1] + rows
+    check_cached(Behind(bbm, [0, 3], [96]), c, table, lens, cu - a, b - a, q[a:b].contiguous(), None if words is None else words[a:b].copy(), H, 2, 64, 32)
+
+
+@pytest.mark.parametrize("max_shared, max_own", [(1, 1), (300, 5000), (5000, 1), (1 << 40, 1 << 40)])
+def test_shared_with_a_wrong_hint(bbm, max_shared, max_own):
+    check_grouped(bbm, [0, 2], [2048], [2300, 2100], [1, 2], 4, 2, 64, 64, hints=[dict(max_shared=max_shared, max_own=max_own)], seed=5)
+
+
+@pytest.mark.parametrize("lens, news", [([2300, 40, 900], [1, 2, 1]), ([300, 150], [140, 130])])
+def test_shared_by_nobody_is_the_attention_of_each(bbm, lens, news):
+    """Without groups, and with groups that share nothing, the cut is that of bbm_kv4_attn, bit for bit."""
+    c, table, cu, T, q, _ = cached_case(bbm, lens, news, 64, 8, 64, 32, seed=4)
+    args = q, c, i32(table), i32(lens), i32(cu)
+    want = bbm.bbm_kv4_attn(*args, max_len=2300)
+    for groups in ((None, None), (i32([0]), i32([])), (i32([0, 1, len(lens)]), i32([0, 0]))):
+        got = bbm.bbm_kv4_shared_attn(*args, *groups, max_own=2300)
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+def test_groups_whose_numbers_are_wrong_stay_inside(bbm):
+    """Offsets outside the requests or out of order, and prefixes longer than requests: nobody else's rows change, and other groups keep their results."""
+    group_cu, shared, lens, news, H, Hk, d, page = [0, 2, 4], [64, 32], [90, 80, 70, 60], [1, 1, 1, 1], 4, 2, 64, 16
+    c, table, cu, T, q, _ = grouped_case(bbm, group_cu, shared, lens, news, H, Hk, d, page, seed=8, before=2, behind=2)
+    args = q, c, i32(table), i32(lens), i32(cu)
+    want = bbm.bbm_kv4_shared_attn(*args, i32(group_cu), i32(shared))
+    for wrong, n in (([0, 2, 9], [64, 32]), ([-7, 2, 4], [64, 32]), ([0, 2, 4], [64, 1 << 30]), ([0, 2, 1], [64, 32]), ([0, 2, 4], [64, 80])):
+        out, lse = torch.full((T, H, d), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((H, T), 7.0, device="cuda")
+        bbm.bbm_kv4_shared_attn(*args, i32(wrong), i32(n), out=out, lse=lse)
+        assert (f64(out)[:2] == 7).all() and (f64(out)[-2:] == 7).all() and torch.equal(out[2:4], want[0][2:4]) and torch.equal(lse[:, 2:4], want[1][:, 2:4])
