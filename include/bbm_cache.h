@@ -1,5 +1,6 @@
 /*
- * bbm_cache.h -- operators on the 4-bit cache of many answers: attention behind prefixes that requests share.  Part of libbbm; the conventions of bbm_tokens.h hold.
+ * bbm_cache.h -- operators on the 4-bit cache of many and long answers: attention behind prefixes that requests share, and the attention
+ * weight that each key has gathered.  Part of libbbm; the conventions of bbm_tokens.h hold.
  *
  * Groups.  Requests group_cu[g] .. group_cu[g+1] - 1 (int32 [S+1], not decreasing, on the device like all below; cut to 0 .. R) are group g: their first
  * shared_lens[g] (int32 [S]; negative ones stand for 0) keys are the same, and lie in front of the new tokens of each of them that has any.  The rows of the block table are complete: the
@@ -27,6 +28,21 @@ int bbm_kv4_shared_attn(const bbm_packed* q, const bbm_packed* o, float* lse, in
                         const int32_t* block_table, int64_t table_stride, int64_t max_pages, int64_t S, const int32_t* group_cu,
                         const int32_t* shared_lens, const uint64_t* mask, int64_t mask_words, const bbm_kv4_cache* cache, int64_t H,
                         float softmax_scale, int64_t max_shared, int64_t max_own, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Weights of the keys.  `weights` and `out` are fp32 [pages][Hk][page], contiguous, 16-byte aligned, a number for each token and key head of the cache; they may be
+ * the same, and overlap in no other way.  For each request with a new token that has a row, each of its keys j and each key head,
+ *   out[j] = decay * weights[j] + the sum over its new tokens i that see j (as in bbm_kv4_attn) and the heads h of the group of exp(softmax_scale <q_i, k_j> - lse[h][i]),
+ * with 0 for weights[j] of the new tokens' own keys, whose slots may hold anything.  With lse of the attention of the same step that is the probability which
+ * the keys got (a row of lse = -infinity gives nothing).  The keys that a group shares get the sum over all its requests, and one decay.  Written are the slots of the keys that there
+ * are (a key without a page is left out), others stay as they are.  A page that lies in two requests' rows
+ * other than as a shared one of the same group gets unspecified numbers.  Deterministic.  Meant for scores (times softmax_scale) up to 2^12, like the gradients.
+ * 0 <= decay <= 1.  max_shared and max_own are hints for the work split, as above.
+ */
+int bbm_kv4_weights(const bbm_packed* q, const float* lse, int64_t T, int64_t R, const int32_t* cu, const int32_t* lens, const int32_t* block_table,
+                    int64_t table_stride, int64_t max_pages, int64_t S, const int32_t* group_cu, const int32_t* shared_lens, const uint64_t* mask,
+                    int64_t mask_words, const bbm_kv4_cache* cache, int64_t H, float softmax_scale, float decay, const float* weights, float* out,
+                    int64_t max_shared, int64_t max_own, void* stream);
 
 #ifdef __cplusplus
 }

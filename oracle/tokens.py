@@ -93,6 +93,16 @@ def bounds(q, k, v, seen, scale, p, o, lse, d_o=None, delta=None, grads=None):
     return e_o, e_lse, e_dq, e_dk, e_dv
 
 
+def key_weights(q, k, seen, scale, lse):
+    """q [n, d], k [m, d], seen [n, m], lse [n]: (what each key gets, how far a kernel may be off that sums n products in fp32): the probabilities from the given lse."""
+    n, d = q.shape
+    with np.errstate(invalid="ignore"):
+        p = np.where(seen & np.isfinite(lse)[:, None], np.exp(np.where(seen, scale * (q @ k.T) - np.where(np.isfinite(lse), lse, 0.0)[:, None], -np.inf)), 0.0)
+    mag = np.where(seen, scale * (np.abs(q) @ np.abs(k).T), 0.0)
+    e = (d + 8) * F * mag + 32 * F * (1 + mag + np.abs(np.where(np.isfinite(lse), lse, 0.0))[:, None])   # of an exponent: the score, both in units of log2, their difference
+    return p.sum(0), ((2 * e + (n + 16) * F) * p).sum(0) + n * U
+
+
 def kv4_encode(x):
     """x [..., 32 n] finite: (codes, scale bytes) of groups of 32, by looking at every exponent and every code."""
     x = np.asarray(x, np.float64).reshape(x.shape[:-1] + (-1, 32))

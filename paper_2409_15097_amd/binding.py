@@ -100,6 +100,7 @@ def _load():
         "bbm_kv4_attn": [pk, pk, vp, i64, i64, vp, vp, vp, i64, i64, vp, i64, cache, i64, cf, i64, vp, size, vp],
         # include/bbm_cache.h
         "bbm_kv4_shared_attn": [pk, pk, vp, i64, i64, vp, vp, vp, i64, i64, i64, vp, vp, vp, i64, cache, i64, cf, i64, i64, vp, size, vp],
+        "bbm_kv4_weights": [pk, vp, i64, i64, vp, vp, vp, i64, i64, i64, vp, vp, vp, i64, cache, i64, cf, cf, vp, vp, i64, i64, vp],
     }.items():
         f = getattr(L, name)
         f.restype, f.argtypes = ci, args

@@ -6,7 +6,7 @@ from typing import Optional
 import torch
 
 from .binding import _check, lib
-from .tokens import KV4Cache, _address, _context, _elsewhere, _gpu, _here, _I64x6, _ints, _lse_out, _out, _packed, _table, _workspace
+from .tokens import KV4Cache, _address, _context, _elsewhere, _gpu, _here, _I64x6, _ints, _lse, _lse_out, _out, _packed, _table, _workspace
 
 
 def _mask(mask: Optional[torch.Tensor], device: int, T: int):
@@ -62,3 +62,43 @@ def _kv4_shared_attn(dev, q, cache, block_table, lens, cu, group_cu, shared_lens
     _check(lib.bbm_kv4_shared_attn(at, at + 24, lse_at, T, R, _ints(cu, dev, R + 1), _ints(lens, dev, R), table, stride, width, S, group_at, shared_at, *_mask(mask, dev, T),
                                    _address(c), H, d ** -0.5 if softmax_scale is None else softmax_scale, max_shared, max_own, *_workspace(workspace, dev), _here(dev)))
     return out, lse
+
+
+def kv4_weights(cache: KV4Cache) -> torch.Tensor:
+    """What each token and key head of the cache has gathered before anything looked at it: zeros, fp32 [pages, Hk, page]."""
+    pages, Hk, page = cache.k.shape[:3]
+    return torch.zeros((pages, Hk, page), dtype=torch.float32, device=cache.k.device)
+
+
+def _weights(x: torch.Tensor, cache: KV4Cache) -> int:
+    assert x.dtype is torch.float32 and x.is_contiguous() and x.shape == cache.k.shape[:3], "contiguous fp32 weights [pages, Hk, page] of the cache"
+    assert x.get_device() == cache.device, "the tensors of a call lie on one GPU"
+    return x.data_ptr()
+
+
+def bbm_kv4_weights(q: torch.Tensor, lse: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor, lens: torch.Tensor, cu: torch.Tensor, weights: torch.Tensor,
+                    group_cu: Optional[torch.Tensor] = None, shared_lens: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None, decay: float = 1.0,
+                    out: Optional[torch.Tensor] = None, max_shared: Optional[int] = None, max_own: Optional[int] = None, softmax_scale: Optional[float] = None,
+                    stream=None) -> torch.Tensor:
+    """Adds to decay * weights (fp32 [pages, Hk, page], see kv4_weights) the probabilities which the step's queries gave to their keys, from the lse of the step's
+    attention; the other arguments are those of bbm_kv4_shared_attn.  Writes out (None: weights themselves), of which only the requests' keys change, and returns it."""
+    dev = _gpu(q)
+    if _elsewhere(dev, stream):
+        with _context(dev, stream):
+            return _kv4_weights(dev, q, lse, cache, block_table, lens, cu, weights, group_cu, shared_lens, mask, decay, out, max_shared, max_own, softmax_scale)
+    return _kv4_weights(dev, q, lse, cache, block_table, lens, cu, weights, group_cu, shared_lens, mask, decay, out, max_shared, max_own, softmax_scale)
+
+
+def _kv4_weights(dev, q, lse, cache, block_table, lens, cu, weights, group_cu, shared_lens, mask, decay, out, max_shared, max_own, softmax_scale):
+    T, H, d = q.shape
+    R, c = lens.shape[0], cache.c_struct
+    assert d == c.d and cache.device == dev, "the cache has another head size, or lies elsewhere"
+    table, stride, width = _table(block_table, dev, R)
+    S, group_at, shared_at = _groups(group_cu, shared_lens, dev)
+    most = width * c.page
+    max_shared, max_own = most if max_shared is None else max(1, max_shared), most if max_own is None else max(1, max_own)
+    out = weights if out is None else out
+    keep = _I64x6(*_packed(q, dev, T, H, d), 0, 0, 0)
+    _check(lib.bbm_kv4_weights(_address(keep), _lse(lse, dev, H, T), T, R, _ints(cu, dev, R + 1), _ints(lens, dev, R), table, stride, width, S, group_at, shared_at, *_mask(mask, dev, T),
+                               _address(c), H, d ** -0.5 if softmax_scale is None else softmax_scale, decay, _weights(weights, cache), _weights(out, cache), max_shared, max_own, _here(dev)))
+    return out

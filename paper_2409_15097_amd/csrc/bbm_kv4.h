@@ -1,7 +1,7 @@
 // The 4-bit cache's format (include/bbm_tokens.h) in device code.
 #pragma once
-#include "bbm_mfma.h"
 #include "bbm_packed.h"
+#include "bbm_tile.h"
 
 namespace bbm {
 
@@ -63,5 +63,30 @@ __device__ __forceinline__ bf16x8 values_of(uint32_t codes, float scale) {
   x.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
   return x.all;
 }
+
+// The group of request r, -1 if it has none; 64 groups at a time.
+__device__ __forceinline__ int group_of(const int32_t* group_cu, int S, int r) {
+  const int lane = threadIdx.x & 63;
+  for (int g0 = 0; g0 < S; g0 += 64) {
+    const int g = min(g0 + lane, S - 1);
+    const uint64_t has = __ballot(group_cu[g] <= r && r < group_cu[g + 1]);
+    if (has) return min(g0 + __ffsll((unsigned long long)has) - 1, S - 1);
+  }
+  return -1;
+}
+
+// Which of 64 keys new token i of a request may see, as far as its order or its words of the mask (NULL: causal) go; w0: the first key, counted from the new tokens on.
+__device__ __forceinline__ uint64_t seen_from(const uint64_t* words, int mask_words, int i, int w0) {
+  if (!words) return bits_up_to(i - w0);
+  auto word = [&](int n) { return n < mask_words ? words[n] : 0ull; };
+  if (w0 <= -64) return ~0ull;
+  if (w0 < 0) return word(0) << -w0 | ((1ull << -w0) - 1ull);
+  const int sh = w0 & 63;
+  return sh ? word(w0 >> 6) >> sh | word((w0 >> 6) + 1) << (64 - sh) : word(w0 >> 6);
+}
+
+// A request's row of the block table, read by scalar loads (through the constant address space: no kernel that reads it writes it).  As a vector load a page's
+// number would be waited for together with the keys and values asked for before it.
+typedef const int32_t __attribute__((address_space(4)))* Table;
 
 }  // namespace bbm

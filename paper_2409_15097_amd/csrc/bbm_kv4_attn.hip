@@ -100,16 +100,6 @@ __device__ __forceinline__ Piece group_piece_of(const Kv4AttnParams& P, int numb
   if (x.len == 0) x.s.end = x.s.begin;  // nothing to do
   return x;
 }
-// The group of request r, -1 if it has none; 64 groups at a time.
-__device__ __forceinline__ int group_of(const Kv4AttnParams& P, int r) {
-  const int lane = threadIdx.x & 63;
-  for (int g0 = 0; g0 < P.S; g0 += 64) {
-    const int g = min(g0 + lane, P.S - 1);
-    const uint64_t has = __ballot(P.group_cu[g] <= r && r < P.group_cu[g + 1]);
-    if (has) return min(g0 + __ffsll((unsigned long long)has) - 1, P.S - 1);
-  }
-  return -1;
-}
 template <bool SHARED>
 __device__ __forceinline__ Piece piece_of(const Kv4AttnParams& P, int number, int width) {
   Piece x;
@@ -123,7 +113,7 @@ __device__ __forceinline__ Piece piece_of(const Kv4AttnParams& P, int number, in
   x.from = 0;
   x.group_parts = 0;
   if constexpr (SHARED) {
-    const int g = group_of(P, x.s.r), shared = g >= 0 ? shared_of(P, g) : 0;
+    const int g = bbm::group_of(P.group_cu, P.S, x.s.r), shared = g >= 0 ? shared_of(P, g) : 0;
     if (shared > 0) {
       Piece all;
       all.len = shared, all.from = 0;
@@ -136,9 +126,7 @@ __device__ __forceinline__ Piece piece_of(const Kv4AttnParams& P, int number, in
   return x;
 }
 
-// A request's row of the block table, read by scalar loads (through the constant address space: no kernel that reads it writes it).  As a vector load a page's
-// number would be waited for together with the keys and values asked for before it.
-typedef const int32_t __attribute__((address_space(4)))* Table;
+using bbm::Table;
 __device__ __forceinline__ Table table_of(const Kv4AttnParams& P, const Piece& x) { return (Table)(uintptr_t)(P.table + x.s.r * P.table_stride); }
 
 template <int X>
@@ -174,16 +162,8 @@ __device__ __forceinline__ bool alone(const Piece& x, const Item& item) { return
 template <bool SHARED>
 __device__ __forceinline__ int slot_of(const Kv4AttnParams& P, const Item& item) { return item.part + (SHARED && !item.group ? P.group_parts : 0); }
 
-// Which of the keys j0 .. j0 + 63 new token i of the request may see, as far as its order or the mask goes.
 __device__ __forceinline__ uint64_t seen_from(const Kv4AttnParams& P, const Piece& x, int i, int j0) {
-  const int w0 = j0 - x.prefix;  // among the new tokens
-  if (!P.mask) return bbm::bits_up_to(i - w0);
-  const uint64_t* const words = P.mask + (int64_t)(x.s.begin + i) * P.mask_words;
-  auto word = [&](int n) { return n < P.mask_words ? words[n] : 0ull; };
-  if (w0 <= -64) return ~0ull;
-  if (w0 < 0) return word(0) << -w0 | ((1ull << -w0) - 1ull);
-  const int sh = w0 & 63;
-  return sh ? word(w0 >> 6) >> sh | word((w0 >> 6) + 1) << (64 - sh) : word(w0 >> 6);
+  return bbm::seen_from(P.mask ? P.mask + (int64_t)(x.s.begin + i) * P.mask_words : nullptr, P.mask_words, i, j0 - x.prefix);
 }
 
 // Writes D / 16 values of column `col`, from element e0 on.

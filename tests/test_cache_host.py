@@ -10,7 +10,7 @@ import pytest
 
 from test_tokens_host import BAD_CACHE, BAD_PACKED, ODD_CACHE, OVERLAP, P, ROOT, cache, pk
 
-NAMES = {"bbm_kv4_shared_attn_workspace_bytes", "bbm_kv4_shared_attn"}
+NAMES = {"bbm_kv4_shared_attn_workspace_bytes", "bbm_kv4_shared_attn", "bbm_kv4_weights"}
 
 
 @pytest.fixture(scope="module")
@@ -60,6 +60,30 @@ def test_shared_attention_refuses(bbm):
     assert sizes(3, 2, 0, 4, 2, 64, 256, 64) == 0                         # one part of each request: nothing to join
     assert sizes(0, 2, 1, 4, 2, 64, 256, 64) == 0 and sizes(3, 2, 3, 4, 2, 64, 256, 64) == 0 and sizes(3, 2, 1, 4, 3, 64, 256, 64) == 0 and sizes(3, 2, 1, 4, 2, 96, 256, 64) == 0
     assert sizes(1 << 20, 1 << 20, 1 << 20, 256, 1, 128, 1 << 62, 1 << 62) > 1 << 35   # (no product wraps)
+
+
+def weights(bbm, q=None, lse=2 * P, T=3, R=2, cu=3 * P, lens=4 * P, table=5 * P, stride=4, width=4, S=1, group=6 * P, shared=7 * P, mask=None, words=0, c=None, H=4, scale=0.125, decay=0.5,
+            w=8 * P, out=9 * P, max_shared=256, max_own=64):
+    return bbm.lib.bbm_kv4_weights(q or pk(), lse, T, R, cu, lens, table, stride, width, S, group, shared, mask, words, c or cache(k=10 * P), H, scale, decay, w, out, max_shared, max_own, None)
+
+
+def test_weights_refuses(bbm):
+    for bad in BAD_CACHE:
+        assert weights(bbm, c=cache(**bad)) == bbm.BBM_EINVAL
+    for bad in ODD_CACHE:
+        assert weights(bbm, c=cache(**bad)) == bbm.BBM_EUNSUPPORTED
+    for bad in BAD_PACKED:
+        if bad is not None:
+            assert weights(bbm, q=bad) == bbm.BBM_EINVAL
+    for kw in (dict(T=-1), dict(R=0), dict(H=3), dict(cu=None), dict(lens=None), dict(table=None), dict(lens=P + 2), dict(lse=P + 2), dict(lse=None), dict(stride=3), dict(width=0),
+               dict(max_shared=0), dict(max_own=0), dict(mask=P + 4, words=1), dict(mask=P, words=0), dict(words=1), dict(scale=0.0), dict(scale=math.nan), dict(S=-1), dict(S=3),
+               dict(group=None), dict(shared=None), dict(group=P + 2), dict(shared=P + 1), dict(decay=-0.5), dict(decay=1.5), dict(decay=math.nan), dict(w=None), dict(out=None),
+               dict(w=P + 4), dict(out=P + 8), dict(out=P), dict(out=2 * P), dict(out=5 * P), dict(out=6 * P), dict(out=10 * P)):
+        assert weights(bbm, **kw) == bbm.BBM_EINVAL, kw
+    for kw in (dict(T=1 << 31), dict(T=1 << 30), dict(scale=2.0 ** -101), dict(width=(1 << 24) + 1, stride=1 << 26), dict(mask=P, words=(1 << 20) + 1),
+               dict(R=1 << 24), dict(R=1 << 20, S=1 << 20, T=1 << 28, H=2, max_shared=1 << 40)):
+        assert weights(bbm, **kw) == bbm.BBM_EUNSUPPORTED, kw
+    assert weights(bbm, T=0) == bbm.BBM_OK and weights(bbm, T=0, S=0, group=None, shared=None, lse=None) == bbm.BBM_OK
 
 
 def test_refusals_pass_under_host_sanitizers(tmp_path):

@@ -4,7 +4,8 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_tokens import cached_case, check_cached, f64, i32
+from oracle import tokens as ot
+from test_gpu_tokens import cached_case, check_cached, close, f64, host_cache, i32, normal
 
 pytestmark = pytest.mark.gpu
 
@@ -133,3 +134,131 @@ def test_groups_whose_numbers_are_wrong_stay_inside(bbm):
         out, lse = torch.full((T, H, d), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((H, T), 7.0, device="cuda")
         bbm.bbm_kv4_shared_attn(*args, i32(wrong), i32(n), out=out, lse=lse)
         assert (f64(out)[:2] == 7).all() and (f64(out)[-2:] == 7).all() and torch.equal(out[2:4], want[0][2:4]) and torch.equal(lse[:, 2:4], want[1][:, 2:4])
+
+
+# ---- weights of the keys
+
+
+def check_weights(bbm, group_cu, shared, c, table, lens, cu, T, q, words, H, Hk, d, page, lse=None, decay=0.75, seed=0, hints=({},)):
+    """Against the definition; returns what was gathered."""
+    mask = None if words is None else torch.from_numpy(words).cuda()
+    groups = (None, None) if group_cu is None else (i32(group_cu), i32(shared))
+    args = c, i32(table), i32(lens), i32(cu)
+    if lse is None:
+        _, lse = bbm.bbm_kv4_attn(q, *args, mask=mask)
+    g = torch.Generator().manual_seed(seed)
+    old = torch.rand(c.k.shape[:3], generator=g).mul_(3)
+    R, G, page_n = len(lens), H // Hk, c.k.shape[0]
+    hk, _ = host_cache(c)
+    nq, nl = f64(q), f64(lse)
+    want, tol, written = f64(old), np.zeros(old.shape), np.zeros(old.shape, bool)
+    of = {r: g for g in range(len(shared or [])) for r in range(group_cu[g], group_cu[g + 1])}
+    decayed = set()
+    fresh_slots = []
+    for r, n in enumerate(lens):
+        a, b, new = max(0, int(cu[r])), min(T, int(cu[r + 1])), int(cu[r + 1] - cu[r])
+        if b <= a:
+            continue
+        m = min(max(n, 0), table.shape[1] * page)
+        common = min(max(0, shared[of[r]]) // 16 * 16, m) if r in of else 0
+        j, i = np.arange(m), np.arange(a, b)[:, None] - int(cu[r])
+        row = np.where(j < common, group_cu[of[r]] if r in of else r, r)
+        pg = table[row, j // page]
+        ok = (pg >= 0) & (pg < page_n)
+        if words is None:
+            seen = (j <= n - new + i) & ok
+        else:
+            nj = j - (n - new)
+            bit = np.zeros((b - a, m), bool)
+            inside = (nj >= 0) & (nj < 64 * words.shape[1])
+            bit[:, inside] = (words[a:b][:, nj[inside] // 64] >> (nj[inside] % 64)) & 1 != 0
+            seen = ((nj < 0) | bit) & ok
+        for h in range(Hk):
+            k = np.where(ok[:, None], hk[np.where(ok, pg, 0), h, j % page], 0.0)
+            gained = [ot.key_weights(nq[a:b, h * G + x], k, seen, d ** -0.5, nl[h * G + x, a:b]) for x in range(G)]
+            for jj in np.nonzero(ok)[0]:
+                at = (int(pg[jj]), h, int(jj) % page)
+                if at not in decayed:
+                    decayed.add(at)
+                    want[at] = 0.0 if jj >= n - new else want[at] * np.float64(np.float32(decay))
+                    tol[at] += 4 * ot.F * want[at]
+                want[at] += sum(x[0][jj] for x in gained)
+                tol[at] += sum(x[1][jj] for x in gained)
+                written[at] = True
+        if words is not None or n - new < m:
+            fresh_slots += [(int(table[r, jj // page]), jj % page) for jj in range(max(0, n - new, common), m) if 0 <= table[r, jj // page] < page_n]
+    # the sums of all queries of a group meet in one number: as many half steps of it as there are terms
+    tol += 2 * ot.F * (T * G + 16) * np.abs(want)
+    got = None
+    for hint in hints:
+        for inplace in (False, True):
+            w = old.clone().cuda()
+            for p, at in fresh_slots:                                     # whatever lay where new tokens went
+                w[p, :, at] = float("nan")
+            src, out = w.clone(), (w if inplace else torch.full_like(w, 7.0))
+            r = bbm.bbm_kv4_weights(q, lse, *args, src if not inplace else w, *groups, mask=mask, decay=decay, out=None if inplace else out, **hint)
+            assert r is out
+            now = f64(out)
+            close("weights", torch.from_numpy(now[written]), want[written], tol[written])
+            rest = now[~written]
+            assert np.array_equal(rest, f64(src)[~written], equal_nan=True) if inplace else (rest == 7.0).all()
+            assert got is None or hint or torch.equal(got[torch.from_numpy(written).cuda()], out[torch.from_numpy(written).cuda()])
+            got = out.clone() if not hint else got
+    return got
+
+
+WEIGHTS = [
+    ([0], [], [1], [1], 1, 1, 16, "plain", None),
+    ([0], [], [0, 3, 17, 40], [1, 1, 1, 0], 4, 2, 16, "fused", None),
+    ([0], [], [63, 64, 65, 200, 1, 0], [1] * 6, 8, 1, 32, "plain", None),
+    ([0], [], [130, 300, 31], [30, 17, 31], 6, 2, 64, "heads", None),                  # a prompt's part; a whole prompt
+    ([0], [], [2900, 9, 1700], [1, 1, 2], 12, 4, 64, "plain", None),
+    ([0], [], [300, 129], [70, 129], 3, 1, 128, "heads", 2),
+    ([0], [], [20, 70, 5], [20, 6, 5], 4, 4, 16, "plain", 1),
+    ([0], [], [40, 90], [40, 60], 71, 1, 32, "plain", None),
+    ([0, 4], [48], [49, 60, 52, 100], [1] * 4, 8, 2, 16, "fused", None),
+    ([1, 3, 3, 6], [37, 500, 130], [20, 40, 38, 131, 150, 300, 9], [1, 2, 1, 1, 0, 5, 3], 6, 2, 32, "heads", None),
+    ([0, 3], [200], [206, 230, 204], [6, 30, 4], 3, 1, 64, "plain", 1),
+    ([0, 30], [96], [100 + i for i in range(30)], [1 + i % 3 for i in range(30)], 16, 2, 32, "plain", None),
+    ([0, 2], [2304], [2400, 2310], [3, 1], 12, 4, 64, "fused", None)]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("group_cu, shared, lens, news, H, Hk, page, layout, tree", WEIGHTS)
+def test_weights(bbm, group_cu, shared, lens, news, H, Hk, d, page, layout, tree):
+    c, table, cu, T, q, words = grouped_case(bbm, group_cu, shared, lens, news, H, Hk, d, page, layout=layout, tree=tree, seed=len(lens), before=2, behind=3)
+    check_weights(bbm, group_cu if shared else None, shared, c, table, lens, cu, T, q, words, H, Hk, d, page, seed=1, hints=[{}, dict(max_shared=300, max_own=40), dict(max_shared=1, max_own=1)])
+
+
+def test_weights_pages_outside_and_a_narrow_table(bbm):
+    group_cu, shared, lens, news, H, Hk, d, page = [0, 2, 4], [256, 64], [500, 300, 90, 70], [1, 3, 2, 1], 4, 2, 128, 32
+    c, table, cu, T, q, _ = grouped_case(bbm, group_cu, shared, lens, news, H, Hk, d, page, seed=3)
+    table[:2, 3], table[0, 15], table[2:, 0], table[3, 2] = -1, 1 << 30, c.k.shape[0], -5
+    for t, n in ((table, lens), (table[:, :9], lens), (table[:, :5], [700, 600, 90, 70])):
+        check_weights(bbm, group_cu, shared, c, t, n, cu, T, q, None, H, Hk, d, page)
+
+
+@pytest.mark.parametrize("front, rows", [(0, 3), (17, 5)])
+@pytest.mark.parametrize("tree", [None, 1])
+def test_weights_rows_that_are_not_there(bbm, tree, front, rows):
+    lens, news, H = [300, 290, 170], [40, 30, 60], 4
+    c, table, cu, T, q, words = grouped_case(bbm, [0], [], lens, news, H, 2, 64, 32, seed=11, tree=tree)
+    a, b = front, news[0] + news[1] + rows
+    check_weights(bbm, None, None, c, table, lens, cu - a, b - a, q[a:b].contiguous(), None if words is None else words[a:b].copy(), H, 2, 64, 32)
+
+
+def test_weights_of_many_requests(bbm):
+    R = 600
+    c, table, cu, T, q, _ = grouped_case(bbm, list(range(0, R + 1, 8)), [16 * (i % 3) for i in range(75)], [33 + i % 9 for i in range(R)], [1] * R, 2, 1, 64, 16)
+    check_weights(bbm, list(range(0, R + 1, 8)), [16 * (i % 3) for i in range(75)], c, table, [33 + i % 9 for i in range(R)], cu, T, q, None, 2, 1, 64, 16)
+
+
+def test_weights_of_rows_that_saw_nothing(bbm):
+    """A log-sum-exp of -infinity gives nothing; what a step's keys get adds up to its queries."""
+    lens, news, H, Hk, d, page = [300, 40], [3, 1], 8, 2, 64, 16
+    c, table, cu, T, q, _ = cached_case(bbm, lens, news, H, Hk, d, page, seed=2)
+    _, lse = bbm.bbm_kv4_attn(q, c, i32(table), i32(lens), i32(cu))
+    got = bbm.bbm_kv4_weights(q, lse, c, i32(table), i32(lens), i32(cu), bbm.kv4_weights(c))
+    assert np.abs(f64(got).sum((0, 2)) - T * (H // Hk)).max() <= 400 * ot.F * T * H * 40
+    lse[:, 1] = -float("inf")
+    check_weights(bbm, None, None, c, table, lens, cu, T, q, None, H, Hk, d, page, lse=lse)
