@@ -1,6 +1,6 @@
 /*
- * bbm_cache.h -- operators on the 4-bit cache of many and long answers: attention behind prefixes that requests share, and the attention
- * weight that each key has gathered.  Part of libbbm; the conventions of bbm_tokens.h hold.
+ * bbm_cache.h -- operators on the 4-bit cache of many and long answers: attention behind prefixes that requests share, the attention
+ * weight that each key has gathered, and the eviction of the keys that gathered least.  Part of libbbm; the conventions of bbm_tokens.h hold.
  *
  * Groups.  Requests group_cu[g] .. group_cu[g+1] - 1 (int32 [S+1], not decreasing, on the device like all below; cut to 0 .. R) are group g: their first
  * shared_lens[g] (int32 [S]; negative ones stand for 0) keys are the same, and lie in front of the new tokens of each of them that has any.  The rows of the block table are complete: the
@@ -43,6 +43,29 @@ int bbm_kv4_weights(const bbm_packed* q, const float* lse, int64_t T, int64_t R,
                     int64_t table_stride, int64_t max_pages, int64_t S, const int32_t* group_cu, const int32_t* shared_lens, const uint64_t* mask,
                     int64_t mask_words, const bbm_kv4_cache* cache, int64_t H, float softmax_scale, float decay, const float* weights, float* out,
                     int64_t max_shared, int64_t max_own, void* stream);
+
+/*
+ * Eviction.  Request r has n = lens[r] keys (negative: 0; cut to max_pages * page) and keeps b = max(budget, f + recent) of them, f = max(0, first[r]) (0 if first is NULL); if n <= b, all
+ * of them, and nothing of it changes.  Otherwise, for each key head, keys 0 .. f - 1 and the last `recent` stay, and of those between the b - f - recent with the largest weights
+ * (equal ones: the lowest positions; a NaN counts as less than any number).  The kept ones move together to positions 0 .. b - 1, codes, scales and weights alike:
+ *   those in front of position b - recent stay where they are; those between it and the last `recent` go to the places of evicted ones, the first to the
+ *   first and so on; the last `recent`, in their order, go to b - recent .. b - 1.
+ * Heads choose for themselves: a position then holds other tokens in other heads (their rotary positions are in the keys).  Positions from b on keep what they held.
+ * Written besides:
+ *   new_lens [R]    min(n, b) (n as cut)
+ *   free_pages      the pages behind position b, back in front of *free_at: entries *free_at - m .. *free_at - 1 of free_pages [n_free] get the m pages given back, in the order of
+ *                   requests and positions (entries of the table that name no page are not given back, nor is a page whose place would lie outside of the list)
+ *   free_next [1]   *free_at - m
+ * The block table is not written: entries behind a request's last page may hold anything, as for bbm_build_slots, which takes from *free_at = free_next on what came back.
+ * free_pages, free_at and free_next may all be NULL (pages are not given back then), free_pages alone if n_free is 0.  Keys on a page outside the cache count as less than a NaN, and what would move from or to one does not.
+ * A page that another request reads too (a shared prefix) has to lie within first[r], which protects it.  new_lens may be lens.  weights as above.
+ * The workspace needs bbm_kv4_evict_workspace_bytes bytes for the same R, Hk and max_pages * page, 16-byte aligned, contents of no matter.  1 <= R <= BBM_SLOTS_MAX_REQUESTS, budget >= 1 (of
+ * what a table holds at most 2^19), recent >= 0.  max_len is a hint (the longest of lens, or an upper bound); any positive number gives the same results.
+ */
+size_t bbm_kv4_evict_workspace_bytes(int64_t R, int64_t Hk, int64_t max_keys);
+int bbm_kv4_evict(const bbm_kv4_cache* cache, float* weights, int64_t R, const int32_t* lens, const int32_t* block_table, int64_t table_stride, int64_t max_pages,
+                  int64_t budget, int64_t recent, const int32_t* first, int32_t* new_lens, int32_t* free_pages, int64_t n_free, const int32_t* free_at, int32_t* free_next,
+                  int64_t max_len, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -124,3 +124,17 @@ def kv4_decode(codes, scales):
 def unpack_nibbles(b):
     """[..., m] bytes: [..., 2 m] codes."""
     return np.stack([b & 15, b >> 4], -1).reshape(b.shape[:-1] + (-1,))
+
+
+def evict(n, budget, recent, first, w):
+    """Which key goes to which position, by pairs (from, to), in one head of a request of n keys with weights w (fp32; -inf for a NaN's place: use None below any number for a key without a page):
+    by sorting.  And how many stay."""
+    f = max(0, first)
+    b = max(budget, f + recent)
+    if n <= b:
+        return [], n
+    size = lambda j: (2, float(w[j])) if w[j] is not None and not np.isnan(w[j]) else ((1, 0.0) if w[j] is not None else (0, 0.0))  # noqa: E731
+    between = sorted(range(f, n - recent), key=lambda j: tuple(-x for x in size(j)) + (j,))
+    kept, edge = set(between[:b - f - recent]), b - recent
+    free = [j for j in range(f, edge) if j not in kept]
+    return list(zip(sorted(j for j in kept if j >= edge), free)) + [(n - recent + i, edge + i) for i in range(recent)], b

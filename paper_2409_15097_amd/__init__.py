@@ -21,7 +21,8 @@ _TOKEN_NAMES = (
     "bbm_prompt_attn_bwd_workspace_bytes", "bbm_prompt_attn_bwd", "bbm_kv4_append", "bbm_kv4_read", "bbm_kv4_attn_workspace_bytes", "bbm_kv4_attn",
 )
 # operators on the cache of many and long answers (include/bbm_cache.h)
-_CACHE_NAMES = ("bbm_kv4_shared_attn_workspace_bytes", "bbm_kv4_shared_attn", "kv4_weights", "bbm_kv4_weights")
+_CACHE_NAMES = ("bbm_kv4_shared_attn_workspace_bytes", "bbm_kv4_shared_attn", "kv4_weights", "bbm_kv4_weights", "Evicted", "bbm_kv4_evict_workspace_bytes",
+                "bbm_kv4_evict")
 __all__ = list(_NAMES + _TOKEN_NAMES + _CACHE_NAMES)
 
 

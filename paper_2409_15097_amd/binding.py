@@ -101,6 +101,7 @@ def _load():
         # include/bbm_cache.h
         "bbm_kv4_shared_attn": [pk, pk, vp, i64, i64, vp, vp, vp, i64, i64, i64, vp, vp, vp, i64, cache, i64, cf, i64, i64, vp, size, vp],
         "bbm_kv4_weights": [pk, vp, i64, i64, vp, vp, vp, i64, i64, i64, vp, vp, vp, i64, cache, i64, cf, cf, vp, vp, i64, i64, vp],
+        "bbm_kv4_evict": [cache, vp, i64, vp, vp, i64, i64, i64, i64, vp, vp, vp, i64, vp, vp, i64, vp, size, vp],
     }.items():
         f = getattr(L, name)
         f.restype, f.argtypes = ci, args
@@ -110,6 +111,8 @@ def _load():
     L.bbm_kv4_attn_workspace_bytes.argtypes = [i64, i64, i64, i64, ci, i64]
     L.bbm_kv4_shared_attn_workspace_bytes.restype = size
     L.bbm_kv4_shared_attn_workspace_bytes.argtypes = [i64, i64, i64, i64, i64, ci, i64, i64]
+    L.bbm_kv4_evict_workspace_bytes.restype = size
+    L.bbm_kv4_evict_workspace_bytes.argtypes = [i64, i64, i64]
     return L
 
 

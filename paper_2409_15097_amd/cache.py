@@ -1,6 +1,7 @@
 """ctypes binding of the operators on the 4-bit cache of many and long answers.  Argument marshalling only; see include/bbm_cache.h for the contract.
 
 Devices, streams and what a call allocates are as in tokens.py."""
+from dataclasses import dataclass
 from typing import Optional
 
 import torch
@@ -102,3 +103,41 @@ def _kv4_weights(dev, q, lse, cache, block_table, lens, cu, weights, group_cu, s
     _check(lib.bbm_kv4_weights(_address(keep), _lse(lse, dev, H, T), T, R, _ints(cu, dev, R + 1), _ints(lens, dev, R), table, stride, width, S, group_at, shared_at, *_mask(mask, dev, T),
                                _address(c), H, d ** -0.5 if softmax_scale is None else softmax_scale, decay, _weights(weights, cache), _weights(out, cache), max_shared, max_own, _here(dev)))
     return out
+
+
+@dataclass
+class Evicted:
+    """What bbm_kv4_evict writes besides the cache (int32 device tensors)."""
+    lens: torch.Tensor                   # [R] tokens of each request in the cache
+    free_next: Optional[torch.Tensor]    # [1] index of the next free page of the list, for the next bbm_build_slots; None without a list
+
+
+def bbm_kv4_evict_workspace_bytes(R: int, Hk: int, max_keys: int) -> int:
+    return int(lib.bbm_kv4_evict_workspace_bytes(R, Hk, max_keys))
+
+
+def bbm_kv4_evict(cache: KV4Cache, weights: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor, budget: int, recent: int = 0, first: Optional[torch.Tensor] = None,
+                  free_pages: Optional[torch.Tensor] = None, free_at: Optional[torch.Tensor] = None, max_len: Optional[int] = None, new_lens: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None, stream=None) -> Evicted:
+    """Thins requests of more than `budget` keys to that many, for each key head those of largest weight beside the first[r] (int32 [R]) and the last `recent` ones, in place;
+    the pages that this frees go back to free_pages (int32 [n]) in front of free_at (int32 [1]).  max_len: an upper bound of lens (None: what the table holds)."""
+    dev = _gpu(lens)
+    if _elsewhere(dev, stream):
+        with _context(dev, stream):
+            return _kv4_evict(dev, cache, weights, block_table, lens, budget, recent, first, free_pages, free_at, max_len, new_lens, workspace)
+    return _kv4_evict(dev, cache, weights, block_table, lens, budget, recent, first, free_pages, free_at, max_len, new_lens, workspace)
+
+
+def _kv4_evict(dev, cache, weights, block_table, lens, budget, recent, first, free_pages, free_at, max_len, new_lens, workspace):
+    R, c = lens.shape[0], cache.c_struct
+    assert cache.device == dev, "the cache lies elsewhere"
+    table, stride, width = _table(block_table, dev, R)
+    assert (free_pages is None) == (free_at is None), "a list of free pages and its index"
+    new_lens = lens.new_empty(R) if new_lens is None else new_lens
+    free_next = None if free_at is None else lens.new_empty(1)
+    if workspace is None:
+        workspace = lens.new_empty(lib.bbm_kv4_evict_workspace_bytes(R, c.Hk, width * c.page), dtype=torch.uint8)
+    free = (None, 0, None, None) if free_at is None else (_ints(free_pages, dev), free_pages.shape[0], _ints(free_at, dev, 1), free_next.data_ptr())
+    _check(lib.bbm_kv4_evict(_address(c), _weights(weights, cache), R, _ints(lens, dev), table, stride, width, budget, recent, None if first is None else _ints(first, dev, R),
+                             _ints(new_lens, dev, R), *free, width * c.page if max_len is None else max(1, max_len), *_workspace(workspace, dev), _here(dev)))
+    return Evicted(new_lens, free_next)

@@ -1,0 +1,350 @@
+// Eviction from the 4-bit cache by the weights that its keys gathered (include/bbm_cache.h).
+//
+// A work-group takes a request and a key head: it finds the smallest weight that stays by counting (11, 11 and 10 bits of the weights as ordered integers, each pass over those that
+// agree with the bits before), writes down which of the places that remain become free, a bit each, in LDS, and moves: a kept key from behind finds the place of its number by
+// bisection over the counts of 64 places, then by counting bits.  Where the moves of the first kind end they read nothing that they write, so their order does not matter; the last
+// keys are shifted by whole rounds of all waves, with a barrier between a round's loads and its stores, in ascending order.
+// A second kernel gives the pages back: one wave a request, behind the sum of what the requests in front of it give back.
+#include "bbm_cache.h"
+#include "bbm_kv4.h"
+
+#include <algorithm>
+
+namespace {
+
+using bbm::Kv4, bbm::scalar;
+
+constexpr int NT = 1024, NWAVES = NT / 64;
+constexpr int kBins = 2048;
+constexpr int64_t kMaxBudget = 1 << 19;  // places that are bits and counts in LDS: 96 KiB
+
+struct EvictParams {
+  Kv4 c;
+  float* weights;
+  const int32_t *lens, *table, *first, *free_at;
+  int32_t *new_lens, *free_pages, *free_next;
+  int32_t* given;  // [R] pages that a request gives back
+  int64_t table_stride, n_free;
+  int32_t R, max_keys, budget, recent;
+};
+
+// What stays of a request: keys f .. f + between - 1 are chosen from, `chosen` of them stay.
+struct Cut {
+  int n, b, f, edge, between, chosen;
+};
+__device__ __forceinline__ Cut cut_of(const EvictParams& P, int r) {
+  Cut x;
+  x.n = max(0, min(P.lens[r], P.max_keys));
+  const int f = P.first ? max(0, P.first[r]) : 0;
+  const int64_t b = max((int64_t)P.budget, (int64_t)f + P.recent);
+  x.b = (int)min(b, (int64_t)x.n);
+  x.f = min(f, x.n);
+  x.edge = x.b - P.recent;  // (of use if x.n > x.b, as are the others)
+  x.between = x.n - P.recent - x.f;
+  x.chosen = x.edge - x.f;
+  return x;
+}
+
+// Weights as integers of the same order; a NaN is 1, a key without a page 0.
+__device__ __forceinline__ uint32_t ordered(uint32_t bits) {
+  if ((bits & 0x7fffffffu) > 0x7f800000u) return 1u;
+  if (bits == 0x80000000u) bits = 0u;
+  return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+}
+
+template <int D>
+__global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
+  extern __shared__ __attribute__((aligned(16))) uint32_t dynamic_s[];  // free places: a bit each, 64 a word, then the number of those in front of each word
+  __shared__ uint32_t bins[kBins];
+  __shared__ int wave_s[2][NWAVES];
+  __shared__ uint32_t found_s[2];  // the bin, what is still to be chosen from it
+  __shared__ int2 moves_s[NWAVES][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = (int)scalar(tid >> 6);
+  const int r = blockIdx.x / P.c.Hk, hk = blockIdx.x % P.c.Hk;
+  const Cut x = cut_of(P, r);
+  const int32_t* const table = P.table + r * P.table_stride;
+  auto page_of = [&](int j) { return table[j >> P.c.page_shift]; };
+  if (hk == 0 && wave == 0 && P.free_at) {  // pages that this request gives back
+    int count = 0;
+    for (int at = ((x.b + P.c.page - 1) >> P.c.page_shift) + lane; at < (x.n + P.c.page - 1) >> P.c.page_shift; at += 64) count += table[at] >= 0 && table[at] < P.c.pages;
+    count = __builtin_amdgcn_readlane(bbm::wave_prefix_sum(count), 63);
+    if (lane == 0) P.given[r] = count;
+  }
+  if (x.n <= x.b) return;
+
+  // the slot of a key in the cache, for all that has a number for each token and head; -1 if it has no page
+  auto slot_of = [&](int j) -> int64_t {
+    const int page = page_of(j);
+    return page >= 0 && page < P.c.pages ? (((int64_t)page * P.c.Hk + hk) << P.c.page_shift) + (j & (P.c.page - 1)) : -1;
+  };
+  auto weight_of = [&](int i) -> uint32_t {  // of key f + i
+    const int64_t s = slot_of(x.f + i);
+    return s < 0 ? 0u : ordered(__float_as_uint(P.weights[s]));
+  };
+
+  // The smallest weight that stays, and how many that equal it do.
+  uint32_t low = 0, need = (uint32_t)x.chosen, equal = 0;
+  if (x.chosen > 0) {
+    constexpr int SHIFT[3] = {21, 10, 0}, BITS[3] = {11, 11, 10};
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+      for (int i = tid; i < kBins; i += NT) bins[i] = 0;
+      __syncthreads();
+      const uint32_t above = pass == 0 ? 0u : ~0u << (pass == 1 ? 21 : 10);
+      for (int i = tid; i < x.between; i += NT) {
+        const uint32_t u = weight_of(i);
+        if (((u ^ low) & above) == 0) atomicAdd(&bins[u >> SHIFT[pass] & ((1u << BITS[pass]) - 1u)], 1u);
+      }
+      __syncthreads();
+      // two bins a thread, the highest first
+      const uint32_t c0 = bins[kBins - 1 - 2 * tid], c1 = bins[kBins - 2 - 2 * tid];
+      int sum = bbm::wave_prefix_sum((int)(c0 + c1));
+      if (lane == 63) wave_s[0][wave] = sum;
+      __syncthreads();
+      for (int w = 0; w < wave; ++w) sum += wave_s[0][w];
+      const uint32_t before = (uint32_t)sum - c0 - c1;
+      if (before < need && need <= (uint32_t)sum) {
+        const bool second = before + c0 < need;
+        found_s[0] = (uint32_t)(kBins - 1 - 2 * tid) - second;
+        found_s[1] = need - before - (second ? c0 : 0u);
+        bins[0] = second ? c1 : c0;  // (everyone has read its own)
+      }
+      __syncthreads();
+      low |= found_s[0] << SHIFT[pass];
+      need = found_s[1];
+      equal = bins[0];
+      __syncthreads();
+    }
+  } else {
+    low = ~0u;
+  }
+
+  // Each wave takes a stretch of the keys between.  Of those that equal the smallest the first `need` stay: how many lie in front of each stretch.
+  const int blocks = (x.between + 63) / 64, per = (blocks + NWAVES - 1) / NWAVES, block0 = min(blocks, wave * per), block1 = min(blocks, block0 + per);
+  int ties = 0;  // in front of this wave's
+  if (equal > need) {
+    int mine = 0;
+    for (int k = block0; k < block1; ++k) {
+      const int i = 64 * k + lane;
+      mine += __popcll(__ballot(i < x.between && weight_of(min(i, x.between - 1)) == low));
+    }
+    if (lane == 0) wave_s[0][wave] = mine;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) ties += wave_s[0][w];
+  }
+  // Which of 64 keys stay; counts the ties as it goes.
+  auto kept = [&](int k, int& ties) -> uint64_t {
+    const int i = 64 * k + lane;
+    const uint32_t u = weight_of(min(i, x.between - 1));
+    const bool in = i < x.between && x.chosen > 0;
+    const uint64_t same = __ballot(in && u == low);
+    const int rank = ties + __popcll(same & ((1ull << lane) - 1ull));
+    ties += __popcll(same);
+    return __ballot(in && (u > low || (u == low && (equal <= need || rank < (int)need))));
+  };
+  // Places: bit i of the first `chosen` is free if key f + i does not stay there.
+  const int words = (x.chosen + 63) / 64;
+  uint64_t* const free_s = reinterpret_cast<uint64_t*>(dynamic_s);
+  int* const before_s = reinterpret_cast<int*>(free_s + words);
+  int behind = 0;  // kept ones of this wave's that have to move
+  for (int k = block0, t = ties; k < block1; ++k) {
+    const uint64_t stay = kept(k, t);
+    const int left = x.chosen - 64 * k;  // places among these
+    const uint64_t places = left >= 64 ? ~0ull : left <= 0 ? 0ull : (1ull << left) - 1ull;
+    if (lane == 0 && places) free_s[k] = places & ~stay;
+    behind += __popcll(stay & ~places);
+  }
+  if (lane == 0) wave_s[1][wave] = behind;
+  __syncthreads();
+  int rank = 0;  // of this wave's first move
+  for (int w = 0; w < wave; ++w) rank += wave_s[1][w];
+  {
+    const int each = (words + NT - 1) / NT, w0 = min(words, tid * each), w1 = min(words, w0 + each);
+    int mine = 0;
+    for (int w = w0; w < w1; ++w) mine += __popcll(free_s[w]);
+    int sum = bbm::wave_prefix_sum(mine);
+    if (lane == 63) wave_s[0][wave] = sum;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) sum += wave_s[0][w];
+    sum -= mine;
+    for (int w = w0; w < w1; ++w) {
+      before_s[w] = sum;
+      sum += __popcll(free_s[w]);
+    }
+  }
+  __syncthreads();
+  // the place of number n
+  auto place_of = [&](int n) {
+    int lo = 0, hi = words;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (before_s[mid] <= n) lo = mid;
+      else hi = mid;
+    }
+    uint64_t bits = free_s[lo];
+    n -= before_s[lo];
+    int at = 0;  // bit n of those that are set: by halves
+#pragma unroll
+    for (int half = 32; half > 0; half >>= 1) {
+      const int c = __popcll(bits & ((1ull << half) - 1ull));
+      if (n >= c) n -= c, at += half, bits >>= half;
+      else bits &= (1ull << half) - 1ull;
+    }
+    return 64 * lo + at;
+  };
+
+  // Eight lanes carry a key: the codes of K and V, 16 bytes each (of D = 64, four lanes), then scales and weight.
+  constexpr int LK = D / 32;  // lanes of a key's codes, groups
+  struct Load {
+    uint4 codes;
+    uint32_t small;
+    uint8_t v_scale;
+  };
+  const int sub = lane & 7;
+  auto carry = [&](int64_t s) __attribute__((always_inline)) {
+    Load y = {};
+    if (s < 0) return y;
+    if (sub < 2 * LK) y.codes = *reinterpret_cast<const uint4*>((sub < LK ? P.c.k : P.c.v) + s * (D / 2) + sub % LK * 16);
+    if (sub == 0) {
+      if constexpr (D == 128) y.small = *reinterpret_cast<const uint32_t*>(P.c.k_scale + s * 4);
+      else y.small = *reinterpret_cast<const uint16_t*>(P.c.k_scale + s * 2);
+    }
+    if (sub == 7) y.small = __float_as_uint(P.weights[s]);
+    if (sub < LK) y.v_scale = P.c.v_scale[((s >> P.c.page_shift) * LK + sub << P.c.page_shift) + (s & (P.c.page - 1))];
+    return y;
+  };
+  auto put = [&](int64_t s, const Load& y) __attribute__((always_inline)) {
+    if (s < 0) return;
+    if (sub < 2 * LK) *reinterpret_cast<uint4*>((sub < LK ? P.c.k : P.c.v) + s * (D / 2) + sub % LK * 16) = y.codes;
+    if (sub == 0) {
+      if constexpr (D == 128) *reinterpret_cast<uint32_t*>(P.c.k_scale + s * 4) = y.small;
+      else *reinterpret_cast<uint16_t*>(P.c.k_scale + s * 2) = (uint16_t)y.small;
+    }
+    if (sub == 7) P.weights[s] = __uint_as_float(y.small);
+    if (sub < LK) P.c.v_scale[((s >> P.c.page_shift) * LK + sub << P.c.page_shift) + (s & (P.c.page - 1))] = y.v_scale;
+  };
+
+  // Kept keys from behind to the free places, 64 of a wave at a time.
+  for (int k = block0, t = ties; k < block1; ++k) {
+    const uint64_t stay = kept(k, t);
+    const int left = x.chosen - 64 * k;
+    const uint64_t go = left >= 64 ? 0ull : left <= 0 ? stay : stay & (~0ull << left);
+    const int count = __popcll(go);
+    if (count == 0) continue;
+    if (go >> lane & 1) {
+      const int at = __popcll(go & ((1ull << lane) - 1ull));
+      moves_s[wave][at] = make_int2(x.f + 64 * k + lane, x.f + place_of(rank + at));
+    }
+    rank += count;
+    __builtin_amdgcn_wave_barrier();
+    for (int m = lane >> 3; m < count; m += 8) {
+      const int2 move = moves_s[wave][m];
+      const int64_t from = slot_of(move.x), to = slot_of(move.y);
+      put(from < 0 ? -1 : to, carry(to < 0 ? -1 : from));
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+  bbm::hand_over();
+
+  // The last keys, in order, by n - b to the front.
+  constexpr int U = 4, ROUND = NWAVES * 8 * U;
+  for (int i0 = 0; i0 < P.recent; i0 += ROUND) {
+    int64_t to[U];
+    Load y[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + (u * NWAVES + wave) * 8 + (lane >> 3);
+      to[u] = -1;
+      if (i < P.recent) {
+        const int64_t from = slot_of(x.n - P.recent + i), s = slot_of(x.edge + i);
+        to[u] = from < 0 ? -1 : s;
+        y[u] = carry(s < 0 ? -1 : from);
+      }
+    }
+    bbm::hand_over();
+#pragma unroll
+    for (int u = 0; u < U; ++u) put(to[u], y[u]);
+  }
+}
+
+// Lengths, and the pages that requests give back, behind those of the requests in front of them.
+__global__ __launch_bounds__(256) void kv4_give_kernel(const EvictParams P) {
+  const int lane = threadIdx.x & 63, r = (int)scalar(blockIdx.x * 4 + (threadIdx.x >> 6));
+  if (r >= P.R) return;
+  const Cut x = cut_of(P, r);
+  if (P.free_at) {
+    int before = 0, all = 0;
+    for (int i = lane; i < P.R; i += 64) {
+      const int c = P.given[i];
+      all += c;
+      before += i < r ? c : 0;
+    }
+    before = __builtin_amdgcn_readlane(bbm::wave_prefix_sum(before), 63);
+    all = __builtin_amdgcn_readlane(bbm::wave_prefix_sum(all), 63);
+    const int64_t first = (int64_t)*P.free_at - all;
+    if (r == 0 && lane == 0) *P.free_next = (int32_t)first;
+    const int32_t* const table = P.table + r * P.table_stride;
+    int64_t to = first + before;
+    const int end = (x.n + P.c.page - 1) >> P.c.page_shift;
+    for (int at = (x.b + P.c.page - 1) >> P.c.page_shift; at < end; at += 64) {
+      const int page = at + lane < end ? table[at + lane] : -1;
+      const uint64_t real = __ballot(page >= 0 && page < P.c.pages);
+      const int64_t mine = to + __popcll(real & ((1ull << lane) - 1ull));
+      if ((real >> lane & 1) && mine >= 0 && mine < P.n_free) P.free_pages[mine] = page;
+      to += __popcll(real);
+    }
+  }
+  if (lane == 0) P.new_lens[r] = x.b;
+}
+
+inline bool sizes_ok(int64_t R, int64_t Hk, int64_t max_keys) { return R >= 1 && R <= BBM_SLOTS_MAX_REQUESTS && Hk >= 1 && max_keys >= 1; }
+
+}  // namespace
+
+extern "C" __attribute__((visibility("default"))) size_t bbm_kv4_evict_workspace_bytes(int64_t R, int64_t Hk, int64_t max_keys) {
+  return sizes_ok(R, Hk, max_keys) ? (size_t)R * sizeof(int32_t) : 0;
+}
+
+extern "C" __attribute__((visibility("default"))) int bbm_kv4_evict(const bbm_kv4_cache* cache, float* weights, int64_t R, const int32_t* lens, const int32_t* block_table,
+                                                                    int64_t table_stride, int64_t max_pages, int64_t budget, int64_t recent, const int32_t* first,
+                                                                    int32_t* new_lens, int32_t* free_pages, int64_t n_free, const int32_t* free_at, int32_t* free_next,
+                                                                    int64_t max_len, void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace bbm;
+  const char* fn = "bbm_kv4_evict";
+  clear_error();
+  if (int rc = check_kv4(fn, cache)) return rc;
+  if (R < 1 || budget < 1 || recent < 0 || max_len < 1)
+    return fail(BBM_EINVAL, "%s: R=%lld, budget=%lld, max_len=%lld must be >= 1, recent=%lld >= 0", fn, (long long)R, (long long)budget, (long long)max_len, (long long)recent);
+  if (int rc = check_table(fn, lens, block_table, table_stride, max_pages, cache->page)) return rc;
+  if (!weights || !aligned(weights, 16)) return fail(BBM_EINVAL, "%s: weights must be a non-NULL 16-byte aligned pointer", fn);
+  if (!new_lens || !aligned(new_lens, 4) || !aligned(first, 4)) return fail(BBM_EINVAL, "%s: new_lens and first must be 4-byte aligned, new_lens not NULL", fn);
+  if ((free_at != nullptr) != (free_next != nullptr) || n_free < 0 || (n_free > 0) > (free_pages != nullptr) || (free_pages != nullptr) > (free_at != nullptr) || !aligned(free_pages, 4) || !aligned(free_at, 4) || !aligned(free_next, 4))
+    return fail(BBM_EINVAL, "%s: free_pages (of n_free=%lld pages), free_at and free_next are given together, 4-byte aligned", fn, (long long)n_free);
+  if (R > BBM_SLOTS_MAX_REQUESTS) return fail(BBM_EUNSUPPORTED, "%s: R=%lld requests, more than %d", fn, (long long)R, BBM_SLOTS_MAX_REQUESTS);
+  if (R * cache->Hk > (1 << 22)) return fail(BBM_EUNSUPPORTED, "%s: problem too large (R=%lld, Hk=%lld)", fn, (long long)R, (long long)cache->Hk);
+  const int64_t max_keys = max_pages * cache->page;
+  if (std::min(budget, max_keys) > kMaxBudget) return fail(BBM_EUNSUPPORTED, "%s: budget=%lld is beyond %lld", fn, (long long)budget, (long long)kMaxBudget);
+  const size_t need = bbm_kv4_evict_workspace_bytes(R, cache->Hk, max_keys);
+  if (!workspace || workspace_bytes < need) return fail(BBM_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, workspace ? workspace_bytes : (size_t)0);
+  if (!aligned(workspace, 16)) return fail(BBM_EINVAL, "%s: workspace must be 16-byte aligned", fn);
+  if (int rc = check_apart(fn, {cache->k, cache->k_scale, cache->v, cache->v_scale, weights, new_lens, free_pages, free_next, workspace}, {block_table, first, free_at})) return rc;
+  if (int rc = check_apart(fn, {cache->k, cache->k_scale, cache->v, cache->v_scale, weights, free_pages, free_next, workspace}, {lens})) return rc;
+  EvictParams P = {};
+  P.c = kv4_of(cache), P.weights = weights;
+  P.lens = lens, P.table = block_table, P.first = first, P.free_at = free_at, P.new_lens = new_lens, P.free_pages = free_pages, P.free_next = free_next;
+  P.given = static_cast<int32_t*>(workspace);
+  P.table_stride = table_stride, P.n_free = n_free, P.R = (int32_t)R, P.max_keys = (int32_t)max_keys;
+  // (more than there are keys is as good as all of them)
+  P.budget = (int32_t)std::min(budget, max_keys), P.recent = (int32_t)std::min(recent, max_keys);
+  const size_t lds = (size_t)ceil_div(P.budget, 64) * 12;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  auto kernel = cache->d == 64 ? kv4_evict_kernel<64> : kv4_evict_kernel<128>;
+  if (lds > (32u << 10)) {
+    // (of the function on the current device; a repeated call changes nothing)
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)(kMaxBudget / 64 * 12));
+    if (e != hipSuccess) return fail(BBM_EHIP, "%s: %s", fn, hipGetErrorString(e));
+  }
+  kernel<<<(unsigned)(R * cache->Hk), NT, lds, s>>>(P);
+  kv4_give_kernel<<<(unsigned)ceil_div(R, 4), 256, 0, s>>>(P);
+  return launch_status(fn);
+}

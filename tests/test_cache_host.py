@@ -10,7 +10,7 @@ import pytest
 
 from test_tokens_host import BAD_CACHE, BAD_PACKED, ODD_CACHE, OVERLAP, P, ROOT, cache, pk
 
-NAMES = {"bbm_kv4_shared_attn_workspace_bytes", "bbm_kv4_shared_attn", "bbm_kv4_weights"}
+NAMES = {"bbm_kv4_shared_attn_workspace_bytes", "bbm_kv4_shared_attn", "bbm_kv4_weights", "bbm_kv4_evict_workspace_bytes", "bbm_kv4_evict"}
 
 
 @pytest.fixture(scope="module")
@@ -84,6 +84,28 @@ def test_weights_refuses(bbm):
                dict(R=1 << 24), dict(R=1 << 20, S=1 << 20, T=1 << 28, H=2, max_shared=1 << 40)):
         assert weights(bbm, **kw) == bbm.BBM_EUNSUPPORTED, kw
     assert weights(bbm, T=0) == bbm.BBM_OK and weights(bbm, T=0, S=0, group=None, shared=None, lse=None) == bbm.BBM_OK
+
+
+def evict(bbm, c=None, w=P, R=2, lens=2 * P, table=3 * P, stride=4, width=4, budget=100, recent=10, first=4 * P, new=5 * P, free=6 * P, n_free=9, at=7 * P, nxt=8 * P, max_len=256, ws=9 * P,
+          ws_bytes=8):
+    return bbm.lib.bbm_kv4_evict(c or cache(k=10 * P, ks=11 * P, v=12 * P, vs=13 * P), w, R, lens, table, stride, width, budget, recent, first, new, free, n_free, at, nxt, max_len, ws, ws_bytes,
+                                 None)
+
+
+def test_evict_refuses(bbm):
+    for bad in BAD_CACHE:
+        assert evict(bbm, c=cache(**bad)) == bbm.BBM_EINVAL
+    for bad in ODD_CACHE:
+        assert evict(bbm, c=cache(**bad)) == bbm.BBM_EUNSUPPORTED
+    for kw in (dict(w=None), dict(w=P + 4), dict(R=0), dict(lens=None), dict(lens=P + 2), dict(table=None), dict(stride=3), dict(width=0), dict(budget=0), dict(recent=-1), dict(first=P + 2),
+               dict(new=None), dict(new=P + 1), dict(free=None), dict(at=None), dict(nxt=None), dict(n_free=-1), dict(free=P + 2), dict(at=P + 2), dict(nxt=P + 2), dict(max_len=0),
+               dict(ws=P + 8), dict(w=3 * P), dict(new=3 * P), dict(nxt=7 * P), dict(free=2 * P), dict(ws=2 * P), dict(new=4 * P), dict(new=P), dict(ws=8 * P), dict(w=10 * P)):
+        assert evict(bbm, **kw) == bbm.BBM_EINVAL, kw
+    for kw in (dict(R=16385, ws_bytes=1 << 20), dict(width=(1 << 24) + 1, stride=1 << 26), dict(budget=(1 << 19) + 1, width=1 << 20, stride=1 << 20),
+               dict(R=16384, ws_bytes=1 << 20, c=cache(k=10 * P, ks=11 * P, v=12 * P, vs=13 * P, Hk=257))):
+        assert evict(bbm, **kw) == bbm.BBM_EUNSUPPORTED, kw
+    assert evict(bbm, ws=None) == bbm.BBM_EWORKSPACE and evict(bbm, ws_bytes=7) == bbm.BBM_EWORKSPACE
+    assert bbm.bbm_kv4_evict_workspace_bytes(2, 2, 256) == 8 and bbm.bbm_kv4_evict_workspace_bytes(0, 2, 256) == 0
 
 
 def test_refusals_pass_under_host_sanitizers(tmp_path):

@@ -262,3 +262,115 @@ def test_weights_of_rows_that_saw_nothing(bbm):
     assert np.abs(f64(got).sum((0, 2)) - T * (H // Hk)).max() <= 400 * ot.F * T * H * 40
     lse[:, 1] = -float("inf")
     check_weights(bbm, None, None, c, table, lens, cu, T, q, None, H, Hk, d, page, lse=lse)
+
+
+# ---- eviction
+
+
+def check_evict(bbm, lens, H, d, page, budget, recent, first=None, weigh=None, spoil=None, free=None, width=None, seed=0, hints=({},)):
+    """Against the definition, key by key; whole tensors are compared, so that nothing else may change."""
+    Hk = H
+    c, table, _, _, _, _ = cached_case(bbm, [max(0, n) for n in lens], [0] * len(lens), Hk, Hk, d, page, seed=seed, behind=1)
+    if width is not None:
+        table = table[:, :width]
+    if spoil is not None:
+        spoil(table, c)
+    g = np.random.default_rng(seed + 1)
+    w = g.random(tuple(c.k.shape[:3])).astype(np.float32) ** 4
+    if weigh is not None:
+        w = weigh(g, w)
+    R, pages = len(lens), c.k.shape[0]
+    names = ("k", "v", "k_scale", "v_scale")
+    was = {x: getattr(c, x).cpu().numpy() for x in names}
+    want, want_w = {x: y.copy() for x, y in was.items()}, w.copy()
+    free = g.permutation(pages + 40).astype(np.int32) if free is None else free
+    at = min(len(free), pages + 3)
+    given, left = [], []
+    for r, n in enumerate(lens):
+        n = min(max(0, n), table.shape[1] * page)
+        page_of = lambda j: table[r, j // page] if 0 <= table[r, j // page] < pages else -1  # noqa: E731
+        f = 0 if first is None else first[r]
+        for h in range(Hk):
+            ws = [w[page_of(j), h, j % page] if page_of(j) >= 0 else None for j in range(n)]
+            moves, b = ot.evict(n, budget, recent, f, ws)
+            for a, z in moves:
+                if page_of(a) < 0 or page_of(z) < 0:
+                    continue
+                src, dst = (page_of(a), h, a % page), (page_of(z), h, z % page)
+                for x in ("k", "v", "k_scale"):
+                    want[x][dst] = was[x][src]
+                want["v_scale"][dst[0], h, :, dst[2]] = was["v_scale"][src[0], h, :, src[2]]
+                want_w[dst] = w[src]
+        left.append(b)
+        given += [int(table[r, p]) for p in range(-(-b // page), -(-n // page)) if 0 <= table[r, p] < pages]
+    list_want = free.copy()
+    for i, p in enumerate(given):
+        if at - len(given) + i >= 0:
+            list_want[at - len(given) + i] = p
+    for hint in hints:
+        for x in names:
+            getattr(c, x).copy_(torch.from_numpy(was[x]))
+        wt, ft, tt = torch.from_numpy(w.copy()).cuda(), i32(free), i32(table)
+        fi = None if first is None else i32(first)
+        lens_t = i32(lens)
+        e = bbm.bbm_kv4_evict(c, wt, tt, lens_t, budget, recent=recent, first=fi, free_pages=ft, free_at=i32([at]), new_lens=lens_t if hint else None, **hint)
+        assert e.lens.cpu().tolist() == left and int(e.free_next) == at - len(given)
+        assert np.array_equal(ft.cpu().numpy(), list_want) and np.array_equal(tt.cpu().numpy(), table)
+        for x in names:
+            assert np.array_equal(getattr(c, x).cpu().numpy(), want[x]), x
+        assert np.array_equal(wt.cpu().numpy().view(np.int32), want_w.view(np.int32))
+    return left
+
+
+def few_values(g, w):
+    """Many equal weights, of both signs, zeros of both signs, infinities and NaNs."""
+    return g.choice(np.array([0.0, -0.0, 1.0, 0.5, -1.0, np.inf, -np.inf, np.nan, 1e-40], np.float32), w.shape)
+
+
+@pytest.mark.parametrize("lens, H, d, page, budget, recent, first", [
+    ([1], 1, 64, 16, 1, 0, None), ([2], 1, 64, 16, 1, 0, None), ([2, 3, 0], 2, 128, 16, 1, 1, None), ([40, 41, 60, -3], 2, 64, 16, 40, 10, [4, 0, 4, 4]),
+    ([100, 33, 300], 3, 128, 32, 32, 0, [0, 5, 90]), ([200, 70], 1, 64, 64, 64, 64, None), ([130, 129, 128, 127], 2, 128, 128, 100, 99, [1, 1, 0, 500]),
+    ([2112, 2048, 2049, 900], 2, 64, 64, 2048, 256, [4, 4, 4, 4]), ([5000, 700], 2, 128, 16, 600, 530, [3, 70]), ([3000, 3100], 1, 64, 32, 2900, 1100, None),
+    ([9000], 2, 64, 128, 1000, 7, [64])])
+@pytest.mark.parametrize("weigh", [None, few_values])
+def test_evict(bbm, lens, H, d, page, budget, recent, first, weigh):
+    check_evict(bbm, lens, H, d, page, budget, recent, first, weigh, hints=[{}, dict(max_len=max(1, max(lens))), dict(max_len=1)])
+
+
+def test_evict_equal_weights_goes_by_position(bbm):
+    check_evict(bbm, [3000, 200], 2, 64, 16, 150, 20, weigh=lambda g, w: w * 0 + 1)
+
+
+def test_evict_pages_outside_and_a_narrow_table(bbm):
+    def spoil(table, c):
+        table[0, 3], table[0, 30], table[1, 1], table[1, -1], table[2, :] = -1, 1 << 30, c.k.shape[0], -5, -1
+    check_evict(bbm, [1000, 500, 300], 2, 128, 16, 200, 30, [5, 5, 5], spoil=spoil, weigh=few_values)
+    check_evict(bbm, [1000, 500, 300], 2, 64, 16, 300, 30, None, width=25)
+
+
+@pytest.mark.parametrize("n_free", [0, 3, 30])
+def test_evict_into_a_short_list(bbm, n_free):
+    """Pages without a place in the list are not written anywhere."""
+    check_evict(bbm, [300, 200, 400], 1, 64, 16, 64, 8, free=np.arange(n_free, dtype=np.int32) + 100)
+
+
+def test_evict_of_many_requests(bbm):
+    R = 500
+    check_evict(bbm, [30 + i * 7 % 90 for i in range(R)], 1, 64, 16, 48, 5, [i % 9 for i in range(R)])
+
+
+def test_evict_without_a_list(bbm):
+    c = bbm.kv4_cache(4, 1, 64, 16)
+    e = bbm.bbm_kv4_evict(c, bbm.kv4_weights(c), i32([[0, 1, 2, 3]]), i32([60]), 20)
+    assert e.free_next is None and e.lens.tolist() == [20]
+
+
+def test_evict_keeps_what_requests_share(bbm):
+    """Requests of a common prefix, all heads at once: the prefix is within `first`, and its pages stay as they are."""
+    c, table, _, _, _, _ = cached_case(bbm, [200, 230, 210], [0, 0, 0], 2, 2, 64, 16, seed=3, behind=1)
+    table[1:, :6] = table[0, :6]
+    before = [x.clone() for x in (c.k, c.v, c.k_scale, c.v_scale)]
+    e = bbm.bbm_kv4_evict(c, torch.rand(c.k.shape[:3], device="cuda"), i32(table), i32([200, 230, 210]), 120, recent=10, first=i32([96] * 3))
+    assert e.lens.tolist() == [120] * 3
+    p = table[0, :6]
+    assert all(torch.equal(x[p], y[p]) for x, y in zip(before, (c.k, c.v, c.k_scale, c.v_scale)))
