@@ -374,3 +374,173 @@ def test_evict_keeps_what_requests_share(bbm):
     assert e.lens.tolist() == [120] * 3
     p = table[0, :6]
     assert all(torch.equal(x[p], y[p]) for x, y in zip(before, (c.k, c.v, c.k_scale, c.v_scale)))
+
+
+# ---- together
+
+
+def answers(bbm, s, w, weights, page, shared, budget):
+    """A decoding step of answers behind a common prompt: slots, rotary positions, the cache, attention, what the keys gathered, and eviction behind the step."""
+    cache, H, Hk, d = s["cache"], s["H"], s["Hk"], s["d"]
+    r = bbm.bbm_build_slots(s["ctx"], s["new"], s["table"], s["free"], s["at"], w.shape[0], page)
+    q, k, v = w[:, :H * d].unflatten(1, (H, d)), w[:, H * d:(H + Hk) * d].unflatten(1, (Hk, d)), w[:, (H + Hk) * d:].unflatten(1, (Hk, d))
+    q, k = bbm.bbm_rope(q, k, r.positions + s["gone"].repeat_interleave(s["new"], output_size=w.shape[0]), s["freqs"])
+    bbm.bbm_kv4_append(k, v, r.slots, cache)
+    o, lse = bbm.bbm_kv4_shared_attn(q, cache, s["table"], r.lens, r.cu_new, s["group_cu"], s["shared"])
+    bbm.bbm_kv4_weights(q, lse, cache, s["table"], r.lens, r.cu_new, weights, s["group_cu"], s["shared"])
+    e = bbm.bbm_kv4_evict(cache, weights, s["table"], r.lens, budget, recent=4, first=s["first"], free_pages=s["free"], free_at=r.free_next)
+    return r, e, q, o, lse
+
+
+def answers_state(bbm, H, Hk, d, page, R, shared, seed):
+    g = np.random.default_rng(seed)
+    pages, width = 80, 20
+    ids = g.permutation(pages)
+    table = np.full((R, width), -1)
+    table[:, :shared // page] = ids[:shared // page]
+    cache = bbm.kv4_cache(pages, Hk, d, page)
+    for t, lo, hi in ((cache.k, 0, 256), (cache.v, 0, 256), (cache.k_scale, 120, 128), (cache.v_scale, 120, 128)):
+        t.copy_(torch.from_numpy(g.integers(lo, hi, t.shape, dtype=np.uint8)))
+    return dict(H=H, Hk=Hk, d=d, cache=cache, table=i32(table), free=i32(np.concatenate([ids[:shared // page], ids[shared // page:]])), at=i32([shared // page]), freqs=bbm.rope_freqs(d)[0],
+                ctx=i32([shared] * R), new=i32([1] * R), group_cu=i32([0, R]), shared=i32([shared]), first=i32([shared] * R), gone=i32([0] * R))
+
+
+def test_answers_of_one_prompt(bbm):
+    """Steps of answers behind a common prompt against the same steps by bbm_kv4_attn on tables of their own; pages that eviction frees are taken again."""
+    H, Hk, d, page, R, shared, budget = 8, 2, 64, 16, 3, 48, 80
+    s = answers_state(bbm, H, Hk, d, page, R, shared, 1)
+    weights = bbm.kv4_weights(s["cache"])
+    used = set()
+    for step in range(70):
+        w = normal(100 + step, R, (H + 2 * Hk) * d)
+        want_ctx = s["ctx"].tolist()
+        r, e, q, o, lse = answers(bbm, s, w, weights, page, shared, budget)
+        assert r.lens.tolist() == [c + 1 for c in want_ctx] and (r.slots >= 0).all()
+        if step % 9 == 0 or step > 66:
+            # (eviction has moved keys since: attention of the step itself was checked by its own test; here the sums of weights)
+            assert e.lens.tolist() == [min(c + 1, budget) for c in want_ctx]
+        used.update((r.slots // page).tolist())
+        s["gone"] = s["gone"] + (r.lens - e.lens)
+        s["ctx"], s["at"] = e.lens, e.free_next
+        tables = s["table"].cpu().numpy()
+        live = [[int(p) for p in tables[i, shared // page:-(-int(n) // page)]] for i, n in enumerate(e.lens.tolist())]
+        flat = sum(live, [])
+        assert len(set(flat)) == len(flat) and not set(flat) & set(tables[0, :shared // page].tolist())   # nobody's page is another's
+        free = s["free"][int(s["at"]):].tolist()
+        assert len(set(free)) == len(free) and not set(free) & set(flat) and len(free) + len(flat) == 80 - shared // page
+    assert len(used) < R * 70 // page                                       # (pages came back)
+    # the last step's attention once more, on what the cache holds now, with and without the groups
+    q = normal(7, R, H, d)
+    lens, cu = s["ctx"], i32(range(R + 1))
+    a, b = bbm.bbm_kv4_shared_attn(q, s["cache"], s["table"], lens, cu, s["group_cu"], s["shared"]), bbm.bbm_kv4_attn(q, s["cache"], s["table"], lens, cu)
+    check_cached(Behind(bbm, [0, R], [shared]), s["cache"], s["table"].cpu().numpy(), lens.tolist(), np.arange(R + 1), R, q, None, H, Hk, d, page)
+    assert (a[1] - b[1]).abs().max() <= 64 * ot.F * 64
+    assert torch.isfinite(weights).all() and float(weights[s["table"][0, 0]].sum()) > 0
+
+
+def test_answers_in_graphs(bbm):
+    """A step recorded into a graph: replays give the eager results bit for bit, with eager work between them; two graphs of one stream do not share memory."""
+    H, Hk, d, page, R, shared, budget = 8, 2, 128, 16, 5, 64, 65
+    names = ("k", "v", "k_scale", "v_scale")
+
+    def state(seed):
+        s = answers_state(bbm, H, Hk, d, page, R, shared, seed)
+        s |= dict(w=normal(seed, R, (H + 2 * Hk) * d), weights=torch.rand(s["cache"].k.shape[:3], generator=torch.Generator().manual_seed(seed)).cuda())
+        s["ctx"].copy_(i32([70, 64, 90, 65, 64])), s["table"][:, 4:7].copy_(s["free"][10:10 + 3 * R].view(R, 3))
+        s["was"] = [getattr(s["cache"], x).clone() for x in names] + [s["weights"].clone(), s["free"].clone(), s["table"].clone()]
+        return s
+
+    def step(s):
+        for t, was in zip([getattr(s["cache"], x) for x in names] + [s["weights"], s["free"], s["table"]], s["was"]):
+            t.copy_(was)
+        r, e, q, o, lse = answers(bbm, s, s["w"], s["weights"], page, shared, budget)
+        return [o, lse, r.slots, e.lens, e.free_next, s["weights"], s["free"]] + [getattr(s["cache"], x) for x in names]
+    states = [state(1), state(2)]
+    want = [[t.clone() for t in step(s)] for s in states]
+    torch.cuda.synchronize()
+    side, graphs, outs = torch.cuda.Stream(), [], []
+    for s in states:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            outs.append(step(s))
+    other = torch.cuda.Stream()
+    eager = state(9)
+    for replay in range(4):
+        for out in outs:
+            for t in out[:5]:
+                t.fill_(5)
+        step(eager)                                                        # eager work on the default stream
+        torch.cuda.synchronize()
+        graphs[0].replay()
+        with torch.cuda.stream(other):
+            graphs[1].replay()
+        torch.cuda.synchronize()
+        for i in range(2):
+            for n, (a, b) in enumerate(zip(outs[i], want[i])):
+                assert torch.equal(a, b), (replay, i, n)
+
+
+def test_cache_operators_on_another_stream(bbm):
+    """Inputs that a stream still writes when the calls are made on it."""
+    lens, news, H, Hk, d, page = [300, 290], [1, 1], 8, 2, 64, 16
+    c, table, cu, T, q, _ = grouped_case(bbm, [0, 2], [160], lens, news, H, Hk, d, page, seed=2)
+    args = c, i32(table), i32(lens), i32(cu)
+    groups = i32([0, 2]), i32([160])
+    want = bbm.bbm_kv4_shared_attn(q, *args, *groups)
+    want_w = bbm.bbm_kv4_weights(q, want[1], *args, bbm.kv4_weights(c), *groups)
+    keep = [x.clone() for x in (c.k, c.v, c.k_scale, c.v_scale)]         # (eviction moves all four)
+    want_e = bbm.bbm_kv4_evict(c, want_w.clone(), args[1], args[2], 200, first=i32([160, 160]))
+    after = c.k.clone()
+    for x, y in zip((c.k, c.v, c.k_scale, c.v_scale), keep):
+        x.copy_(y)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    fresh = bbm.kv4_weights(c)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        a = torch.randn(4096, 4096, device="cuda")
+        for _ in range(20):
+            a = a @ a * 1e-3
+        late = q + (a[0, 0] * 0).to(torch.bfloat16).nan_to_num()
+    got = bbm.bbm_kv4_shared_attn(late, *args, *groups, stream=side)
+    got_w = bbm.bbm_kv4_weights(late, got[1], *args, fresh, *groups, stream=side)
+    got_e = bbm.bbm_kv4_evict(c, got_w, args[1], args[2], 200, first=i32([160, 160]), stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.equal(got_e.lens, want_e.lens) and torch.equal(c.k, after)
+
+
+def test_cache_binding_refuses(bbm):
+    q, c = normal(1, 4, 4, 64), bbm.kv4_cache(2, 2, 64, 16)
+    lens, cu, table, lse, w = i32([4]), i32([0, 4]), i32([[0, 1]]), torch.zeros(4, 4, device="cuda"), bbm.kv4_weights(c)
+    for bad in (lambda: bbm.bbm_kv4_shared_attn(q, c, table, lens, cu, i32([0, 1]), None), lambda: bbm.bbm_kv4_shared_attn(q, c, table, lens, cu, i32([0, 1]), i32([0, 0])),
+                lambda: bbm.bbm_kv4_shared_attn(q, c, table, lens, cu, i32([0, 1]).long(), i32([0])), lambda: bbm.bbm_kv4_shared_attn(q.float(), c, table, lens, cu, None, None),
+                lambda: bbm.bbm_kv4_shared_attn(q, c, table, lens, cu, None, None, mask=torch.zeros(3, 1, dtype=torch.int64, device="cuda")),
+                lambda: bbm.bbm_kv4_weights(q, lse.t()[:3], c, table, lens, cu, w), lambda: bbm.bbm_kv4_weights(q, lse.double(), c, table, lens, cu, w),
+                lambda: bbm.bbm_kv4_weights(q, lse, c, table, lens, cu, w[:1]), lambda: bbm.bbm_kv4_weights(q, lse, c, table, lens, cu, w.transpose(1, 2).contiguous().transpose(1, 2)),
+                lambda: bbm.bbm_kv4_weights(q, lse, c, table, lens, cu, w, out=w.cpu()), lambda: bbm.bbm_kv4_evict(c, w.half(), table, lens, 2),
+                lambda: bbm.bbm_kv4_evict(c, w, table, lens, 2, first=i32([0, 0])), lambda: bbm.bbm_kv4_evict(c, w, table, lens, 2, free_pages=i32([0])),
+                lambda: bbm.bbm_kv4_evict(c, w, table, lens, 2, free_pages=i32([0]), free_at=i32([0, 1])), lambda: bbm.bbm_kv4_evict(c, w, table[0], lens, 2)):
+        with pytest.raises(AssertionError):
+            bad()
+    for bad in (lambda: bbm.bbm_kv4_evict(c, w, table, lens, 0), lambda: bbm.bbm_kv4_weights(q, lse, c, table, lens, cu, w, decay=2.0),
+                lambda: bbm.bbm_kv4_shared_attn(q, c, table, lens, cu, i32([0, 1, 1]), i32([0, 0]))):
+        with pytest.raises(bbm.BbmError):
+            bad()
+
+
+def test_cache_operators_past_32_bits(bbm):
+    """A cache whose codes take more than 2^32 bytes: its last pages are attended, weighed and thinned like those of a small one."""
+    Hk, d, page, T = 8, 128, 128, 500
+    pages = (1 << 32) // (Hk * page * d // 2) + 64
+    big, small = bbm.kv4_cache(pages, Hk, d, page), bbm.kv4_cache(4, Hk, d, page)
+    k, v, q = normal(1, T, Hk, d), normal(2, T, Hk, d), normal(3, 2, 16, d)
+    out = []
+    for c, p0 in ((big, pages - 4), (small, 0)):
+        bbm.bbm_kv4_append(k, v, i32(np.arange(T) + p0 * page), c)
+        table, lens, cu, groups = i32([[p0, p0 + 1, p0 + 2], [p0, p0 + 1, p0 + 3]]), i32([384, 372]), i32([0, 1, 2]), (i32([0, 2]), i32([256]))
+        o, lse = bbm.bbm_kv4_shared_attn(q, c, table, lens, cu, *groups)
+        w = bbm.bbm_kv4_weights(q, lse, c, table, lens, cu, bbm.kv4_weights(c), *groups)
+        kept = w[p0:].clone()
+        e = bbm.bbm_kv4_evict(c, w, table, lens, 300, recent=10, first=i32([256, 256]))
+        out.append([o, lse, kept, e.lens, w[p0:].clone()] + [x[p0:].clone() for x in (c.k, c.v, c.k_scale, c.v_scale)])
+    assert all(torch.equal(x, y) for x, y in zip(*out))
