@@ -64,15 +64,21 @@ __device__ __forceinline__ bf16x8 values_of(uint32_t codes, float scale) {
   return x.all;
 }
 
-// The group of request r, -1 if it has none; 64 groups at a time.
-__device__ __forceinline__ int group_of(const int32_t* group_cu, int S, int r) {
+// The group of request r and its shared keys, -1 and 0 if it has none; 64 groups in one trip to memory.
+struct Group {
+  int g, keys;
+};
+__device__ __forceinline__ Group group_of(const int32_t* group_cu, const int32_t* shared_lens, int S, int r) {
   const int lane = threadIdx.x & 63;
   for (int g0 = 0; g0 < S; g0 += 64) {
-    const int g = min(g0 + lane, S - 1);
-    const uint64_t has = __ballot(group_cu[g] <= r && r < group_cu[g + 1]);
-    if (has) return min(g0 + __ffsll((unsigned long long)has) - 1, S - 1);
+    const int g = min(g0 + lane, S - 1), c0 = group_cu[g], c1 = group_cu[g + 1], keys = shared_lens[g];
+    const uint64_t has = __ballot(c0 <= r && r < c1);
+    if (has) {
+      const int l = __ffsll((unsigned long long)has) - 1;
+      return {min(g0 + l, S - 1), __builtin_amdgcn_readlane(keys, l)};
+    }
   }
-  return -1;
+  return {-1, 0};
 }
 
 // Which of 64 keys new token i of a request may see, as far as its order or its words of the mask (NULL: causal) go; w0: the first key, counted from the new tokens on.

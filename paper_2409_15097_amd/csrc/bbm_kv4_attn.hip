@@ -82,14 +82,14 @@ __device__ __forceinline__ void cut_keys(const Kv4AttnParams& P, Piece& x, int p
   x.parts = n > 0 ? (n - 1) / x.keys + 1 : 1;
 }
 // The keys that group g shares, in whole blocks of 16: what is left over is each request's own.
-__device__ __forceinline__ int shared_of(const Kv4AttnParams& P, int g) {
-  return (int)scalar((int)max((int64_t)0, min((int64_t)P.shared_lens[g], (int64_t)P.max_pages << P.c.page_shift)) & ~15);
+__device__ __forceinline__ int shared_keys(const Kv4AttnParams& P, int keys) {
+  return (int)max((int64_t)0, min((int64_t)keys, (int64_t)P.max_pages << P.c.page_shift)) & ~15;
 }
 __device__ __forceinline__ int request_at(const Kv4AttnParams& P, int g) { return min(max(P.group_cu[g], 0), P.R); }
 __device__ __forceinline__ Piece group_piece_of(const Kv4AttnParams& P, int number, int width) {
   Piece x;
   x.s = bbm::find_piece_of([&](int g) __attribute__((always_inline)) { return P.cu[request_at(P, g)]; }, P.S, P.T, P.G, width, number);
-  x.len = x.s.end > x.s.begin ? shared_of(P, x.s.r) : 0;
+  x.len = x.s.end > x.s.begin ? shared_keys(P, (int)scalar(P.shared_lens[x.s.r])) : 0;
   x.s.r = min((int)scalar(request_at(P, x.s.r)), P.R - 1);  // (the first request's row of the table)
   x.cols = (x.s.end - x.s.begin) * P.G;
   x.col0 = x.s.piece * width;
@@ -113,7 +113,7 @@ __device__ __forceinline__ Piece piece_of(const Kv4AttnParams& P, int number, in
   x.from = 0;
   x.group_parts = 0;
   if constexpr (SHARED) {
-    const int g = bbm::group_of(P.group_cu, P.S, x.s.r), shared = g >= 0 ? shared_of(P, g) : 0;
+    const int shared = shared_keys(P, bbm::group_of(P.group_cu, P.shared_lens, P.S, x.s.r).keys);
     if (shared > 0) {
       Piece all;
       all.len = shared, all.from = 0;
@@ -644,9 +644,12 @@ constexpr int64_t kOccupy = 512, kBusy = 2048, kPartKeys = 1024, kLongPartKeys =
 // 32 / 8 heads over 4096 keys, us, narrow / wide: 16 requests of 8 tokens (32 columns) 30 / 42, of 16 40 / 44, of 32 (16 x 32 x 32 rows) 61 / 51; 4 requests
 // of 64 35 / 43; 3 of 32 over 1000 keys 10 / 25; trees of 256 nodes, 8 x 32 heads, 88 / 53.
 constexpr int64_t kWideColumns = 64, kWideRows = 16384;
-inline Plan plan_of(int64_t T, int64_t R, int64_t G, int64_t Hk, int64_t max_len) {
+#ifndef GW
+#define GW 64
+#endif
+inline Plan plan_of(int64_t T, int64_t R, int64_t G, int64_t Hk, int64_t max_len, int64_t group=0) {
   Plan p;
-  const bool wide = T * G >= kWideColumns * R && T * G * Hk >= kWideRows;
+  const bool wide = group ? T * G >= group * R : T * G >= kWideColumns * R && T * G * Hk >= kWideRows;
   p.width = wide ? 128 : 16;
   p.pieces = bbm::count_pieces(T, R, G, p.width);
   const int64_t busy = std::max(std::min(T, R), bbm::ceil_div(T * G, p.width)) * Hk;  // pieces that belong to a request, or few fewer
@@ -761,7 +764,7 @@ struct SharedPlan {
 inline SharedPlan shared_plan_of(int64_t T, int64_t R, int64_t S, int64_t G, int64_t Hk, int64_t max_shared, int64_t max_own) {
   SharedPlan p;
   p.own = plan_of(T, R, G, Hk, max_own);
-  p.group = plan_of(T, std::max<int64_t>(S, 1), G, Hk, max_shared);
+  p.group = plan_of(T, std::max<int64_t>(S, 1), G, Hk, max_shared, GW);
   if (S == 0) p.group.pieces = 0, p.group.parts = 0;
   return p;
 }

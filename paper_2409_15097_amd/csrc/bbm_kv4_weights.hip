@@ -1,25 +1,29 @@
 // Weights that the keys of the 4-bit cache gather (include/bbm_cache.h): out = decay * weights + the sum of exp(scale <q, k> - lse) over the queries that see a key.
 //
-// One kernel, no exchange between work-groups: a wave owns 64 keys of one key head at a time and walks the columns (query token, head of the group) of its request, or of
-// its group for shared keys, 16 at a time:
-//   S = K Q^T (16 keys x 16 columns x 32 elements an instruction): lane (n, q) = (l % 16, l / 16) loads D / 4 elements of key n from q * D / 4 on, and of column n likewise, and has
-//   the scores of keys 4 q .. 4 q + 3 with column n; their exponentials are added up in the lane, and over 16 lanes at the end.
-// With up to 16 columns the cache's bytes are the bound (half of the attention's, values are not read: 17/32 byte an element, and 8 a key), so the next keys are under
-// way while these are used; with more, the codes are converted once for all columns, and the products and exponentials are the bound.
+// A work-group owns its keys: no sums pass between work-groups, and nothing depends on an order.  The queries of a request (of a group, for its shared keys) and a key head are
+// columns: column c is query token c / G, head c % G of the group.
+// Narrow, for few columns: bound by the cache's bytes (half of the attention's, values are not read: 17/32 byte an element, and 8 a key).  A wave takes 64 keys at a time, the next ones
+// under way while these are used, and 16 columns: S = K Q^T by 16 keys x 16 columns x 32 elements an instruction; lane (n, q) = (l % 16, l / 16) loads D / 4 elements of key n from
+// q * D / 4 on, and of column n likewise, and has the scores of keys 4 q .. 4 q + 3 with column n.
+// Wide, for many: bound by the exponentials and the products.  A work-group takes 128 keys, whose codes are converted once into operands in registers, and walks tiles of 64 columns
+// through LDS; a wave has 64 of the keys and 32 columns of every tile.
+// Either way a lane adds up the exponentials of its column, and lanes meet once, behind the last column.
 #include "bbm_cache.h"
 #include "bbm_kv4.h"
+#include "bbm_prompt.h"
 
 #include <algorithm>
 
 namespace {
 
-using bbm::bf16x8, bbm::Kv4, bbm::scalar;
+using bbm::bf16x8, bbm::f32x16, bbm::Kv4, bbm::scalar;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int NW = 4;
-constexpr int NB = 4;                // blocks of 16 keys that a wave has
-constexpr int kStep = 16 * NB * NW;  // keys of a work-group's step
+constexpr int NB = 4;                // blocks of 16 keys that a wave of the narrow kernel has
+constexpr int kStep = 16 * NB * NW;  // keys of its work-group's step
+constexpr int kWideKeys = 128, kWideCols = 64;
 
 struct WeightParams {
   Kv4 c;
@@ -32,9 +36,12 @@ struct WeightParams {
   const uint64_t* mask;
   int32_t T, R, S, G, max_pages, mask_words;
   int32_t group_parts, own_parts;  // work-groups of a group and key head, of a request and key head
-  int32_t group_wgs, own_wgs;      // of all of them
+  int32_t group_wgs, own_wgs;      // of all of them in this launch (the groups' come first)
+  int32_t tile_tokens, tile_heads; // of the wide kernel: what the columns of a tile are
   float rc, decay;                 // softmax_scale * log2(e)
 };
+
+typedef bbm::InPlace<WeightParams> Args;
 
 // Whose keys a work-group has, and who looks at them.
 struct Owner {
@@ -44,45 +51,103 @@ struct Owner {
   int prefix;       // keys in front of the new tokens (causal: of the first one that has a row here)
   int fresh;        // from this key on, new tokens
 };
-__device__ __forceinline__ int max_keys(const WeightParams& P) { return (int)min((int64_t)P.max_pages << P.c.page_shift, (int64_t)0x7fffffff); }
-__device__ __forceinline__ int shared_of(const WeightParams& P, int g) { return (int)scalar(max(0, min(P.shared_lens[g], max_keys(P))) & ~15); }
-__device__ __forceinline__ int row_cut(const WeightParams& P, int c) { return min(max(c, 0), P.T); }
-__device__ __forceinline__ int request_cut(const WeightParams& P, int g) { return min(max(P.group_cu[g], 0), P.R); }
-__device__ __forceinline__ Owner owner_of_group(const WeightParams& P, int g) {
-  const int r0 = request_cut(P, g), r1 = request_cut(P, g + 1);
+__device__ __forceinline__ int max_keys(Args P) { return (int)min((int64_t)P->max_pages << P->c.page_shift, (int64_t)0x7fffffff); }
+// The keys that a group shares, in whole blocks of 16: what is left over is each request's own.
+__device__ __forceinline__ int shared_keys(Args P, int keys) { return max(0, min(keys, max_keys(P))) & ~15; }
+__device__ __forceinline__ int row_cut(Args P, int c) { return min(max(c, 0), P->T); }
+__device__ __forceinline__ int request_cut(Args P, int g) { return min(max(bbm::global(P->group_cu)[g], 0), P->R); }
+__device__ __forceinline__ Owner owner_of_group(Args P, int g) {
+  const int r0 = request_cut(P, g), r1 = request_cut(P, g + 1), shared = (int)scalar(bbm::global(P->shared_lens)[g]);
   Owner x;
-  x.begin = (int)scalar(row_cut(P, P.cu[r0])), x.end = (int)scalar(row_cut(P, P.cu[r1]));
-  x.r = min((int)scalar(r0), P.R - 1);
+  x.begin = (int)scalar(row_cut(P, bbm::global(P->cu)[r0])), x.end = (int)scalar(row_cut(P, bbm::global(P->cu)[r1]));
+  x.r = min((int)scalar(r0), P->R - 1);
   x.from = 0;
-  x.len = x.prefix = x.fresh = shared_of(P, g);
+  x.len = x.prefix = x.fresh = shared_keys(P, shared);
   return x;
 }
-__device__ __forceinline__ Owner owner_of_request(const WeightParams& P, int r) {
-  const int c0 = (int)scalar(P.cu[r]), c1 = (int)scalar(P.cu[r + 1]), len = (int)scalar(P.lens[r]);
+__device__ __forceinline__ Owner owner_of_request(Args P, int r) {
+  const bbm::Group shared = bbm::group_of(bbm::global(P->group_cu), bbm::global(P->shared_lens), P->S, r);  // (one trip to memory for all that is known of a request)
+  const int c0 = (int)scalar(bbm::global(P->cu)[r]), c1 = (int)scalar(bbm::global(P->cu)[r + 1]), len = (int)scalar(bbm::global(P->lens)[r]);
   Owner x;
   x.r = r;
   x.begin = row_cut(P, c0), x.end = row_cut(P, c1);
   x.fresh = (int)((uint32_t)len - (uint32_t)max(0, c1 - c0));
-  x.prefix = P.mask ? x.fresh : (int)((uint32_t)x.fresh + (uint32_t)x.begin - (uint32_t)c0);
+  x.prefix = bbm::global(P->mask) ? x.fresh : (int)((uint32_t)x.fresh + (uint32_t)x.begin - (uint32_t)c0);
   x.len = max(0, min(len, max_keys(P)));
-  const int g = bbm::group_of(P.group_cu, P.S, r);
-  x.from = g >= 0 ? min(shared_of(P, g), x.len) : 0;
+  x.from = min(shared_keys(P, shared.keys), x.len);
   return x;
 }
 
+// Which keys a work-group begins with, and how far the next ones are.
+struct Share {
+  Owner x;
+  int hk, part, parts, cols;
+};
+// Of the wide kernel the work-groups of a request and key head go to one XCD, whose cache holds their queries, and heads of all requests to every XCD (in the order of the requests, three
+// prompts of 1500, 420 and 839 tokens were on one third of the chip each, and a step took 254 us); the narrow one's, which read nothing twice, to all in turn.
+template <bool WIDE>
+__device__ __forceinline__ Share share_of(Args P, bool group) {
+  const int wg = (int)blockIdx.x - (group ? 0 : P->group_wgs), owners = group ? P->S : P->R;
+  Share y = {};
+  y.parts = group ? P->group_parts : P->own_parts;
+  int owner;
+  if (WIDE) {
+    const bbm::Work w = bbm::work_of(wg, owners * P->c.Hk);
+    y.hk = w.plane / owners, owner = w.plane % owners, y.part = w.number;
+    if (y.part >= y.parts) return y;
+  } else {
+    const int rest = wg / y.parts;
+    y.part = wg % y.parts, y.hk = rest % P->c.Hk, owner = rest / P->c.Hk;
+  }
+  y.x = group ? owner_of_group(P, owner) : owner_of_request(P, owner);
+  y.cols = max(0, y.x.end - y.x.begin) * P->G;
+  return y;
+}
+
+// A column, and where its query and its log-sum-exp lie; `ahead` columns further, cut to (tokens, heads).
+struct Column {
+  int col, i, g;
+  const __bf16* q;
+  const float* lse;
+};
+struct Stride {
+  int cols, i, g;
+};
+__device__ __forceinline__ Stride stride_of(Args P, int cols) { return {cols, cols / P->G, cols % P->G}; }
+__device__ __forceinline__ Column column_of(Args P, const __bf16* q0, const float* lse0, int c) {
+  Column y;
+  y.col = c, y.i = c / P->G, y.g = c - y.i * P->G;
+  y.q = q0 + y.i * P->q_row + y.g * P->q_head;
+  y.lse = lse0 + (int64_t)y.g * P->T + y.i;
+  return y;
+}
+__device__ __forceinline__ void advance(Args P, Column& y, const Stride& s) {
+  y.col += s.cols, y.i += s.i;
+  y.q += s.i * P->q_row + s.g * P->q_head;
+  y.lse += (int64_t)s.g * P->T + s.i;
+  if (s.g != 0) {  // (of a group of 1, 2, 4 .. heads the head stays)
+    y.g += s.g;
+    const bool over = y.g >= P->G;
+    y.g -= over ? P->G : 0, y.i += over;
+    y.q += over ? P->q_row - P->G * P->q_head : 0;
+    y.lse += over ? 1 - (int64_t)P->G * P->T : 0;
+  }
+}
+__device__ __forceinline__ float minus_lse(float l) { return l != -INFINITY ? l * -kLog2e : -INFINITY; }  // (a row that saw nothing gives nothing)
+// Which of the keys from j on the new token of a column sees.
+__device__ __forceinline__ uint64_t seen_by(Args P, const Owner& x, int i, int j) {
+  i = min(i, x.end - x.begin - 1);
+  return bbm::seen_from(bbm::global(P->mask) ? bbm::global(P->mask) + (int64_t)(x.begin + i) * P->mask_words : nullptr, P->mask_words, i, j - x.prefix);
+}
+
 template <int D>
-__global__ __launch_bounds__(64 * NW, 3) void kv4_weights_kernel(const WeightParams P) {
+__device__ __forceinline__ void narrow(Args P, const Share& own) {
   constexpr int KS = D / 32;  // steps of a product, and words of codes that a lane loads of a key
   const int lane = threadIdx.x & 63, n = lane & 15, kq = lane >> 4;
   const int wave = (int)scalar(threadIdx.x >> 6);
-  const int ahead = (P.group_wgs + 7) & ~7;  // (a multiple of 8, so that both kinds spread over the XCDs alike)
-  const bool group = (int)blockIdx.x < ahead;
-  const int wg = (int)blockIdx.x - (group ? 0 : ahead), total = group ? P.group_wgs : P.own_wgs, parts = group ? P.group_parts : P.own_parts;
-  if (wg >= total) return;
-  const int at = bbm::logical_wg(wg, total), part = at % parts, hk = at / parts % P.c.Hk, unit = at / parts / P.c.Hk;
-  const Owner x = group ? owner_of_group(P, unit) : owner_of_request(P, unit);
-  const int cols = (x.end - x.begin) * P.G;
-  if (x.end <= x.begin) return;
+  const Owner& x = own.x;
+  const int hk = own.hk, cols = own.cols;
+  if (cols == 0) return;
 
   struct Raw {
     uint32_t k[NB][KS], ks[NB];
@@ -90,26 +155,26 @@ __global__ __launch_bounds__(64 * NW, 3) void kv4_weights_kernel(const WeightPar
     int64_t place;   // where they lie
     int have;        // how many of them are there
   };
-  const bbm::Table table = (bbm::Table)(uintptr_t)(P.table + x.r * P.table_stride);
+  const bbm::Table table = (bbm::Table)(uintptr_t)(bbm::global(P->table) + x.r * P->table_stride);
   struct Pages {
     int p[NB];
   };
   auto pages_at = [&](int j) __attribute__((always_inline)) {
     Pages y;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) y.p[b] = table[scalar(min(j + 16 * b, x.len - 1) >> P.c.page_shift)];
+    for (int b = 0; b < NB; ++b) y.p[b] = table[scalar(min(j + 16 * b, x.len - 1) >> P->c.page_shift)];
     return y;
   };
   // the wave's 64 keys from j on; of those that are not there zeros, and of the weights the cache's first
-  auto load = [&](Raw& z, int j, const Pages& pages) __attribute__((always_inline)) {
+  auto load = [&](Raw& z, int j, const Pages& pages, const float* weights) __attribute__((always_inline)) {
     z.have = 0;
     z.place = 0;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const int jb = j + 16 * b, page = pages.p[b];
-      const bool there = jb < x.len && page >= 0 && page < P.c.pages;
-      const int64_t key = ((int64_t)page * P.c.Hk + hk) * P.c.page + (jb & (P.c.page - 1));
-      const __amdgpu_buffer_rsrc_t k_r = bbm::buffer_of(P.c.k + key * (D / 2), there ? 16 * (D / 2) : 0), ks_r = bbm::buffer_of(P.c.k_scale + key * (D / 32), there ? D / 2 : 0);
+      const bool there = jb < x.len && page >= 0 && page < P->c.pages;
+      const int64_t key = ((int64_t)page * P->c.Hk + hk) * P->c.page + (jb & (P->c.page - 1));
+      const __amdgpu_buffer_rsrc_t k_r = bbm::buffer_of(bbm::global(P->c.k) + key * (D / 2), there ? 16 * (D / 2) : 0), ks_r = bbm::buffer_of(bbm::global(P->c.k_scale) + key * (D / 32), there ? D / 2 : 0);
       if constexpr (D == 128) {
         const bbm::u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(k_r, n * (D / 2) + kq * 16, 0, 0);
         for (int i = 0; i < 4; ++i) z.k[b][i] = w[i];
@@ -120,52 +185,28 @@ __global__ __launch_bounds__(64 * NW, 3) void kv4_weights_kernel(const WeightPar
       z.ks[b] = __builtin_amdgcn_raw_buffer_load_b8(ks_r, n * (D / 32) + kq * D / 128, 0, 0);
       if (n == b && there) z.have = max(0, min(4, x.len - jb - 4 * kq)), z.place = key + 4 * kq;
     }
-    z.old = *reinterpret_cast<const f32x4*>(P.weights + z.place);
+    z.old = *reinterpret_cast<const f32x4*>(weights + z.place);
   };
-  auto store = [&](const Raw& z, int j, f32x4 (&sum)[NB]) __attribute__((always_inline)) {
+  auto store = [&](const Raw& z, int j, f32x4 (&sum)[NB], float keep, int fresh_from) __attribute__((always_inline)) {
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) sum[b][r] = bbm::row_sum<16>(sum[b][r]);
     f32x4 y = n == 0 ? sum[0] : n == 1 ? sum[1] : n == 2 ? sum[2] : sum[3];
-    const int fresh = x.fresh - (j + 16 * n + 4 * kq);  // how many of the four were there before
+    const int fresh = fresh_from - (j + 16 * n + 4 * kq);  // how many of the four were there before
 #pragma unroll
-    for (int r = 0; r < 4; ++r) y[r] += r < fresh ? P.decay * z.old[r] : 0.0f;
+    for (int r = 0; r < 4; ++r) y[r] += r < fresh ? keep * z.old[r] : 0.0f;
     if (z.have == 4) {
-      *reinterpret_cast<f32x4*>(P.out + z.place) = y;
+      *reinterpret_cast<f32x4*>(bbm::global(P->out) + z.place) = y;
     } else {
 #pragma unroll
       for (int r = 0; r < 3; ++r)
-        if (r < z.have) P.out[z.place + r] = y[r];
+        if (r < z.have) bbm::global(P->out)[z.place + r] = y[r];
     }
   };
 
-  // The lane's column, 16 further with every tile: its token and head, and where its query and its log-sum-exp lie.
-  struct Column {
-    int col, i, g;
-    const __bf16* q;
-    const float* lse;
-  };
-  const int di = 16 / P.G, dg = 16 % P.G;
-  const __bf16* const q0 = P.q + (int64_t)x.begin * P.q_row + (int64_t)hk * P.G * P.q_head + kq * (D / 4);
-  const float* const lse0 = P.lse + (int64_t)hk * P.G * P.T + x.begin;
-  auto column = [&](int c) __attribute__((always_inline)) {
-    Column y;
-    y.col = c, y.i = c / P.G, y.g = c - y.i * P.G;
-    y.q = q0 + y.i * P.q_row + y.g * P.q_head;
-    y.lse = lse0 + (int64_t)y.g * P.T + y.i;
-    return y;
-  };
-  auto advance = [&](Column& y) __attribute__((always_inline)) {
-    y.col += 16, y.i += di, y.g += dg;
-    y.q += di * P.q_row + dg * P.q_head;
-    y.lse += (int64_t)dg * P.T + di;
-    if (y.g >= P.G) {
-      y.g -= P.G, y.i += 1;
-      y.q += P.q_row - P.G * P.q_head;
-      y.lse += 1 - (int64_t)P.G * P.T;
-    }
-  };
+  const __bf16* const q0 = bbm::global(P->q) + (int64_t)x.begin * P->q_row + (int64_t)hk * P->G * P->q_head + kq * (D / 4);
+  const float* const lse0 = bbm::global(P->lse) + (int64_t)hk * P->G * P->T + x.begin;
   struct Query {
     bf16x8 q[KS];
     float nl;  // what is added to its exponents
@@ -178,103 +219,247 @@ __global__ __launch_bounds__(64 * NW, 3) void kv4_weights_kernel(const WeightPar
     const float l = *(there ? y.lse : lse0);
 #pragma unroll
     for (int s = 0; s < KS; ++s) z.q[s] = *reinterpret_cast<const bf16x8*>(p + 8 * s);
-    z.nl = there && l != -INFINITY ? l * -kLog2e : -INFINITY;
+    z.nl = there ? minus_lse(l) : -INFINITY;
     return z;
   };
-  // the exponentials of 16 keys from j on with the lane's column; all_see: the last key that all 16 columns see
-  auto add = [&](f32x4& sum, f32x4 s, const Query& z, const Column& y, int j, int all_see) __attribute__((always_inline)) {
-    f32x4 p;
+  // 64 keys from j on with 16 columns; all_see: the last key that all of them see
+  auto use = [&](const Raw& a, f32x4 (&sum)[NB], const Query& z, const Column& y, int j, int all_see) __attribute__((always_inline)) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], P.rc, z.nl));
-    if (j + 15 > all_see) {
-      const int i = min(y.i, x.end - x.begin - 1);
-      const uint32_t seen = (uint32_t)bbm::seen_from(P.mask ? P.mask + (int64_t)(x.begin + i) * P.mask_words : nullptr, P.mask_words, i, j + 4 * kq - x.prefix);
+    for (int b = 0; b < NB; ++b) {
+      f32x4 s = f32x4{0.0f, 0.0f, 0.0f, 0.0f}, p;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) p[r] = seen >> r & 1 ? p[r] : 0.0f;
+      for (int i = 0; i < KS; ++i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bbm::values_of(a.k[b][i], bbm::scale_of(a.ks[b])), z.q[i], s, 0, 0, 0);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], P->rc, z.nl));
+      if (j + 16 * b + 15 > all_see) {
+        const uint32_t seen = (uint32_t)seen_by(P, x, y.i, j + 16 * b + 4 * kq);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[r] = seen >> r & 1 ? p[r] : 0.0f;
+      }
+      sum[b] = p;
     }
-    sum += p;
   };
 
-  int j = x.from + part * kStep + wave * (16 * NB);
-  if (j >= x.len) return;
-  const int next = parts * kStep;
-  if (cols <= 16) {
-    const Column y = column(n);
+  const int j0 = x.from + own.part * kStep + wave * (16 * NB), next = own.parts * kStep;
+  if (j0 >= x.len) return;
+  Column y = column_of(P, q0, lse0, n);
+  const Stride ahead = stride_of(P, 16);
+  // 16 columns at a time over all keys; those behind the first 16 are added to what was stored.
+#pragma unroll 1
+  for (int c = 0; c < cols; c += 16) {
     const Query z = fetch(y);
-    const int all_see = P.mask ? x.prefix - 1 : x.prefix;
-    auto use = [&](Raw& a, int j) __attribute__((always_inline)) {
+    const int all_see = P->mask ? x.prefix - 1 : x.prefix + c / P->G;
+    const float* const old = c == 0 ? bbm::global(P->weights) : bbm::global(P->out);
+    const float keep = c == 0 ? P->decay : 1.0f;
+    const int fresh = c == 0 ? x.fresh : x.len;
+    auto step = [&](const Raw& a, int j) __attribute__((always_inline)) {
       f32x4 sum[NB];
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        f32x4 s = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        sum[b] = s;
-#pragma unroll
-        for (int i = 0; i < KS; ++i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bbm::values_of(a.k[b][i], bbm::scale_of(a.ks[b])), z.q[i], s, 0, 0, 0);
-        add(sum[b], s, z, y, j + 16 * b, all_see);
-      }
-      store(a, j, sum);
+      use(a, sum, z, y, j, all_see);
+      store(a, j, sum, keep, fresh);
     };
     // the next keys are asked for before these are used, their pages a step before that
     Raw a, b;
-    load(a, j, pages_at(j));
+    int j = j0;
+    load(a, j, pages_at(j), old);
     Pages pages = pages_at(j + next);
 #pragma unroll 1
     for (;;) {
-      load(b, j + next, pages);
+      load(b, j + next, pages, old);
       pages = pages_at(j + 2 * next);
-      use(a, j);
+      step(a, j);
       j += next;
-      if (j >= x.len) return;
-      load(a, j + next, pages);
+      if (j >= x.len) break;
+      load(a, j + next, pages, old);
       pages = pages_at(j + 2 * next);
-      use(b, j);
+      step(b, j);
       j += next;
-      if (j >= x.len) return;
+      if (j >= x.len) break;
     }
-  }
-#pragma unroll 1
-  for (; j < x.len; j += next) {
-    Raw a;
-    load(a, j, pages_at(j));
-    // (a causal key is seen by no column in front of its own token's)
-    const int start = P.mask ? 0 : min(max(0, j - x.prefix), x.end - x.begin - 1) * P.G & ~15;
-    Column y = column(start + n);
-    Query z = fetch(y);
-    bf16x8 k[NB][KS];
-    f32x4 sum[NB];
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      sum[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int i = 0; i < KS; ++i) k[b][i] = bbm::values_of(a.k[b][i], bbm::scale_of(a.ks[b]));
-    }
-    int i0 = start / P.G, g0 = start - i0 * P.G;  // the tile's first column
-#pragma unroll 1
-    for (int c = start; c < cols; c += 16) {
-      const int all_see = P.mask ? x.prefix - 1 : x.prefix + i0;
-      Column yn = y;
-      advance(yn);
-      const Query zn = fetch(yn);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        f32x4 s = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int i = 0; i < KS; ++i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[b][i], z.q[i], s, 0, 0, 0);
-        add(sum[b], s, z, y, j + 16 * b, all_see);
-      }
-      y = yn, z = zn;
-      i0 += di, g0 += dg;
-      if (g0 >= P.G) g0 -= P.G, i0 += 1;
-    }
-    store(a, j, sum);
+    advance(P, y, ahead);
   }
 }
 
-// Work-groups of an owner: enough to fill the chip, no more than it has steps for.
-constexpr int64_t kFill = 2048, kMaxParts = 1 << 17;  // (two steps behind a key are still a 32-bit number)
-inline int64_t parts_of(int64_t owners, int64_t Hk, int64_t keys, bool many_columns) {
-  const int64_t steps = bbm::ceil_div(std::min<int64_t>(keys, bbm::kMaxTokens), kStep);
-  return std::min(many_columns ? steps : std::min(steps, bbm::ceil_div(kFill, owners * Hk)), kMaxParts);
+template <int D>
+__device__ __forceinline__ void wide(Args P, const Share& own) {
+  using L = bbm::TL<D>;
+  constexpr int KS = D / 16, RC = D / 8;
+  constexpr int ROWS = 64 * NW / RC, PIECES = kWideCols / ROWS;  // rows of a tile that the threads fetch at a time
+  __shared__ __attribute__((aligned(16))) __bf16 q_s[2][L::ELEMS];
+  __shared__ float sum_s[2][kWideKeys];
+  const int tid = threadIdx.x, lane = tid & 63, lq = lane & 31, hh = lane >> 5;
+  const int wave = (int)scalar(tid >> 6), key_half = wave >> 1, col_half = wave & 1;
+  const Owner& x = own.x;
+  const int hk = own.hk;
+  if (own.cols == 0) return;
+  const int32_t* const table = bbm::global(P->table) + x.r * P->table_stride;
+  bbm::TileAddr<D> A;
+  A.init(lane);
+  // the slot of a key in what has a number for each token and head, -1 if it is not there
+  auto slot_of = [&](int j) -> int64_t {
+    const int page = table[min(j, x.len - 1) >> P->c.page_shift];
+    return j < x.len && page >= 0 && page < P->c.pages ? (((int64_t)page * P->c.Hk + hk) << P->c.page_shift) + (j & (P->c.page - 1)) : -1;
+  };
+
+  // A tile's columns are `heads` heads of `tokens` tokens, side by side (of 64 columns those behind them are not used, and repeat the first one): what a thread fetches of a tile lies
+  // at the same distance from the tile's first query every time.
+  const int tokens = P->tile_tokens, heads = P->tile_heads, n = x.end - x.begin, G = P->G;
+  const int64_t q_row = P->q_row, q_head = P->q_head;
+  const float rc = P->rc;
+  const bool masked = P->mask != nullptr;
+  uint32_t off[PIECES];
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+    const int c = tid / RC + ROWS * p, t = c / heads;
+    off[p] = (uint32_t)((t < tokens ? t * q_row + (c - t * heads) * q_head : 0) + tid % RC * 8) * 2u;
+  }
+  const int my_c = 32 * col_half + lq, my_t = my_c / heads, my_h = my_c - my_t * heads;
+  const bool used = my_t < tokens;
+  const float* const lse0 = bbm::global(P->lse) + (int64_t)hk * G * P->T + x.begin;
+  const int64_t my_lse = (int64_t)my_h * P->T + my_t;
+  const __bf16* const q0 = bbm::global(P->q) + (int64_t)x.begin * q_row + (int64_t)hk * G * q_head;
+  struct Tile {
+    int i, h;  // its first token and head
+  };
+  auto after = [&](Tile t) __attribute__((always_inline)) {
+    t.h += heads;
+    if (t.h >= G) t.h = 0, t.i += tokens;
+    return t;
+  };
+
+#pragma unroll 1
+  for (int j0 = x.from + own.part * kWideKeys; j0 < x.len; j0 += own.parts * kWideKeys) {
+    // (a causal key is seen by no token in front of its own)
+    Tile now = {masked ? 0 : min(max(0, j0 - x.prefix), n - 1) / tokens * tokens, 0}, next = now;
+    bf16x8 staged[PIECES];
+    float l;
+    auto fetch = [&]() __attribute__((always_inline)) {  // (of tokens and heads that are not there: zeros, or what lies between those that are)
+      const int ts = min(tokens, n - next.i), hs = min(heads, G - next.h);
+      const __amdgpu_buffer_rsrc_t r = bbm::buffer_of(q0 + next.i * q_row + next.h * q_head, ts > 0 ? (int)(((ts - 1) * q_row + (hs - 1) * q_head + D) * 2) : 0);
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) staged[p] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(r, off[p], 0, 0));
+      l = lse0[my_t < ts && my_h < hs ? my_lse + (int64_t)next.h * P->T + next.i : 0];
+      next = after(next);
+    };
+    auto put = [&](__bf16* dst) __attribute__((always_inline)) {
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) {
+        const int r = tid / RC + ROWS * p;
+        *reinterpret_cast<bf16x8*>(dst + r % L::NBLK * L::TBLK + r / L::NBLK * D + (tid % RC ^ (r >> 2 & 3)) * 8) = staged[p];
+      }
+    };
+    // A tile is asked for two steps before it is used, and goes to LDS one step before.
+    fetch();
+    // this wave's keys as operands: lane (l % 32, l / 32) has elements 16 t + 8 (l / 32) .. of key l % 32, and zeros of one that is not there
+    bf16x8 k[2][KS];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      const int64_t s = slot_of(j0 + 64 * key_half + 32 * kb + lq);
+      uint32_t w[KS], scales = 0;
+      for (int t = 0; t < KS; ++t) w[t] = 0;
+      if (s >= 0) {
+        const uint32_t* const codes = reinterpret_cast<const uint32_t*>(bbm::global(P->c.k) + s * (D / 2)) + hh;
+#pragma unroll
+        for (int t = 0; t < KS; ++t) w[t] = codes[2 * t];
+        if constexpr (D == 128) scales = *reinterpret_cast<const uint32_t*>(bbm::global(P->c.k_scale) + s * 4);
+        else scales = *reinterpret_cast<const uint16_t*>(bbm::global(P->c.k_scale) + s * 2);
+      }
+#pragma unroll
+      for (int t = 0; t < KS; ++t) k[kb][t] = bbm::values_of(w[t], bbm::scale_of(scales >> (8 * (t / 2)) & 0xff));
+    }
+    f32x16 sum[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+      for (int e = 0; e < 16; ++e) sum[kb][e] = 0.0f;
+
+    const int64_t place = tid < kWideKeys ? slot_of(j0 + tid) : -1;  // of the key that this thread writes
+    const float old = place >= 0 && j0 + tid < x.fresh ? P->decay * bbm::global(P->weights)[place] : 0.0f;
+    put(q_s[0]);
+    float l_now = l;
+    fetch();
+    int buf = 0;
+#pragma unroll 1
+    for (; now.i < n; now = after(now), buf ^= 1) {
+      const float nl = used ? minus_lse(l_now) : -INFINITY;
+      __syncthreads();  // the tile is there, and everyone is done with the other buffer
+      const __bf16* const tile = q_s[0] + buf * L::ELEMS;
+      f32x16 s[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+        for (int e = 0; e < 16; ++e) s[kb][e] = 0.0f;
+#pragma unroll
+      for (int t = 0; t < KS; ++t) {
+        const bf16x8 f = A.row_frag(tile, col_half, t);
+        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[0][t], f, s[0], 0, 0, 0);
+        s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[1][t], f, s[1], 0, 0, 0);
+      }
+      put(q_s[0] + (buf ^ 1) * L::ELEMS);
+      l_now = l;
+      fetch();
+      const int j = j0 + 64 * key_half, all_see = masked ? x.prefix - 1 : x.prefix + now.i;
+      if (j + 63 <= all_see && now.i + tokens <= n && now.h + heads <= G) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+          for (int e = 0; e < 16; ++e) sum[kb][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][e], rc, nl));
+      } else {
+        const bool there = now.i + my_t < n && now.h + my_h < G;
+        const uint64_t seen = there ? seen_by(P, x, now.i + my_t, j) : 0;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          const uint32_t w = (uint32_t)(seen >> (32 * kb)) >> (4 * hh);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][e], rc, nl));
+            sum[kb][e] += w >> (8 * (e / 4) + e % 4) & 1 ? p : 0.0f;
+          }
+        }
+      }
+    }
+    // over the columns: 32 lanes, then the two waves of the same keys
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float y = bbm::row_sum<16>(sum[kb][e]);
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+        const float both = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+        if (lq == 0) sum_s[col_half][64 * key_half + 32 * kb + 8 * (e / 4) + 4 * hh + e % 4] = both;
+      }
+    __syncthreads();
+    if (place >= 0) bbm::global(P->out)[place] = sum_s[0][tid] + sum_s[1][tid] + old;
+    __syncthreads();
+  }
+}
+
+template <int D, bool WIDE>
+__global__ __launch_bounds__(64 * NW, WIDE ? 2 : D == 128 ? 3 : 4) void kv4_weights_kernel(const WeightParams) {
+  Args P = bbm::kernel_args<WeightParams>();
+  const Share own = share_of<WIDE>(P, (int)blockIdx.x < P->group_wgs);
+  if constexpr (WIDE) wide<D>(P, own);
+  else narrow<D>(P, own);
+}
+// The groups' keys have many columns, the requests' few: both side by side.
+template <int D>
+__global__ __launch_bounds__(64 * NW, 2) void kv4_weights_both_kernel(const WeightParams) {
+  Args P = bbm::kernel_args<WeightParams>();
+  if ((int)blockIdx.x < P->group_wgs) wide<D>(P, share_of<true>(P, true));
+  else narrow<D>(P, share_of<false>(P, false));
+}
+
+// Work-groups of an owner: of the narrow kernel enough to fill the chip, of the wide one as many as it has pieces.
+constexpr int64_t kFill = 1024, kMaxParts = 1 << 17;  // (two steps behind a key are still a 32-bit number)
+inline int64_t parts_of(int64_t owners, int64_t Hk, int64_t keys, bool wide) {
+  keys = std::min<int64_t>(keys, bbm::kMaxTokens);
+  return std::min(wide ? bbm::ceil_div(keys, kWideKeys) : std::min(bbm::ceil_div(keys, kStep), bbm::ceil_div(kFill, owners * Hk)), kMaxParts);
+}
+// Columns of an owner, on average, from which on its codes are better converted once.
+constexpr int64_t kWideFrom = 32;
+
+template <int D>
+void launch(const WeightParams& P, bool group_wide, bool own_wide, hipStream_t s) {
+  const unsigned wgs = (unsigned)(P.group_wgs + P.own_wgs);
+  if (own_wide) kv4_weights_kernel<D, true><<<wgs, 64 * NW, 0, s>>>(P);
+  else if (group_wide) kv4_weights_both_kernel<D><<<wgs, 64 * NW, 0, s>>>(P);
+  else kv4_weights_kernel<D, false><<<wgs, 64 * NW, 0, s>>>(P);
 }
 
 }  // namespace
@@ -308,14 +493,18 @@ extern "C" __attribute__((visibility("default"))) int bbm_kv4_weights(const bbm_
   P.cu = cu, P.lens = lens, P.table = block_table, P.group_cu = group_cu, P.shared_lens = shared_lens, P.mask = mask;
   P.T = (int32_t)T, P.R = (int32_t)R, P.S = (int32_t)S, P.G = (int32_t)G, P.max_pages = (int32_t)max_pages, P.mask_words = (int32_t)mask_words;
   P.rc = softmax_scale * kLog2e, P.decay = decay;
-  const int64_t group_parts = S > 0 ? parts_of(S, cache->Hk, max_shared, T * G > 16 * S) : 1, own_parts = parts_of(R, cache->Hk, max_own, T * G > 16 * R);
-  const int64_t group_wgs = S * cache->Hk * group_parts, own_wgs = R * cache->Hk * own_parts;
+  const bool own_wide = T * G > kWideFrom * R, group_wide = S > 0 && T * G > kWideFrom * S;  // (of the requests only if of the groups, S <= R)
+  const int64_t group_parts = S > 0 ? parts_of(S, cache->Hk, max_shared, group_wide) : 1, own_parts = parts_of(R, cache->Hk, max_own, own_wide);
+  auto count = [&](int64_t owners, int64_t parts, bool wide) { return wide ? work_groups(owners * cache->Hk, parts) : owners * cache->Hk * parts; };
+  const int64_t group_wgs = count(S, group_parts, group_wide), own_wgs = count(R, own_parts, own_wide);
   if (R * cache->Hk >= kMaxWgs || group_wgs >= kMaxWgs / 2 || own_wgs >= kMaxWgs / 2)
     return fail(BBM_EUNSUPPORTED, "%s: problem too large (R=%lld, Hk=%lld, keys %lld and %lld)", fn, (long long)R, (long long)cache->Hk, (long long)max_shared, (long long)max_own);
+  // (heads of a tile that a buffer's 31 bits reach: of rows up to 2^22 elements apart 64 tokens are within 2^29 bytes)
+  const int64_t reach = q->head_stride > 0 ? 1 + (1ll << 29) / q->head_stride : kWideCols;
+  P.tile_heads = (int32_t)std::min({G, (int64_t)kWideCols, reach}), P.tile_tokens = kWideCols / P.tile_heads;
   P.group_parts = (int32_t)group_parts, P.own_parts = (int32_t)own_parts, P.group_wgs = (int32_t)group_wgs, P.own_wgs = (int32_t)own_wgs;
-  const unsigned wgs = (unsigned)(((group_wgs + 7) & ~7ll) + own_wgs);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (cache->d == 64) kv4_weights_kernel<64><<<wgs, 64 * NW, 0, s>>>(P);
-  else kv4_weights_kernel<128><<<wgs, 64 * NW, 0, s>>>(P);
+  if (cache->d == 64) launch<64>(P, group_wide, own_wide, s);
+  else launch<128>(P, group_wide, own_wide, s);
   return launch_status(fn);
 }
