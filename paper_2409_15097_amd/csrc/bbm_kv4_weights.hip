@@ -6,7 +6,7 @@
 // under way while these are used, and 16 columns: S = K Q^T by 16 keys x 16 columns x 32 elements an instruction; lane (n, q) = (l % 16, l / 16) loads D / 4 elements of key n from
 // q * D / 4 on, and of column n likewise, and has the scores of keys 4 q .. 4 q + 3 with column n.
 // Wide, for many: bound by the exponentials and the products.  A work-group takes 128 keys, whose codes are converted once into operands in registers, and walks tiles of 64 columns
-// through LDS; a wave has 64 of the keys and 32 columns of every tile.
+// through LDS; a wave has 32 of the keys and 32 columns of every tile.
 // Either way a lane adds up the exponentials of its column, and lanes meet once, behind the last column.
 #include "bbm_cache.h"
 #include "bbm_kv4.h"
@@ -20,7 +20,7 @@ using bbm::bf16x8, bbm::f32x16, bbm::Kv4, bbm::scalar;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int NW = 4;
+constexpr int NW = 8;
 constexpr int NB = 4;                // blocks of 16 keys that a wave of the narrow kernel has
 constexpr int kStep = 16 * NB * NW;  // keys of its work-group's step
 constexpr int kWideKeys = 128, kWideCols = 64;
@@ -83,18 +83,35 @@ struct Share {
   Owner x;
   int hk, part, parts, cols;
 };
-// Of the wide kernel the work-groups of a request and key head go to one XCD, whose cache holds their queries, and heads of all requests to every XCD (in the order of the requests, three
-// prompts of 1500, 420 and 839 tokens were on one third of the chip each, and a step took 254 us); the narrow one's, which read nothing twice, to all in turn.
+// Of up to 64 owners number `at` in the order of their work (queries times keys), the most first: the longest prompt's work-groups are not to be the last ones that start.
+__device__ __forceinline__ int by_work(Args P, bool group, int owners, int at) {
+  if (owners > 64 || owners == 1) return at;
+  const int lane = threadIdx.x & 63, o = min(lane, owners - 1);
+  const int r0 = group ? request_cut(P, o) : o, r1 = group ? request_cut(P, o + 1) : o + 1;
+  const int rows = max(0, row_cut(P, bbm::global(P->cu)[r1]) - row_cut(P, bbm::global(P->cu)[r0])), keys = max(0, group ? bbm::global(P->shared_lens)[o] : bbm::global(P->lens)[o]);
+  const float work = lane < owners ? (float)rows * (float)keys : -1.0f;
+  int rank = 0;
+  for (int j = 0; j < owners; ++j) {
+    const float other = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(work), j));
+    rank += other > work || (other == work && j < lane);
+  }
+  return min(__ffsll((unsigned long long)__ballot(lane < owners && rank == at)) - 1, owners - 1);
+}
+
+// Of the wide kernel an owner's work-groups lie one behind the other, those of a key head on one XCD, whose cache holds their queries (all of a request on one XCD: three prompts of 1500,
+// 420 and 839 tokens were on a third of the chip each, and took 254 us; in the order of the requests instead of their work, 168).
 template <bool WIDE>
 __device__ __forceinline__ Share share_of(Args P, bool group) {
-  const int wg = (int)blockIdx.x - (group ? 0 : P->group_wgs), owners = group ? P->S : P->R;
+  const int wg = (int)blockIdx.x - (group ? 0 : P->group_wgs);
   Share y = {};
   y.parts = group ? P->group_parts : P->own_parts;
   int owner;
   if (WIDE) {
-    const bbm::Work w = bbm::work_of(wg, owners * P->c.Hk);
-    y.hk = w.plane / owners, owner = w.plane % owners, y.part = w.number;
+    const int owners = group ? P->S : P->R, each = 8 * P->c.Hk * ((y.parts + 7) / 8), at = wg / each;
+    const bbm::Work w = bbm::work_of(wg - at * each, P->c.Hk);
+    y.hk = w.plane, y.part = w.number;
     if (y.part >= y.parts) return y;
+    owner = by_work(P, group, owners, at);
   } else {
     const int rest = wg / y.parts;
     y.part = wg % y.parts, y.hk = rest % P->c.Hk, owner = rest / P->c.Hk;
@@ -287,7 +304,7 @@ __device__ __forceinline__ void wide(Args P, const Share& own) {
   __shared__ __attribute__((aligned(16))) __bf16 q_s[2][L::ELEMS];
   __shared__ float sum_s[2][kWideKeys];
   const int tid = threadIdx.x, lane = tid & 63, lq = lane & 31, hh = lane >> 5;
-  const int wave = (int)scalar(tid >> 6), key_half = wave >> 1, col_half = wave & 1;
+  const int wave = (int)scalar(tid >> 6), key_part = wave >> 1, col_half = wave & 1;
   const Owner& x = own.x;
   const int hk = own.hk;
   if (own.cols == 0) return;
@@ -349,30 +366,23 @@ __device__ __forceinline__ void wide(Args P, const Share& own) {
     };
     // A tile is asked for two steps before it is used, and goes to LDS one step before.
     fetch();
-    // this wave's keys as operands: lane (l % 32, l / 32) has elements 16 t + 8 (l / 32) .. of key l % 32, and zeros of one that is not there
-    bf16x8 k[2][KS];
+    // This wave's keys as operands: lane (l % 32, l / 32) has elements 16 t + 8 (l / 32) .. of key l % 32; and the key that this thread writes.  (What is read for one that is not there,
+    // the cache's first, is left out of what is written.)
+    const int64_t mine = slot_of(j0 + 32 * key_part + lq), place = tid < kWideKeys ? slot_of(j0 + tid) : -1;
+    const int64_t from = max(mine, (int64_t)0);
+    const uint32_t* const codes = reinterpret_cast<const uint32_t*>(bbm::global(P->c.k) + from * (D / 2)) + hh;
+    uint32_t w[KS], scales;
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      const int64_t s = slot_of(j0 + 64 * key_half + 32 * kb + lq);
-      uint32_t w[KS], scales = 0;
-      for (int t = 0; t < KS; ++t) w[t] = 0;
-      if (s >= 0) {
-        const uint32_t* const codes = reinterpret_cast<const uint32_t*>(bbm::global(P->c.k) + s * (D / 2)) + hh;
+    for (int t = 0; t < KS; ++t) w[t] = codes[2 * t];
+    if constexpr (D == 128) scales = *reinterpret_cast<const uint32_t*>(bbm::global(P->c.k_scale) + from * 4);
+    else scales = *reinterpret_cast<const uint16_t*>(bbm::global(P->c.k_scale) + from * 2);
+    const float held = bbm::global(P->weights)[max(place, (int64_t)0)], old = j0 + tid < x.fresh ? P->decay * held : 0.0f;
+    bf16x8 k[KS];
 #pragma unroll
-        for (int t = 0; t < KS; ++t) w[t] = codes[2 * t];
-        if constexpr (D == 128) scales = *reinterpret_cast<const uint32_t*>(bbm::global(P->c.k_scale) + s * 4);
-        else scales = *reinterpret_cast<const uint16_t*>(bbm::global(P->c.k_scale) + s * 2);
-      }
-#pragma unroll
-      for (int t = 0; t < KS; ++t) k[kb][t] = bbm::values_of(w[t], bbm::scale_of(scales >> (8 * (t / 2)) & 0xff));
-    }
-    f32x16 sum[2];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-      for (int e = 0; e < 16; ++e) sum[kb][e] = 0.0f;
+    for (int t = 0; t < KS; ++t) k[t] = bbm::values_of(w[t], bbm::scale_of(scales >> (8 * (t / 2)) & 0xff));
+    f32x16 sum;
+    for (int e = 0; e < 16; ++e) sum[e] = 0.0f;
 
-    const int64_t place = tid < kWideKeys ? slot_of(j0 + tid) : -1;  // of the key that this thread writes
-    const float old = place >= 0 && j0 + tid < x.fresh ? P->decay * bbm::global(P->weights)[place] : 0.0f;
     put(q_s[0]);
     float l_now = l;
     fetch();
@@ -382,48 +392,35 @@ __device__ __forceinline__ void wide(Args P, const Share& own) {
       const float nl = used ? minus_lse(l_now) : -INFINITY;
       __syncthreads();  // the tile is there, and everyone is done with the other buffer
       const __bf16* const tile = q_s[0] + buf * L::ELEMS;
-      f32x16 s[2];
+      f32x16 s;
+      for (int e = 0; e < 16; ++e) s[e] = 0.0f;
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-        for (int e = 0; e < 16; ++e) s[kb][e] = 0.0f;
-#pragma unroll
-      for (int t = 0; t < KS; ++t) {
-        const bf16x8 f = A.row_frag(tile, col_half, t);
-        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[0][t], f, s[0], 0, 0, 0);
-        s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[1][t], f, s[1], 0, 0, 0);
-      }
+      for (int t = 0; t < KS; ++t) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[t], A.row_frag(tile, col_half, t), s, 0, 0, 0);
       put(q_s[0] + (buf ^ 1) * L::ELEMS);
       l_now = l;
       fetch();
-      const int j = j0 + 64 * key_half, all_see = masked ? x.prefix - 1 : x.prefix + now.i;
-      if (j + 63 <= all_see && now.i + tokens <= n && now.h + heads <= G) {
+      const int j = j0 + 32 * key_part, all_see = masked ? x.prefix - 1 : x.prefix + now.i;
+      if (j + 31 <= all_see && now.i + tokens <= n && now.h + heads <= G) {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-          for (int e = 0; e < 16; ++e) sum[kb][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][e], rc, nl));
+        for (int e = 0; e < 16; ++e) sum[e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], rc, nl));
       } else {
         const bool there = now.i + my_t < n && now.h + my_h < G;
-        const uint64_t seen = there ? seen_by(P, x, now.i + my_t, j) : 0;
+        const uint32_t seen = (there ? (uint32_t)seen_by(P, x, now.i + my_t, j) : 0) >> (4 * hh);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          const uint32_t w = (uint32_t)(seen >> (32 * kb)) >> (4 * hh);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][e], rc, nl));
-            sum[kb][e] += w >> (8 * (e / 4) + e % 4) & 1 ? p : 0.0f;
-          }
+        for (int e = 0; e < 16; ++e) {
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], rc, nl));
+          sum[e] += seen >> (8 * (e / 4) + e % 4) & 1 ? p : 0.0f;
         }
       }
     }
     // over the columns: 32 lanes, then the two waves of the same keys
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float y = bbm::row_sum<16>(sum[kb][e]);
-        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
-        const float both = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-        if (lq == 0) sum_s[col_half][64 * key_half + 32 * kb + 8 * (e / 4) + 4 * hh + e % 4] = both;
-      }
+    for (int e = 0; e < 16; ++e) {
+      const float y = bbm::row_sum<16>(sum[e]);
+      const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+      const float both = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+      if (lq == 0) sum_s[col_half][32 * key_part + 8 * (e / 4) + 4 * hh + e % 4] = both;
+    }
     __syncthreads();
     if (place >= 0) bbm::global(P->out)[place] = sum_s[0][tid] + sum_s[1][tid] + old;
     __syncthreads();
@@ -431,7 +428,7 @@ __device__ __forceinline__ void wide(Args P, const Share& own) {
 }
 
 template <int D, bool WIDE>
-__global__ __launch_bounds__(64 * NW, WIDE ? 2 : D == 128 ? 3 : 4) void kv4_weights_kernel(const WeightParams) {
+__global__ __launch_bounds__(64 * NW, 4) void kv4_weights_kernel(const WeightParams) {
   Args P = bbm::kernel_args<WeightParams>();
   const Share own = share_of<WIDE>(P, (int)blockIdx.x < P->group_wgs);
   if constexpr (WIDE) wide<D>(P, own);
@@ -439,14 +436,14 @@ __global__ __launch_bounds__(64 * NW, WIDE ? 2 : D == 128 ? 3 : 4) void kv4_weig
 }
 // The groups' keys have many columns, the requests' few: both side by side.
 template <int D>
-__global__ __launch_bounds__(64 * NW, 2) void kv4_weights_both_kernel(const WeightParams) {
+__global__ __launch_bounds__(64 * NW, 4) void kv4_weights_both_kernel(const WeightParams) {
   Args P = bbm::kernel_args<WeightParams>();
   if ((int)blockIdx.x < P->group_wgs) wide<D>(P, share_of<true>(P, true));
   else narrow<D>(P, share_of<false>(P, false));
 }
 
 // Work-groups of an owner: of the narrow kernel enough to fill the chip, of the wide one as many as it has pieces.
-constexpr int64_t kFill = 1024, kMaxParts = 1 << 17;  // (two steps behind a key are still a 32-bit number)
+constexpr int64_t kFill = 512, kMaxParts = 1 << 17;  // (two steps behind a key are still a 32-bit number)
 inline int64_t parts_of(int64_t owners, int64_t Hk, int64_t keys, bool wide) {
   keys = std::min<int64_t>(keys, bbm::kMaxTokens);
   return std::min(wide ? bbm::ceil_div(keys, kWideKeys) : std::min(bbm::ceil_div(keys, kStep), bbm::ceil_div(kFill, owners * Hk)), kMaxParts);
@@ -495,7 +492,7 @@ extern "C" __attribute__((visibility("default"))) int bbm_kv4_weights(const bbm_
   P.rc = softmax_scale * kLog2e, P.decay = decay;
   const bool own_wide = T * G > kWideFrom * R, group_wide = S > 0 && T * G > kWideFrom * S;  // (of the requests only if of the groups, S <= R)
   const int64_t group_parts = S > 0 ? parts_of(S, cache->Hk, max_shared, group_wide) : 1, own_parts = parts_of(R, cache->Hk, max_own, own_wide);
-  auto count = [&](int64_t owners, int64_t parts, bool wide) { return wide ? work_groups(owners * cache->Hk, parts) : owners * cache->Hk * parts; };
+  auto count = [&](int64_t owners, int64_t parts, bool wide) { return owners * (wide ? work_groups(cache->Hk, parts) : cache->Hk * parts); };
   const int64_t group_wgs = count(S, group_parts, group_wide), own_wgs = count(R, own_parts, own_wide);
   if (R * cache->Hk >= kMaxWgs || group_wgs >= kMaxWgs / 2 || own_wgs >= kMaxWgs / 2)
     return fail(BBM_EUNSUPPORTED, "%s: problem too large (R=%lld, Hk=%lld, keys %lld and %lld)", fn, (long long)R, (long long)cache->Hk, (long long)max_shared, (long long)max_own);
