@@ -4,7 +4,7 @@
 // agree with the bits before), writes down which of the places that remain become free, a bit each, in LDS, and moves: a kept key from behind finds the place of its number by
 // bisection over the counts of 64 places, then by counting bits.  Where the moves of the first kind end they read nothing that they write, so their order does not matter; the last
 // keys are shifted by whole rounds of all waves, with a barrier between a round's loads and its stores, in ascending order.
-// A second kernel gives the pages back: one wave a request, behind the sum of what the requests in front of it give back.
+// The pages go back by a wave for each request, behind the sum of what the requests in front of it give: of up to 256 requests in one more work-group, else by a second kernel.
 #include "bbm_cache.h"
 #include "bbm_kv4.h"
 
@@ -16,16 +16,20 @@ using bbm::Kv4, bbm::scalar;
 
 constexpr int NT = 1024, NWAVES = NT / 64;
 constexpr int kBins = 2048;
+constexpr int kGiveTogether = 256;  // requests whose pages one work-group gives back, while the others move keys
 constexpr int64_t kMaxBudget = 1 << 19;  // places that are bits and counts in LDS: 96 KiB
+// Of the 160 KiB of a CU's LDS: what a work-group may ask for without more, and what two and one of them may have beside 17 KiB of bins, sums and moves.
+constexpr int64_t kPlain = 44 << 10, kTwo = 62 << 10, kOne = 140 << 10;
 
 struct EvictParams {
   Kv4 c;
   float* weights;
   const int32_t *lens, *table, *first, *free_at;
   int32_t *new_lens, *free_pages, *free_next;
-  int32_t* given;  // [R] pages that a request gives back
+  int32_t* given;  // [R] pages that a request gives back; NULL if the first work-group sees to them
   int64_t table_stride, n_free;
   int32_t R, max_keys, budget, recent;
+  int32_t held;  // keys whose weights LDS has room for
 };
 
 // What stays of a request: keys f .. f + between - 1 are chosen from, `chosen` of them stay.
@@ -45,6 +49,36 @@ __device__ __forceinline__ Cut cut_of(const EvictParams& P, int r) {
   return x;
 }
 
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(bbm::wave_prefix_sum(x), 63); }
+
+// By a wave: the pages that request r gives back; those, behind the `before` of `all` that the requests in front of it give, and the request's length.
+__device__ __forceinline__ int pages_given(const EvictParams& P, int r) {
+  const Cut x = cut_of(P, r);
+  const int32_t* const table = P.table + r * P.table_stride;
+  int count = 0;
+  for (int at = ((x.b + P.c.page - 1) >> P.c.page_shift) + (threadIdx.x & 63); at < (x.n + P.c.page - 1) >> P.c.page_shift; at += 64) count += table[at] >= 0 && table[at] < P.c.pages;
+  return wave_sum(count);
+}
+__device__ __forceinline__ void give(const EvictParams& P, int r, int before, int all) {
+  const int lane = threadIdx.x & 63;
+  const Cut x = cut_of(P, r);
+  if (P.free_at) {
+    const int64_t first = (int64_t)*P.free_at - all;
+    if (r == 0 && lane == 0) *P.free_next = (int32_t)first;
+    const int32_t* const table = P.table + r * P.table_stride;
+    int64_t to = first + before;
+    const int end = (x.n + P.c.page - 1) >> P.c.page_shift;
+    for (int at = (x.b + P.c.page - 1) >> P.c.page_shift; at < end; at += 64) {
+      const int page = at + lane < end ? table[at + lane] : -1;
+      const uint64_t real = __ballot(page >= 0 && page < P.c.pages);
+      const int64_t mine = to + __popcll(real & ((1ull << lane) - 1ull));
+      if ((real >> lane & 1) && mine >= 0 && mine < P.n_free) P.free_pages[mine] = page;
+      to += __popcll(real);
+    }
+  }
+  if (lane == 0) P.new_lens[r] = x.b;
+}
+
 // Weights as integers of the same order; a NaN is 1, a key without a page 0.
 __device__ __forceinline__ uint32_t ordered(uint32_t bits) {
   if ((bits & 0x7fffffffu) > 0x7f800000u) return 1u;
@@ -54,21 +88,36 @@ __device__ __forceinline__ uint32_t ordered(uint32_t bits) {
 
 template <int D>
 __global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
-  extern __shared__ __attribute__((aligned(16))) uint32_t dynamic_s[];  // free places: a bit each, 64 a word, then the number of those in front of each word
-  __shared__ uint32_t bins[kBins];
+  // free places, a bit each, 64 a word; the number of those in front of each word; the weights of the keys between (P.held of them)
+  extern __shared__ __attribute__((aligned(16))) uint32_t dynamic_s[];
   __shared__ int wave_s[2][NWAVES];
-  __shared__ uint32_t found_s[2];  // the bin, what is still to be chosen from it
-  __shared__ int2 moves_s[NWAVES][64];
+  __shared__ uint32_t found_s[2];            // the bin, what is still to be chosen from it
+  __shared__ int2 moves_s[NWAVES][2 * 64];  // of a wave: from and to, as slots
+  uint32_t* const bins = reinterpret_cast<uint32_t*>(moves_s);
+  static_assert(sizeof(moves_s) >= kBins * sizeof(uint32_t) && sizeof(moves_s) >= kGiveTogether * sizeof(int), "bins, and pages of requests, lie in the place of moves");
   const int tid = threadIdx.x, lane = tid & 63, wave = (int)scalar(tid >> 6);
-  const int r = blockIdx.x / P.c.Hk, hk = blockIdx.x % P.c.Hk;
+  const int wg = (int)blockIdx.x - (P.given ? 0 : 1);
+  if (wg < 0) {
+    int* const given_s = reinterpret_cast<int*>(moves_s);
+    for (int r = wave; r < P.R; r += NWAVES) {
+      const int n = P.free_at ? pages_given(P, r) : 0;
+      if (lane == 0) given_s[r] = n;
+    }
+    __syncthreads();
+    for (int r = wave; r < P.R; r += NWAVES) {
+      int before = 0, all = 0;
+      for (int i = lane; i < P.R; i += 64) all += given_s[i], before += i < r ? given_s[i] : 0;
+      give(P, r, wave_sum(before), wave_sum(all));
+    }
+    return;
+  }
+  const int r = wg / P.c.Hk, hk = wg % P.c.Hk;
   const Cut x = cut_of(P, r);
   const int32_t* const table = P.table + r * P.table_stride;
   auto page_of = [&](int j) { return table[j >> P.c.page_shift]; };
-  if (hk == 0 && wave == 0 && P.free_at) {  // pages that this request gives back
-    int count = 0;
-    for (int at = ((x.b + P.c.page - 1) >> P.c.page_shift) + lane; at < (x.n + P.c.page - 1) >> P.c.page_shift; at += 64) count += table[at] >= 0 && table[at] < P.c.pages;
-    count = __builtin_amdgcn_readlane(bbm::wave_prefix_sum(count), 63);
-    if (lane == 0) P.given[r] = count;
+  if (P.given && hk == 0 && wave == 0 && P.free_at) {
+    const int n = pages_given(P, r);
+    if (lane == 0) P.given[r] = n;
   }
   if (x.n <= x.b) return;
 
@@ -77,10 +126,16 @@ __global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
     const int page = page_of(j);
     return page >= 0 && page < P.c.pages ? (((int64_t)page * P.c.Hk + hk) << P.c.page_shift) + (j & (P.c.page - 1)) : -1;
   };
-  auto weight_of = [&](int i) -> uint32_t {  // of key f + i
+  const int words = (x.chosen + 63) / 64;
+  uint64_t* const free_s = reinterpret_cast<uint64_t*>(dynamic_s);
+  int* const before_s = reinterpret_cast<int*>(free_s + words);
+  uint32_t* const held_s = reinterpret_cast<uint32_t*>(before_s + words);
+  const bool held = x.between <= P.held;
+  auto weight_in_memory = [&](int i) -> uint32_t {  // of key f + i
     const int64_t s = slot_of(x.f + i);
-    return s < 0 ? 0u : ordered(__float_as_uint(P.weights[s]));
+    return s < 0 ? 0u : ordered(__float_as_uint(P.weights[max(s, (int64_t)0)]));
   };
+  auto weight_of = [&](int i) -> uint32_t { return held ? held_s[i] : weight_in_memory(i); };
 
   // The smallest weight that stays, and how many that equal it do.
   uint32_t low = 0, need = (uint32_t)x.chosen, equal = 0;
@@ -91,9 +146,20 @@ __global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
       for (int i = tid; i < kBins; i += NT) bins[i] = 0;
       __syncthreads();
       const uint32_t above = pass == 0 ? 0u : ~0u << (pass == 1 ? 21 : 10);
-      for (int i = tid; i < x.between; i += NT) {
-        const uint32_t u = weight_of(i);
-        if (((u ^ low) & above) == 0) atomicAdd(&bins[u >> SHIFT[pass] & ((1u << BITS[pass]) - 1u)], 1u);
+      constexpr int U = 8;  // (so many loads under way)
+      for (int i0 = tid; i0 < x.between; i0 += U * NT) {
+        uint32_t u[U];
+#pragma unroll
+        for (int n = 0; n < U; ++n) {
+          const int i = min(i0 + n * NT, x.between - 1);
+          u[n] = pass == 0 ? weight_in_memory(i) : weight_of(i);
+        }
+#pragma unroll
+        for (int n = 0; n < U; ++n) {
+          if (i0 + n * NT >= x.between) continue;
+          if (pass == 0 && held) held_s[i0 + n * NT] = u[n];
+          if (((u[n] ^ low) & above) == 0) atomicAdd(&bins[u[n] >> SHIFT[pass] & ((1u << BITS[pass]) - 1u)], 1u);
+        }
       }
       __syncthreads();
       // two bins a thread, the highest first
@@ -132,28 +198,37 @@ __global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
     __syncthreads();
     for (int w = 0; w < wave; ++w) ties += wave_s[0][w];
   }
-  // Which of 64 keys stay; counts the ties as it goes.
-  auto kept = [&](int k, int& ties) -> uint64_t {
-    const int i = 64 * k + lane;
-    const uint32_t u = weight_of(min(i, x.between - 1));
-    const bool in = i < x.between && x.chosen > 0;
-    const uint64_t same = __ballot(in && u == low);
-    const int rank = ties + __popcll(same & ((1ull << lane) - 1ull));
-    ties += __popcll(same);
-    return __ballot(in && (u > low || (u == low && (equal <= need || rank < (int)need))));
+  // f(block, which of its 64 keys stay) for the blocks of this wave in order, the weights of four of them read together.
+  auto for_kept = [&](auto f) __attribute__((always_inline)) {
+    constexpr int U = 4;
+    int before = ties;
+    for (int k0 = block0; k0 < block1; k0 += U) {
+      uint32_t u[U];
+#pragma unroll
+      for (int n = 0; n < U; ++n) u[n] = weight_of(min(64 * (k0 + n) + lane, x.between - 1));
+#pragma unroll
+      for (int n = 0; n < U; ++n) {
+        if (k0 + n >= block1) continue;
+        const bool in = 64 * (k0 + n) + lane < x.between && x.chosen > 0;
+        uint64_t stay = __ballot(in && u[n] >= low);
+        if (equal > need) {
+          const uint64_t same = __ballot(in && u[n] == low);
+          const int rank = before + __popcll(same & ((1ull << lane) - 1ull));
+          stay &= ~__ballot(in && u[n] == low && rank >= (int)need);
+          before += __popcll(same);
+        }
+        f(k0 + n, stay);
+      }
+    }
   };
   // Places: bit i of the first `chosen` is free if key f + i does not stay there.
-  const int words = (x.chosen + 63) / 64;
-  uint64_t* const free_s = reinterpret_cast<uint64_t*>(dynamic_s);
-  int* const before_s = reinterpret_cast<int*>(free_s + words);
   int behind = 0;  // kept ones of this wave's that have to move
-  for (int k = block0, t = ties; k < block1; ++k) {
-    const uint64_t stay = kept(k, t);
+  for_kept([&](int k, uint64_t stay) __attribute__((always_inline)) {
     const int left = x.chosen - 64 * k;  // places among these
     const uint64_t places = left >= 64 ? ~0ull : left <= 0 ? 0ull : (1ull << left) - 1ull;
     if (lane == 0 && places) free_s[k] = places & ~stay;
     behind += __popcll(stay & ~places);
-  }
+  });
   if (lane == 0) wave_s[1][wave] = behind;
   __syncthreads();
   int rank = 0;  // of this wave's first move
@@ -224,30 +299,52 @@ __global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
     if (sub < LK) P.c.v_scale[((s >> P.c.page_shift) * LK + sub << P.c.page_shift) + (s & (P.c.page - 1))] = y.v_scale;
   };
 
-  // Kept keys from behind to the free places, 64 of a wave at a time.
-  for (int k = block0, t = ties; k < block1; ++k) {
-    const uint64_t stay = kept(k, t);
+  // Kept keys from behind to the free places: a wave writes down its moves until it has 64, and makes them, four times eight under way together.
+  auto token_slot = [&](int j) {
+    const int page = page_of(j);
+    return page >= 0 && page < P.c.pages ? (page << P.c.page_shift) + (j & (P.c.page - 1)) : -1;
+  };
+  auto row_of = [&](int slot) -> int64_t { return (((int64_t)(slot >> P.c.page_shift) * P.c.Hk + hk) << P.c.page_shift) + (slot & (P.c.page - 1)); };
+  constexpr int U = 4;
+  int waiting = 0;
+  auto make_moves = [&](int count) __attribute__((always_inline)) {
+    for (int m0 = 0; m0 < count; m0 += 8 * U) {
+      int64_t to[U];
+      Load y[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int m = m0 + 8 * u + (lane >> 3);
+        const int2 move = moves_s[wave][min(m, count - 1)];
+        const bool real = m < count && move.x >= 0 && move.y >= 0;
+        to[u] = real ? row_of(move.y) : -1;
+        y[u] = carry(real ? row_of(move.x) : -1);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) put(to[u], y[u]);
+    }
+  };
+  for_kept([&](int k, uint64_t stay) __attribute__((always_inline)) {
     const int left = x.chosen - 64 * k;
     const uint64_t go = left >= 64 ? 0ull : left <= 0 ? stay : stay & (~0ull << left);
     const int count = __popcll(go);
-    if (count == 0) continue;
+    if (count == 0) return;
     if (go >> lane & 1) {
       const int at = __popcll(go & ((1ull << lane) - 1ull));
-      moves_s[wave][at] = make_int2(x.f + 64 * k + lane, x.f + place_of(rank + at));
+      moves_s[wave][waiting + at] = make_int2(token_slot(x.f + 64 * k + lane), token_slot(x.f + place_of(rank + at)));
     }
     rank += count;
-    __builtin_amdgcn_wave_barrier();
-    for (int m = lane >> 3; m < count; m += 8) {
-      const int2 move = moves_s[wave][m];
-      const int64_t from = slot_of(move.x), to = slot_of(move.y);
-      put(from < 0 ? -1 : to, carry(to < 0 ? -1 : from));
-    }
-    __builtin_amdgcn_wave_barrier();
-  }
+    waiting += count;
+    if (waiting < 64) return;
+    make_moves(64);
+    waiting -= 64;
+    const int2 rest = moves_s[wave][64 + lane];
+    moves_s[wave][lane] = rest;
+  });
+  if (waiting > 0) make_moves(waiting);
   bbm::hand_over();
 
   // The last keys, in order, by n - b to the front.
-  constexpr int U = 4, ROUND = NWAVES * 8 * U;
+  constexpr int ROUND = NWAVES * 8 * U;
   for (int i0 = 0; i0 < P.recent; i0 += ROUND) {
     int64_t to[U];
     Load y[U];
@@ -267,34 +364,17 @@ __global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
   }
 }
 
-// Lengths, and the pages that requests give back, behind those of the requests in front of them.
+// Lengths, and the pages that requests give back, by a kernel of its own behind the other.
 __global__ __launch_bounds__(256) void kv4_give_kernel(const EvictParams P) {
   const int lane = threadIdx.x & 63, r = (int)scalar(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (r >= P.R) return;
-  const Cut x = cut_of(P, r);
-  if (P.free_at) {
-    int before = 0, all = 0;
-    for (int i = lane; i < P.R; i += 64) {
-      const int c = P.given[i];
-      all += c;
-      before += i < r ? c : 0;
-    }
-    before = __builtin_amdgcn_readlane(bbm::wave_prefix_sum(before), 63);
-    all = __builtin_amdgcn_readlane(bbm::wave_prefix_sum(all), 63);
-    const int64_t first = (int64_t)*P.free_at - all;
-    if (r == 0 && lane == 0) *P.free_next = (int32_t)first;
-    const int32_t* const table = P.table + r * P.table_stride;
-    int64_t to = first + before;
-    const int end = (x.n + P.c.page - 1) >> P.c.page_shift;
-    for (int at = (x.b + P.c.page - 1) >> P.c.page_shift; at < end; at += 64) {
-      const int page = at + lane < end ? table[at + lane] : -1;
-      const uint64_t real = __ballot(page >= 0 && page < P.c.pages);
-      const int64_t mine = to + __popcll(real & ((1ull << lane) - 1ull));
-      if ((real >> lane & 1) && mine >= 0 && mine < P.n_free) P.free_pages[mine] = page;
-      to += __popcll(real);
-    }
+  int before = 0, all = 0;
+  for (int i = lane; P.free_at && i < P.R; i += 64) {
+    const int c = P.given[i];
+    all += c;
+    before += i < r ? c : 0;
   }
-  if (lane == 0) P.new_lens[r] = x.b;
+  give(P, r, wave_sum(before), wave_sum(all));
 }
 
 inline bool sizes_ok(int64_t R, int64_t Hk, int64_t max_keys) { return R >= 1 && R <= BBM_SLOTS_MAX_REQUESTS && Hk >= 1 && max_keys >= 1; }
@@ -332,19 +412,25 @@ extern "C" __attribute__((visibility("default"))) int bbm_kv4_evict(const bbm_kv
   EvictParams P = {};
   P.c = kv4_of(cache), P.weights = weights;
   P.lens = lens, P.table = block_table, P.first = first, P.free_at = free_at, P.new_lens = new_lens, P.free_pages = free_pages, P.free_next = free_next;
-  P.given = static_cast<int32_t*>(workspace);
+  // (lengths that are written over would be read by work-groups of the same launch)
+  const bool together = R <= kGiveTogether && new_lens != lens;
+  P.given = together ? nullptr : static_cast<int32_t*>(workspace);
   P.table_stride = table_stride, P.n_free = n_free, P.R = (int32_t)R, P.max_keys = (int32_t)max_keys;
   // (more than there are keys is as good as all of them)
   P.budget = (int32_t)std::min(budget, max_keys), P.recent = (int32_t)std::min(recent, max_keys);
-  const size_t lds = (size_t)ceil_div(P.budget, 64) * 12;
+  // Weights in LDS: of what a request may have at most, as far as it leaves room for two work-groups a CU, or for one if they fit then and not before.
+  const int64_t places = ceil_div(P.budget, 64) * 12, most = std::min(max_len, max_keys) * 4;
+  const int64_t room = most + places <= kTwo ? most : most + places <= kOne ? most : std::max<int64_t>(0, kTwo - places);
+  P.held = (int32_t)(std::min(room, most) / 4);
+  const size_t lds = (size_t)(places + 4 * (int64_t)P.held);
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto kernel = cache->d == 64 ? kv4_evict_kernel<64> : kv4_evict_kernel<128>;
-  if (lds > (32u << 10)) {
+  if (lds > (size_t)kPlain) {
     // (of the function on the current device; a repeated call changes nothing)
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)(kMaxBudget / 64 * 12));
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)std::max(kOne, kMaxBudget / 64 * 12));
     if (e != hipSuccess) return fail(BBM_EHIP, "%s: %s", fn, hipGetErrorString(e));
   }
-  kernel<<<(unsigned)(R * cache->Hk), NT, lds, s>>>(P);
-  kv4_give_kernel<<<(unsigned)ceil_div(R, 4), 256, 0, s>>>(P);
+  kernel<<<(unsigned)(R * cache->Hk + together), NT, lds, s>>>(P);
+  if (!together) kv4_give_kernel<<<(unsigned)ceil_div(R, 4), 256, 0, s>>>(P);
   return launch_status(fn);
 }
