@@ -29,7 +29,7 @@ struct EvictParams {
   int32_t* given;  // [R] pages that a request gives back; NULL if the first work-group sees to them
   int64_t table_stride, n_free;
   int32_t R, max_keys, budget, recent;
-  int32_t held;  // keys whose weights LDS has room for
+  int32_t held, held_pages;  // keys whose weights, and entries of the table, that LDS has room for
 };
 
 // What stays of a request: keys f .. f + between - 1 are chosen from, `chosen` of them stay.
@@ -88,7 +88,7 @@ __device__ __forceinline__ uint32_t ordered(uint32_t bits) {
 
 template <int D>
 __global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
-  // free places, a bit each, 64 a word; the number of those in front of each word; the weights of the keys between (P.held of them)
+  // free places, a bit each, 64 a word; the number of those in front of each word; the request's pages (P.held_pages); the weights of the keys between (P.held of them)
   extern __shared__ __attribute__((aligned(16))) uint32_t dynamic_s[];
   __shared__ int wave_s[2][NWAVES];
   __shared__ uint32_t found_s[2];            // the bin, what is still to be chosen from it
@@ -114,22 +114,28 @@ __global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
   const int r = wg / P.c.Hk, hk = wg % P.c.Hk;
   const Cut x = cut_of(P, r);
   const int32_t* const table = P.table + r * P.table_stride;
-  auto page_of = [&](int j) { return table[j >> P.c.page_shift]; };
   if (P.given && hk == 0 && wave == 0 && P.free_at) {
     const int n = pages_given(P, r);
     if (lane == 0) P.given[r] = n;
   }
   if (x.n <= x.b) return;
 
+  const int words = (x.chosen + 63) / 64, pages = (x.n + P.c.page - 1) >> P.c.page_shift;
+  uint64_t* const free_s = reinterpret_cast<uint64_t*>(dynamic_s);
+  int* const before_s = reinterpret_cast<int*>(free_s + words);
+  int32_t* const pages_s = before_s + words;
+  const bool pages_held = pages <= P.held_pages;
+  if (pages_held) {
+    for (int i = tid; i < pages; i += NT) pages_s[i] = table[i];
+    __syncthreads();
+  }
+  auto page_of = [&](int j) { return pages_held ? pages_s[j >> P.c.page_shift] : table[j >> P.c.page_shift]; };
   // the slot of a key in the cache, for all that has a number for each token and head; -1 if it has no page
   auto slot_of = [&](int j) -> int64_t {
     const int page = page_of(j);
     return page >= 0 && page < P.c.pages ? (((int64_t)page * P.c.Hk + hk) << P.c.page_shift) + (j & (P.c.page - 1)) : -1;
   };
-  const int words = (x.chosen + 63) / 64;
-  uint64_t* const free_s = reinterpret_cast<uint64_t*>(dynamic_s);
-  int* const before_s = reinterpret_cast<int*>(free_s + words);
-  uint32_t* const held_s = reinterpret_cast<uint32_t*>(before_s + words);
+  uint32_t* const held_s = reinterpret_cast<uint32_t*>(pages_s + P.held_pages);
   const bool held = x.between <= P.held;
   auto weight_in_memory = [&](int i) -> uint32_t {  // of key f + i
     const int64_t s = slot_of(x.f + i);
@@ -418,11 +424,12 @@ extern "C" __attribute__((visibility("default"))) int bbm_kv4_evict(const bbm_kv
   P.table_stride = table_stride, P.n_free = n_free, P.R = (int32_t)R, P.max_keys = (int32_t)max_keys;
   // (more than there are keys is as good as all of them)
   P.budget = (int32_t)std::min(budget, max_keys), P.recent = (int32_t)std::min(recent, max_keys);
-  // Weights in LDS: of what a request may have at most, as far as it leaves room for two work-groups a CU, or for one if they fit then and not before.
-  const int64_t places = ceil_div(P.budget, 64) * 12, most = std::min(max_len, max_keys) * 4;
-  const int64_t room = most + places <= kTwo ? most : most + places <= kOne ? most : std::max<int64_t>(0, kTwo - places);
-  P.held = (int32_t)(std::min(room, most) / 4);
-  const size_t lds = (size_t)(places + 4 * (int64_t)P.held);
+  // Pages and weights in LDS: of what a request may have at most, if they leave room for two work-groups a CU, or for one; else as many weights as leave room for two.
+  const int64_t places = ceil_div(P.budget, 64) * 12, keys = std::min(max_len, max_keys), table_bytes = ceil_div(keys, cache->page) * 4;
+  const int64_t bytes = places + table_bytes <= kTwo ? table_bytes : 0, most = places + bytes + 4 * keys;
+  P.held_pages = (int32_t)(bytes / 4);
+  P.held = (int32_t)(most <= kOne ? keys : std::max<int64_t>(0, kTwo - places - bytes) / 4);
+  const size_t lds = (size_t)(places + bytes + 4 * (int64_t)P.held);
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto kernel = cache->d == 64 ? kv4_evict_kernel<64> : kv4_evict_kernel<128>;
   if (lds > (size_t)kPlain) {
