@@ -179,19 +179,19 @@ __device__ __forceinline__ void put_column(const Kv4AttnParams& P, const Piece& 
   if (P.lse && e0 == 0) P.lse[(int64_t)h * P.T + t] = l > 0.0f ? bbm::log_sum(m, l, P.rc) : -INFINITY;
 }
 
+// lds_a, lds_b: 16 columns' results of two waves each.
+template <int D>
+constexpr int kNarrowLd = D + 4;  // row of the results in LDS
 template <int D, bool SHARED>
-__global__ __launch_bounds__(64 * NW, D == 128 ? 3 : 5) void kv4_narrow_kernel(const Kv4AttnParams P) {
+__device__ __forceinline__ void narrow(const Kv4AttnParams& P, const Item& item, float* lds_a, float* lds_b, float (*m_s)[16], float (*l_s)[16]) {
   constexpr int KD = D / 4;        // elements of K a lane loads of its key
   constexpr int KS = D / 32;       // steps of the first product
   constexpr int VD = D / 16;       // elements of V a lane loads of a key, instructions of the second product
-  constexpr int LD = D + 4;        // row of the results in LDS
-  __shared__ __attribute__((aligned(16))) float o_s[NW][16][LD];
-  __shared__ float m_s[NW][16], l_s[NW][16];
+  constexpr int LD = kNarrowLd<D>;
+  auto o_s = [&](int w, int c) { return (w < 2 ? lds_a : lds_b) + ((w & 1) * 16 + c) * LD; };
 
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, kq = lane >> 4;
   const int wave = (int)scalar(tid >> 6);
-  const Item item = item_of<SHARED>(P);
-  if (SHARED && item.none) return;
   const int number = item.number, part = item.part, hk = item.hk;
   const Piece x = SHARED && item.group ? group_piece_of(P, number, 16) : piece_of<SHARED>(P, number, 16);
   if (x.s.end <= x.s.begin || part >= x.parts) return;
@@ -344,7 +344,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 3 : 5) void kv4_narrow_kernel(c
 #pragma unroll
   for (int r = 0; r < 4; ++r)
 #pragma unroll
-    for (int j = 0; j < VD; j += 4) *reinterpret_cast<f32x4*>(&o_s[wave][n][(4 * kq + r) * VD + j]) = f32x4{acc[j][r], acc[j + 1][r], acc[j + 2][r], acc[j + 3][r]};
+    for (int j = 0; j < VD; j += 4) *reinterpret_cast<f32x4*>(o_s(wave, n) + (4 * kq + r) * VD + j) = f32x4{acc[j][r], acc[j + 1][r], acc[j + 2][r], acc[j + 3][r]};
   __syncthreads();
   const int c = tid >> 4, e0 = (tid & 15) * VD, col = x.col0 + c;
   if (col >= x.cols) return;
@@ -358,7 +358,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 3 : 5) void kv4_narrow_kernel(c
     const float f = bbm::weight(m_s[w][c], m_fin, P.rc);
     sum += f * l_s[w][c];
 #pragma unroll
-    for (int e = 0; e < VD; ++e) v[e] += f * o_s[w][c][e0 + e];
+    for (int e = 0; e < VD; ++e) v[e] += f * o_s(w, c)[e0 + e];
   }
   if (alone<SHARED>(x, item)) {
     put_column<D>(P, x, hk, col, e0, v, m, sum);
@@ -373,20 +373,13 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 3 : 5) void kv4_narrow_kernel(c
 // 128 columns of a piece, a wave 32 of them, one lane a column, with the products of the kernels for prompts: the codes of 64 keys at a time are converted once
 // for all of them, on their way to LDS, where the tile is read as keys and values in bf16 are.
 template <int D, bool SHARED>
-__global__ __launch_bounds__(64 * NW, 2) void kv4_wide_kernel(const Kv4AttnParams P) {
+__device__ __forceinline__ void wide(const Kv4AttnParams& P, const Item& item, __bf16* k_s0, __bf16* k_s1, __bf16* v_s0, __bf16* v_s1, uint32_t (*there_s)[NW]) {
   using L = bbm::TL<D>;
   constexpr int KS = D / 16, DB = D / 32, RC = D / 8, RPB = 64 / RC;
   constexpr int W = D / 32;  // 32-bit words of codes a thread converts of a tensor
-  __shared__ __attribute__((aligned(16))) __bf16 k_s0[L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 k_s1[L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 v_s0[L::ELEMS];
-  __shared__ __attribute__((aligned(16))) __bf16 v_s1[L::ELEMS];
-  __shared__ __attribute__((aligned(16))) uint32_t there_s[2][NW];  // which of a tile's keys are there, 16 a wave
 
   const int tid = threadIdx.x, lane = tid & 63, lq = lane & 31, hh = lane >> 5;
   const int wave = (int)scalar(tid >> 6);
-  const Item item = item_of<SHARED>(P);
-  if (SHARED && item.none) return;
   const int number = item.number, part = item.part, hk = item.hk;
   const Piece x = SHARED && item.group ? group_piece_of(P, number, 128) : piece_of<SHARED>(P, number, 128);
   if (x.s.end <= x.s.begin || part >= x.parts) return;
@@ -579,6 +572,48 @@ __global__ __launch_bounds__(64 * NW, 2) void kv4_wide_kernel(const Kv4AttnParam
   if (P.lse && hh == 0 && lq < wcols) P.lse[(int64_t)my_h * P.T + x.s.begin + my_i] = l > 0.0f ? bbm::log_sum(top.m, l, P.rc) : -INFINITY;
 }
 
+template <int D, bool SHARED>
+__global__ __launch_bounds__(64 * NW, D == 128 ? 3 : 5) void kv4_narrow_kernel(const Kv4AttnParams P) {
+  __shared__ __attribute__((aligned(16))) float o_s[NW][16][kNarrowLd<D>];
+  __shared__ float m_s[NW][16], l_s[NW][16];
+  const Item item = item_of<SHARED>(P);
+  if (SHARED && item.none) return;
+  narrow<D, SHARED>(P, item, &o_s[0][0][0], &o_s[2][0][0], m_s, l_s);
+}
+
+// (there_s: which of a tile's keys are there, 16 a wave)
+#define BBM_WIDE_LDS                                                             \
+  using L = bbm::TL<D>;                                                          \
+  __shared__ __attribute__((aligned(16))) __bf16 k_s0[L::ELEMS];                 \
+  __shared__ __attribute__((aligned(16))) __bf16 k_s1[L::ELEMS];                 \
+  __shared__ __attribute__((aligned(16))) __bf16 v_s0[L::ELEMS];                 \
+  __shared__ __attribute__((aligned(16))) __bf16 v_s1[L::ELEMS];                 \
+  __shared__ __attribute__((aligned(16))) uint32_t there_s[2][NW]
+
+template <int D, bool SHARED>
+__global__ __launch_bounds__(64 * NW, 2) void kv4_wide_kernel(const Kv4AttnParams P) {
+  BBM_WIDE_LDS;
+  const Item item = item_of<SHARED>(P);
+  if (SHARED && item.none) return;
+  wide<D, SHARED>(P, item, k_s0, k_s1, v_s0, v_s1, there_s);
+}
+
+// Groups of many columns side by side with requests of few, in the same LDS.
+template <int D>
+__global__ __launch_bounds__(64 * NW, 2) void kv4_both_kernel(const Kv4AttnParams P) {
+  BBM_WIDE_LDS;
+  static_assert(2 * 16 * kNarrowLd<D> * sizeof(float) <= sizeof(k_s0) && 2 * NW * 16 * sizeof(float) <= sizeof(k_s1), "the results of two waves, and all statistics, must fit in a tile buffer");
+  const Item item = item_of<true>(P);
+  if (item.none) return;
+  if (item.group) {
+    wide<D, true>(P, item, k_s0, k_s1, v_s0, v_s1, there_s);
+  } else {
+    float(*const m_s)[16] = reinterpret_cast<float(*)[16]>(k_s1);
+    narrow<D, true>(P, item, reinterpret_cast<float*>(k_s0), reinterpret_cast<float*>(v_s0), m_s, m_s + NW);
+  }
+}
+#undef BBM_WIDE_LDS
+
 // Joins the parts of a piece's columns in a fixed order, 16 lanes a column.  With many parts (SIDE = 4) a wave takes one column and four parts side by
 // side, whose sums meet at the end; with few, a column for every 16 lanes: a wave costs more to start than to add up four records.
 template <int D, int SIDE, bool SHARED>
@@ -644,12 +679,9 @@ constexpr int64_t kOccupy = 512, kBusy = 2048, kPartKeys = 1024, kLongPartKeys =
 // 32 / 8 heads over 4096 keys, us, narrow / wide: 16 requests of 8 tokens (32 columns) 30 / 42, of 16 40 / 44, of 32 (16 x 32 x 32 rows) 61 / 51; 4 requests
 // of 64 35 / 43; 3 of 32 over 1000 keys 10 / 25; trees of 256 nodes, 8 x 32 heads, 88 / 53.
 constexpr int64_t kWideColumns = 64, kWideRows = 16384;
-#ifndef GW
-#define GW 64
-#endif
-inline Plan plan_of(int64_t T, int64_t R, int64_t G, int64_t Hk, int64_t max_len, int64_t group=0) {
+inline Plan plan_of(int64_t T, int64_t R, int64_t G, int64_t Hk, int64_t max_len) {
   Plan p;
-  const bool wide = group ? T * G >= group * R : T * G >= kWideColumns * R && T * G * Hk >= kWideRows;
+  const bool wide = T * G >= kWideColumns * R && T * G * Hk >= kWideRows;
   p.width = wide ? 128 : 16;
   p.pieces = bbm::count_pieces(T, R, G, p.width);
   const int64_t busy = std::max(std::min(T, R), bbm::ceil_div(T * G, p.width)) * Hk;  // pieces that belong to a request, or few fewer
@@ -761,11 +793,31 @@ namespace {
 struct SharedPlan {
   Plan group, own;
 };
+#ifndef GW
+#define GW 64
+#endif
+#ifndef GO
+#define GO 384
+#endif
+#ifndef GK
+#define GK 512
+#endif
 inline SharedPlan shared_plan_of(int64_t T, int64_t R, int64_t S, int64_t G, int64_t Hk, int64_t max_shared, int64_t max_own) {
   SharedPlan p;
   p.own = plan_of(T, R, G, Hk, max_own);
-  p.group = plan_of(T, std::max<int64_t>(S, 1), G, Hk, max_shared, GW);
-  if (S == 0) p.group.pieces = 0, p.group.parts = 0;
+  if (S == 0) {
+    p.group = Plan{p.own.width, 0, 0, kStep};
+    return p;
+  }
+  p.group = plan_of(T, S, G, Hk, max_shared);
+  if (p.own.width == 128 || T * G >= GW * S) {
+    p.group.width = 128;
+    p.group.pieces = bbm::count_pieces(T, S, G, 128);
+    const int64_t busy = std::max(std::min(T, S), bbm::ceil_div(T * G, 128)) * Hk;
+    p.group.parts = std::max<int64_t>(1, std::min(bbm::ceil_div(GO, busy), max_shared / GK));
+    p.group.part_keys = bbm::ceil_div(bbm::ceil_div(max_shared, p.group.parts), kStep) * kStep;
+    p.group.parts = bbm::ceil_div(max_shared, p.group.part_keys);
+  }
   return p;
 }
 inline size_t shared_workspace(const SharedPlan& p, int64_t T, int64_t H, int d) {
@@ -775,14 +827,11 @@ inline size_t shared_workspace(const SharedPlan& p, int64_t T, int64_t H, int d)
 template <int D>
 void launch_shared(Kv4AttnParams P, const SharedPlan& p, hipStream_t s) {
   const int64_t group = p.group.pieces * P.c.Hk * p.group.parts, own = p.own.pieces * P.c.Hk * p.own.parts;
-  auto go = [&](int width, int64_t group_wgs, int64_t own_wgs) {
-    P.group_wgs = (int32_t)group_wgs, P.own_wgs = (int32_t)own_wgs;
-    const unsigned wgs = (unsigned)(((group_wgs + 7) & ~7ll) + own_wgs);
-    if (width == 16) kv4_narrow_kernel<D, true><<<wgs, 64 * NW, 0, s>>>(P);
-    else kv4_wide_kernel<D, true><<<wgs, 64 * NW, 0, s>>>(P);
-  };
-  if (group > 0 && p.group.width != p.own.width) go(p.group.width, group, 0), go(p.own.width, 0, own);
-  else go(p.own.width, group, own);
+  P.group_wgs = (int32_t)group, P.own_wgs = (int32_t)own;
+  const unsigned wgs = (unsigned)(((group + 7) & ~7ll) + own);
+  if (p.own.width == 128) kv4_wide_kernel<D, true><<<wgs, 64 * NW, 0, s>>>(P);
+  else if (p.group.width == 128 && group > 0) kv4_both_kernel<D><<<wgs, 64 * NW, 0, s>>>(P);
+  else kv4_narrow_kernel<D, true><<<wgs, 64 * NW, 0, s>>>(P);
   if (p.group.parts + p.own.parts > 4)
     kv4_join_kernel<D, 4, true><<<dim3((unsigned)bbm::count_pieces(P.T, P.R, P.G, 4), (unsigned)P.c.Hk), 256, 0, s>>>(P);
   else if (p.group.parts + p.own.parts > 1)
