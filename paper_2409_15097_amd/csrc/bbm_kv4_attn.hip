@@ -796,8 +796,8 @@ struct SharedPlan {
 // Groups take the wide kernel from this many columns of a group on, on average, and are cut into shorter parts than requests: there are few of them, and the join has to be there anyway.
 // 32 / 8 heads of 128, us, narrow / wide: 16 requests of one token behind 8192 common keys (64 columns) 19 / 23, 32 (128 columns) 26 / 28, 67 (268) 43 / 41, 16 of 5 tokens on average behind 6000
 // (320) 47 / 43, 256 behind 32768 (1024) 263 / 185.  Parts of at least 512 keys for the narrow kernel / 1024: 32 requests behind 1024 keys 15.1 / 16.2, four heads of 64 behind 8192
-// 11.4 / 13.0, 8 requests behind 8192 16.3 / 15.6; for the wide one / 256: 32 behind 8192 28 / 34.  512 work-groups of the wide kernel / 384 / 1024: 256 behind 32768 185 / 193 / 198.
-constexpr int64_t kGroupWideColumns = 192, kGroupPartKeys = 512;
+// 11.4 / 13.0, 8 requests behind 8192 16.3 / 15.6; of 640 for the wide one / 512: 67 requests behind 8192 37.4 / 41.0.  512 work-groups of the wide kernel / 384 / 1024: 256 behind 32768 185 / 193 / 198.
+constexpr int64_t kGroupWideColumns = 192, kGroupPartKeys = 512, kGroupWidePartKeys = 640;
 inline SharedPlan shared_plan_of(int64_t T, int64_t R, int64_t S, int64_t G, int64_t Hk, int64_t max_shared, int64_t max_own) {
   SharedPlan p;
   p.own = plan_of(T, R, G, Hk, max_own);
@@ -809,7 +809,7 @@ inline SharedPlan shared_plan_of(int64_t T, int64_t R, int64_t S, int64_t G, int
   p.group.width = wide ? 128 : 16;
   p.group.pieces = bbm::count_pieces(T, S, G, p.group.width);
   const int64_t busy = std::max(std::min(T, S), bbm::ceil_div(T * G, p.group.width)) * Hk;
-  p.group.parts = std::max<int64_t>(1, std::min(bbm::ceil_div(kOccupy, busy), max_shared / kGroupPartKeys));
+  p.group.parts = std::max<int64_t>(1, std::min(bbm::ceil_div(kOccupy, busy), max_shared / (wide ? kGroupWidePartKeys : kGroupPartKeys)));
   p.group.part_keys = bbm::ceil_div(bbm::ceil_div(max_shared, p.group.parts), kStep) * kStep;
   p.group.parts = bbm::ceil_div(max_shared, p.group.part_keys);
   return p;
