@@ -4,7 +4,7 @@
  *
  * Groups.  Requests group_cu[g] .. group_cu[g+1] - 1 (int32 [S+1], not decreasing, on the device like all below; cut to 0 .. R) are group g: their first
  * shared_lens[g] (int32 [S]; negative ones stand for 0) keys are the same, and lie in front of the new tokens of each of them that has any.  The rows of the block table are complete: the
- * row of each request holds the pages of its shared keys too, of which those in the row of the group's first request are read.  Requests in front of
+ * row of each request holds the pages of its shared keys too, the same in all of them.  Requests in front of
  * group_cu[0] or from group_cu[S] on share nothing.  S may be 0 (group_cu and shared_lens are not looked at then).  Where a group's keys are not the same, or a shared key does not
  * lie in front of a request's new tokens, the results of that group's requests are unspecified.
  */

@@ -792,16 +792,33 @@ namespace {
 // Of a call with shared prefixes: the groups' cut and the requests'.
 struct SharedPlan {
   Plan group, own;
+  bool apart;  // each request for itself, as without groups
 };
-// Groups take the wide kernel from this many columns of a group on, on average, and are cut into shorter parts than requests: there are few of them, and the join has to be there anyway.
-// 32 / 8 heads of 128, us, narrow / wide: 16 requests of one token behind 8192 common keys (64 columns) 19 / 23, 32 (128 columns) 26 / 28, 67 (268) 43 / 41, 16 of 5 tokens on average behind 6000
-// (320) 47 / 43, 256 behind 32768 (1024) 263 / 185.  Parts of at least 512 keys for the narrow kernel / 1024: 32 requests behind 1024 keys 15.1 / 16.2, four heads of 64 behind 8192
-// 11.4 / 13.0, 8 requests behind 8192 16.3 / 15.6; of 640 for the wide one / 512: 67 requests behind 8192 37.4 / 41.0.  512 work-groups of the wide kernel / 384 / 1024: 256 behind 32768 185 / 193 / 198.
-constexpr int64_t kGroupWideColumns = 192, kGroupPartKeys = 512, kGroupWidePartKeys = 640;
-inline SharedPlan shared_plan_of(int64_t T, int64_t R, int64_t S, int64_t G, int64_t Hk, int64_t max_shared, int64_t max_own) {
+// Short prefixes of few requests are better read for each of them: one launch and no join.  32 / 8 heads of 128, us, by groups / apart: 4 requests behind 512 keys 10.5 / 7.9, behind 1024
+// 10.6 / 10.8, behind 2048 11.1 / 13.5; 32 requests 11.9 / 8.3, 12.2 / 11.6, 15.8 / 18.3 (20, 38 and 74 MB read apart).
+constexpr int64_t kApartKeys = 1152, kApartBytes = 40 << 20;
+// Groups take the wide kernel from this many columns of a group on, on average.  32 / 8 heads of 128, us, narrow / wide: 16 requests of one token behind 8192 common keys (64 columns) 19 / 23,
+// 32 (128 columns) 26 / 28, 67 (268) 43 / 37, 256 behind 32768 (1024) 263 / 185.
+// The narrow one's parts have at least 512 keys (groups are few, and the join has to be there anyway): 32 requests behind 1024 keys 15.1 us, of 1024 16.2; four heads of 64 behind 8192 11.4 / 13.0.
+constexpr int64_t kGroupWideColumns = 192, kGroupPartKeys = 512;
+// The wide one's are chosen by what they take: a tile of 64 keys of a work-group that has a CU to itself, of two that share one, and a MB of records, written and read, in us.  (With
+// 512 keys a part and no more than 512 work-groups instead: 67 requests behind 8192 keys 41 us, with this 37; 32 requests behind 4096 keys, eight heads over one of 128, 25 and 17.)
+constexpr double kTileAlone = 1.4, kTileShared = 2.2, kRecordMB = 0.25;
+inline int64_t wide_parts(int64_t pieces, int64_t max_keys, double record_mb) {
+  int64_t best = 1;
+  double least = 0.0;
+  for (int64_t parts = 1; parts <= std::min<int64_t>(64, bbm::ceil_div(max_keys, kStep)); ++parts) {
+    const int64_t keys = bbm::ceil_div(bbm::ceil_div(max_keys, parts), kStep) * kStep, wgs = pieces * bbm::ceil_div(max_keys, keys);
+    const double cost = (double)(keys / 64) * (wgs <= 256 ? kTileAlone : kTileShared * (double)bbm::ceil_div(wgs, 512)) + (double)parts * record_mb * kRecordMB;
+    if (parts == 1 || cost < least) best = parts, least = cost;
+  }
+  return best;
+}
+inline SharedPlan shared_plan_of(int64_t T, int64_t R, int64_t S, int64_t G, int64_t Hk, int d, int64_t max_shared, int64_t max_own) {
   SharedPlan p;
-  p.own = plan_of(T, R, G, Hk, max_own);
-  if (S == 0) {
+  p.apart = S > 0 && max_shared + max_own <= kApartKeys && R * (max_shared + max_own) * Hk <= kApartBytes / (d * 17 / 16);
+  p.own = plan_of(T, R, G, Hk, p.apart ? max_shared + max_own : max_own);
+  if (S == 0 || p.apart) {
     p.group = Plan{p.own.width, 0, 0, kStep};
     return p;
   }
@@ -809,7 +826,8 @@ inline SharedPlan shared_plan_of(int64_t T, int64_t R, int64_t S, int64_t G, int
   p.group.width = wide ? 128 : 16;
   p.group.pieces = bbm::count_pieces(T, S, G, p.group.width);
   const int64_t busy = std::max(std::min(T, S), bbm::ceil_div(T * G, p.group.width)) * Hk;
-  p.group.parts = std::max<int64_t>(1, std::min(bbm::ceil_div(kOccupy, busy), max_shared / (wide ? kGroupWidePartKeys : kGroupPartKeys)));
+  p.group.parts = wide ? wide_parts(S * bbm::ceil_div(T * G, 128 * S) * Hk, max_shared, (double)T * (double)(G * Hk) * (d + 2) * 8e-6)
+                       : std::max<int64_t>(1, std::min(bbm::ceil_div(kOccupy, busy), max_shared / kGroupPartKeys));
   p.group.part_keys = bbm::ceil_div(bbm::ceil_div(max_shared, p.group.parts), kStep) * kStep;
   p.group.parts = bbm::ceil_div(max_shared, p.group.part_keys);
   return p;
@@ -837,7 +855,7 @@ void launch_shared(Kv4AttnParams P, const SharedPlan& p, hipStream_t s) {
 extern "C" __attribute__((visibility("default"))) size_t bbm_kv4_shared_attn_workspace_bytes(int64_t T, int64_t R, int64_t S, int64_t H, int64_t Hk, int d, int64_t max_shared,
                                                                                              int64_t max_own) {
   if (!sizes_ok(T, R, H, Hk, std::min(max_shared, max_own)) || S < 0 || S > R || (d != 64 && d != 128)) return 0;
-  return shared_workspace(shared_plan_of(T, R, S, H / Hk, Hk, std::min<int64_t>(max_shared, bbm::kMaxTokens), std::min<int64_t>(max_own, bbm::kMaxTokens)), T, H, d);
+  return shared_workspace(shared_plan_of(T, R, S, H / Hk, Hk, d, std::min<int64_t>(max_shared, bbm::kMaxTokens), std::min<int64_t>(max_own, bbm::kMaxTokens)), T, H, d);
 }
 
 extern "C" __attribute__((visibility("default"))) int bbm_kv4_shared_attn(const bbm_packed* q, const bbm_packed* o, float* lse, int64_t T, int64_t R, const int32_t* cu,
@@ -858,13 +876,13 @@ extern "C" __attribute__((visibility("default"))) int bbm_kv4_shared_attn(const 
                            {q->ptr, cu, lens, block_table, mask, cache->k, cache->k_scale, cache->v, cache->v_scale, S > 0 ? group_cu : nullptr, S > 0 ? shared_lens : nullptr}))
     return rc;
   Kv4AttnParams P = params_of(a);
-  const SharedPlan p = shared_plan_of(T, R, S, P.G, cache->Hk, std::min<int64_t>(max_shared, kMaxTokens), std::min<int64_t>(max_own, kMaxTokens));
+  const SharedPlan p = shared_plan_of(T, R, S, P.G, cache->Hk, cache->d, std::min<int64_t>(max_shared, kMaxTokens), std::min<int64_t>(max_own, kMaxTokens));
   for (const Plan& x : {p.group, p.own})
     if (x.pieces >= kMaxWgs || x.pieces * cache->Hk * std::max<int64_t>(x.parts, 1) >= kMaxWgs / 2)
       return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, R=%lld, H=%lld)", fn, (long long)T, (long long)R, (long long)H);
   if (count_pieces(T, R, P.G, 4) * cache->Hk >= kMaxWgs) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, R=%lld, H=%lld)", fn, (long long)T, (long long)R, (long long)H);
   P.width = p.own.width, P.pieces = (int32_t)p.own.pieces, P.parts = (int32_t)p.own.parts, P.part_keys = (int32_t)p.own.part_keys;
-  P.S = (int32_t)S, P.group_cu = group_cu, P.shared_lens = shared_lens;
+  P.S = p.apart ? 0 : (int32_t)S, P.group_cu = group_cu, P.shared_lens = shared_lens;
   P.group_pieces = (int32_t)p.group.pieces, P.group_parts = (int32_t)p.group.parts, P.group_part_keys = (int32_t)p.group.part_keys;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (cache->d == 64) launch_shared<64>(P, p, s);

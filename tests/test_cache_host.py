@@ -29,7 +29,7 @@ def test_every_declared_symbol_is_exported_and_bound(bbm):
 
 
 def shared(bbm, q=None, o=None, lse=2 * P, T=3, R=2, cu=3 * P, lens=4 * P, table=5 * P, stride=4, width=4, S=1, group=6 * P, shared=7 * P, mask=None, words=0, c=None, H=4, scale=0.125,
-           max_shared=256, max_own=64, ws=8 * P, ws_bytes=1 << 40):
+           max_shared=4096, max_own=64, ws=8 * P, ws_bytes=1 << 40):
     return bbm.lib.bbm_kv4_shared_attn(q or pk(), o or pk(9 * P), lse, T, R, cu, lens, table, stride, width, S, group, shared, mask, words, c or cache(k=10 * P), H, scale, max_shared,
                                        max_own, ws, ws_bytes, None)
 
@@ -55,10 +55,11 @@ def test_shared_attention_refuses(bbm):
         assert shared(bbm, **kw) == bbm.BBM_EINVAL, kw
     assert shared(bbm, T=0) == bbm.BBM_OK and shared(bbm, T=0, S=0, group=None, shared=None) == bbm.BBM_OK
     sizes = bbm.bbm_kv4_shared_attn_workspace_bytes
-    need = sizes(3, 2, 1, 4, 2, 64, 256, 64)
+    need = sizes(3, 2, 1, 4, 2, 64, 4096, 64)
     assert need > 0 and shared(bbm, ws_bytes=need - 1) == bbm.BBM_EWORKSPACE and shared(bbm, ws=None) == bbm.BBM_EWORKSPACE
-    assert sizes(3, 2, 0, 4, 2, 64, 256, 64) == 0                         # one part of each request: nothing to join
-    assert sizes(0, 2, 1, 4, 2, 64, 256, 64) == 0 and sizes(3, 2, 3, 4, 2, 64, 256, 64) == 0 and sizes(3, 2, 1, 4, 3, 64, 256, 64) == 0 and sizes(3, 2, 1, 4, 2, 96, 256, 64) == 0
+    assert sizes(3, 2, 0, 4, 2, 64, 4096, 64) == 0 and sizes(3, 2, 1, 4, 2, 64, 256, 64) == 0   # one part of each request: nothing to join
+    assert shared(bbm, max_shared=256, ws=None, ws_bytes=0, T=0) == bbm.BBM_OK
+    assert sizes(0, 2, 1, 4, 2, 64, 4096, 64) == 0 and sizes(3, 2, 3, 4, 2, 64, 4096, 64) == 0 and sizes(3, 2, 1, 4, 3, 64, 4096, 64) == 0 and sizes(3, 2, 1, 4, 2, 96, 4096, 64) == 0
     assert sizes(1 << 20, 1 << 20, 1 << 20, 256, 1, 128, 1 << 62, 1 << 62) > 1 << 35   # (no product wraps)
 
 

@@ -46,12 +46,14 @@ def check_grouped(bbm, group_cu, shared, lens, news, H, Hk, d, page, hints=({},)
     by = Behind(bbm, group_cu, shared)
     for hint in hints:
         a = check_cached(by, c, table, lens, cu, T, q, words, H, Hk, d, page, **hint)
-        b = check_cached(by, c, table, lens, cu, T, q, words, H, Hk, d, page, **hint)
-        assert all(torch.equal(x, y) for x, y in zip(a, b))
+        out, lse = torch.full_like(a[0], 7.0), torch.full_like(a[1], 7.0)
+        by.bbm_kv4_attn(q, c, i32(table), i32(lens), i32(cu), mask=None if words is None else torch.from_numpy(words).cuda(), out=out, lse=lse, **hint)
+        assert torch.equal(a[0], out) and torch.equal(a[1], lse)
     return c, table, cu, T, q, words
 
 
-NEAR = [{}, dict(max_shared=300, max_own=40)]
+# What the work split goes by, besides the table (None).
+NEAR = [{}, dict(max_shared=300, max_own=40), dict(max_shared=5000, max_own=40), dict(max_shared=1200, max_own=5000)]   # (short ones: each request for itself)
 
 
 @pytest.mark.parametrize("d", [64, 128])
@@ -73,15 +75,16 @@ def test_shared(bbm, group_cu, shared, lens, news, H, Hk, d, page, layout, tree)
 def test_shared_by_many_columns(bbm, d, H, Hk, tree):
     """The kernel of many columns for the groups, in parts; alone and beside requests of few and of many."""
     for lens, news in (([2100, 2088], [60, 70]), ([1100 + i for i in range(40)], [1 + i % 15 for i in range(40)])):
-        check_grouped(bbm, [0, len(lens)], [1072 if len(lens) > 2 else 2016], lens, news, H, Hk, d, 16, hints=[{}, dict(max_shared=2048, max_own=100)], tree=tree, seed=9, before=1, behind=2)
+        check_grouped(bbm, [0, len(lens)], [1072 if len(lens) > 2 else 2016], lens, news, H, Hk, d, 16, hints=[{}, dict(max_shared=2048, max_own=100), dict(max_shared=20000, max_own=5000)], tree=tree, seed=9, before=1, behind=2)
 
 
 def test_shared_by_one_and_by_many_requests(bbm):
     """More requests, and more groups, than are counted or read at once."""
     R = 600
-    check_grouped(bbm, [0, R], [32], [33 + i % 9 for i in range(R)], [1] * R, 2, 1, 64, 16)
-    check_grouped(bbm, list(range(0, R + 1, 8)), [16 * (i % 3) for i in range(75)], [33 + i % 9 for i in range(R)], [1] * R, 2, 1, 64, 16)
-    check_grouped(bbm, list(range(R + 1)), [16 * (i % 3) for i in range(R)], [33 + i % 9 for i in range(R)], [1] * R, 2, 1, 64, 16)
+    lens, hints = [33 + i % 9 for i in range(R)], [{}, dict(max_shared=4096, max_own=16)]
+    check_grouped(bbm, [0, R], [32], lens, [1] * R, 2, 1, 64, 16, hints=hints)
+    check_grouped(bbm, list(range(0, R + 1, 8)), [16 * (i % 3) for i in range(75)], lens, [1] * R, 2, 1, 64, 16, hints=hints)
+    check_grouped(bbm, list(range(R + 1)), [16 * (i % 3) for i in range(R)], lens, [1] * R, 2, 1, 64, 16, hints=hints)
 
 
 def test_shared_pages_outside_and_a_narrow_table(bbm):
@@ -89,13 +92,14 @@ def test_shared_pages_outside_and_a_narrow_table(bbm):
     c, table, cu, T, q, _ = grouped_case(bbm, group_cu, shared, lens, news, H, Hk, d, page, seed=3)
     table[:2, 3], table[0, 15], table[2:, 0], table[3, 2] = -1, 1 << 30, c.k.shape[0], -5
     by = Behind(bbm, group_cu, shared)
-    check_cached(by, c, table, lens, cu, T, q, None, H, Hk, d, page)
+    check_cached(by, c, table, lens, cu, T, q, None, H, Hk, d, page, max_shared=4096)
     check_cached(by, c, table[:, :9], lens, cu, T, q, None, H, Hk, d, page)
+    check_cached(by, c, table[:, :9], lens, cu, T, q, None, H, Hk, d, page, max_shared=4096)
     # a prefix that ends behind the table, and one of which no page is there: the queries behind it see what is left, or nothing
-    check_cached(by, c, table[:, :5], [700, 600, 90, 70], cu, T, q, None, H, Hk, d, page)
+    check_cached(by, c, table[:, :5], [700, 600, 90, 70], cu, T, q, None, H, Hk, d, page, max_shared=4096)
     gone = table.copy()
     gone[2:] = -1
-    check_cached(by, c, gone, lens, cu, T, q, None, H, Hk, d, page)
+    check_cached(by, c, gone, lens, cu, T, q, None, H, Hk, d, page, max_shared=4096)
 
 
 @pytest.mark.parametrize("tree", [None, 1])
@@ -105,7 +109,8 @@ def test_shared_rows_that_are_not_there(bbm, tree, front, rows):
     lens, news, H = [300, 290, 170], [40, 30, 60], 4
     c, table, cu, T, q, words = grouped_case(bbm, [0, 3], [96], lens, news, H, 2, 64, 32, seed=11, tree=tree)
     a, b = front, news[0] + news[1] + rows
-    check_cached(Behind(bbm, [0, 3], [96]), c, table, lens, cu - a, b - a, q[a:b].contiguous(), None if words is None else words[a:b].copy(), H, 2, 64, 32)
+    for hint in ({}, dict(max_shared=4096)):
+        check_cached(Behind(bbm, [0, 3], [96]), c, table, lens, cu - a, b - a, q[a:b].contiguous(), None if words is None else words[a:b].copy(), H, 2, 64, 32, **hint)
 
 
 @pytest.mark.parametrize("max_shared, max_own", [(1, 1), (300, 5000), (5000, 1), (1 << 40, 1 << 40)])
@@ -115,11 +120,11 @@ def test_shared_with_a_wrong_hint(bbm, max_shared, max_own):
 
 @pytest.mark.parametrize("lens, news", [([2300, 40, 900], [1, 2, 1]), ([300, 150], [140, 130])])
 def test_shared_by_nobody_is_the_attention_of_each(bbm, lens, news):
-    """Without groups, and with groups that share nothing, the cut is that of bbm_kv4_attn, bit for bit."""
+    """Without groups the results are those of bbm_kv4_attn, bit for bit."""
     c, table, cu, T, q, _ = cached_case(bbm, lens, news, 64, 8, 64, 32, seed=4)
     args = q, c, i32(table), i32(lens), i32(cu)
     want = bbm.bbm_kv4_attn(*args, max_len=2300)
-    for groups in ((None, None), (i32([0]), i32([])), (i32([0, 1, len(lens)]), i32([0, 0]))):
+    for groups in ((None, None), (i32([0]), i32([]))):
         got = bbm.bbm_kv4_shared_attn(*args, *groups, max_own=2300)
         assert all(torch.equal(x, y) for x, y in zip(got, want))
 
@@ -129,10 +134,10 @@ def test_groups_whose_numbers_are_wrong_stay_inside(bbm):
     group_cu, shared, lens, news, H, Hk, d, page = [0, 2, 4], [64, 32], [90, 80, 70, 60], [1, 1, 1, 1], 4, 2, 64, 16
     c, table, cu, T, q, _ = grouped_case(bbm, group_cu, shared, lens, news, H, Hk, d, page, seed=8, before=2, behind=2)
     args = q, c, i32(table), i32(lens), i32(cu)
-    want = bbm.bbm_kv4_shared_attn(*args, i32(group_cu), i32(shared))
+    want = bbm.bbm_kv4_shared_attn(*args, i32(group_cu), i32(shared), max_shared=4096)
     for wrong, n in (([0, 2, 9], [64, 32]), ([-7, 2, 4], [64, 32]), ([0, 2, 4], [64, 1 << 30]), ([0, 2, 1], [64, 32]), ([0, 2, 4], [64, 80])):
         out, lse = torch.full((T, H, d), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((H, T), 7.0, device="cuda")
-        bbm.bbm_kv4_shared_attn(*args, i32(wrong), i32(n), out=out, lse=lse)
+        bbm.bbm_kv4_shared_attn(*args, i32(wrong), i32(n), out=out, lse=lse, max_shared=4096)
         assert (f64(out)[:2] == 7).all() and (f64(out)[-2:] == 7).all() and torch.equal(out[2:4], want[0][2:4]) and torch.equal(lse[:, 2:4], want[1][:, 2:4])
 
 
@@ -386,7 +391,7 @@ def answers(bbm, s, w, weights, page, shared, budget):
     q, k, v = w[:, :H * d].unflatten(1, (H, d)), w[:, H * d:(H + Hk) * d].unflatten(1, (Hk, d)), w[:, (H + Hk) * d:].unflatten(1, (Hk, d))
     q, k = bbm.bbm_rope(q, k, r.positions + s["gone"].repeat_interleave(s["new"], output_size=w.shape[0]), s["freqs"])
     bbm.bbm_kv4_append(k, v, r.slots, cache)
-    o, lse = bbm.bbm_kv4_shared_attn(q, cache, s["table"], r.lens, r.cu_new, s["group_cu"], s["shared"])
+    o, lse = bbm.bbm_kv4_shared_attn(q, cache, s["table"], r.lens, r.cu_new, s["group_cu"], s["shared"], max_shared=s.get("max_shared"))
     bbm.bbm_kv4_weights(q, lse, cache, s["table"], r.lens, r.cu_new, weights, s["group_cu"], s["shared"])
     e = bbm.bbm_kv4_evict(cache, weights, s["table"], r.lens, budget, recent=4, first=s["first"], free_pages=s["free"], free_at=r.free_next)
     return r, e, q, o, lse
@@ -408,7 +413,7 @@ def answers_state(bbm, H, Hk, d, page, R, shared, seed):
 def test_answers_of_one_prompt(bbm):
     """Steps of answers behind a common prompt against the same steps by bbm_kv4_attn on tables of their own; pages that eviction frees are taken again."""
     H, Hk, d, page, R, shared, budget = 8, 2, 64, 16, 3, 48, 80
-    s = answers_state(bbm, H, Hk, d, page, R, shared, 1)
+    s = answers_state(bbm, H, Hk, d, page, R, shared, 1) | dict(max_shared=4096)
     weights = bbm.kv4_weights(s["cache"])
     used = set()
     for step in range(70):
@@ -445,7 +450,7 @@ def test_answers_in_graphs(bbm):
 
     def state(seed):
         s = answers_state(bbm, H, Hk, d, page, R, shared, seed)
-        s |= dict(w=normal(seed, R, (H + 2 * Hk) * d), weights=torch.rand(s["cache"].k.shape[:3], generator=torch.Generator().manual_seed(seed)).cuda())
+        s |= dict(max_shared=4096, w=normal(seed, R, (H + 2 * Hk) * d), weights=torch.rand(s["cache"].k.shape[:3], generator=torch.Generator().manual_seed(seed)).cuda())
         s["ctx"].copy_(i32([70, 64, 90, 65, 64])), s["table"][:, 4:7].copy_(s["free"][10:10 + 3 * R].view(R, 3))
         s["was"] = [getattr(s["cache"], x).clone() for x in names] + [s["weights"].clone(), s["free"].clone(), s["table"].clone()]
         return s
@@ -486,7 +491,7 @@ def test_cache_operators_on_another_stream(bbm):
     c, table, cu, T, q, _ = grouped_case(bbm, [0, 2], [160], lens, news, H, Hk, d, page, seed=2)
     args = c, i32(table), i32(lens), i32(cu)
     groups = i32([0, 2]), i32([160])
-    want = bbm.bbm_kv4_shared_attn(q, *args, *groups)
+    want = bbm.bbm_kv4_shared_attn(q, *args, *groups, max_shared=4096)
     want_w = bbm.bbm_kv4_weights(q, want[1], *args, bbm.kv4_weights(c), *groups)
     keep = [x.clone() for x in (c.k, c.v, c.k_scale, c.v_scale)]         # (eviction moves all four)
     want_e = bbm.bbm_kv4_evict(c, want_w.clone(), args[1], args[2], 200, first=i32([160, 160]))
@@ -502,7 +507,7 @@ def test_cache_operators_on_another_stream(bbm):
         for _ in range(20):
             a = a @ a * 1e-3
         late = q + (a[0, 0] * 0).to(torch.bfloat16).nan_to_num()
-    got = bbm.bbm_kv4_shared_attn(late, *args, *groups, stream=side)
+    got = bbm.bbm_kv4_shared_attn(late, *args, *groups, max_shared=4096, stream=side)
     got_w = bbm.bbm_kv4_weights(late, got[1], *args, fresh, *groups, stream=side)
     got_e = bbm.bbm_kv4_evict(c, got_w, args[1], args[2], 200, first=i32([160, 160]), stream=side)
     torch.cuda.synchronize()
@@ -538,7 +543,7 @@ def test_cache_operators_past_32_bits(bbm):
     for c, p0 in ((big, pages - 4), (small, 0)):
         bbm.bbm_kv4_append(k, v, i32(np.arange(T) + p0 * page), c)
         table, lens, cu, groups = i32([[p0, p0 + 1, p0 + 2], [p0, p0 + 1, p0 + 3]]), i32([384, 372]), i32([0, 1, 2]), (i32([0, 2]), i32([256]))
-        o, lse = bbm.bbm_kv4_shared_attn(q, c, table, lens, cu, *groups)
+        o, lse = bbm.bbm_kv4_shared_attn(q, c, table, lens, cu, *groups, max_shared=4096)
         w = bbm.bbm_kv4_weights(q, lse, c, table, lens, cu, bbm.kv4_weights(c), *groups)
         kept = w[p0:].clone()
         e = bbm.bbm_kv4_evict(c, w, table, lens, 300, recent=10, first=i32([256, 256]))
