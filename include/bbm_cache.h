@@ -37,7 +37,7 @@ int bbm_kv4_shared_attn(const bbm_packed* q, const bbm_packed* o, float* lse, in
  * the keys got (a row of lse = -infinity gives nothing).  The keys that a group shares get the sum over all its requests, and one decay.  Written are the slots of the keys that there
  * are (a key without a page is left out), others stay as they are.  A page that lies in two requests' rows
  * other than as a shared one of the same group gets unspecified numbers.  Deterministic.  Meant for scores (times softmax_scale) up to 2^12, like the gradients.
- * 0 <= decay <= 1.  max_shared and max_own are hints for the work split, as above.
+ * 0 <= decay <= 1; R * Hk below 2^19, other sizes as in bbm_kv4_attn.  max_shared and max_own are hints for the work split, as above.
  */
 int bbm_kv4_weights(const bbm_packed* q, const float* lse, int64_t T, int64_t R, const int32_t* cu, const int32_t* lens, const int32_t* block_table,
                     int64_t table_stride, int64_t max_pages, int64_t S, const int32_t* group_cu, const int32_t* shared_lens, const uint64_t* mask,
@@ -59,7 +59,7 @@ int bbm_kv4_weights(const bbm_packed* q, const float* lse, int64_t T, int64_t R,
  * The block table is not written: entries behind a request's last page may hold anything, as for bbm_build_slots, which takes from *free_at = free_next on what came back.
  * free_pages, free_at and free_next may all be NULL (pages are not given back then), free_pages alone if n_free is 0.  Keys on a page outside the cache count as less than a NaN, and what would move from or to one does not.
  * A page that another request reads too (a shared prefix) has to lie within first[r], which protects it.  new_lens may be lens.  weights as above.
- * The workspace needs bbm_kv4_evict_workspace_bytes bytes for the same R, Hk and max_pages * page, 16-byte aligned, contents of no matter.  1 <= R <= BBM_SLOTS_MAX_REQUESTS, budget >= 1 (of
+ * The workspace needs bbm_kv4_evict_workspace_bytes bytes for the same R, Hk and max_pages * page, 16-byte aligned, contents of no matter.  1 <= R <= BBM_SLOTS_MAX_REQUESTS, R * Hk at most 2^21, budget >= 1 (of
  * what a table holds at most 2^19), recent >= 0.  max_len is a hint (the longest of lens, or an upper bound); any positive number gives the same results.
  */
 size_t bbm_kv4_evict_workspace_bytes(int64_t R, int64_t Hk, int64_t max_keys);

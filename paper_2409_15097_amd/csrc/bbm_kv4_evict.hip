@@ -407,7 +407,7 @@ extern "C" __attribute__((visibility("default"))) int bbm_kv4_evict(const bbm_kv
   if ((free_at != nullptr) != (free_next != nullptr) || n_free < 0 || (n_free > 0) > (free_pages != nullptr) || (free_pages != nullptr) > (free_at != nullptr) || !aligned(free_pages, 4) || !aligned(free_at, 4) || !aligned(free_next, 4))
     return fail(BBM_EINVAL, "%s: free_pages (of n_free=%lld pages), free_at and free_next are given together, 4-byte aligned", fn, (long long)n_free);
   if (R > BBM_SLOTS_MAX_REQUESTS) return fail(BBM_EUNSUPPORTED, "%s: R=%lld requests, more than %d", fn, (long long)R, BBM_SLOTS_MAX_REQUESTS);
-  if (R * cache->Hk > (1 << 22)) return fail(BBM_EUNSUPPORTED, "%s: problem too large (R=%lld, Hk=%lld)", fn, (long long)R, (long long)cache->Hk);
+  if (R * cache->Hk > (1 << 21)) return fail(BBM_EUNSUPPORTED, "%s: problem too large (R=%lld, Hk=%lld)", fn, (long long)R, (long long)cache->Hk);
   const int64_t max_keys = max_pages * cache->page;
   if (std::min(budget, max_keys) > kMaxBudget) return fail(BBM_EUNSUPPORTED, "%s: budget=%lld is beyond %lld", fn, (long long)budget, (long long)kMaxBudget);
   const size_t need = bbm_kv4_evict_workspace_bytes(R, cache->Hk, max_keys);

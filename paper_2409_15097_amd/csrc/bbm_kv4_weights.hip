@@ -442,11 +442,13 @@ __global__ __launch_bounds__(64 * NW, 4) void kv4_weights_both_kernel(const Weig
   else narrow<D>(P, share_of<false>(P, false));
 }
 
-// Work-groups of an owner: of the narrow kernel enough to fill the chip, of the wide one as many as it has pieces.
-constexpr int64_t kFill = 512, kMaxParts = 1 << 17;  // (two steps behind a key are still a 32-bit number)
+// Work-groups of an owner: of the narrow kernel enough to fill the chip, of the wide one as many as it has pieces (a launch counts threads in 32 bits: of many owners or a long table fewer,
+// which then take several pieces each).
+constexpr int64_t kFill = 512, kMaxParts = 1 << 17, kMaxOwners = 1 << 19, kMaxWideWgs = 1 << 21;  // (two steps of kMaxParts behind a key are still a 32-bit number)
 inline int64_t parts_of(int64_t owners, int64_t Hk, int64_t keys, bool wide) {
   keys = std::min<int64_t>(keys, bbm::kMaxTokens);
-  return std::min(wide ? bbm::ceil_div(keys, kWideKeys) : std::min(bbm::ceil_div(keys, kStep), bbm::ceil_div(kFill, owners * Hk)), kMaxParts);
+  if (!wide) return std::min(bbm::ceil_div(keys, kStep), bbm::ceil_div(kFill, owners * Hk));
+  return std::min({bbm::ceil_div(keys, kWideKeys), kMaxParts, std::max<int64_t>(8, kMaxWideWgs / (owners * Hk) / 8 * 8)});
 }
 // Columns of an owner, on average, from which on its codes are better converted once.
 constexpr int64_t kWideFrom = 32;
@@ -480,7 +482,7 @@ extern "C" __attribute__((visibility("default"))) int bbm_kv4_weights(const bbm_
   if (!(decay >= 0.0f && decay <= 1.0f)) return fail(BBM_EINVAL, "%s: decay=%g is outside 0 .. 1", fn, (double)decay);
   if (!weights || !out || !aligned(weights, 16) || !aligned(out, 16)) return fail(BBM_EINVAL, "%s: weights and out must be non-NULL 16-byte aligned pointers", fn);
   const int64_t G = H / cache->Hk;
-  if (T * G > kMaxTokens) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, H=%lld)", fn, (long long)T, (long long)H);
+  if (T * G > kMaxTokens || R * cache->Hk >= kMaxOwners) return fail(BBM_EUNSUPPORTED, "%s: problem too large (T=%lld, R=%lld, H=%lld)", fn, (long long)T, (long long)R, (long long)H);
   if (T == 0) return BBM_OK;
   if (int rc = check_apart(fn, {out}, {q->ptr, lse, cu, lens, block_table, mask, cache->k, cache->k_scale, S > 0 ? group_cu : nullptr, S > 0 ? shared_lens : nullptr})) return rc;
   WeightParams P = {};
@@ -494,8 +496,6 @@ extern "C" __attribute__((visibility("default"))) int bbm_kv4_weights(const bbm_
   const int64_t group_parts = S > 0 ? parts_of(S, cache->Hk, max_shared, group_wide) : 1, own_parts = parts_of(R, cache->Hk, max_own, own_wide);
   auto count = [&](int64_t owners, int64_t parts, bool wide) { return owners * (wide ? work_groups(cache->Hk, parts) : cache->Hk * parts); };
   const int64_t group_wgs = count(S, group_parts, group_wide), own_wgs = count(R, own_parts, own_wide);
-  if (R * cache->Hk >= kMaxWgs || group_wgs >= kMaxWgs / 2 || own_wgs >= kMaxWgs / 2)
-    return fail(BBM_EUNSUPPORTED, "%s: problem too large (R=%lld, Hk=%lld, keys %lld and %lld)", fn, (long long)R, (long long)cache->Hk, (long long)max_shared, (long long)max_own);
   // (heads of a tile that a buffer's 31 bits reach: of rows up to 2^22 elements apart 64 tokens are within 2^29 bytes)
   const int64_t reach = q->head_stride > 0 ? 1 + (1ll << 29) / q->head_stride : kWideCols;
   P.tile_heads = (int32_t)std::min({G, (int64_t)kWideCols, reach}), P.tile_tokens = kWideCols / P.tile_heads;

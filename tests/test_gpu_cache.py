@@ -5,7 +5,8 @@ import pytest
 import torch
 
 from oracle import tokens as ot
-from test_gpu_tokens import cached_case, check_cached, close, f64, host_cache, i32, normal
+from test_gpu_tokens import (OUT_LAYOUTS, SIZES, c_packed, cached_case, check_cached, close, f64, host_cache, i32, normal, output_in, same_and_nothing_else, sized_bounds, sized_query,
+                             sized_rows)
 
 pytestmark = pytest.mark.gpu
 
@@ -127,6 +128,65 @@ def test_shared_by_nobody_is_the_attention_of_each(bbm, lens, news):
     for groups in ((None, None), (i32([0]), i32([]))):
         got = bbm.bbm_kv4_shared_attn(*args, *groups, max_own=2300)
         assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+GROUPED = [([2300, 2290, 2400], [1, 1, 2], 8, 2, 64), ([2300, 2290, 2400], [1, 1, 2], 8, 2, 128), ([2300, 2320, 2350], [130, 130, 130], 8, 1, 64), ([2300, 2320, 2350], [130, 130, 130], 8, 1, 128)]
+
+
+@pytest.mark.parametrize("base, gap, scale", SIZES)
+@pytest.mark.parametrize("lens, news, H, Hk, d, sign", [([170, 200, 165], [3, 1, 1], 4, 2, 64, 1), ([1300, 1290], [130, 130], 8, 2, 128, -1)])
+def test_shared_scores_of_any_size(bbm, lens, news, H, Hk, d, sign, base, gap, scale):
+    """Sums of a prefix and of what lies behind it meet under one maximum: few columns and many."""
+    page, shared = 32, 96 if len(lens) == 3 else 1024
+    n, R = sum(lens), len(lens)
+    c = bbm.kv4_cache(-(-n // page) + R, Hk, d, page)
+    width = max(-(-m // page) for m in lens)
+    table, slots, at = np.full((R, width), -1), [], 0
+    for r, m in enumerate(lens):
+        pages = -(-m // page)
+        table[r, :pages] = np.arange(at, at + pages)
+        slots += list(at * page + np.arange(m))
+        at += pages
+    bbm.bbm_kv4_append(sized_rows(1, n, Hk, d, sign, base, gap), normal(2, n, Hk, d), i32(slots), c)
+    table[1:, :shared // page] = table[0, :shared // page]
+    hk, hv = host_cache(c)
+    cu, T = np.concatenate([[0], np.cumsum(news)]), sum(news)
+    q = sized_query(T, H, d, base)
+    o, lse = bbm.bbm_kv4_shared_attn(q, c, i32(table), i32(lens), i32(cu), i32([0, R]), i32([shared]), softmax_scale=2.0 ** scale, max_shared=4096, max_own=300)
+    q = f64(q)
+    for r, m in enumerate(lens):
+        a, b = cu[r], cu[r + 1]
+        seen = np.arange(m) <= m - news[r] + np.arange(b - a)[:, None]
+        pg, j = table[r, np.arange(m) // page], np.arange(m) % page
+        for h in range(0, H, max(1, H // 4)):
+            kk, vv = hk[pg, h * Hk // H, j], hv[pg, h * Hk // H, j]
+            wo, wl, p = ot.attention(q[a:b, h], kk, vv, seen, 2.0 ** scale)
+            e_o, e_l = sized_bounds(seen, p, vv, wo, wl)
+            close(f"request {r}, head {h}: O", o[a:b, h], wo, e_o), close(f"request {r}, head {h}: lse", lse[h, a:b], wl, e_l)
+
+
+@OUT_LAYOUTS
+@pytest.mark.parametrize("lens, news, H, Hk, d", GROUPED)
+def test_shared_outputs_in_other_layouts(bbm, lens, news, H, Hk, d, layout):
+    c, table, cu, T, q, _ = grouped_case(bbm, [0, 3], [2048], lens, news, H, Hk, d, 32, seed=15, before=2, behind=3)
+    args = q, c, i32(table), i32(lens), i32(cu), i32([0, 3]), i32([2048])
+    want, _ = bbm.bbm_kv4_shared_attn(*args)
+    o, o_all = output_in(layout, T, H, d)
+    bbm.bbm_kv4_shared_attn(*args, out=o)
+    same_and_nothing_else(o, o_all, want, slice(int(cu[0]), int(cu[-1])))
+
+
+@pytest.mark.parametrize("lens, news, H, Hk, d", GROUPED)
+def test_shared_without_a_log_sum_exp(bbm, lens, news, H, Hk, d):
+    import ctypes
+    c, table, cu, T, q, _ = grouped_case(bbm, [0, 3], [2048], lens, news, H, Hk, d, 32, seed=17)
+    tab, ln, offsets, gc, sh = i32(table), i32(lens), i32(cu), i32([0, 3]), i32([2048])
+    want, _ = bbm.bbm_kv4_shared_attn(q, c, tab, ln, offsets, gc, sh, max_shared=2048, max_own=400)
+    need = bbm.bbm_kv4_shared_attn_workspace_bytes(T, 3, 1, H, Hk, d, 2048, 400)
+    ws, o = torch.full((need,), 255, dtype=torch.uint8, device="cuda"), torch.full_like(want, 7.0)
+    assert bbm.lib.bbm_kv4_shared_attn(c_packed(q), c_packed(o), None, T, 3, offsets.data_ptr(), ln.data_ptr(), tab.data_ptr(), tab.stride(0), tab.shape[1], 1, gc.data_ptr(), sh.data_ptr(),
+                                       None, 0, ctypes.byref(c.c_struct), H, d ** -0.5, 2048, 400, ws.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == bbm.BBM_OK
+    assert torch.equal(o, want)
 
 
 def test_groups_whose_numbers_are_wrong_stay_inside(bbm):
@@ -269,6 +329,36 @@ def test_weights_of_rows_that_saw_nothing(bbm):
     check_weights(bbm, None, None, c, table, lens, cu, T, q, None, H, Hk, d, page, lse=lse)
 
 
+@pytest.mark.parametrize("max_own", [1, 1 << 40])
+def test_weights_of_many_columns_and_requests(bbm, max_own):
+    """Pieces that a work-group takes one after the other, and hints beyond any table."""
+    R = 20
+    lens, news = [300 + 11 * i for i in range(R)], [40 + i for i in range(R)]
+    c, table, cu, T, q, _ = cached_case(bbm, lens, news, 2, 2, 64, 16, seed=6)
+    check_weights(bbm, None, None, c, table, lens, cu, T, q, None, 2, 2, 64, 16, hints=[dict(max_own=max_own)])
+
+
+def test_weights_of_heads_far_apart(bbm):
+    """Heads so far apart that a tile's columns are one head's tokens; and the layout with all tokens of a head side by side."""
+    lens, news, H, Hk, d, page = [300, 170], [70, 45], 4, 2, 64, 16
+    c, table, cu, T, q, _ = cached_case(bbm, lens, news, H, Hk, d, page, seed=8)
+    _, lse = bbm.bbm_kv4_attn(q, c, i32(table), i32(lens), i32(cu))
+    store = torch.empty((1 << 29) + 8 + T * 2 * d, dtype=torch.bfloat16, device="cuda")
+    far = store.as_strided((T, 2, d), (2 * d, (1 << 29) + 8, 1))
+    args = c, i32(table), i32(lens), i32(cu)
+    one = bbm.kv4_cache(c.k.shape[0], 1, d, page)
+    for x in ("k", "v", "k_scale", "v_scale"):
+        getattr(one, x).copy_(getattr(c, x)[:, :1])
+    far.copy_(q[:, :2])
+    want = bbm.bbm_kv4_weights(q[:, :2].contiguous(), lse[:2].contiguous(), one, *args[1:], bbm.kv4_weights(one))
+    got = bbm.bbm_kv4_weights(far, lse[:2].contiguous(), one, *args[1:], bbm.kv4_weights(one))
+    # (the same terms in another order: two heads' tokens in one tile, or one behind the other)
+    tol = 2 * ot.F * (T * 2 + 16) * f64(want)
+    close("weights", got, f64(want), tol)
+    heads = q[:, :2].transpose(0, 1).contiguous().transpose(0, 1)
+    assert torch.equal(bbm.bbm_kv4_weights(heads, lse[:2].contiguous(), one, *args[1:], bbm.kv4_weights(one)), want)
+
+
 # ---- eviction
 
 
@@ -362,6 +452,51 @@ def test_evict_into_a_short_list(bbm, n_free):
 def test_evict_of_many_requests(bbm):
     R = 500
     check_evict(bbm, [30 + i * 7 % 90 for i in range(R)], 1, 64, 16, 48, 5, [i % 9 for i in range(R)])
+
+
+@pytest.mark.parametrize("lens, budget, recent, table_pages", [([25000, 9000], 3000, 700, 1600), ([45000], 600, 16, 2900)])
+def test_evict_of_long_requests_in_a_graph(bbm, lens, budget, recent, table_pages):
+    """Weights that take most of a CU's LDS, and more than fit; recorded before it has run once, replayed on what other requests left."""
+    Hk, d, page, R = 2, 64, 16, len(lens)
+    g = np.random.default_rng(5)
+    pages = sum(-(-n // page) for n in lens) + 5
+    ids, table, at = g.permutation(pages), np.full((R, table_pages), -1), 0
+    for r, n in enumerate(lens):
+        table[r, :-(-n // page)] = ids[at:at + -(-n // page)]
+        at += -(-n // page)
+    c = bbm.kv4_cache(pages, Hk, d, page)
+    names = ("k", "v", "k_scale", "v_scale")
+    was = {x: g.integers(0, 255, getattr(c, x).shape, dtype=np.uint8) for x in names}
+    w = g.random(tuple(c.k.shape[:3])).astype(np.float32)
+    want, want_w = {x: y.copy() for x, y in was.items()}, w.copy()
+    for r, n in enumerate(lens):
+        slot = lambda j: (table[r, j // page], j % page)  # noqa: E731
+        for h in range(Hk):
+            ws = w[table[r, np.arange(n) // page], h, np.arange(n) % page]
+            between = np.lexsort((np.arange(n - recent), -ws[:n - recent]))
+            kept, edge = np.zeros(n, bool), budget - recent
+            kept[between[:edge]] = True
+            src = np.concatenate([np.nonzero(kept[edge:n - recent])[0] + edge, np.arange(n - recent, n)])
+            dst = np.concatenate([np.nonzero(~kept[:edge])[0], np.arange(edge, budget)])
+            (a, i), (b, j) = slot(src), slot(dst)
+            for x in ("k", "v", "k_scale"):
+                want[x][b, h, j] = was[x][a, h, i]
+            want["v_scale"][b, h, :, j] = was["v_scale"][a, h, :, i]
+            want_w[b, h, j] = w[a, h, i]
+    wt, tt, ln = torch.empty(w.shape, device="cuda"), i32(table), i32(lens)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        e = bbm.bbm_kv4_evict(c, wt, tt, ln, budget, recent=recent, max_len=max(lens))
+    for _ in range(3):
+        for x in names:
+            getattr(c, x).copy_(torch.from_numpy(was[x]))
+        wt.copy_(torch.from_numpy(w))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert e.lens.tolist() == [budget] * R and np.array_equal(wt.cpu().numpy(), want_w)
+        for x in names:
+            assert np.array_equal(getattr(c, x).cpu().numpy(), want[x]), x
 
 
 def test_evict_without_a_list(bbm):
