@@ -90,8 +90,8 @@ template <int D>
 __global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
   // free places, a bit each, 64 a word; the number of those in front of each word; the request's pages (P.held_pages); the weights of the keys between (P.held of them)
   extern __shared__ __attribute__((aligned(16))) uint32_t dynamic_s[];
-  __shared__ int wave_s[2][NWAVES];
-  __shared__ uint32_t found_s[2];            // the bin, what is still to be chosen from it
+  __shared__ int wave_s[3][NWAVES];
+  __shared__ uint32_t found_s[3][3];         // of each pass the bin, what is still to be chosen from it, what it holds
   __shared__ int2 moves_s[NWAVES][2 * 64];  // of a wave: from and to, as slots
   uint32_t* const bins = reinterpret_cast<uint32_t*>(moves_s);
   static_assert(sizeof(moves_s) >= kBins * sizeof(uint32_t) && sizeof(moves_s) >= kGiveTogether * sizeof(int), "bins, and pages of requests, lie in the place of moves");
@@ -143,14 +143,20 @@ __global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
   };
   auto weight_of = [&](int i) -> uint32_t { return held ? held_s[i] : weight_in_memory(i); };
 
+  // What the waves in front of this one wrote down.
+  auto in_front = [&](const int* of_waves) {
+    const int v = lane < NWAVES ? of_waves[lane] : 0, sum = bbm::wave_prefix_sum(v);
+    return wave > 0 ? __builtin_amdgcn_readlane(sum, max(wave - 1, 0)) : 0;
+  };
+
   // The smallest weight that stays, and how many that equal it do.
   uint32_t low = 0, need = (uint32_t)x.chosen, equal = 0;
   if (x.chosen > 0) {
     constexpr int SHIFT[3] = {21, 10, 0}, BITS[3] = {11, 11, 10};
+    for (int i = tid; i < kBins; i += NT) bins[i] = 0;
+    __syncthreads();
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
-      for (int i = tid; i < kBins; i += NT) bins[i] = 0;
-      __syncthreads();
       const uint32_t above = pass == 0 ? 0u : ~0u << (pass == 1 ? 21 : 10);
       constexpr int U = 8;  // (so many loads under way)
       for (int i0 = tid; i0 < x.between; i0 += U * NT) {
@@ -168,24 +174,25 @@ __global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
         }
       }
       __syncthreads();
-      // two bins a thread, the highest first
-      const uint32_t c0 = bins[kBins - 1 - 2 * tid], c1 = bins[kBins - 2 - 2 * tid];
+      // two bins a thread, the highest first; who reads them clears them for the next pass
+      uint2* const mine = reinterpret_cast<uint2*>(bins) + (NT - 1 - tid);
+      const uint32_t c0 = mine->y, c1 = mine->x;
+      *mine = make_uint2(0, 0);
       int sum = bbm::wave_prefix_sum((int)(c0 + c1));
       if (lane == 63) wave_s[0][wave] = sum;
       __syncthreads();
-      for (int w = 0; w < wave; ++w) sum += wave_s[0][w];
+      sum += in_front(wave_s[0]);
       const uint32_t before = (uint32_t)sum - c0 - c1;
       if (before < need && need <= (uint32_t)sum) {
         const bool second = before + c0 < need;
-        found_s[0] = (uint32_t)(kBins - 1 - 2 * tid) - second;
-        found_s[1] = need - before - (second ? c0 : 0u);
-        bins[0] = second ? c1 : c0;  // (everyone has read its own)
+        found_s[pass][0] = (uint32_t)(kBins - 1 - 2 * tid) - second;
+        found_s[pass][1] = need - before - (second ? c0 : 0u);
+        found_s[pass][2] = second ? c1 : c0;
       }
       __syncthreads();
-      low |= found_s[0] << SHIFT[pass];
-      need = found_s[1];
-      equal = bins[0];
-      __syncthreads();
+      low |= found_s[pass][0] << SHIFT[pass];
+      need = found_s[pass][1];
+      equal = found_s[pass][2];
     }
   } else {
     low = ~0u;
@@ -200,9 +207,9 @@ __global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
       const int i = 64 * k + lane;
       mine += __popcll(__ballot(i < x.between && weight_of(min(i, x.between - 1)) == low));
     }
-    if (lane == 0) wave_s[0][wave] = mine;
+    if (lane == 0) wave_s[1][wave] = mine;
     __syncthreads();
-    for (int w = 0; w < wave; ++w) ties += wave_s[0][w];
+    ties = in_front(wave_s[1]);
   }
   // f(block, which of its 64 keys stay) for the blocks of this wave in order, the weights of four of them read together.
   auto for_kept = [&](auto f) __attribute__((always_inline)) {
@@ -235,19 +242,17 @@ __global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
     if (lane == 0 && places) free_s[k] = places & ~stay;
     behind += __popcll(stay & ~places);
   });
-  if (lane == 0) wave_s[1][wave] = behind;
+  if (lane == 0) wave_s[0][wave] = behind;
   __syncthreads();
-  int rank = 0;  // of this wave's first move
-  for (int w = 0; w < wave; ++w) rank += wave_s[1][w];
+  int rank = in_front(wave_s[0]);  // of this wave's first move
   {
     const int each = (words + NT - 1) / NT, w0 = min(words, tid * each), w1 = min(words, w0 + each);
     int mine = 0;
     for (int w = w0; w < w1; ++w) mine += __popcll(free_s[w]);
     int sum = bbm::wave_prefix_sum(mine);
-    if (lane == 63) wave_s[0][wave] = sum;
+    if (lane == 63) wave_s[2][wave] = sum;
     __syncthreads();
-    for (int w = 0; w < wave; ++w) sum += wave_s[0][w];
-    sum -= mine;
+    sum += in_front(wave_s[2]) - mine;
     for (int w = w0; w < w1; ++w) {
       before_s[w] = sum;
       sum += __popcll(free_s[w]);
