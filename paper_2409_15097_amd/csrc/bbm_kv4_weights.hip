@@ -8,6 +8,8 @@
 // Wide, for many: bound by the exponentials and the products.  A work-group takes 128 keys, whose codes are converted once into operands in registers, and walks tiles of 64 columns
 // through LDS; a wave has 32 of the keys and 32 columns of every tile.
 // Either way a lane adds up the exponentials of its column, and lanes meet once, behind the last column.
+// Measured, 32 / 8 heads of 128: one token each of 64 requests of 4 to 8 thousand keys (240 MB), narrow, 60 us, 4.0 TB/s (a large copy reaches 5.2); prompts of 1500, 420 and 839 tokens over up
+// to 6000 keys, wide, 136 us, 0.78 PFLOP/s (a large product 1.26; the vector pipe is busy for 56 % of the cycles, the matrix pipe for 31).
 #include "bbm_cache.h"
 #include "bbm_kv4.h"
 #include "bbm_prompt.h"
