@@ -53,9 +53,9 @@ int bbm_kv4_weights(const bbm_packed* q, const float* lse, int64_t T, int64_t R,
  * Heads choose for themselves: a position then holds other tokens in other heads (their rotary positions are in the keys).  Positions from b on keep what they held.
  * Written besides:
  *   new_lens [R]    min(n, b) (n as cut)
- *   free_pages      the pages behind position b, back in front of *free_at: entries *free_at - m .. *free_at - 1 of free_pages [n_free] get the m pages given back, in the order of
- *                   requests and positions (entries of the table that name no page are not given back, nor is a page whose place would lie outside of the list)
- *   free_next [1]   *free_at - m
+ *   free_pages      the pages behind position b, back in front of *free_at: with e = min(*free_at, n_free) entries e - m .. e - 1 of free_pages [n_free] get the m pages given back, in
+ *                   the order of requests and positions (entries of the table that name no page are not given back, nor is a page whose place would lie in front of the list)
+ *   free_next [1]   e - m
  * The block table is not written: entries behind a request's last page may hold anything, as for bbm_build_slots, which takes from *free_at = free_next on what came back.
  * free_pages, free_at and free_next may all be NULL (pages are not given back then), free_pages alone if n_free is 0.  Keys on a page outside the cache count as less than a NaN, and what would move from or to one does not.
  * A page that another request reads too (a shared prefix) has to lie within first[r], which protects it.  new_lens may be lens.  weights as above.

@@ -362,7 +362,7 @@ def test_weights_of_heads_far_apart(bbm):
 # ---- eviction
 
 
-def check_evict(bbm, lens, H, d, page, budget, recent, first=None, weigh=None, spoil=None, free=None, width=None, seed=0, hints=({},)):
+def check_evict(bbm, lens, H, d, page, budget, recent, first=None, weigh=None, spoil=None, free=None, width=None, seed=0, hints=({},), short_by=0):
     """Against the definition, key by key; whole tensors are compared, so that nothing else may change."""
     Hk = H
     c, table, _, _, _, _ = cached_case(bbm, [max(0, n) for n in lens], [0] * len(lens), Hk, Hk, d, page, seed=seed, behind=1)
@@ -379,7 +379,7 @@ def check_evict(bbm, lens, H, d, page, budget, recent, first=None, weigh=None, s
     was = {x: getattr(c, x).cpu().numpy() for x in names}
     want, want_w = {x: y.copy() for x, y in was.items()}, w.copy()
     free = g.permutation(pages + 40).astype(np.int32) if free is None else free
-    at = min(len(free), pages + 3)
+    at = len(free) if short_by else min(len(free), pages + 3)             # (of a list that was too short more was asked for than it had)
     given, left = [], []
     for r, n in enumerate(lens):
         n = min(max(0, n), table.shape[1] * page)
@@ -408,7 +408,7 @@ def check_evict(bbm, lens, H, d, page, budget, recent, first=None, weigh=None, s
         wt, ft, tt = torch.from_numpy(w.copy()).cuda(), i32(free), i32(table)
         fi = None if first is None else i32(first)
         lens_t = i32(lens)
-        e = bbm.bbm_kv4_evict(c, wt, tt, lens_t, budget, recent=recent, first=fi, free_pages=ft, free_at=i32([at]), new_lens=lens_t if hint else None, **hint)
+        e = bbm.bbm_kv4_evict(c, wt, tt, lens_t, budget, recent=recent, first=fi, free_pages=ft, free_at=i32([at + short_by]), new_lens=lens_t if hint else None, **hint)
         assert e.lens.cpu().tolist() == left and int(e.free_next) == at - len(given)
         assert np.array_equal(ft.cpu().numpy(), list_want) and np.array_equal(tt.cpu().numpy(), table)
         for x in names:
@@ -447,6 +447,11 @@ def test_evict_pages_outside_and_a_narrow_table(bbm):
 def test_evict_into_a_short_list(bbm, n_free):
     """Pages without a place in the list are not written anywhere."""
     check_evict(bbm, [300, 200, 400], 1, 64, 16, 64, 8, free=np.arange(n_free, dtype=np.int32) + 100)
+
+
+def test_evict_into_a_list_that_was_too_short(bbm):
+    """What the last step asked for and did not get is not where pages go back to."""
+    check_evict(bbm, [300, 200, 400], 1, 64, 16, 64, 8, free=np.arange(60, dtype=np.int32) + 100, short_by=7)
 
 
 def test_evict_of_many_requests(bbm):
