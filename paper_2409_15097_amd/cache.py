@@ -133,10 +133,12 @@ def _kv4_evict(dev, cache, weights, block_table, lens, budget, recent, first, fr
     assert cache.device == dev, "the cache lies elsewhere"
     table, stride, width = _table(block_table, dev, R)
     assert (free_pages is None) == (free_at is None), "a list of free pages and its index"
-    new_lens = lens.new_empty(R) if new_lens is None else new_lens
-    free_next = None if free_at is None else lens.new_empty(1)
-    if workspace is None:
-        workspace = lens.new_empty(lib.bbm_kv4_evict_workspace_bytes(R, c.Hk, width * c.page), dtype=torch.uint8)
+    # (one allocation for what the call gives and what it needs)
+    need = 0 if workspace is not None else -(-lib.bbm_kv4_evict_workspace_bytes(R, c.Hk, width * c.page) // 16) * 4
+    own, lens_out, free_next = torch.split_with_sizes(lens.new_empty(need + R + 1), (need, R, 1))
+    workspace = own if workspace is None else workspace
+    new_lens = lens_out if new_lens is None else new_lens
+    free_next = None if free_at is None else free_next
     free = (None, 0, None, None) if free_at is None else (_ints(free_pages, dev), free_pages.shape[0], _ints(free_at, dev, 1), free_next.data_ptr())
     _check(lib.bbm_kv4_evict(_address(c), _weights(weights, cache), R, _ints(lens, dev), table, stride, width, budget, recent, None if first is None else _ints(first, dev, R),
                              _ints(new_lens, dev, R), *free, width * c.page if max_len is None else max(1, max_len), *_workspace(workspace, dev), _here(dev)))
