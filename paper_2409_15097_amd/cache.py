@@ -2,6 +2,7 @@
 
 Devices, streams and what a call allocates are as in tokens.py."""
 from dataclasses import dataclass
+from functools import lru_cache
 from typing import Optional
 
 import torch
@@ -27,6 +28,7 @@ def _groups(group_cu: Optional[torch.Tensor], shared_lens: Optional[torch.Tensor
     return S, _ints(group_cu, device, S + 1), _ints(shared_lens, device, S)
 
 
+@lru_cache(maxsize=256)   # (of sizes alone; asking the library is 0.5 us of a call that takes the host 12)
 def bbm_kv4_shared_attn_workspace_bytes(T: int, R: int, S: int, H: int, Hk: int, d: int, max_shared: int, max_own: int) -> int:
     return int(lib.bbm_kv4_shared_attn_workspace_bytes(T, R, S, H, Hk, d, max_shared, max_own))
 
@@ -56,7 +58,7 @@ def _kv4_shared_attn(dev, q, cache, block_table, lens, cu, group_cu, shared_lens
     out, to = _out(out, q, dev, T, H, d)
     lse, lse_at = _lse_out(lse, q, dev, H, T)
     if workspace is None:
-        need = lib.bbm_kv4_shared_attn_workspace_bytes(T, R, S, H, c.Hk, d, max_shared, max_own)
+        need = bbm_kv4_shared_attn_workspace_bytes(T, R, S, H, c.Hk, d, max_shared, max_own)
         workspace = q.new_empty(need, dtype=torch.uint8) if need else None
     keep = _I64x6(*packed, *to)
     at = _address(keep)

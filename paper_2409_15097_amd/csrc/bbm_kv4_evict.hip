@@ -5,7 +5,7 @@
 // bisection over the counts of 64 places, then by counting bits.  Where the moves of the first kind end they read nothing that they write, so their order does not matter; the last
 // keys are shifted by whole rounds of all waves, with a barrier between a round's loads and its stores, in ascending order.
 // The pages go back by a wave for each request, behind the sum of what the requests in front of it give: of up to 256 requests in one more work-group, else by a second kernel.
-// Bound by latency where little moves: 1040 keys to 1024, 4 heads of 64, 14 us, 64 requests of up to 2112 keys to 2048, 8 heads of 128, 16; by pieces of 64 bytes all over the cache
+// Bound by latency where little moves: 1040 keys to 1024, 4 heads of 64, 11.5 us, 64 requests of up to 2112 keys to 2048, 8 heads of 128, 14; by pieces of 64 bytes all over the cache
 // where much does: 16 requests of up to 32000 keys to 4000, 62 us, 2.3 TB/s (with weights read from memory in every pass and moves of 64 keys at a time 108; 70 with the pages from memory).
 #include "bbm_cache.h"
 #include "bbm_kv4.h"
