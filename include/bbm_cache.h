@@ -34,7 +34,7 @@ int bbm_kv4_shared_attn(const bbm_packed* q, const bbm_packed* o, float* lse, in
  * the same, and overlap in no other way.  For each request with a new token that has a row, each of its keys j and each key head,
  *   out[j] = decay * weights[j] + the sum over its new tokens i that see j (as in bbm_kv4_attn) and the heads h of the group of exp(softmax_scale <q_i, k_j> - lse[h][i]),
  * with 0 for weights[j] of the new tokens' own keys, whose slots may hold anything.  With lse of the attention of the same step that is the probability which
- * the keys got (a row of lse = -infinity gives nothing).  The keys that a group shares get the sum over all its requests, and one decay.  Written are the slots of the keys that there
+ * the keys got (a row of lse = -infinity gives nothing, whatever its query holds).  The keys that a group shares get the sum over all its requests, and one decay.  Written are the slots of the keys that there
  * are (a key without a page is left out), others stay as they are.  A page that lies in two requests' rows
  * other than as a shared one of the same group gets unspecified numbers.  Deterministic.  Meant for scores (times softmax_scale) up to 2^12, like the gradients.
  * 0 <= decay <= 1; R * Hk below 2^19, other sizes as in bbm_kv4_attn.  max_shared and max_own are hints for the work split, as above.

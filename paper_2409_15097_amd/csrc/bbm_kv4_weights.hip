@@ -30,7 +30,7 @@ constexpr int kWideKeys = 128, kWideCols = 64;
 struct WeightParams {
   Kv4 c;
   const __bf16* q;
-  const float* lse;
+  const uint32_t* lse;  // (its bits)
   const float* weights;
   float* out;
   int64_t q_row, q_head, table_stride;
@@ -127,13 +127,13 @@ __device__ __forceinline__ Share share_of(Args P, bool group) {
 struct Column {
   int col, i, g;
   const __bf16* q;
-  const float* lse;
+  const uint32_t* lse;  // its bits
 };
 struct Stride {
   int cols, i, g;
 };
 __device__ __forceinline__ Stride stride_of(Args P, int cols) { return {cols, cols / P->G, cols % P->G}; }
-__device__ __forceinline__ Column column_of(Args P, const __bf16* q0, const float* lse0, int c) {
+__device__ __forceinline__ Column column_of(Args P, const __bf16* q0, const uint32_t* lse0, int c) {
   Column y;
   y.col = c, y.i = c / P->G, y.g = c - y.i * P->G;
   y.q = q0 + y.i * P->q_row + y.g * P->q_head;
@@ -152,7 +152,9 @@ __device__ __forceinline__ void advance(Args P, Column& y, const Stride& s) {
     y.lse += over ? 1 - (int64_t)P->G * P->T : 0;
   }
 }
-__device__ __forceinline__ float minus_lse(float l) { return l != -INFINITY ? l * -kLog2e : -INFINITY; }  // (a row that saw nothing gives nothing)
+// A row that saw nothing, whose log-sum-exp is -infinity, gives nothing.  (That is told from the bits as they lie in memory: as floats the compiler takes all for numbers.)
+__device__ __forceinline__ bool gives_nothing(uint32_t lse) { return lse == 0xff800000u; }
+__device__ __forceinline__ float minus_lse(uint32_t lse) { return gives_nothing(lse) ? -INFINITY : __uint_as_float(lse) * -kLog2e; }
 // Which of the keys from j on the new token of a column sees.
 __device__ __forceinline__ uint64_t seen_by(Args P, const Owner& x, int i, int j) {
   i = min(i, x.end - x.begin - 1);
@@ -225,20 +227,24 @@ __device__ __forceinline__ void narrow(Args P, const Share& own) {
   };
 
   const __bf16* const q0 = bbm::global(P->q) + (int64_t)x.begin * P->q_row + (int64_t)hk * P->G * P->q_head + kq * (D / 4);
-  const float* const lse0 = bbm::global(P->lse) + (int64_t)hk * P->G * P->T + x.begin;
+  const uint32_t* const lse0 = bbm::global(P->lse) + (int64_t)hk * P->G * P->T + x.begin;
   struct Query {
     bf16x8 q[KS];
     float nl;  // what is added to its exponents
   };
-  // (columns behind the last read the first one's query, and add nothing)
+  // (columns behind the last read the first one's query, and add nothing: a zero's product and -infinity give nothing whatever the query holds, as for a row that saw nothing)
   auto fetch = [&](const Column& y) __attribute__((always_inline)) {
     Query z;
     const bool there = y.col < cols;
     const __bf16* const p = there ? y.q : q0;
-    const float l = *(there ? y.lse : lse0);
+    const uint32_t l = *(there ? y.lse : lse0);
+    const bool nothing = !there || gives_nothing(l);
+    z.nl = nothing ? -INFINITY : minus_lse(l);
 #pragma unroll
-    for (int s = 0; s < KS; ++s) z.q[s] = *reinterpret_cast<const bf16x8*>(p + 8 * s);
-    z.nl = there ? minus_lse(l) : -INFINITY;
+    for (int s = 0; s < KS; ++s) {
+      const bbm::u32x4 w = *reinterpret_cast<const bbm::u32x4*>(p + 8 * s);
+      z.q[s] = __builtin_bit_cast(bf16x8, nothing ? bbm::u32x4{} : w);
+    }
     return z;
   };
   // 64 keys from j on with 16 columns; all_see: the last key that all of them see
@@ -331,9 +337,10 @@ __device__ __forceinline__ void wide(Args P, const Share& own) {
     const int c = tid / RC + ROWS * p, t = c / heads;
     off[p] = (uint32_t)((t < tokens ? t * q_row + (c - t * heads) * q_head : 0) + tid % RC * 8) * 2u;
   }
-  const int my_c = 32 * col_half + lq, my_t = my_c / heads, my_h = my_c - my_t * heads;
-  const bool used = my_t < tokens;
-  const float* const lse0 = bbm::global(P->lse) + (int64_t)hk * G * P->T + x.begin;
+  const int c = 32 * col_half + lq;
+  const bool used = c < tokens * heads;
+  const int my_t = used ? c / heads : 0, my_h = used ? c - my_t * heads : 0;
+  const uint32_t* const lse0 = bbm::global(P->lse) + (int64_t)hk * G * P->T + x.begin;
   const int64_t my_lse = (int64_t)my_h * P->T + my_t;
   const __bf16* const q0 = bbm::global(P->q) + (int64_t)x.begin * q_row + (int64_t)hk * G * q_head;
   struct Tile {
@@ -350,7 +357,7 @@ __device__ __forceinline__ void wide(Args P, const Share& own) {
     // (a causal key is seen by no token in front of its own)
     Tile now = {masked ? 0 : min(max(0, j0 - x.prefix), n - 1) / tokens * tokens, 0}, next = now;
     bf16x8 staged[PIECES];
-    float l;
+    uint32_t l;
     auto fetch = [&]() __attribute__((always_inline)) {  // (of tokens and heads that are not there: zeros, or what lies between those that are)
       const int ts = min(tokens, n - next.i), hs = min(heads, G - next.h);
       const __amdgpu_buffer_rsrc_t r = bbm::buffer_of(q0 + next.i * q_row + next.h * q_head, ts > 0 ? (int)(((ts - 1) * q_row + (hs - 1) * q_head + D) * 2) : 0);
@@ -386,11 +393,12 @@ __device__ __forceinline__ void wide(Args P, const Share& own) {
     for (int e = 0; e < 16; ++e) sum[e] = 0.0f;
 
     put(q_s[0]);
-    float l_now = l;
+    uint32_t l_now = l;
     fetch();
     int buf = 0;
 #pragma unroll 1
     for (; now.i < n; now = after(now), buf ^= 1) {
+      const bool nothing = gives_nothing(l_now);
       const float nl = used ? minus_lse(l_now) : -INFINITY;
       __syncthreads();  // the tile is there, and everyone is done with the other buffer
       const __bf16* const tile = q_s[0] + buf * L::ELEMS;
@@ -402,11 +410,12 @@ __device__ __forceinline__ void wide(Args P, const Share& own) {
       l_now = l;
       fetch();
       const int j = j0 + 32 * key_part, all_see = masked ? x.prefix - 1 : x.prefix + now.i;
-      if (j + 31 <= all_see && now.i + tokens <= n && now.h + heads <= G) {
+      // (A row that saw nothing may hold no number, which times nothing is none; so may the first one, which columns that are not used repeat, but then all that it sees has none.)
+      if (j + 31 <= all_see && now.i + tokens <= n && now.h + heads <= G && !__any(nothing)) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) sum[e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], rc, nl));
       } else {
-        const bool there = now.i + my_t < n && now.h + my_h < G;
+        const bool there = used && !nothing && now.i + my_t < n && now.h + my_h < G;
         const uint32_t seen = (there ? (uint32_t)seen_by(P, x, now.i + my_t, j) : 0) >> (4 * hh);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -489,7 +498,7 @@ extern "C" __attribute__((visibility("default"))) int bbm_kv4_weights(const bbm_
   if (int rc = check_apart(fn, {out}, {q->ptr, lse, cu, lens, block_table, mask, cache->k, cache->k_scale, S > 0 ? group_cu : nullptr, S > 0 ? shared_lens : nullptr})) return rc;
   WeightParams P = {};
   P.c = kv4_of(cache);
-  P.q = static_cast<const __bf16*>(q->ptr), P.lse = lse, P.weights = weights, P.out = out;
+  P.q = static_cast<const __bf16*>(q->ptr), P.lse = reinterpret_cast<const uint32_t*>(lse), P.weights = weights, P.out = out;
   P.q_row = q->row_stride, P.q_head = q->head_stride, P.table_stride = table_stride;
   P.cu = cu, P.lens = lens, P.table = block_table, P.group_cu = group_cu, P.shared_lens = shared_lens, P.mask = mask;
   P.T = (int32_t)T, P.R = (int32_t)R, P.S = (int32_t)S, P.G = (int32_t)G, P.max_pages = (int32_t)max_pages, P.mask_words = (int32_t)mask_words;

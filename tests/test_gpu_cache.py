@@ -329,6 +329,45 @@ def test_weights_of_rows_that_saw_nothing(bbm):
     check_weights(bbm, None, None, c, table, lens, cu, T, q, None, H, Hk, d, page, lse=lse)
 
 
+@pytest.mark.parametrize("rows", [[0], [5], [0, 1, 40, 41]])
+@pytest.mark.parametrize("group_cu, shared, lens, news, H, Hk, d, tree", [
+    ([0], [], [3, 300, 50], [3, 4, 2], 3, 1, 64, None),                         # few columns, the first request's new tokens all there is of it
+    ([0], [], [8, 300, 50], [8, 4, 2], 3, 1, 128, 1),
+    ([0], [], [70, 300, 50], [70, 30, 20], 6, 2, 128, None),                    # many; 63 of a tile's 64 are used
+    ([0], [], [70, 300, 50], [60, 64, 20], 12, 2, 64, 1),
+    ([0], [], [200, 300], [130, 90], 8, 2, 128, None),
+    ([0, 3], [48], [55, 60, 52], [3, 4, 2], 6, 2, 64, None),
+    ([0, 40], [96], [100 + i for i in range(40)], [3] * 40, 6, 2, 128, None)])
+def test_weights_of_queries_that_are_no_numbers(bbm, group_cu, shared, lens, news, H, Hk, d, tree, rows):
+    """What such a row holds reaches the keys that it sees, and none at all if its log-sum-exp is -infinity."""
+    c, table, cu, T, q, words = grouped_case(bbm, group_cu, shared, lens, news, H, Hk, d, 16, seed=9, tree=tree)
+    rows = [r for r in rows if r < T]
+    if tree:
+        words[rows] = 0
+    mask = None if words is None else torch.from_numpy(words).cuda()
+    groups = (i32(group_cu), i32(shared)) if shared else (None, None)
+    old = bbm.kv4_weights(c).fill_(1.5)
+
+    def gather(q, lse, decay=0.5):
+        return bbm.bbm_kv4_weights(q, lse, c, i32(table), i32(lens), i32(cu), old, *groups, mask=mask, decay=decay, out=torch.zeros_like(old))
+
+    _, lse = bbm.bbm_kv4_attn(q, c, i32(table), i32(lens), i32(cu), mask=mask)
+    none, only = lse.clone(), torch.full_like(lse, -float("inf"))
+    none[:, rows] = -float("inf")
+    only[:, rows] = lse[:, rows]
+    only[:, rows] = torch.where(torch.isinf(only[:, rows]), only[:, rows], torch.zeros_like(only[:, rows]))
+    want = gather(q, none)
+    seen = gather(q, only, 0.0) > 0
+    assert want.isfinite().all()
+    for value in (float("nan"), float("inf")):
+        bad, bad_lse = q.clone(), none.clone()
+        bad[rows] = value
+        assert torch.equal(gather(bad, none), want)
+        bad_lse[:, rows] = float("nan")
+        got = gather(bad, bad_lse)
+        assert torch.equal(got[~seen], want[~seen]) and got[seen].isnan().all()
+
+
 @pytest.mark.parametrize("max_own", [1, 1 << 40])
 def test_weights_of_many_columns_and_requests(bbm, max_own):
     """Pieces that a work-group takes one after the other, and hints beyond any table."""
