@@ -176,6 +176,30 @@ def test_shared_outputs_in_other_layouts(bbm, lens, news, H, Hk, d, layout):
     same_and_nothing_else(o, o_all, want, slice(int(cu[0]), int(cu[-1])))
 
 
+@pytest.mark.parametrize("rows", [[0], [5], [1, 2, 40]])
+@pytest.mark.parametrize("group_cu, shared, lens, news, H, Hk, d, tree", [
+    ([0, 3], [48], [55, 60, 52], [3, 4, 2], 6, 2, 64, None), ([0, 2], [2304], [2400, 2310], [3, 3], 12, 4, 128, 1), ([0, 40], [640], [660 + i for i in range(40)], [3] * 40, 6, 2, 128, None),
+    ([0, 70], [2048], [2060 + i for i in range(70)], [1] * 70, 8, 2, 64, None), ([0, 2], [256], [400, 420], [130, 90], 8, 2, 128, None)])
+def test_shared_queries_that_are_no_numbers(bbm, group_cu, shared, lens, news, H, Hk, d, tree, rows):
+    """Rows beside one whose query holds no number are what they should be (to the bit they need not be: a maximum moves when one of its wave's does)."""
+    c, table, cu, T, q, words = grouped_case(bbm, group_cu, shared, lens, news, H, Hk, d, 16, seed=9, tree=tree)
+    rows = [r for r in rows if r < T]
+
+    class Beside(Behind):
+        def bbm_kv4_attn(self, q, *args, out, lse, **kw):
+            super().bbm_kv4_attn(q, *args, out=out, lse=lse, **kw)
+            bad, o, l = q.clone(), out.clone(), lse.clone()
+            bad[rows] = value
+            super().bbm_kv4_attn(bad, *args, out=o, lse=l, **kw)
+            others = [r for r in range(T) if r not in rows]
+            out[others], lse[:, others] = o[others], l[:, others]
+            return out, lse
+
+    for value in (float("nan"), float("inf")):
+        for hint in NEAR:
+            check_cached(Beside(bbm, group_cu, shared), c, table, lens, cu, T, q, words, H, Hk, d, 16, **hint)
+
+
 @pytest.mark.parametrize("lens, news, H, Hk, d", GROUPED)
 def test_shared_without_a_log_sum_exp(bbm, lens, news, H, Hk, d):
     import ctypes
