@@ -9,7 +9,7 @@
 // through LDS; a wave has 32 of the keys and 32 columns of every tile.
 // Either way a lane adds up the exponentials of its column, and lanes meet once, behind the last column.
 // Measured, 32 / 8 heads of 128: one token each of 64 requests of 4 to 8 thousand keys (240 MB), narrow, 60 us, 4.0 TB/s (a large copy reaches 5.2); prompts of 1500, 420 and 839 tokens over up
-// to 6000 keys, wide, 136 us, 0.78 PFLOP/s (a large product 1.26; the vector pipe is busy for 56 % of the cycles, the matrix pipe for 31).
+// to 6000 keys, wide, 143 us, 0.74 PFLOP/s (a large product 1.26; the vector pipe is busy for 55 % of the cycles, the matrix pipe for 30).
 #include "bbm_cache.h"
 #include "bbm_kv4.h"
 #include "bbm_prompt.h"
@@ -398,7 +398,7 @@ __device__ __forceinline__ void wide(Args P, const Share& own) {
     int buf = 0;
 #pragma unroll 1
     for (; now.i < n; now = after(now), buf ^= 1) {
-      const bool nothing = gives_nothing(l_now);
+      const bool nothing = gives_nothing(l_now);  // (what that costs: 2 to 4 %; sums that are added up again where one is no number took 1 % less of these prompts, and 4 % more of 64 tokens each)
       const float nl = used ? minus_lse(l_now) : -INFINITY;
       __syncthreads();  // the tile is there, and everyone is done with the other buffer
       const __bf16* const tile = q_s[0] + buf * L::ELEMS;
