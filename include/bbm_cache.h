@@ -4,7 +4,8 @@
  *
  * Groups.  Requests group_cu[g] .. group_cu[g+1] - 1 (int32 [S+1], not decreasing, on the device like all below; cut to 0 .. R) are group g: their first
  * shared_lens[g] (int32 [S]; negative ones stand for 0) keys are the same, and lie in front of the new tokens of each of them that has any.  The rows of the block table are complete: the
- * row of each request holds the pages of its shared keys too, the same in all of them.  Requests in front of
+ * row of each request holds the pages of its shared keys too.  Pages whose keys are all shared are the same in all rows; of one that is shared in part (shared_lens is no multiple of the page) each
+ * request has a copy of its own, since it goes on there.  Requests in front of
  * group_cu[0] or from group_cu[S] on share nothing.  S may be 0 (group_cu and shared_lens are not looked at then).  Where a group's keys are not the same, or a shared key does not
  * lie in front of a request's new tokens, the results of that group's requests are unspecified.
  */
@@ -34,9 +35,10 @@ int bbm_kv4_shared_attn(const bbm_packed* q, const bbm_packed* o, float* lse, in
  * the same, and overlap in no other way.  For each request with a new token that has a row, each of its keys j and each key head,
  *   out[j] = decay * weights[j] + the sum over its new tokens i that see j (as in bbm_kv4_attn) and the heads h of the group of exp(softmax_scale <q_i, k_j> - lse[h][i]),
  * with 0 for weights[j] of the new tokens' own keys, whose slots may hold anything.  With lse of the attention of the same step that is the probability which
- * the keys got (a row of lse = -infinity gives nothing, whatever its query holds).  The keys that a group shares get the sum over all its requests, and one decay.  Written are the slots of the keys that there
+ * the keys got (a row of lse = -infinity gives nothing, whatever its query holds).  The keys that a group shares get the sum over all its requests, and one decay; those on a page
+ * that is shared in part what the requests gave to their copies, each for itself.  Written are the slots of the keys that there
  * are (a key without a page is left out), others stay as they are.  A page that lies in two requests' rows
- * other than as a shared one of the same group gets unspecified numbers.  Deterministic.  Meant for scores (times softmax_scale) up to 2^12, like the gradients.
+ * other than as a wholly shared one of the same group gets unspecified numbers.  Deterministic.  Meant for scores (times softmax_scale) up to 2^12, like the gradients.
  * 0 <= decay <= 1; R * Hk below 2^19, other sizes as in bbm_kv4_attn.  max_shared and max_own are hints for the work split, as above.
  */
 int bbm_kv4_weights(const bbm_packed* q, const float* lse, int64_t T, int64_t R, const int32_t* cu, const int32_t* lens, const int32_t* block_table,

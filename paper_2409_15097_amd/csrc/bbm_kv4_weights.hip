@@ -54,8 +54,8 @@ struct Owner {
   int fresh;        // from this key on, new tokens
 };
 __device__ __forceinline__ int max_keys(Args P) { return (int)min((int64_t)P->max_pages << P->c.page_shift, (int64_t)0x7fffffff); }
-// The keys that a group shares, in whole blocks of 16: what is left over is each request's own.
-__device__ __forceinline__ int shared_keys(Args P, int keys) { return max(0, min(keys, max_keys(P))) & ~15; }
+// The keys that a group shares, in whole pages: a page shared in part is another one for each request, since requests go on in it, and what is left over lies there for each of them.
+__device__ __forceinline__ int shared_keys(Args P, int keys) { return max(0, min(keys, max_keys(P))) & ~(P->c.page - 1); }
 __device__ __forceinline__ int row_cut(Args P, int c) { return min(max(c, 0), P->T); }
 __device__ __forceinline__ int request_cut(Args P, int g) { return min(max(bbm::global(P->group_cu)[g], 0), P->R); }
 __device__ __forceinline__ Owner owner_of_group(Args P, int g) {

@@ -422,6 +422,40 @@ def test_weights_of_heads_far_apart(bbm):
     assert torch.equal(bbm.bbm_kv4_weights(heads, lse[:2].contiguous(), one, *args[1:], bbm.kv4_weights(one)), want)
 
 
+class SharedInPart:
+    """bbm_kv4_weights with the shared lengths as they are, where the definition has those of whole pages."""
+
+    def __init__(self, bbm, shared):
+        self.bbm, self.shared, self.bbm_kv4_attn = bbm, i32(shared), bbm.bbm_kv4_attn
+
+    def bbm_kv4_weights(self, q, lse, c, table, lens, cu, w, group_cu, shared_lens, **kw):
+        return self.bbm.bbm_kv4_weights(q, lse, c, table, lens, cu, w, group_cu, self.shared, **kw)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("group_cu, shared, lens, news, H, Hk, page", [
+    ([0, 3], [100], [140, 130, 101], [1, 1, 1], 4, 2, 64),
+    ([0, 2], [40], [60, 50], [1, 2], 4, 1, 128),                              # no page is whole
+    ([1, 3, 5], [47, 80], [30, 60, 50, 90, 100], [1, 1, 3, 2, 1], 6, 2, 32),
+    ([0, 2], [300], [340, 333], [30, 33], 8, 2, 32),                          # many columns
+    ([0, 2], [300], [340, 333], [30, 33], 8, 2, 128),
+    ([0, 40], [112], [120 + i for i in range(40)], [2] * 40, 8, 2, 64),       # for the group alone
+    ([0, 2], [2300], [2400, 2310], [3, 1], 12, 4, 128)])
+def test_weights_behind_a_page_shared_in_part(bbm, group_cu, shared, lens, news, H, Hk, d, page):
+    """A prefix that ends inside a page, of which each request has a copy of its own, since it goes on there: the copies' keys gather for themselves, and attention is the same either way."""
+    c, table, cu, T, q, _ = grouped_case(bbm, group_cu, shared, lens, news, H, Hk, d, page, seed=6, before=1, behind=2)
+    for g, n in enumerate(shared):
+        for r in range(group_cu[g] + 1, group_cu[g + 1]):
+            a, b = table[group_cu[g], n // page], table[r, n // page]
+            for x in (c.k, c.v, c.k_scale):
+                x[b, :, :n % page] = x[a, :, :n % page]
+            c.v_scale[b, ..., :n % page] = c.v_scale[a, ..., :n % page]
+    hints = [{}, dict(max_shared=4096, max_own=40), dict(max_shared=1, max_own=1)]
+    check_weights(SharedInPart(bbm, shared), group_cu, [n // page * page for n in shared], c, table, lens, cu, T, q, None, H, Hk, d, page, hints=hints)
+    for hint in hints:
+        check_cached(Behind(bbm, group_cu, shared), c, table, lens, cu, T, q, None, H, Hk, d, page, **hint)
+
+
 # ---- eviction
 
 
