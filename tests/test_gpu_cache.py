@@ -456,6 +456,68 @@ def test_weights_behind_a_page_shared_in_part(bbm, group_cu, shared, lens, news,
         check_cached(Behind(bbm, group_cu, shared), c, table, lens, cu, T, q, None, H, Hk, d, page, **hint)
 
 
+def gathered(c, table, lens, cu, T, q, lse, old, H, Hk, page, scale, decay, gain=ot.key_weights):
+    """(what causal requests' keys hold behind a step, how far it may be off), [pages, Hk, page] in 64 bits; pages that requests share are decayed once."""
+    (hk, _), nq, nl, G = host_cache(c), f64(q), f64(lse), H // Hk
+    there, fresh = np.zeros((c.k.shape[0], page), bool), np.zeros((c.k.shape[0], page), bool)
+    at = [(table[r, np.arange(n) // page], np.arange(n) % page) for r, n in enumerate(lens)]
+    for r, (pg, j) in enumerate(at):
+        new = int(cu[r + 1] - cu[r])
+        there[pg, j] = True
+        fresh[pg[len(pg) - new:], j[len(pg) - new:]] = True
+    want = np.where(there[:, None], np.where(fresh[:, None], 0.0, np.float64(np.float32(decay)) * old), old)
+    tol = np.where(there[:, None], 4 * ot.F * want, 0.0)
+    for r, (pg, j) in enumerate(at):
+        a, b, n = int(cu[r]), int(cu[r + 1]), len(pg)
+        seen = np.arange(n) <= n - (b - a) + np.arange(b - a)[:, None]
+        for h in range(H):
+            w, e = gain(nq[a:b, h], hk[pg, h // G, j], seen, scale, nl[h, a:b])
+            want[pg, h // G, j] += w
+            tol[pg, h // G, j] += e
+    # the sums of all queries of a group meet in one number: as many half steps of it as there are terms
+    return want, tol + np.where(there[:, None], 2 * ot.F * (T * G + 16) * want, 0.0)
+
+
+SCALED = [([0], [], [70, 200], [3, 1], 4, 2, 64, 1), ([0, 3], [96], [170, 200, 165], [3, 1, 1], 4, 2, 128, -1), ([0], [], [300, 150], [140, 130], 8, 2, 64, -1),
+          ([0], [], [300, 150], [140, 130], 8, 2, 128, 1), ([0, 40], [96], [120 + i for i in range(40)], [2] * 40, 8, 2, 128, 1)]
+
+
+def check_scaled(bbm, group_cu, shared, c, table, lens, cu, T, q, H, Hk, page, scale, gain=ot.key_weights):
+    args, groups = (c, i32(table), i32(lens), i32(cu)), (i32(group_cu), i32(shared)) if shared else (None, None)
+    _, lse = bbm.bbm_kv4_shared_attn(q, *args, *groups, softmax_scale=scale, max_shared=4096)
+    old = torch.rand(c.k.shape[:3], generator=torch.Generator().manual_seed(3)).mul_(3)
+    want, tol = gathered(c, table, lens, cu, T, q, lse, f64(old), H, Hk, page, scale, 0.75, gain)
+    close("weights", bbm.bbm_kv4_weights(q, lse, *args, old.cuda(), *groups, decay=0.75, softmax_scale=scale), want, tol)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -7, 0.3, 2.0])
+@pytest.mark.parametrize("group_cu, shared, lens, news, H, Hk, d, sign", SCALED)
+def test_weights_with_other_scales(bbm, group_cu, shared, lens, news, H, Hk, d, sign, scale):
+    c, table, cu, T, q, _ = grouped_case(bbm, group_cu, shared, lens, news, H, Hk, d, 32, seed=21)
+    check_scaled(bbm, group_cu, shared, c, table, lens, cu, T, q, H, Hk, 32, scale)
+
+
+def sized_gain(q, k, seen, scale, lse):
+    """ot.key_weights of scores that fp32 holds exactly: an exponent is off by the roundings of lse and of the scale in units of log2, relative to lse and to the score, and by
+    those of their difference x (the constant, the multiply-add) and of the exponential."""
+    s = scale * (q @ k.T)
+    x = np.where(seen, s - lse[:, None], -np.inf)
+    p = np.exp(x)
+    e = ot.F * (np.abs(lse)[:, None] + np.abs(s) + 3 * np.abs(np.where(seen, x, 0.0)) + 8)
+    return p.sum(0), (1.001 * e * p).sum(0) + len(q) * ot.U
+
+
+@pytest.mark.parametrize("base, gap, scale", [(2, -2, 3), (10, -1, 0), (12, -1, 0), (16, -4, -4), (20, -2, -8), (30, 8, -18)])
+@pytest.mark.parametrize("group_cu, shared, lens, news, H, Hk, d, sign", SCALED)
+def test_weights_of_scores_up_to_2_to_the_12(bbm, group_cu, shared, lens, news, H, Hk, d, sign, base, gap, scale):
+    page = 32
+    c, table, cu, T, _, _ = grouped_case(bbm, group_cu, shared, lens, news, H, Hk, d, page, seed=22)
+    slots = np.concatenate([table[r, np.arange(n) // page] * page + np.arange(n) % page for r, n in enumerate(lens)])
+    slots = np.unique(slots)
+    bbm.bbm_kv4_append(sized_rows(1, len(slots), Hk, d, sign, base, gap), normal(2, len(slots), Hk, d), i32(slots), c)
+    check_scaled(bbm, group_cu, shared, c, table, lens, cu, T, sized_query(T, H, d, base), H, Hk, page, 2.0 ** scale, sized_gain)
+
+
 # ---- eviction
 
 
@@ -680,6 +742,59 @@ def test_answers_of_one_prompt(bbm):
     assert torch.isfinite(weights).all() and float(weights[s["table"][0, 0]].sum()) > 0
 
 
+class Given:
+    """An attention whose results are there already."""
+
+    def __init__(self, o, lse):
+        self.o, self.lse = o, lse
+
+    def bbm_kv4_attn(self, *args, out, lse, **kw):
+        out.copy_(self.o), lse.copy_(self.lse)
+
+
+@pytest.mark.parametrize("H, Hk, d, page, R, shared, budget, recent, steps", [(8, 2, 64, 16, 3, 48, 80, 4, 60), (8, 2, 128, 32, 2, 64, 100, 30, 50), (4, 4, 64, 16, 5, 0, 40, 7, 50)])
+def test_answers_step_by_step(bbm, H, Hk, d, page, R, shared, budget, recent, steps):
+    """What every step of answers behind a common prompt gives: attention, gathered weights and evicted caches against their definitions, from what the step before left."""
+    s = answers_state(bbm, H, Hk, d, page, R, shared, 2)
+    cache, tab = s["cache"], s["table"]
+    names = ("k", "v", "k_scale", "v_scale")
+    weights, evictions = bbm.kv4_weights(cache), 0
+    for step in range(steps):
+        w = normal(200 + step, R, (H + 2 * Hk) * d)
+        q, k, v = w[:, :H * d].unflatten(1, (H, d)), w[:, H * d:(H + Hk) * d].unflatten(1, (Hk, d)), w[:, (H + Hk) * d:].unflatten(1, (Hk, d))
+        r = bbm.bbm_build_slots(s["ctx"], s["new"], tab, s["free"], s["at"], R, page)
+        positions = r.positions + s["gone"]
+        assert positions.tolist() == [shared + step] * R                    # (as if nothing had ever gone)
+        q, k = bbm.bbm_rope(q, k, positions, s["freqs"])
+        bbm.bbm_kv4_append(k, v, r.slots, cache)
+        table, lens, cu = tab.cpu().numpy(), r.lens.tolist(), np.arange(R + 1)
+        o, lse = bbm.bbm_kv4_shared_attn(q, cache, tab, r.lens, r.cu_new, s["group_cu"], s["shared"], max_shared=4096)
+        check_cached(Given(o, lse), cache, table, lens, cu, R, q, None, H, Hk, d, page)
+        want, tol = gathered(cache, table, lens, cu, R, q, lse, f64(weights), H, Hk, page, d ** -0.5, 0.9)
+        bbm.bbm_kv4_weights(q, lse, cache, tab, r.lens, r.cu_new, weights, s["group_cu"], s["shared"], decay=0.9)
+        close(f"step {step}: weights", weights, want, tol)
+        was, was_w = {x: getattr(cache, x).cpu().numpy() for x in names}, weights.cpu().numpy()
+        e = bbm.bbm_kv4_evict(cache, weights, tab, r.lens, budget, recent=recent, first=s["first"], free_pages=s["free"], free_at=r.free_next)
+        want, want_w, left = {x: y.copy() for x, y in was.items()}, was_w.copy(), []
+        for i, n in enumerate(lens):
+            pg, j = table[i, np.arange(n) // page], np.arange(n) % page
+            for h in range(Hk):
+                moves, b = ot.evict(n, budget, recent, shared, list(was_w[pg, h, j]))
+                evictions += len(moves) > 0
+                for a, z in moves:
+                    for x in ("k", "v", "k_scale"):
+                        want[x][pg[z], h, j[z]] = was[x][pg[a], h, j[a]]
+                    want["v_scale"][pg[z], h, :, j[z]] = was["v_scale"][pg[a], h, :, j[a]]
+                    want_w[pg[z], h, j[z]] = was_w[pg[a], h, j[a]]
+            left.append(b)
+        assert e.lens.tolist() == left and np.array_equal(weights.cpu().numpy(), want_w)
+        for x in names:
+            assert np.array_equal(getattr(cache, x).cpu().numpy(), want[x]), (step, x)
+        s["gone"] = s["gone"] + (r.lens - e.lens)
+        s["ctx"], s["at"] = e.lens, e.free_next
+    assert evictions > steps // 4
+
+
 def test_answers_in_graphs(bbm):
     """A step recorded into a graph: replays give the eager results bit for bit, with eager work between them; two graphs of one stream do not share memory."""
     H, Hk, d, page, R, shared, budget = 8, 2, 128, 16, 5, 64, 65
@@ -749,6 +864,28 @@ def test_cache_operators_on_another_stream(bbm):
     got_e = bbm.bbm_kv4_evict(c, got_w, args[1], args[2], 200, first=i32([160, 160]), stream=side)
     torch.cuda.synchronize()
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.equal(got_e.lens, want_e.lens) and torch.equal(c.k, after)
+
+
+def test_weights_on_another_stream(bbm):
+    """Queries that a stream still writes when the call is made on it, few columns and many."""
+    for lens, news in (([300, 290], [1, 1]), ([300, 290], [40, 30])):
+        H, Hk, d, page = 8, 2, 64, 16
+        c, table, cu, T, q, _ = grouped_case(bbm, [0, 2], [160], lens, news, H, Hk, d, page, seed=2)
+        args, groups = (c, i32(table), i32(lens), i32(cu)), (i32([0, 2]), i32([160]))
+        _, lse = bbm.bbm_kv4_shared_attn(q, *args, *groups)
+        want = bbm.bbm_kv4_weights(q, lse, *args, bbm.kv4_weights(c), *groups)
+        fresh, side = bbm.kv4_weights(c), torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        late = torch.zeros_like(q)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            a = torch.randn(4096, 4096, device="cuda")
+            for _ in range(20):
+                a = a @ a * 1e-3
+            late.copy_(q)
+        got = bbm.bbm_kv4_weights(late, lse, *args, fresh, *groups, stream=side)
+        torch.cuda.synchronize()
+        assert got is fresh and torch.equal(got, want) and float(want.sum()) > 0
 
 
 def test_cache_binding_refuses(bbm):
