@@ -217,11 +217,10 @@ __global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
     __syncthreads();
     ties = in_front(wave_s[1]);
   }
-  // f(block, which of its 64 keys stay) for the blocks of this wave in order, the weights of four of them read together.
-  auto for_kept = [&](auto f) __attribute__((always_inline)) {
+  // f(block, which of its 64 keys stay) for the blocks of this wave from `from` on in order, the weights of four of them read together; before: the equal ones in front of the next block.
+  auto for_kept = [&](int from, int& before, auto f) __attribute__((always_inline)) {
     constexpr int U = 4;
-    int before = ties;
-    for (int k0 = block0; k0 < block1; k0 += U) {
+    for (int k0 = from; k0 < block1; k0 += U) {
       uint32_t u[U];
 #pragma unroll
       for (int n = 0; n < U; ++n) u[n] = weight_of(min(64 * (k0 + n) + lane, x.between - 1));
@@ -241,8 +240,13 @@ __global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
     }
   };
   // Places: bit i of the first `chosen` is free if key f + i does not stay there.
+  // The moves begin in the block where the places end, with what stays there and the equal ones behind it as they are now: weights in memory change under those who would read them again.
+  const int edge_block = x.chosen / 64;
+  uint64_t edge_stay = 0;
+  int edge_ties = ties, before = ties;
   int behind = 0;  // kept ones of this wave's that have to move
-  for_kept([&](int k, uint64_t stay) __attribute__((always_inline)) {
+  for_kept(block0, before, [&](int k, uint64_t stay) __attribute__((always_inline)) {
+    if (k == edge_block) edge_stay = stay, edge_ties = before;
     const int left = x.chosen - 64 * k;  // places among these
     const uint64_t places = left >= 64 ? ~0ull : left <= 0 ? 0ull : (1ull << left) - 1ull;
     if (lane == 0 && places) free_s[k] = places & ~stay;
@@ -340,7 +344,9 @@ __global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
       for (int u = 0; u < U; ++u) put(to[u], y[u]);
     }
   };
-  for_kept([&](int k, uint64_t stay) __attribute__((always_inline)) {
+  before = ties;
+  for_kept(max(block0, edge_block), before, [&](int k, uint64_t stay) __attribute__((always_inline)) {
+    if (k == edge_block) stay = edge_stay, before = edge_ties;
     const int left = x.chosen - 64 * k;
     const uint64_t go = left >= 64 ? 0ull : left <= 0 ? stay : stay & (~0ull << left);
     const int count = __popcll(go);

@@ -663,6 +663,47 @@ def test_evict_of_long_requests_in_a_graph(bbm, lens, budget, recent, table_page
             assert np.array_equal(getattr(c, x).cpu().numpy(), want[x]), x
 
 
+@pytest.mark.parametrize("lens, budget, recent, hint", [([45000, 3000, 38000], 22000, 300, 45000), ([60000], 40000, 0, 60000), ([9000, 8000, 700], 4000, 100, 1), ([9000, 5000], 4992, 64, 1)])
+@pytest.mark.parametrize("shares", [(0.5, 0.3, 0.2), (0.9, 0.02, 0.08), (0.05, 0.9, 0.05), (0.3, 0.0, 0.7)])
+def test_evict_of_equal_weights_read_from_memory(bbm, lens, budget, recent, hint, shares):
+    """Requests whose weights do not fit into LDS, and the same by a hint that is too small: keys move while others still look for theirs among weights of few values."""
+    Hk, d, page = 2, 64, 16
+    g = np.random.default_rng(len(lens) + budget)
+    pages, width = sum(-(-n // page) for n in lens) + 5, -(-max(lens) // page)
+    ids, table, at = g.permutation(pages), np.full((len(lens), width), -1), 0
+    for r, n in enumerate(lens):
+        table[r, :-(-n // page)] = ids[at:at + -(-n // page)]
+        at += -(-n // page)
+    c = bbm.kv4_cache(pages, Hk, d, page)
+    names = ("k", "v", "k_scale", "v_scale")
+    was = {x: g.integers(0, 255, getattr(c, x).shape, dtype=np.uint8) for x in names}
+    w = g.choice(np.array([0.0, 0.5, 2.0], np.float32), c.k.shape[:3], p=shares)
+    want, want_w = {x: y.copy() for x, y in was.items()}, w.copy()
+    for r, n in enumerate(lens):
+        if n <= budget:
+            continue
+        pg, j = table[r, np.arange(n) // page], np.arange(n) % page
+        for h in range(Hk):
+            between = np.lexsort((np.arange(n - recent), -w[pg, h, j][:n - recent]))
+            kept, edge = np.zeros(n, bool), budget - recent
+            kept[between[:edge]] = True
+            src = np.concatenate([np.nonzero(kept[edge:n - recent])[0] + edge, np.arange(n - recent, n)])
+            dst = np.concatenate([np.nonzero(~kept[:edge])[0], np.arange(edge, budget)])
+            for x in ("k", "v", "k_scale"):
+                want[x][pg[dst], h, j[dst]] = was[x][pg[src], h, j[src]]
+            want["v_scale"][pg[dst], h, :, j[dst]] = was["v_scale"][pg[src], h, :, j[src]]
+            want_w[pg[dst], h, j[dst]] = w[pg[src], h, j[src]]
+    tt, ln = i32(table), i32(lens)
+    for _ in range(2):
+        for x in names:
+            getattr(c, x).copy_(torch.from_numpy(was[x]))
+        wt = torch.from_numpy(w).cuda()
+        e = bbm.bbm_kv4_evict(c, wt, tt, ln, budget, recent=recent, max_len=hint)
+        assert e.lens.tolist() == [min(n, budget) for n in lens] and np.array_equal(wt.cpu().numpy(), want_w)
+        for x in names:
+            assert np.array_equal(getattr(c, x).cpu().numpy(), want[x]), x
+
+
 def test_evict_without_a_list(bbm):
     c = bbm.kv4_cache(4, 1, 64, 16)
     e = bbm.bbm_kv4_evict(c, bbm.kv4_weights(c), i32([[0, 1, 2, 3]]), i32([60]), 20)
