@@ -40,6 +40,8 @@ int bbm_kv4_shared_attn(const bbm_packed* q, const bbm_packed* o, float* lse, in
  * are (a key without a page is left out), others stay as they are.  A page that lies in two requests' rows
  * other than as a wholly shared one of the same group gets unspecified numbers.  Deterministic.  Meant for scores (times softmax_scale) up to 2^12, like the gradients.
  * 0 <= decay <= 1; R * Hk below 2^19, other sizes as in bbm_kv4_attn.  max_shared and max_own are hints for the work split, as above.
+ * The kernel and its work split go by averages over the requests.  Requests of few and of many new tokens, or a very long one among short ones, are better given in calls of their own: parts of cu,
+ * lens and block_table, and q and lse as they are, since rows outside the offsets are nobody's (255 requests of one token and one of 1500: 8.1 ms in one call, 0.29 in two).
  */
 int bbm_kv4_weights(const bbm_packed* q, const float* lse, int64_t T, int64_t R, const int32_t* cu, const int32_t* lens, const int32_t* block_table,
                     int64_t table_stride, int64_t max_pages, int64_t S, const int32_t* group_cu, const int32_t* shared_lens, const uint64_t* mask,

@@ -518,6 +518,21 @@ def test_weights_of_scores_up_to_2_to_the_12(bbm, group_cu, shared, lens, news, 
     check_scaled(bbm, group_cu, shared, c, table, lens, cu, T, sized_query(T, H, d, base), H, Hk, page, 2.0 ** scale, sized_gain)
 
 
+@pytest.mark.parametrize("cut", [1, 3, 5])
+def test_weights_of_a_step_in_two_calls(bbm, cut):
+    """Requests of few and of many new tokens in calls of their own, on the step's tensors: parts of offsets, lengths and table, whose other rows are nobody's."""
+    lens, news, H, Hk, d, page = [300, 170, 250, 90, 400, 333], [130, 1, 1, 2, 1, 1], 8, 2, 64, 16
+    c, table, cu, T, q, _ = cached_case(bbm, lens, news, H, Hk, d, page, seed=12, before=1, behind=2)
+    tab, ln, offsets = i32(table), i32(lens), i32(cu)
+    _, lse = bbm.bbm_kv4_attn(q, c, tab, ln, offsets)
+    old = torch.rand(c.k.shape[:3], generator=torch.Generator().manual_seed(3)).mul_(3)
+    want, tol = gathered(c, table, lens, cu, T, q, lse, f64(old), H, Hk, page, d ** -0.5, 0.75)
+    w = old.cuda()
+    for a, b in ((0, cut), (cut, 6)):
+        bbm.bbm_kv4_weights(q, lse, c, tab[a:b], ln[a:b], offsets[a:b + 1], w, decay=0.75)
+    close("weights", w, want, tol)
+
+
 # ---- eviction
 
 
