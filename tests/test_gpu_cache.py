@@ -533,6 +533,21 @@ def test_weights_of_a_step_in_two_calls(bbm, cut):
     close("weights", w, want, tol)
 
 
+@pytest.mark.parametrize("H, Hk", [(4, 2), (64, 1)])
+def test_weights_of_groups_whose_numbers_are_wrong_stay_inside(bbm, H, Hk):
+    """Few columns and many: keys of other groups get what they get, pages of nobody keep what they hold."""
+    group_cu, shared, lens, news, d, page = [0, 2, 4], [64, 32], [90, 80, 70, 60], [1, 1, 1, 1], 64, 16
+    c, table, cu, T, q, _ = grouped_case(bbm, group_cu, shared, lens, news, H, Hk, d, page, seed=8, before=2, behind=2)
+    args = c, i32(table), i32(lens), i32(cu)
+    _, lse = bbm.bbm_kv4_attn(q, *args)
+    old = torch.rand(c.k.shape[:3], generator=torch.Generator().manual_seed(1)).cuda()
+    want = bbm.bbm_kv4_weights(q, lse, *args, old, i32(group_cu), i32(shared), out=old.clone())
+    sure, nobody = np.unique(table[:2][table[:2] >= 0]), np.setdiff1d(np.arange(c.k.shape[0]), table)
+    for wrong, n in (([0, 2, 9], [64, 32]), ([-7, 2, 4], [64, 32]), ([0, 2, 4], [64, 1 << 30]), ([0, 2, 1], [64, 32]), ([0, 2, 4], [64, 80]), ([0, 2, 4], [64, -5])):
+        got = bbm.bbm_kv4_weights(q, lse, *args, old, i32(wrong), i32(n), out=old.clone())
+        assert len(nobody) > 0 and torch.equal(got[sure], want[sure]) and torch.equal(got[nobody], old[nobody])
+
+
 # ---- eviction
 
 
