@@ -54,7 +54,8 @@ int bbm_kv4_weights(const bbm_packed* q, const float* lse, int64_t T, int64_t R,
  * (equal ones: the lowest positions; a NaN counts as less than any number).  The kept ones move together to positions 0 .. b - 1, codes, scales and weights alike:
  *   those in front of position b - recent stay where they are; those between it and the last `recent` go to the places of evicted ones, the first to the
  *   first and so on; the last `recent`, in their order, go to b - recent .. b - 1.
- * Heads choose for themselves: a position then holds other tokens in other heads (their rotary positions are in the keys).  Positions from b on keep what they held.
+ * Heads choose for themselves: a position then holds other tokens in other heads.  Their rotary positions are in the keys; those of later tokens run on, which is bbm_build_slots' positions plus
+ * what the request has lost so far (the sums of lens - new_lens).  Positions from b on keep what they held.
  * Written besides:
  *   new_lens [R]    min(n, b) (n as cut)
  *   free_pages      the pages behind position b, back in front of *free_at: with e = min(*free_at, n_free) entries e - m .. e - 1 of free_pages [n_free] get the m pages given back, in

@@ -122,7 +122,8 @@ def bbm_kv4_evict(cache: KV4Cache, weights: torch.Tensor, block_table: torch.Ten
                   free_pages: Optional[torch.Tensor] = None, free_at: Optional[torch.Tensor] = None, max_len: Optional[int] = None, new_lens: Optional[torch.Tensor] = None,
                   workspace: Optional[torch.Tensor] = None, stream=None) -> Evicted:
     """Thins requests of more than `budget` keys to that many, for each key head those of largest weight beside the first[r] (int32 [R]) and the last `recent` ones, in place;
-    the pages that this frees go back to free_pages (int32 [n]) in front of free_at (int32 [1]).  max_len: an upper bound of lens (None: what the table holds)."""
+    the pages that this frees go back to free_pages (int32 [n]) in front of free_at (int32 [1]).  max_len: an upper bound of lens (None: what the table holds).  Later tokens are
+    turned (bbm_rope) by the positions of bbm_build_slots plus the sums of lens - Evicted.lens."""
     dev = _gpu(lens)
     if _elsewhere(dev, stream):
         with _context(dev, stream):
