@@ -10,10 +10,11 @@
 //   O^T += V^T P^T    over 32 keys: lane (n, q) loads elements n * D / 16 .. of the keys 4 q .. 4 q + 3 of both blocks of 16, converts pairs of elements,
 //                     and pairs the keys by byte permutes; row n of instruction j is element n * D / 16 + j.  The lane's scores are of the same eight keys
 //                     (the layout of the first product's result), so P goes from one product to the other in place.
+// Sums, maxima and O are fp32 until O's one rounding.  P is rounded to bf16 for its product, which the matrix instruction asks for: that puts O off by as much again as its own rounding does, no more.
 // Measured: one token each of 64 requests of 9.8 to 16 thousand keys, 32 / 8 heads of 128 (861 MB), narrow, 162 - 176 us, 4.9 - 5.3 TB/s (a large copy reaches
 // 4.8), and 5.2 for the join; trees of 256 nodes of 8 requests, 32 heads, over 805 to 1280 keys, wide, 52 us, 0.65 PFLOP/s counted as the products of all pairs.
 // Behind shared prefixes (include/bbm_cache.h) a group's requests together are columns over the keys that they share, and each for itself over the rest; the parts of both meet in the join.
-// 67 requests of one token behind 8192 common keys, 500 to 1000 of their own, 32 / 8 heads of 128: 32 us and 6 for the join; 256 requests behind 32768: 170 and 16.
+// 67 requests of one token behind 8192 common keys, 500 to 1000 of their own, 32 / 8 heads of 128: 32 us and 6 for the join; 256 requests behind 32768: 170 to 190 in all, of which the join is 16.
 #include "bbm_cache.h"
 #include "bbm_kv4.h"
 #include "bbm_softmax.h"
@@ -797,14 +798,18 @@ struct SharedPlan {
   bool apart;  // each request for itself, as without groups
 };
 // Short prefixes of few requests are better read for each of them: one launch and no join.  32 / 8 heads of 128, us, by groups / apart: 4 requests behind 512 keys 10.5 / 7.9, behind 1024
-// 10.6 / 10.8, behind 2048 11.1 / 13.5; 32 requests 11.9 / 8.3, 12.2 / 11.6, 15.8 / 18.3 (20, 38 and 74 MB read apart).
+// 10.6 / 10.8, behind 2048 11.1 / 13.5; 32 requests 11.9 / 8.3, 12.2 / 11.6, 15.8 / 18.3 (20, 38 and 74 MB read apart).  Heads of 64: 9.8 / 7.3, 9.9 / 9.8, 10.2 / 12.4; 10.8 / 7.6,
+// 11.0 / 10.2, 13.7 / 16.5.
 constexpr int64_t kApartKeys = 1152, kApartBytes = 40 << 20;
 // Groups take the wide kernel from this many columns of a group on, on average.  32 / 8 heads of 128, us, narrow / wide: 16 requests of one token behind 8192 common keys (64 columns) 19 / 23,
-// 32 (128 columns) 26 / 28, 67 (268) 43 / 37, 256 behind 32768 (1024) 263 / 185.
+// 32 (128 columns) 26 / 28, 67 (268) 43 / 37, 256 behind 32768 (1024) 263 / 185; heads of 64, 64 columns 16.3 / 16.6, 128 22.5 / 26.6, 192 25.6 / 26.0, 268 33.5 / 32.5, 1024 247 / 124.
+// (The columns are an average over the groups, rows that are in none counted in: one large group among groups of few columns gets the narrow kernel too.)
 // The narrow one's parts have at least 512 keys (groups are few, and the join has to be there anyway): 32 requests behind 1024 keys 15.1 us, of 1024 16.2; four heads of 64 behind 8192 11.4 / 13.0.
 constexpr int64_t kGroupWideColumns = 192, kGroupPartKeys = 512;
 // The wide one's are chosen by what they take: a tile of 64 keys of a work-group that has a CU to itself, of two that share one, and a MB of records, written and read, in us.  (With
-// 512 keys a part and no more than 512 work-groups instead: 67 requests behind 8192 keys 41 us, with this 37; 32 requests behind 4096 keys, eight heads over one of 128, 25 and 17.)
+// 512 keys a part and no more than 512 work-groups instead: 67 requests behind 8192 keys 41 us, with this 37; 32 requests behind 4096 keys, eight heads over one of 128, 25 and 17.)  They are
+// times of heads of 128, used for heads of 64 too.  What is chosen / the best of 13 numbers of parts from 1 to 64, us: 67 requests behind 8192 keys 33.6 / 33.2, of 64 30.9 / 27.3; 256 behind 32768
+// 190 / 180, 134 / 122; 100 behind 16384 72 / 57, 52 / 43; 32 behind 4096, eight heads over one, 16.2 / 16.5, 12.7 / 12.8.
 constexpr double kTileAlone = 1.4, kTileShared = 2.2, kRecordMB = 0.25;
 inline int64_t wide_parts(int64_t pieces, int64_t max_keys, double record_mb) {
   int64_t best = 1;

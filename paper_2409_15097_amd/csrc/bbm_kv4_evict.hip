@@ -5,8 +5,10 @@
 // bisection over the counts of 64 places, then by counting bits.  Where the moves of the first kind end they read nothing that they write, so their order does not matter; the last
 // keys are shifted by whole rounds of all waves, with a barrier between a round's loads and its stores, in ascending order.
 // The pages go back by a wave for each request, behind the sum of what the requests in front of it give: of up to 256 requests in one more work-group, else by a second kernel.
-// Bound by latency where little moves: 1040 keys to 1024, 4 heads of 64, 11.5 us, 64 requests of up to 2112 keys to 2048, 8 heads of 128, 14; by pieces of 64 bytes all over the cache
-// where much does: 16 requests of up to 32000 keys to 4000, 62 us, 2.3 TB/s (with weights read from memory in every pass and moves of 64 keys at a time 108; 70 with the pages from memory).
+// Measured on caches that nothing has thinned (a second call on the same keys and weights finds most of the chosen ones in front, and moves half as many).  Bound by latency: 1040 keys to
+// 1024, 4 heads of 64, 11.5 us, 64 requests of up to 2112 keys to 2048, 8 heads of 128, 17; 16 requests of up to 32000 keys to 4000, 118 us, 1.2 TB/s of what has to move, 4 such requests
+// 108: a work-group takes 100 us, of which reading the weights is 18, the rest of the choice 7, places 7, the moves of 3000 keys and the last 500 67.  (250 with weights read from memory in every
+// pass and pages given back by a second launch; 140 with the pages from memory.)  One request of 100 thousand keys to 8000, whose weights do not fit into LDS, 382 us.
 #include "bbm_cache.h"
 #include "bbm_kv4.h"
 
@@ -177,7 +179,7 @@ __global__ __launch_bounds__(NT) void kv4_evict_kernel(const EvictParams P) {
           }
         }
       };
-      if (x.between <= 2 * NT) count(bbm::IntC<2>{});  // (of 1000 to 2000 keys with eight 14.1 and 16.5 us a call, with two 11.5 and 13.9)
+      if (x.between <= 2 * NT) count(bbm::IntC<2>{});  // (of 1000 and up to 2112 keys with eight 17.3 and 20.1 us a call, with two 15.9 and 17.6)
       else count(bbm::IntC<8>{});
       __syncthreads();
       // two bins a thread, the highest first; who reads them clears them for the next pass

@@ -9,7 +9,8 @@
 // through LDS; a wave has 32 of the keys and 32 columns of every tile.
 // Either way a lane adds up the exponentials of its column, and lanes meet once, behind the last column.
 // Measured, 32 / 8 heads of 128: one token each of 64 requests of 4 to 8 thousand keys (240 MB), narrow, 60 us, 4.0 TB/s (a large copy reaches 5.2); prompts of 1500, 420 and 839 tokens over up
-// to 6000 keys, wide, 143 us, 0.74 PFLOP/s (a large product 1.26; the vector pipe is busy for 55 % of the cycles, the matrix pipe for 30).
+// to 6000 keys, wide, 143 us, 0.74 PFLOP/s (a large product 1.26; the vector pipe is busy for 55 % of the cycles, the matrix pipe for 30: a tile's products stand in front of its exponentials).
+// Heads of 64, the same requests of one token, 133 MB: 46 us, 2.9 TB/s: what a wave does for a key does not shrink with its bytes.
 #include "bbm_cache.h"
 #include "bbm_kv4.h"
 #include "bbm_prompt.h"
@@ -461,7 +462,10 @@ inline int64_t parts_of(int64_t owners, int64_t Hk, int64_t keys, bool wide) {
   if (!wide) return std::min(bbm::ceil_div(keys, kStep), bbm::ceil_div(kFill, owners * Hk));
   return std::min({bbm::ceil_div(keys, kWideKeys), kMaxParts, std::max<int64_t>(8, kMaxWideWgs / (owners * Hk) / 8 * 8)});
 }
-// Columns of an owner, on average, from which on its codes are better converted once.
+// Columns of an owner, on average, from which on its codes are converted once.  32 / 8 heads of 128, us, narrow / wide: one request of 8192 keys, 16 columns 6.1 / 10.1, 32 8.8 / 10.4, 48
+// 11.8 / 10.5, 64 14.5 / 9.9, 256 50 / 15; a group behind 8192 keys, 32 columns 8.9 / 13.9, 64 15.0 / 13.7, 268 53 / 25; heads of 64 alike (32 8.5 / 8.1, 48 11.3 / 8.2; 32 8.5 / 11.6, 64 13.9 / 11.2).
+// That is the border for few owners.  Of many the wide kernel's work-groups, one for every 128 keys, cost more than their columns do: 16 requests of 2048 to 4096 keys, 32 columns 21 / 63, 48
+// 29 / 64, 64 36 / 61, 128 68 / 69, 256 127 / 84; 64 of 1024 to 2048, 64 columns 56 / 151, 256 199 / 202.
 constexpr int64_t kWideFrom = 32;
 
 template <int D>
